@@ -312,6 +312,94 @@ zipmoe_status zipmoe_decode_expert_ffn_noalloc(const uint16_t *tokens, uint32_t 
                                                const zipmoe_compressed_experts *experts, uint16_t *out,
                                                uint32_t *status_word, zipmoe_stream stream);
 
+/* ---- the rest of the expert sublayer (device) ---------------------------------
+ * What surrounds the experts in a decode step: the residual's addition with the norm, the router whose choice
+ * decides which experts are needed, and the experts that are already recovered (the planner's pool F).  (The paper
+ * takes these from the host framework; its scheduler only sees the router's choice and the time p_n.) */
+
+#define ZIPMOE_NORM_RESIDUAL_F32 1u /* residual and residual_out are fp32 (else bf16 patterns) */
+
+/* Residual addition and root-mean-square norm of `rows` rows of `cols` elements:
+ *     h = x + residual                       (h = x where residual is NULL)
+ *     residual_out = h                       (rounded to bf16 unless ZIPMOE_NORM_RESIDUAL_F32)
+ *     y = h / sqrt(mean(h^2) + eps) * weight (from the unrounded h, in fp32)
+ *     out = bf16(y)
+ *     scales = max |y| / 448 over the row, or over each `group` columns of it;  out_q = e4m3(y / scale)
+ * A group of zeros has scale 0 and zeros; q * scale gives the row back.  One launch on `stream`, asynchronous;
+ * every input is read once.  A row whose sum of squares exceeds fp32 (elements of about 1e19) gives zeros, as the
+ * formula in fp32 does; NaN and infinities come out as NaN.
+ * device in : x (rows x_pitch elements apart), residual (rows residual_pitch apart; may be NULL), weight[cols] bf16
+ * device out: residual_out (rows residual_out_pitch apart; may be NULL, may be `residual` itself with the same pitch,
+ *             may not overlap anything else), out (rows out_pitch apart; may be NULL, may be x itself with the same pitch), out_q
+ *             (e4m3 bytes, rows out_pitch apart; may be NULL), scales[rows][ceil(cols / group)] dense (NULL exactly
+ *             if out_q is).  One of out and out_q must be given.
+ * group     : 32, 64, 128 or 256 columns; 0, or any value >= cols, is the whole row.
+ * Pitches are in elements, at least cols.  Any element alignment; rows and weight that start on 16-byte boundaries
+ * are faster.  rows = 0 does nothing.  Limits: cols <= 32768 (ZIPMOE_ERR_UNSUPPORTED otherwise). */
+zipmoe_status zipmoe_add_rmsnorm(const uint16_t *x, uint64_t x_pitch, const void *residual, uint64_t residual_pitch,
+                                 void *residual_out, uint64_t residual_out_pitch, const uint16_t *weight, uint32_t rows,
+                                 uint32_t cols, float eps, uint16_t *out, uint8_t *out_q, uint64_t out_pitch, float *scales,
+                                 uint32_t group, uint32_t flags, zipmoe_stream stream);
+
+#define ZIPMOE_ROUTE_SOFTMAX_ALL 1u /* weights are the softmax over all experts, not renormalised over the chosen */
+
+/* The router: which experts every token goes to, and with what weights.
+ *     logit[t, e] = sum_h tokens[t, h] * gate[e, h] + bias[e]        (fp32 accumulation)
+ *     topk_ids[t, 0..k) = the k experts with the largest logits, largest first, equal ones lowest index first
+ *     topk_weights[t, j] = exp(logit of choice j) / sum of exp(logit) over the chosen experts
+ * An expert whose logit is -infinity (a bias of -infinity switches it off) is never chosen: where fewer than k are
+ * left, the remaining ids are -1 with weight 0.  A NaN logit counts as larger than every number, and makes the
+ * token's weights NaN.  One launch on `stream`, asynchronous.
+ * device in : tokens (T rows of `hidden`, token_pitch elements apart), gate [n_experts, hidden] bf16 patterns (both
+ *             16-byte aligned, hidden and token_pitch multiples of 8), bias[n_experts] fp32 or NULL
+ * device out: topk_ids [T, k], topk_weights [T, k], logits [T, n_experts] fp32 (may be NULL); status_word (nullable)
+ *             as for zipmoe_decode: code 3 when a wait ran out.
+ * Limits: n_experts <= 256, k <= 8, k <= n_experts, hidden <= 32768 (ZIPMOE_ERR_UNSUPPORTED otherwise).  T = 0 does
+ * nothing. */
+zipmoe_status zipmoe_route(const uint16_t *tokens, uint32_t T, uint64_t token_pitch, const uint16_t *gate,
+                           uint32_t n_experts, uint32_t hidden, const float *bias, uint32_t k, uint32_t flags,
+                           int32_t *topk_ids, float *topk_weights, float *logits, uint32_t *status_word,
+                           zipmoe_stream stream);
+
+/* The recovered experts of one MoE layer.  A HOST struct; `table` is DEVICE memory holding what
+ * zipmoe_resident_experts_plan wrote. */
+typedef struct {
+  uint32_t n_experts, hidden, inter, reserved; /* hidden, inter: multiples of 8                                   */
+  const void *table;                           /* device [3 * n_experts * ZIPMOE_RESIDENT_ENTRY_BYTES], 64-byte aligned */
+} zipmoe_resident_experts;
+#define ZIPMOE_RESIDENT_ENTRY_BYTES 128u
+
+/* Describes recovered experts to zipmoe_expert_ffn: one opaque entry per tensor, which the caller copies to the
+ * device as it is.  Written once per layer (and again for an expert whose tensors move).
+ * host in : tensors[3 * n_experts] DEVICE addresses, tensors[3e+0] = w1 (gate) [inter, hidden], 3e+1 = w3 (up)
+ *           [inter, hidden], 3e+2 = w2 (down) [hidden, inter]: dense row-major bf16, 16-byte aligned, for example
+ *           where zipmoe_decode put them.  The memory itself is not touched.
+ * host out: table[3 * n_experts * ZIPMOE_RESIDENT_ENTRY_BYTES]
+ * Limits: n_experts <= 256, hidden and inter multiples of 8, at most 32768 (ZIPMOE_ERR_UNSUPPORTED otherwise). */
+zipmoe_status zipmoe_resident_experts_plan(const uint16_t *const *tensors, uint32_t n_experts, uint32_t hidden,
+                                           uint32_t inter, void *table);
+
+/* Scratch zipmoe_expert_ffn needs for T tokens with k experts each.  Host only. */
+zipmoe_status zipmoe_expert_ffn_workspace_bytes(uint32_t T, uint32_t k, const zipmoe_resident_experts *experts,
+                                                uint64_t *workspace_bytes);
+
+/* Expert execution on recovered weights (Section 3.3: the GPU work p_n of the tokens routed to expert n, for experts
+ * found in pool F): what zipmoe_decode_expert_ffn computes, from bf16 tensors.  For every token t and choice j with
+ * e = topk_ids[t, j]:
+ *     g = W1_e x_t,  u = W3_e x_t,  h = bf16(SiLU(g) * u),  y = W2_e h
+ *     out[t] = bf16( sum_j topk_weights[t, j] * y )
+ * A negative id is no expert (zipmoe_route writes -1) and adds nothing; a token without experts gets zeros.  An id
+ * of n_experts or more adds nothing either and sets status_word (code 1).  An expert listed twice by a token counts
+ * with both weights.  Weights are read once for all tokens of the call, and only those of experts that have tokens.
+ * device in : tokens [T, hidden] bf16 patterns; topk_ids [T, k]; topk_weights [T, k] fp32 or NULL (= 1.0)
+ * device out: out [T, hidden] bf16 patterns; workspace: scratch of at least zipmoe_expert_ffn_workspace_bytes,
+ *             16-byte aligned (256 is better), not shared by calls that may overlap; status_word (nullable) as for
+ *             zipmoe_decode.
+ * Limits: T <= 256, k <= 8 (ZIPMOE_ERR_UNSUPPORTED otherwise); T = 0 does nothing. */
+zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, const int32_t *topk_ids, const float *topk_weights,
+                                uint32_t k, const zipmoe_resident_experts *experts, uint16_t *out, void *workspace,
+                                uint64_t workspace_bytes, uint32_t *status_word, zipmoe_stream stream);
+
 /* ---- cache-pool planning (host only, no CUDA) ------------------------------
  * The paper's planner sizes four cache pools for experts in different compression states -- F full
  * tensors, C compressed (E-chunks and SM-chunks), S SM-chunks only, E E-chunks only -- from a

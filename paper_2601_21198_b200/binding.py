@@ -338,6 +338,70 @@ def zipmoe_decode_expert_ffn_noalloc(tokens, T, topk_ids, topk_weights, k, exper
                                                  ctypes.byref(experts), _ptr(out), _ptr(status_word), _ptr(stream)))
 
 
+# ---- the rest of the expert sublayer: norm, router, experts that are already recovered --------------------
+NORM_RESIDUAL_F32 = 1       # zipmoe_add_rmsnorm flag: residual and residual_out are fp32
+ROUTE_SOFTMAX_ALL = 1       # zipmoe_route flag: weights are not renormalised over the chosen experts
+RESIDENT_ENTRY_BYTES = 128
+
+
+class ResidentExpertsStruct(ctypes.Structure):
+    """zipmoe_resident_experts."""
+    _fields_ = [("n_experts", _u32), ("hidden", _u32), ("inter", _u32), ("reserved", _u32), ("table", _vp)]
+
+
+_lib.zipmoe_add_rmsnorm.argtypes = [_vp, _u64, _vp, _u64, _vp, _u64, _vp, _u32, _u32, ctypes.c_float, _vp, _vp, _u64, _vp,
+                                    _u32, _u32, _vp]
+_lib.zipmoe_route.argtypes = [_vp, _u32, _u64, _vp, _u32, _u32, _vp, _u32, _u32, _vp, _vp, _vp, _vp, _vp]
+_lib.zipmoe_resident_experts_plan.argtypes = [ctypes.POINTER(_vp), _u32, _u32, _u32, _vp]
+_lib.zipmoe_expert_ffn_workspace_bytes.argtypes = [_u32, _u32, ctypes.POINTER(ResidentExpertsStruct), ctypes.POINTER(_u64)]
+_lib.zipmoe_expert_ffn.argtypes = [_vp, _u32, _vp, _vp, _u32, ctypes.POINTER(ResidentExpertsStruct), _vp, _vp, _u64, _vp, _vp]
+for _f in ("zipmoe_add_rmsnorm", "zipmoe_route", "zipmoe_resident_experts_plan", "zipmoe_expert_ffn_workspace_bytes",
+           "zipmoe_expert_ffn"):
+    getattr(_lib, _f).restype = _int
+
+
+def zipmoe_add_rmsnorm(x, x_pitch, residual, residual_pitch, residual_out, residual_out_pitch, weight, rows, cols, eps, out,
+                       out_q, out_pitch, scales=None, group=0, flags=0, stream=None):
+    """Pointer arguments are device tensors (or raw device addresses, or None); pitches in elements."""
+    _check("zipmoe_add_rmsnorm",
+           _lib.zipmoe_add_rmsnorm(_ptr(x), x_pitch, _ptr(residual), residual_pitch, _ptr(residual_out), residual_out_pitch,
+                                   _ptr(weight), rows, cols, eps, _ptr(out), _ptr(out_q), out_pitch, _ptr(scales), group,
+                                   flags, _ptr(stream)))
+
+
+def zipmoe_route(tokens, T, token_pitch, gate, n_experts, hidden, bias, k, flags, topk_ids, topk_weights, logits=None,
+                 status_word=None, stream=None):
+    """Pointer arguments are device tensors (or raw device addresses, or None)."""
+    _check("zipmoe_route",
+           _lib.zipmoe_route(_ptr(tokens), T, token_pitch, _ptr(gate), n_experts, hidden, _ptr(bias), k, flags,
+                             _ptr(topk_ids), _ptr(topk_weights), _ptr(logits), _ptr(status_word), _ptr(stream)))
+
+
+def zipmoe_resident_experts_plan(tensors, n_experts, hidden, inter):
+    """tensors: 3 * n_experts device tensors (or addresses).  Returns the table (numpy uint8), to be copied to the device."""
+    ptrs = (_vp * max(len(tensors), 1))(*[_ptr(t) for t in tensors])
+    if len(tensors) != 3 * n_experts:
+        raise ValueError("three tensors per expert are wanted")
+    table = np.zeros(3 * n_experts * RESIDENT_ENTRY_BYTES, np.uint8)
+    _check("zipmoe_resident_experts_plan", _lib.zipmoe_resident_experts_plan(ptrs, n_experts, hidden, inter, _ptr(table)))
+    return table
+
+
+def zipmoe_expert_ffn_workspace_bytes(T, k, experts):
+    out = _u64(0)
+    _check("zipmoe_expert_ffn_workspace_bytes",
+           _lib.zipmoe_expert_ffn_workspace_bytes(T, k, ctypes.byref(experts), ctypes.byref(out)))
+    return out.value
+
+
+def zipmoe_expert_ffn(tokens, T, topk_ids, topk_weights, k, experts, out, workspace, workspace_bytes, status_word=None,
+                      stream=None):
+    """Pointer arguments are device tensors (or raw device addresses); `experts` is a ResidentExpertsStruct."""
+    _check("zipmoe_expert_ffn",
+           _lib.zipmoe_expert_ffn(_ptr(tokens), T, _ptr(topk_ids), _ptr(topk_weights), k, ctypes.byref(experts), _ptr(out),
+                                  _ptr(workspace), workspace_bytes, _ptr(status_word), _ptr(stream)))
+
+
 class LaunchInfo(ctypes.Structure):
     _fields_ = [("payload_bytes", _u64), ("sm_bytes", _u64), ("out_elems", _u64), ("n_chunks", _u32), ("n_tiles", _u32),
                 ("n_tables", _u32), ("max_record_bytes", _u32), ("max_code_len", _u32), ("flags", _u32)]
@@ -469,4 +533,183 @@ class DeviceExperts:
         s = torch.cuda.current_stream(self.dev.device) if stream is None else stream
         zipmoe_decode_expert_ffn(tokens, T, topk_ids, topk_weights, k, self.struct, out, ws, ws.numel(),
                                  self.dev.status, s.cuda_stream)
+        return out
+
+
+_KINDS = {}
+
+
+def _kind(name):
+    """The torch types that hold a kind of element: bf16 values may come as int16 bit patterns, e4m3 as bytes."""
+    if not _KINDS:
+        import torch
+        _KINDS.update({"bf16": (torch.bfloat16, torch.int16, torch.uint16), "e4m3": (torch.float8_e4m3fn, torch.uint8),
+                       "fp32": (torch.float32,), "int32": (torch.int32,)})
+    return _KINDS[name]
+
+
+def _stream_of(device, stream):
+    """The handle of a torch stream, of the device's current one where none is given."""
+    if stream is None:
+        import torch
+        stream = torch.cuda.current_stream(device)
+    return stream.cuda_stream
+
+
+def _empty(shape, dtype, device, stream):
+    """New device memory for work on `stream` (None: the current one): it must come from that stream's own pool, or
+    what was queued on another stream for its last user could still be running."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _rows(name, t, rows, cols, kind):
+    """Row pitch, in elements, of a [rows, cols] device tensor whose rows are dense."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError("%s: shape %s, wanted (%d, %d)" % (name, tuple(t.shape), rows, cols))
+    if t.dtype not in _kind(kind) or not t.is_cuda:
+        raise ValueError("%s: a device tensor of %s is wanted, not %s on %s" % (name, kind, t.dtype, t.device))
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("%s: the elements of a row are not next to each other" % name)
+    return t.stride(0) if rows > 1 else cols
+
+
+def _dense(name, t, shape, kind):
+    if tuple(t.shape) != shape or t.dtype not in _kind(kind) or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError("%s: a contiguous device tensor %s of %s is wanted, not %s of %s on %s" %
+                         (name, shape, kind, tuple(t.shape), t.dtype, t.device))
+
+
+class RmsNorm:
+    """Residual addition and root-mean-square norm with one weight vector (bf16, or int16 bf16 patterns).  x and out are
+    bf16 tensors or int16 patterns [rows, cols] whose rows may lie apart; the residual stream is of that kind or fp32."""
+
+    def __init__(self, weight, eps=1e-6):
+        _dense("weight", weight, (weight.numel(),), "bf16")
+        self.weight, self.eps, self.cols = weight, float(eps), weight.numel()
+
+    def n_groups(self, group):
+        return 1 if group <= 0 or group >= self.cols else -(-self.cols // group)
+
+    def _call(self, x, residual, residual_out, out, out_q, scales, group, stream):
+        rows, cols = x.shape[0], self.cols
+        x_pitch = _rows("x", x, rows, cols, "bf16")
+        res_pitch = res_out_pitch = cols
+        flags = 0
+        if residual is not None:
+            kind = "fp32" if residual.element_size() == 4 else "bf16"
+            flags = NORM_RESIDUAL_F32 if kind == "fp32" else 0
+            res_pitch = _rows("residual", residual, rows, cols, kind)
+            if residual_out is not None:
+                res_out_pitch = _rows("residual_out", residual_out, rows, cols, kind)
+        elif residual_out is not None:
+            raise ValueError("residual_out without a residual")
+        out_pitch = cols
+        if out is not None:
+            out_pitch = _rows("out", out, rows, cols, "bf16")
+        if out_q is not None:
+            q_pitch = _rows("out_q", out_q, rows, cols, "e4m3")
+            if out is not None and out_pitch != q_pitch:
+                raise ValueError("out and out_q have rows %d and %d apart" % (out_pitch, q_pitch))
+            out_pitch = q_pitch
+            _dense("scales", scales, (rows, self.n_groups(group)), "fp32")
+        zipmoe_add_rmsnorm(x, x_pitch, residual, res_pitch, residual_out, res_out_pitch, self.weight, rows, cols, self.eps,
+                           out, out_q, out_pitch, scales, group, flags, _stream_of(x.device, stream))
+
+    def add_norm(self, x, residual=None, residual_out=None, out=None, stream=None):
+        """Returns out [rows, cols] (bf16); residual_out (may be `residual` itself) gets x + residual."""
+        if out is None:
+            out = _empty(x.shape, x.dtype, x.device, stream)
+        self._call(x, residual, residual_out, out, None, None, 0, stream)
+        return out
+
+    def add_norm_8bit(self, x, residual=None, residual_out=None, out_q=None, scales=None, group=0, out=None, stream=None):
+        """Returns (out_q [rows, cols] e4m3, scales [rows, groups] fp32); `out`, if given, gets the bf16 rows as well."""
+        if out_q is None:
+            out_q = _empty(x.shape, _kind("e4m3")[0], x.device, stream)
+        if scales is None:
+            scales = _empty((x.shape[0], self.n_groups(group)), _kind("fp32")[0], x.device, stream)
+        self._call(x, residual, residual_out, out, out_q, scales, group, stream)
+        return out_q, scales
+
+
+class Router:
+    """The router of one layer: gate [n_experts, hidden] (bf16, or int16 patterns), bias [n_experts] fp32 or None."""
+
+    def __init__(self, gate, k, bias=None, renormalise=True):
+        import torch
+        self.n_experts, self.hidden = gate.shape
+        _dense("gate", gate, (self.n_experts, self.hidden), "bf16")
+        if bias is not None:
+            _dense("bias", bias, (self.n_experts,), "fp32")
+        self.gate, self.bias, self.k = gate, bias, int(k)
+        self.flags = 0 if renormalise else ROUTE_SOFTMAX_ALL
+        self.status = torch.zeros(1, dtype=torch.int32, device=gate.device)
+
+    def route(self, tokens, ids=None, weights=None, logits=None, stream=None):
+        """tokens [T, hidden] -> ids [T, k] int32, weights [T, k] fp32; logits, if given, gets [T, n_experts] fp32."""
+        T = tokens.shape[0]
+        pitch = _rows("tokens", tokens, T, self.hidden, "bf16")
+        if ids is None:
+            ids = _empty((T, self.k), _kind("int32")[0], tokens.device, stream)
+        else:
+            _dense("ids", ids, (T, self.k), "int32")
+        if weights is None:
+            weights = _empty((T, self.k), _kind("fp32")[0], tokens.device, stream)
+        else:
+            _dense("weights", weights, (T, self.k), "fp32")
+        if logits is not None:
+            _dense("logits", logits, (T, self.n_experts), "fp32")
+        zipmoe_route(tokens, T, pitch, self.gate, self.n_experts, self.hidden, self.bias, self.k, self.flags, ids, weights,
+                     logits, self.status, _stream_of(tokens.device, stream))
+        return ids, weights
+
+
+class ResidentExperts:
+    """Recovered experts of one layer: tensors[3*e + j] (j: 0 w1 [inter, hidden], 1 w3, 2 w2 [hidden, inter]) are dense
+    bf16 (or int16 pattern) device tensors, for example the slices of a DevicePlan.decode output."""
+
+    def __init__(self, tensors, hidden, inter):
+        import torch
+        if len(tensors) % 3 or not tensors:
+            raise ValueError("three tensors per expert are wanted")
+        for i, t in enumerate(tensors):
+            if t.numel() != hidden * inter:
+                raise ValueError("tensor %d: %d elements, wanted %d x %d" % (i, t.numel(), hidden, inter))
+            _dense("tensor %d" % i, t, tuple(t.shape), "bf16")
+        self.tensors = list(tensors)      # the experts' memory is theirs: keep it while the table points at it
+        self.device = tensors[0].device
+        self.hidden, self.inter = hidden, inter
+        self.table = torch.from_numpy(zipmoe_resident_experts_plan(self.tensors, len(tensors) // 3, hidden, inter)).to(self.device)
+        self.struct = ResidentExpertsStruct(len(tensors) // 3, hidden, inter, 0, self.table.data_ptr())
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._ws = {}
+
+    @classmethod
+    def from_decode(cls, plan, out, hidden, inter):
+        """The experts that one decode launch recovered: `plan` a DecodePlan over 3 * n_experts blobs, `out` its output."""
+        return cls([plan.tensor_slice(out, i) for i in range(len(plan.infos))], hidden, inter)
+
+    def ffn(self, tokens, topk_ids, topk_weights, out=None, stream=None):
+        """tokens [T, hidden] bf16 (or int16 patterns), topk_ids [T, k] int32, topk_weights [T, k] float32 or None: device
+        tensors.  Returns out [T, hidden].  The workspace is kept per size and stream, so calls on different streams may
+        overlap."""
+        T, k = topk_ids.shape
+        _dense("tokens", tokens, (T, self.hidden), "bf16")
+        _dense("topk_ids", topk_ids, (T, k), "int32")
+        if topk_weights is not None:
+            _dense("topk_weights", topk_weights, (T, k), "fp32")
+        s = _stream_of(self.device, stream)
+        ws = self._ws.get((T, k, s))
+        if ws is None:
+            n = zipmoe_expert_ffn_workspace_bytes(T, k, self.struct)
+            ws = self._ws[(T, k, s)] = _empty(max(n, 16), _kind("e4m3")[1], self.device, stream)
+        if out is None:
+            out = _empty((T, self.hidden), tokens.dtype, self.device, stream)
+        else:
+            _dense("out", out, (T, self.hidden), "bf16")
+        zipmoe_expert_ffn(tokens, T, topk_ids, topk_weights, k, self.struct, out, ws, ws.numel(), self.status, s)
         return out
