@@ -383,6 +383,11 @@ zipmoe_status zipmoe_resident_experts_plan(const uint16_t *const *tensors, uint3
 zipmoe_status zipmoe_expert_ffn_workspace_bytes(uint32_t T, uint32_t k, const zipmoe_resident_experts *experts,
                                                 uint64_t *workspace_bytes);
 
+/* Prepares a new workspace for zipmoe_expert_ffn (one small kernel on `stream`): once, before its first use.  Every
+ * call leaves the workspace ready for the next one, whatever the sizes of either.
+ * device out: workspace (16-byte aligned). */
+zipmoe_status zipmoe_expert_ffn_workspace_init(void *workspace, uint64_t workspace_bytes, zipmoe_stream stream);
+
 /* Expert execution on recovered weights (Section 3.3: the GPU work p_n of the tokens routed to expert n, for experts
  * found in pool F): what zipmoe_decode_expert_ffn computes, from bf16 tensors.  For every token t and choice j with
  * e = topk_ids[t, j]:
@@ -391,10 +396,12 @@ zipmoe_status zipmoe_expert_ffn_workspace_bytes(uint32_t T, uint32_t k, const zi
  * A negative id is no expert (zipmoe_route writes -1) and adds nothing; a token without experts gets zeros.  An id
  * of n_experts or more adds nothing either and sets status_word (code 1).  An expert listed twice by a token counts
  * with both weights.  Weights are read once for all tokens of the call, and only those of experts that have tokens.
+ * One cooperative launch on `stream` (its blocks wait for one another), asynchronous.
  * device in : tokens [T, hidden] bf16 patterns; topk_ids [T, k]; topk_weights [T, k] fp32 or NULL (= 1.0)
  * device out: out [T, hidden] bf16 patterns; workspace: scratch of at least zipmoe_expert_ffn_workspace_bytes,
- *             16-byte aligned (256 is better), not shared by calls that may overlap; status_word (nullable) as for
- *             zipmoe_decode.
+ *             16-byte aligned, prepared by zipmoe_expert_ffn_workspace_init (one that is not sets status_word to 1 and
+ *             leaves out as it was), not shared by calls that may overlap; status_word (nullable) as for zipmoe_decode:
+ *             code 3 when a wait ran out.
  * Limits: T <= 256, k <= 8 (ZIPMOE_ERR_UNSUPPORTED otherwise); T = 0 does nothing. */
 zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, const int32_t *topk_ids, const float *topk_weights,
                                 uint32_t k, const zipmoe_resident_experts *experts, uint16_t *out, void *workspace,

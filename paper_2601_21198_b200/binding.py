@@ -354,6 +354,8 @@ _lib.zipmoe_add_rmsnorm.argtypes = [_vp, _u64, _vp, _u64, _vp, _u64, _vp, _u32, 
 _lib.zipmoe_route.argtypes = [_vp, _u32, _u64, _vp, _u32, _u32, _vp, _u32, _u32, _vp, _vp, _vp, _vp, _vp]
 _lib.zipmoe_resident_experts_plan.argtypes = [ctypes.POINTER(_vp), _u32, _u32, _u32, _vp]
 _lib.zipmoe_expert_ffn_workspace_bytes.argtypes = [_u32, _u32, ctypes.POINTER(ResidentExpertsStruct), ctypes.POINTER(_u64)]
+_lib.zipmoe_expert_ffn_workspace_init.argtypes = [_vp, _u64, _vp]
+_lib.zipmoe_expert_ffn_workspace_init.restype = _int
 _lib.zipmoe_expert_ffn.argtypes = [_vp, _u32, _vp, _vp, _u32, ctypes.POINTER(ResidentExpertsStruct), _vp, _vp, _u64, _vp, _vp]
 for _f in ("zipmoe_add_rmsnorm", "zipmoe_route", "zipmoe_resident_experts_plan", "zipmoe_expert_ffn_workspace_bytes",
            "zipmoe_expert_ffn"):
@@ -392,6 +394,12 @@ def zipmoe_expert_ffn_workspace_bytes(T, k, experts):
     _check("zipmoe_expert_ffn_workspace_bytes",
            _lib.zipmoe_expert_ffn_workspace_bytes(T, k, ctypes.byref(experts), ctypes.byref(out)))
     return out.value
+
+
+def zipmoe_expert_ffn_workspace_init(workspace, workspace_bytes, stream=None):
+    """Prepares a new device workspace; once, before its first zipmoe_expert_ffn."""
+    _check("zipmoe_expert_ffn_workspace_init",
+           _lib.zipmoe_expert_ffn_workspace_init(_ptr(workspace), workspace_bytes, _ptr(stream)))
 
 
 def zipmoe_expert_ffn(tokens, T, topk_ids, topk_weights, k, experts, out, workspace, workspace_bytes, status_word=None,
@@ -706,7 +714,8 @@ class ResidentExperts:
         ws = self._ws.get((T, k, s))
         if ws is None:
             n = zipmoe_expert_ffn_workspace_bytes(T, k, self.struct)
-            ws = self._ws[(T, k, s)] = _empty(max(n, 16), _kind("e4m3")[1], self.device, stream)
+            ws = self._ws[(T, k, s)] = _empty(n, _kind("e4m3")[1], self.device, stream)
+            zipmoe_expert_ffn_workspace_init(ws, n, s)
         if out is None:
             out = _empty((T, self.hidden), tokens.dtype, self.device, stream)
         else:

@@ -1,84 +1,560 @@
 // The routed SwiGLU experts of a few tokens on recovered bf16 weights (pool F of the planner): the counterpart of
 // the fused decode + FFN for experts that need no decoding.
 //     g = W1 x,  u = W3 x,  h = bf16(SiLU(g) * u),  y = W2 h,  out[t] = bf16(sum_j w[t, j] * y)
-// Bound: the active experts' weights, 6 * hidden * inter bytes each, read once.
-// One warp per (choice, row): dot products in fp32.
+//
+// Bound: the active experts' weights, 6 * hidden * inter bytes each, read once.  At up to 256 tokens the products
+// are a fraction of what the tensor cores do in that time, so everything here serves one aim: that the weight stream
+// never pauses.  ONE persistent kernel, one block per SM, does the whole call:
+//   * A step is 32 KB of weights: 128 rows x 64 columns of W1 and of W3 (phase 0), or 256 rows x 64 columns of W2
+//     (phase 1), with the tokens' 64 columns.  A job is all steps of one expert and row block.  The steps of all jobs
+//     of a phase form one sequence, cut into equal shares, so every SM streams the same number of bytes whatever the
+//     experts and their sizes.
+//   * One thread feeds weights into a ring of shared-memory stages (TMA, 128-byte swizzle) and runs ahead as far as the
+//     ring allows, across jobs and across the phase boundary: W2 is under way while the last h is computed.
+//   * Another thread adds the activations of every step: in phase 0 the 64 columns of ALL tokens (a box of the token
+//     matrix - columns of the result that no choice asks for are never read back); in phase 1 the h rows of the
+//     expert's own tokens, which phase 0 stores in the order the tensor core wants them, so that they are one bulk copy.
+//   * One thread issues the MMAs: weights are the M = 128 operand, tokens the N operand, two accumulators (g and u of
+//     the same rows, or two row blocks of y) in tensor memory, double-buffered up to 128 tokens.
+//   * Four warps read the accumulators back.  A job inside one share goes straight on.  Of a job that is cut, each
+//     block stores its partial sums; in phase 0 the block that arrives last adds them in share order and goes on, in
+//     phase 1 the combination of the experts adds them.  No atomics on values: the same bits whatever the timing.
+// Blocks wait for one another twice (all h stored; all y stored), hence the cooperative launch.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <cstring>
 
 #include "zipmoe.h"
-#include "decode_device.cuh"
+#include "tensor_core.cuh"
 
 namespace zipmoe_dev {
 
+constexpr uint32_t kResMaxGrid = 256;
+constexpr uint32_t kResThreads = 256;
+constexpr uint32_t kResStageA = 32768;            // weights of a step
+constexpr uint32_t kResMagic = 0x5A464631u;       // marks a workspace that zipmoe_expert_ffn_workspace_init prepared
+
+// The workspace starts with this: zero when no call is running (every call leaves it so).
+struct ResidentSync {
+  uint32_t magic, pad0[31];
+  uint32_t h_done, pad1[31];      // blocks that have stored all their h
+  uint32_t y_done, pad2[31];      // blocks that have stored all their y
+  uint32_t exited, pad3[31];
+  uint32_t cut[kResMaxGrid];      // [c]: blocks that have stored their part of the phase 0 job cut at the end of block c's share
+};
+
 struct ResidentArgs {
-  const uint16_t *tokens;
   const int32_t *ids;
   const float *weights;
   const uint8_t *table;
   uint16_t *out;
-  uint16_t *h;         // [T * k][I]
+  ResidentSync *sync;
+  uint8_t *h;               // per active expert: [inter / 64][rows padded to 8][64] bf16, swizzled as the operand wants it
+  float *part;              // [block][2][2][T][128]: partial sums of a share's two cut jobs (0: begun by others, 1: begun here)
+  float *y;                 // [choices][H]: jobs that lie inside one share
   uint32_t *status;
-  uint32_t T, k, E, H, I;
+  uint64_t limit_ns;
+  uint32_t T, k, E, H, I, N, stages, acc_bufs, tmem_cols, extra_tx;
 };
 
-__device__ __forceinline__ const uint16_t *resident_tensor(const ResidentArgs &a, uint32_t tensor) {
-  return *reinterpret_cast<const uint16_t *const *>(a.table + (size_t)tensor * ZIPMOE_RESIDENT_ENTRY_BYTES);
+// How U units are shared out among P blocks: block c takes [c*U/P, (c+1)*U/P), and P <= U.
+__device__ __forceinline__ uint32_t share_first(uint32_t c, uint32_t U, uint32_t P) { return (uint32_t)((uint64_t)c * U / P); }
+__device__ __forceinline__ uint32_t share_of(uint32_t u, uint32_t U, uint32_t P) {
+  return (uint32_t)(((uint64_t)(u + 1) * P - 1) / U);
 }
-__device__ __forceinline__ float dot_row(const uint16_t *p, const uint16_t *q, uint32_t n, uint32_t lane) {
-  float sum = 0.f;
-  for (uint32_t c = lane * 8; c < n; c += 256) {
-    const uint4 a = *reinterpret_cast<const uint4 *>(p + c), b = *reinterpret_cast<const uint4 *>(q + c);
-    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      sum = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), sum);
-      sum = fmaf(__uint_as_float(x[i] & 0xFFFF0000u), __uint_as_float(y[i] & 0xFFFF0000u), sum);
+
+// One phase: jobs of KS steps, RB row blocks per active expert.
+struct Phase {
+  uint32_t KS, RB, U, P;
+};
+struct Piece {
+  uint32_t job, a, rb, s0, n;   // steps s0 .. s0 + n of one job: active expert a, row block rb
+};
+__device__ __forceinline__ bool next_piece(const Phase &p, uint32_t &u, uint32_t end, Piece &q) {
+  if (u >= end) return false;
+  q.job = u / p.KS;
+  q.a = q.job / p.RB;
+  q.rb = q.job - q.a * p.RB;
+  q.s0 = u - q.job * p.KS;
+  q.n = min(p.KS - q.s0, end - u);
+  u += q.n;
+  return true;
+}
+
+struct Active {
+  uint32_t e, n, h_row, slot;   // expert; its tokens; first row of its h block; first of its choices
+};
+
+__host__ __device__ inline uint32_t resident_control_bytes(uint32_t E, uint32_t T) {
+  return E * ((T + 31) / 32) * 4 + E * (uint32_t)sizeof(Active) + ((E * 2 + 15) / 16) * 16 + 256;
+}
+
+// The four reading warps give up together or not at all: their barriers count 128 threads.
+__device__ __forceinline__ bool all_agree(bool ok) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\t"
+      "barrier.cta.red.and.pred p, 1, 128, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r)
+      : "r"((uint32_t)ok)
+      : "memory");
+  return r != 0;
+}
+
+__device__ __forceinline__ float silu_times(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
+
+__global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __grid_constant__ CUtensorMap x_map, const ResidentArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x, G = gridDim.x;
+  const uint32_t W = (a.T + 31) / 32;
+  const uint32_t stage_bytes = kResStageA + a.N * 128;
+  // [stages, 1024-byte aligned][token masks of the experts][active experts][expert -> active][barriers ...]
+  uint8_t *stages = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint32_t *mask = reinterpret_cast<uint32_t *>(stages + a.stages * stage_bytes);
+  Active *act = reinterpret_cast<Active *>(mask + ((a.E * W + 3) & ~3u));
+  uint16_t *active_of = reinterpret_cast<uint16_t *>(act + a.E);
+  uint64_t *bars = reinterpret_cast<uint64_t *>(reinterpret_cast<uint8_t *>(active_of) + ((a.E * 2 + 15) / 16) * 16);
+  uint32_t *words = reinterpret_cast<uint32_t *>(bars + 2 * 8 + 4);
+  volatile uint32_t *dead = words + 1;
+  const uint32_t stage0 = smem_addr(stages);
+  const uint32_t full = smem_addr(bars), empty = full + 8 * 8, acc_full = full + 8 * 16, acc_empty = acc_full + 16;
+  const WaitLimit lim = {dead, a.status, a.limit_ns};
+
+  for (uint32_t i = tid; i < a.E * W; i += kResThreads) mask[i] = 0;
+  if (tid == 0) {
+    for (uint32_t s = 0; s < a.stages; ++s) {
+      mbar_init(full + 8 * s, 2);     // the weights' producer and the activations'
+      mbar_init(empty + 8 * s, 1);
+    }
+    for (uint32_t b = 0; b < 2; ++b) {
+      mbar_init(acc_full + 8 * b, 1);
+      mbar_init(acc_empty + 8 * b, 4);
+    }
+    *dead = 0;
+    prefetch_map(&x_map);
+  }
+  fence_barrier_init();
+  if (warp == 2) tmem_alloc(smem_addr(words), a.tmem_cols);
+  const bool prepared = a.sync->magic == kResMagic;
+  tc_before_sync();
+  __syncthreads();
+  tc_after_sync();
+  const uint32_t tmem = words[0];
+
+  // ---- which tokens every expert has: the same in every block ----
+  for (uint32_t i = tid; i < a.T * a.k; i += kResThreads) {
+    const int32_t e = __ldg(a.ids + i);
+    if (e >= 0 && e < (int32_t)a.E) {
+      const uint32_t t = i / a.k;
+      atomicOr(&mask[(uint32_t)e * W + (t >> 5)], 1u << (t & 31));
+    } else if (e >= 0) {
+      report(a.status, kStatusBadDescriptor);
     }
   }
+  __syncthreads();
+  if (warp == 0) {   // experts 8 * lane .. 8 * lane + 7
+    uint32_t cnt[8], n_act = 0, n_rows = 0, n_slots = 0;
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-  return sum;
-}
-
-// grid (ceil(I / 8), T * k)
-__global__ void __launch_bounds__(256) resident_gate_up_kernel(const ResidentArgs a) {
-  const uint32_t lane = threadIdx.x & 31, row = blockIdx.x * 8 + (threadIdx.x >> 5), slot = blockIdx.y;
-  const int32_t e = a.ids[slot];
-  if (e >= (int32_t)a.E) report(a.status, kStatusBadDescriptor);
-  if (e < 0 || e >= (int32_t)a.E || row >= a.I) return;
-  const uint16_t *x = a.tokens + (size_t)(slot / a.k) * a.H;
-  const float g = dot_row(resident_tensor(a, 3 * e) + (size_t)row * a.H, x, a.H, lane);
-  const float u = dot_row(resident_tensor(a, 3 * e + 1) + (size_t)row * a.H, x, a.H, lane);
-  if (lane == 0) a.h[(size_t)slot * a.I + row] = __bfloat16_as_ushort(__float2bfloat16_rn(g / (1.0f + __expf(-g)) * u));
-}
-
-// grid (ceil(H / 8), T)
-__global__ void __launch_bounds__(256) resident_down_kernel(const ResidentArgs a) {
-  const uint32_t lane = threadIdx.x & 31, row = blockIdx.x * 8 + (threadIdx.x >> 5), t = blockIdx.y;
-  if (row >= a.H) return;
-  float sum = 0.f;
-  for (uint32_t j = 0; j < a.k; ++j) {
-    const uint32_t slot = t * a.k + j;
-    const int32_t e = a.ids[slot];
-    if (e < 0 || e >= (int32_t)a.E) continue;
-    const float y = dot_row(resident_tensor(a, 3 * e + 2) + (size_t)row * a.I, a.h + (size_t)slot * a.I, a.I, lane);
-    sum += (a.weights ? a.weights[slot] : 1.0f) * y;
+    for (uint32_t i = 0; i < 8; ++i) {
+      const uint32_t e = 8 * lane + i;
+      cnt[i] = 0;
+      if (e < a.E)
+        for (uint32_t w = 0; w < W; ++w) cnt[i] += __popc(mask[e * W + w]);
+      n_act += cnt[i] ? 1 : 0;
+      n_rows += (cnt[i] + 7) & ~7u;
+      n_slots += cnt[i];
+    }
+    uint32_t at = n_act, row = n_rows, slot = n_slots;   // inclusive sums over the lanes
+    for (uint32_t d = 1; d < 32; d <<= 1) {
+      const uint32_t p = __shfl_up_sync(0xFFFFFFFFu, at, d), q = __shfl_up_sync(0xFFFFFFFFu, row, d), r = __shfl_up_sync(0xFFFFFFFFu, slot, d);
+      if (lane >= d) {
+        at += p;
+        row += q;
+        slot += r;
+      }
+    }
+    if (lane == 31) words[2] = at;
+    at -= n_act;
+    row -= n_rows;
+    slot -= n_slots;
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+      const uint32_t e = 8 * lane + i;
+      if (e < a.E && cnt[i]) {
+        act[at] = Active{e, cnt[i], row, slot};
+        active_of[e] = (uint16_t)at;
+        ++at;
+        row += (cnt[i] + 7) & ~7u;
+        slot += cnt[i];
+      }
+    }
   }
-  if (lane == 0) a.out[(size_t)t * a.H + row] = __bfloat16_as_ushort(__float2bfloat16_rn(sum));
+  __syncthreads();
+  const uint32_t n_active = prepared ? words[2] : 0;
+  Phase ph[2];
+  ph[0].KS = (a.H + 63) / 64;
+  ph[0].RB = (a.I + 127) / 128;
+  ph[1].KS = (a.I + 63) / 64;
+  ph[1].RB = (a.H + 255) / 256;
+#pragma unroll
+  for (uint32_t p = 0; p < 2; ++p) {
+    ph[p].U = n_active * ph[p].RB * ph[p].KS;
+    ph[p].P = min(G, ph[p].U);
+  }
+  // this block's share of a phase
+  auto first = [&](uint32_t p) { return cta < ph[p].P ? share_first(cta, ph[p].U, ph[p].P) : 0u; };
+  auto last = [&](uint32_t p) { return cta < ph[p].P ? share_first(cta + 1, ph[p].U, ph[p].P) : 0u; };
+
+  if (warp == 0 && lane == 0) {
+    // ---- weights ----
+    const uint64_t policy = policy_evict_first();
+    uint32_t st = 0, round = 0;
+    bool ok = true;
+    for (uint32_t p = 0; p < 2 && ok; ++p) {
+      uint32_t u = first(p), seen = 0xFFFFFFFFu;
+      const uint32_t end = last(p);
+      Piece q;
+      while (ok && next_piece(ph[p], u, end, q)) {
+        const uint32_t e = act[q.a].e;
+        const uint8_t *m0 = a.table + (size_t)(3 * e + 2 * p) * ZIPMOE_RESIDENT_ENTRY_BYTES;
+        const uint8_t *m1 = p == 0 ? m0 + ZIPMOE_RESIDENT_ENTRY_BYTES : m0;
+        const int32_t y0 = (int32_t)(q.rb * (p == 0 ? 128 : 256)), y1 = p == 0 ? y0 : y0 + 128;
+        if (seen != e) {
+          acquire_map(m0);
+          if (p == 0) acquire_map(m1);
+          seen = e;
+        }
+        for (uint32_t s = q.s0; s < q.s0 + q.n; ++s) {
+          if (round > 0 && !wait_bar(empty + 8 * st, (round - 1) & 1, lim)) {
+            ok = false;
+            break;
+          }
+          const uint32_t dst = stage0 + st * stage_bytes, bar = full + 8 * st;
+          mbar_expect_tx(bar, kResStageA + a.extra_tx);
+          tma_load_2d(dst, m0, (int32_t)(s * 64), y0, bar, policy);
+          tma_load_2d(dst + 16384, m1, (int32_t)(s * 64), y1, bar, policy);
+          if (++st == a.stages) {
+            st = 0;
+            ++round;
+          }
+        }
+      }
+    }
+  } else if (warp == 1 && lane == 0) {
+    // ---- activations ----
+    const uint64_t policy = policy_evict_last();
+    uint32_t st = 0, round = 0;
+    bool ok = true;
+    for (uint32_t p = 0; p < 2 && ok; ++p) {
+      uint32_t u = first(p);
+      const uint32_t end = last(p);
+      if (p == 1 && u < end) {
+        ok = wait_count(&a.sync->h_done, ph[0].P, lim);
+        fence_async_all();       // what other blocks stored is now read by the copy engine
+      }
+      Piece q;
+      while (ok && next_piece(ph[p], u, end, q)) {
+        const uint32_t rows = (act[q.a].n + 7) & ~7u;
+        const uint8_t *h = a.h + ((size_t)act[q.a].h_row * ph[1].KS) * 128;
+        for (uint32_t s = q.s0; s < q.s0 + q.n; ++s) {
+          if (round > 0 && !wait_bar(empty + 8 * st, (round - 1) & 1, lim)) {
+            ok = false;
+            break;
+          }
+          const uint32_t dst = stage0 + st * stage_bytes + kResStageA, bar = full + 8 * st;
+          if (p == 0) {
+            mbar_expect_tx(bar, a.N * 128);
+            tma_load_2d(dst, &x_map, (int32_t)(s * 64), 0, bar, policy);
+          } else {
+            mbar_expect_tx(bar, rows * 128);
+            bulk_load(dst, h + (size_t)s * rows * 128, rows * 128, bar, policy);
+          }
+          if (++st == a.stages) {
+            st = 0;
+            ++round;
+          }
+        }
+      }
+    }
+  } else if (warp == 2 && lane == 0) {
+    // ---- MMAs ----
+    uint32_t st = 0, round = 0, piece = 0;
+    bool ok = true;
+    for (uint32_t p = 0; p < 2 && ok; ++p) {
+      uint32_t u = first(p);
+      const uint32_t end = last(p);
+      Piece q;
+      while (ok && next_piece(ph[p], u, end, q)) {
+        const uint32_t b = piece % a.acc_bufs, use = piece / a.acc_bufs;
+        if (use > 0 && !wait_bar(acc_empty + 8 * b, (use - 1) & 1, lim)) {
+          ok = false;
+          break;
+        }
+        tc_after_sync();
+        // columns: all tokens (phase 0), or the expert's own (phase 1; the rows after them hold what was there before,
+        // and give columns that nobody reads)
+        const uint32_t idesc = bf16_idesc(p == 0 ? a.N : (act[q.a].n + 15) & ~15u);
+        const uint32_t d0 = tmem + b * 2 * a.N, d1 = d0 + a.N;
+        for (uint32_t s = 0; s < q.n; ++s) {
+          if (!wait_bar(full + 8 * st, round & 1, lim)) {
+            ok = false;
+            break;
+          }
+          tc_after_sync();
+          const uint32_t at = stage0 + st * stage_bytes;
+          const uint64_t a0 = swizzled_desc(at), a1 = swizzled_desc(at + 16384), bd = swizzled_desc(at + kResStageA);
+#pragma unroll
+          for (uint32_t j = 0; j < 4; ++j) {
+            tc_mma(d0, a0 + 2 * j, bd + 2 * j, idesc, s > 0 || j > 0);
+            tc_mma(d1, a1 + 2 * j, bd + 2 * j, idesc, s > 0 || j > 0);
+          }
+          tc_commit(empty + 8 * st);
+          if (++st == a.stages) {
+            st = 0;
+            ++round;
+          }
+        }
+        if (ok) tc_commit(acc_full + 8 * b);
+        ++piece;
+      }
+    }
+  } else if (warp >= 4) {
+    // ---- accumulators back; thread = one row of the job's 128 (twice) ----
+    const uint32_t w = warp - 4, row = 32 * w + lane, etid = tid - 128;
+    uint32_t piece = 0;
+    bool ok = true;
+    for (uint32_t p = 0; p < 2 && ok; ++p) {
+      uint32_t u = first(p);
+      const uint32_t end = last(p);
+      Piece q;
+      while (ok && next_piece(ph[p], u, end, q)) {
+        const uint32_t b = piece % a.acc_bufs, use = piece / a.acc_bufs;
+        ++piece;
+        const Active ex = act[q.a];
+        const bool whole = q.n == ph[p].KS;
+        float *mine = a.part + ((size_t)cta * 2 + (q.s0 > 0 ? 0 : 1)) * (2 * a.T * 128) + row;
+        // a finished pair of sums of the expert's i-th token
+        const uint32_t rows = (ex.n + 7) & ~7u, ir = q.rb * 128 + row;
+        uint8_t *h = a.h + ((size_t)ex.h_row * ph[1].KS + (size_t)(ir >> 6) * rows) * 128 + (ir & 7) * 2;
+        const uint32_t chunk = (ir & 63) >> 3;
+        auto finish = [&](uint32_t i, float v0, float v1) {
+          if (p == 0) {
+            if (ir < ph[1].KS * 64)     // (rows between inter and the next multiple of 64 are zeros: W2 has no columns there)
+              *reinterpret_cast<uint16_t *>(h + i * 128 + ((chunk ^ (i & 7)) << 4)) =
+                  ir < a.I ? __bfloat16_as_ushort(__float2bfloat16_rn(silu_times(v0, v1))) : (uint16_t)0;
+          } else {
+            float *y = a.y + (size_t)(ex.slot + i) * a.H;
+            const uint32_t c = q.rb * 256 + row;
+            if (c < a.H) y[c] = v0;
+            if (c + 128 < a.H) y[c + 128] = v1;
+          }
+        };
+        auto emit = [&](uint32_t i, float v0, float v1) {
+          if (whole) {
+            finish(i, v0, v1);
+          } else {
+            mine[(size_t)i * 128] = v0;
+            mine[(size_t)(a.T + i) * 128] = v1;
+          }
+        };
+        ok = all_agree(wait_bar(acc_full + 8 * b, use & 1, lim));
+        if (!ok) break;
+        tc_after_sync();
+        const uint32_t d0 = tmem + ((32 * w) << 16) + b * 2 * a.N, d1 = d0 + a.N;
+        uint32_t i = 0;
+        const uint32_t cols = p == 0 ? a.T : ex.n;
+        for (uint32_t c = 0; c < cols; c += 8) {
+          const uint32_t want = p == 0 ? (mask[ex.e * W + (c >> 5)] >> (c & 31)) & 0xFFu : (cols - c >= 8 ? 0xFFu : (1u << (cols - c)) - 1);
+          if (want == 0) continue;
+          uint32_t v0[8], v1[8];
+          tmem_load8(d0 + c, v0);
+          tmem_load8(d1 + c, v1);
+          tmem_wait();
+#pragma unroll
+          for (uint32_t n = 0; n < 8; ++n)
+            if ((want >> n) & 1) emit(i++, __uint_as_float(v0[n]), __uint_as_float(v1[n]));
+        }
+        tc_before_sync();
+        __syncwarp();
+        if (lane == 0) arrive(acc_empty + 8 * b);
+        if (whole || p == 1) continue;
+        // a job of phase 0 that is cut: the block that stores its part last adds all parts, in share order
+        const uint32_t c0 = share_of(q.job * ph[0].KS, ph[0].U, ph[0].P);
+        const uint32_t c1 = share_of(q.job * ph[0].KS + ph[0].KS - 1, ph[0].U, ph[0].P);
+        __threadfence();
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (etid == 0) {
+          words[3] = atomicAdd(&a.sync->cut[c0], 1u) == c1 - c0;
+          __threadfence();
+        }
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (words[3]) {
+          for (uint32_t n0 = 0; n0 < ex.n; n0 += 4) {
+            float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
+            for (uint32_t c = c0; c <= c1; ++c) {
+              const float *part = a.part + ((size_t)c * 2 + (c == c0 ? 1 : 0)) * (2 * a.T * 128) + row;
+#pragma unroll
+              for (uint32_t n = 0; n < 4; ++n)
+                if (n0 + n < ex.n) {
+                  s0[n] += __ldcg(part + (size_t)(n0 + n) * 128);
+                  s1[n] += __ldcg(part + (size_t)(a.T + n0 + n) * 128);
+                }
+            }
+#pragma unroll
+            for (uint32_t n = 0; n < 4; ++n)
+              if (n0 + n < ex.n) finish(n0 + n, s0[n], s1[n]);
+          }
+        }
+      }
+      // everything this block stores in the phase is out: tell the others
+      if (ok && cta < ph[p].P) {
+        __threadfence();
+        if (p == 0) fence_async_all();
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (etid == 0) add_release(p == 0 ? &a.sync->h_done : &a.sync->y_done, 1u);
+      }
+    }
+  }
+  __syncwarp();
+  tc_before_sync();
+  __syncthreads();
+  tc_after_sync();
+  if (*dead)   // let the copies and MMAs that this block has under way end before its memory goes to somebody else
+    for (uint32_t i = 0; i < 200; ++i) __nanosleep(1000);
+  if (warp == 2) tmem_free(tmem, a.tmem_cols);
+  if (tid == 0 && !*dead) wait_count(&a.sync->y_done, ph[1].P, lim);
+  __syncthreads();
+
+  // ---- out[t] = sum over the token's choices; 8 lanes per 4 columns, one per choice ----
+  if (!*dead && prepared) {
+    const uint32_t j = lane & 7, vecs = a.H / 4;
+    const uint64_t items = (uint64_t)a.T * vecs;
+    const uint32_t per_block = kResThreads / 8;
+    for (uint64_t it0 = (uint64_t)cta * per_block; it0 < items; it0 += (uint64_t)G * per_block) {
+      const uint64_t it = it0 + (tid >> 3);
+      float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+      uint32_t t = 0, c = 0;
+      if (it < items) {
+        t = (uint32_t)(it / vecs);
+        c = (uint32_t)(it - (uint64_t)t * vecs) * 4;
+        const int32_t e = j < a.k ? __ldg(a.ids + t * a.k + j) : -1;
+        if (e >= 0 && e < (int32_t)a.E) {
+          const uint32_t ai = active_of[e];
+          uint32_t i = __popc(mask[e * W + (t >> 5)] & ((1u << (t & 31)) - 1));
+          for (uint32_t w = 0; w < (t >> 5); ++w) i += __popc(mask[e * W + w]);
+          const uint32_t u0 = (ai * ph[1].RB + c / 256) * ph[1].KS;
+          const uint32_t c0 = share_of(u0, ph[1].U, ph[1].P), c1 = share_of(u0 + ph[1].KS - 1, ph[1].U, ph[1].P);
+          if (c0 == c1) {
+            s = __ldcg(reinterpret_cast<const float4 *>(a.y + (size_t)(act[ai].slot + i) * a.H + c));
+          } else {
+            for (uint32_t b = c0; b <= c1; ++b) {
+              const float4 v = __ldcg(reinterpret_cast<const float4 *>(
+                  a.part + ((size_t)b * 2 + (b == c0 ? 1 : 0)) * (2 * a.T * 128) + (size_t)(((c >> 7) & 1) * a.T + i) * 128 + (c & 127)));
+              s.x += v.x;
+              s.y += v.y;
+              s.z += v.z;
+              s.w += v.w;
+            }
+          }
+          const float wt = a.weights ? __ldg(a.weights + t * a.k + j) : 1.0f;
+          s.x *= wt;
+          s.y *= wt;
+          s.z *= wt;
+          s.w *= wt;
+        }
+      }
+#pragma unroll
+      for (int d = 4; d > 0; d >>= 1) {
+        s.x += __shfl_xor_sync(0xFFFFFFFFu, s.x, d);
+        s.y += __shfl_xor_sync(0xFFFFFFFFu, s.y, d);
+        s.z += __shfl_xor_sync(0xFFFFFFFFu, s.z, d);
+        s.w += __shfl_xor_sync(0xFFFFFFFFu, s.w, d);
+      }
+      if (it < items && j == 0) {
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(s.x, s.y), hi = __floats2bfloat162_rn(s.z, s.w);
+        *reinterpret_cast<uint2 *>(a.out + (size_t)t * a.H + c) =
+            make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
+      }
+    }
+  }
+  __syncthreads();
+  if (tid == 0) {
+    if (!prepared) report(a.status, kStatusBadDescriptor);
+    if (prepared) {
+      __threadfence();
+      if (atomicAdd(&a.sync->exited, 1u) == G - 1) {   // the last block leaves the counters as it found them
+        for (uint32_t c = 0; c < kResMaxGrid; ++c) a.sync->cut[c] = 0;
+        a.sync->h_done = 0;
+        a.sync->y_done = 0;
+        a.sync->exited = 0;
+      }
+    }
+  }
+}
+
+__global__ void resident_init_kernel(ResidentSync *s) {
+  uint32_t *w = reinterpret_cast<uint32_t *>(s);
+  for (uint32_t i = threadIdx.x; i < sizeof(ResidentSync) / 4; i += blockDim.x) w[i] = i == 0 ? kResMagic : 0u;
 }
 
 }  // namespace zipmoe_dev
 
 namespace {
+
 constexpr uint32_t kResidentMaxT = 256, kResidentMaxK = 8, kResidentMaxExperts = 256, kResidentMaxDim = 32768;
 bool dims_ok(uint32_t E, uint32_t H, uint32_t I) {
   return E > 0 && E <= kResidentMaxExperts && H > 0 && I > 0 && H % 8 == 0 && I % 8 == 0 && H <= kResidentMaxDim &&
          I <= kResidentMaxDim;
 }
+
+struct ResidentDevice {
+  int sms = 0;
+  bool ready = false;
+};
+ResidentDevice g_resident_dev[64];
+
+// SMs of the current device; 148 where there is none (a host-only size query)
+uint32_t resident_grid() {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < 64) {
+    if (g_resident_dev[dev].sms == 0 && cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess)
+      g_resident_dev[dev].sms = sms;
+    if (g_resident_dev[dev].sms > 0) return std::min<uint32_t>((uint32_t)g_resident_dev[dev].sms, zipmoe_dev::kResMaxGrid);
+  }
+  (void)cudaGetLastError();   // no device: not an error for a size query
+  return 148;
+}
+
+struct ResidentPlan {
+  uint32_t grid, N, stages, acc_bufs, tmem_cols, smem;
+  uint64_t off_h, off_part, off_y, total;
+};
+
+zipmoe_status resident_plan(uint32_t T, uint32_t k, const zipmoe_resident_experts *ex, ResidentPlan *p) {
+  if (T > kResidentMaxT || k == 0 || k > kResidentMaxK || !dims_ok(ex->n_experts, ex->hidden, ex->inter))
+    return ZIPMOE_ERR_UNSUPPORTED;
+  const uint64_t E = ex->n_experts, H = ex->hidden, I = ex->inter;
+  p->grid = resident_grid();
+  p->N = std::max(16u, (T + 15) / 16 * 16);
+  p->acc_bufs = p->N <= 128 ? 2 : 1;     // two accumulators of N columns each, of the 512 there are
+  p->tmem_cols = 32;
+  while (p->tmem_cols < p->acc_bufs * 2 * p->N) p->tmem_cols <<= 1;
+  const uint32_t control = zipmoe_dev::resident_control_bytes(ex->n_experts, T) + 1024, stage = zipmoe_dev::kResStageA + p->N * 128;
+  p->stages = std::min(8u, (227u * 1024u - control) / stage);
+  p->smem = control + p->stages * stage;
+  auto up = [](uint64_t v) { return (v + 255) / 256 * 256; };
+  const uint64_t choices = (uint64_t)T * k, rows = choices + 7 * std::min(E, choices);
+  uint64_t at = up(sizeof(zipmoe_dev::ResidentSync));
+  p->off_h = at; at = up(at + rows * ((I + 63) / 64) * 128);
+  p->off_part = at; at = up(at + (uint64_t)p->grid * 2 * 2 * T * 128 * 4);
+  p->off_y = at; at = up(at + choices * H * 4);
+  p->total = at;
+  return ZIPMOE_OK;
+}
+
 }  // namespace
 
 extern "C" zipmoe_status zipmoe_resident_experts_plan(const uint16_t *const *tensors, uint32_t n_experts, uint32_t hidden,
@@ -87,19 +563,32 @@ extern "C" zipmoe_status zipmoe_resident_experts_plan(const uint16_t *const *ten
   if (!tensors || !table) return ZIPMOE_ERR_INVALID_ARG;
   for (uint32_t i = 0; i < 3 * n_experts; ++i)
     if (!tensors[i] || (reinterpret_cast<uintptr_t>(tensors[i]) & 15)) return ZIPMOE_ERR_INVALID_ARG;
-  std::memset(table, 0, (size_t)3 * n_experts * ZIPMOE_RESIDENT_ENTRY_BYTES);
-  for (uint32_t i = 0; i < 3 * n_experts; ++i)
-    std::memcpy(static_cast<uint8_t *>(table) + (size_t)i * ZIPMOE_RESIDENT_ENTRY_BYTES, &tensors[i], sizeof(tensors[i]));
+  static_assert(sizeof(CUtensorMap) == ZIPMOE_RESIDENT_ENTRY_BYTES, "an entry is a tensor map");
+  for (uint32_t i = 0; i < 3 * n_experts; ++i) {
+    CUtensorMap map;
+    const uint32_t rows = i % 3 < 2 ? inter : hidden, cols = i % 3 < 2 ? hidden : inter;
+    if (!zipmoe_host::make_bf16_map(&map, tensors[i], rows, cols, cols, 128, true)) return ZIPMOE_ERR_CUDA;
+    std::memcpy(static_cast<uint8_t *>(table) + (size_t)i * ZIPMOE_RESIDENT_ENTRY_BYTES, &map, sizeof(map));
+  }
   return ZIPMOE_OK;
 }
 
 extern "C" zipmoe_status zipmoe_expert_ffn_workspace_bytes(uint32_t T, uint32_t k, const zipmoe_resident_experts *ex,
                                                            uint64_t *workspace_bytes) {
   if (!ex || !workspace_bytes) return ZIPMOE_ERR_INVALID_ARG;
-  if (T > kResidentMaxT || k == 0 || k > kResidentMaxK || !dims_ok(ex->n_experts, ex->hidden, ex->inter))
-    return ZIPMOE_ERR_UNSUPPORTED;
-  *workspace_bytes = (uint64_t)T * k * ex->inter * 2;
+  ResidentPlan p;
+  const zipmoe_status rc = resident_plan(T, k, ex, &p);
+  if (rc != ZIPMOE_OK) return rc;
+  *workspace_bytes = p.total;
   return ZIPMOE_OK;
+}
+
+extern "C" zipmoe_status zipmoe_expert_ffn_workspace_init(void *workspace, uint64_t workspace_bytes, zipmoe_stream stream) {
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)) return ZIPMOE_ERR_INVALID_ARG;
+  if (workspace_bytes < sizeof(zipmoe_dev::ResidentSync)) return ZIPMOE_ERR_BUFFER_TOO_SMALL;
+  zipmoe_dev::resident_init_kernel<<<1, 256, 0, reinterpret_cast<cudaStream_t>(stream)>>>(
+      static_cast<zipmoe_dev::ResidentSync *>(workspace));
+  return cudaGetLastError() == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
 }
 
 extern "C" zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, const int32_t *topk_ids,
@@ -108,31 +597,61 @@ extern "C" zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, c
                                            uint32_t *status_word, zipmoe_stream stream_) {
   using namespace zipmoe_dev;
   zipmoe_host::TraceRange trace("zipmoe_expert_ffn");
-  uint64_t need = 0;
-  const zipmoe_status rc = zipmoe_expert_ffn_workspace_bytes(T, k, ex, &need);
+  if (!ex) return ZIPMOE_ERR_INVALID_ARG;
+  ResidentPlan p;
+  const zipmoe_status rc = resident_plan(T, k, ex, &p);
   if (rc != ZIPMOE_OK) return rc;
   if (T == 0) return ZIPMOE_OK;
   if (!tokens || !topk_ids || !out || !workspace || !ex->table) return ZIPMOE_ERR_INVALID_ARG;
-  if (workspace_bytes < need) return ZIPMOE_ERR_BUFFER_TOO_SMALL;
   if (((reinterpret_cast<uintptr_t>(tokens) | reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(workspace)) & 15) ||
       (reinterpret_cast<uintptr_t>(ex->table) & 63) ||
       ((reinterpret_cast<uintptr_t>(topk_ids) | reinterpret_cast<uintptr_t>(topk_weights) | reinterpret_cast<uintptr_t>(status_word)) & 3))
     return ZIPMOE_ERR_INVALID_ARG;
-  cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
+  if (workspace_bytes < p.total) return ZIPMOE_ERR_BUFFER_TOO_SMALL;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return ZIPMOE_ERR_CUDA;
+  if (!g_resident_dev[dev].ready) {
+    int major = 0;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) return ZIPMOE_ERR_CUDA;
+    if (major != 10) return ZIPMOE_ERR_UNSUPPORTED;
+    if (cudaFuncSetAttribute(resident_ffn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024) != cudaSuccess)
+      return ZIPMOE_ERR_CUDA;
+    g_resident_dev[dev].ready = true;
+  }
+  CUtensorMap x_map;
+  if (!zipmoe_host::make_bf16_map(&x_map, tokens, T, ex->hidden, ex->hidden, p.N, false)) return ZIPMOE_ERR_CUDA;
+  uint8_t *ws = static_cast<uint8_t *>(workspace);
   ResidentArgs a;
-  a.tokens = tokens;
   a.ids = topk_ids;
   a.weights = topk_weights;
   a.table = static_cast<const uint8_t *>(ex->table);
   a.out = out;
-  a.h = static_cast<uint16_t *>(workspace);
+  a.sync = reinterpret_cast<ResidentSync *>(ws);
+  a.h = ws + p.off_h;
+  a.part = reinterpret_cast<float *>(ws + p.off_part);
+  a.y = reinterpret_cast<float *>(ws + p.off_y);
   a.status = status_word;
+  uint32_t tries = 0;
+  zipmoe_host::wait_fault_setting(&a.extra_tx, &tries);
+  a.limit_ns = tries < zipmoe_host::kWaitTries ? 1000000ull : 1000000000ull;   // (1 ms in the tests of the limit)
   a.T = T;
   a.k = k;
   a.E = ex->n_experts;
   a.H = ex->hidden;
   a.I = ex->inter;
-  resident_gate_up_kernel<<<dim3((a.I + 7) / 8, T * k), 256, 0, stream>>>(a);
-  resident_down_kernel<<<dim3((a.H + 7) / 8, T), 256, 0, stream>>>(a);
-  return cudaGetLastError() == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
+  a.N = p.N;
+  a.stages = p.stages;
+  a.acc_bufs = p.acc_bufs;
+  a.tmem_cols = p.tmem_cols;
+  cudaLaunchAttribute together;
+  together.id = cudaLaunchAttributeCooperative;
+  together.val.cooperative = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.stream = reinterpret_cast<cudaStream_t>(stream_);
+  cfg.attrs = &together;
+  cfg.numAttrs = 1;
+  cfg.gridDim = dim3(p.grid);
+  cfg.blockDim = dim3(kResThreads);
+  cfg.dynamicSmemBytes = p.smem;
+  return cudaLaunchKernelEx(&cfg, resident_ffn_kernel, x_map, a) == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
 }
