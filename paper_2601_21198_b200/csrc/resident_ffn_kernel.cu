@@ -11,11 +11,14 @@
 //     experts and their sizes.
 //   * One thread feeds weights into a ring of shared-memory stages (TMA, 128-byte swizzle) and runs ahead as far as the
 //     ring allows, across jobs and across the phase boundary: W2 is under way while the last h is computed.
-//   * Another thread adds the activations of every step: in phase 0 the 64 columns of ALL tokens (a box of the token
-//     matrix - columns of the result that no choice asks for are never read back); in phase 1 the h rows of the
-//     expert's own tokens, which phase 0 stores in the order the tensor core wants them, so that they are one bulk copy.
-//   * One thread issues the MMAs: weights are the M = 128 operand, tokens the N operand, two accumulators (g and u of
-//     the same rows, or two row blocks of y) in tensor memory, double-buffered up to 128 tokens.
+//   * Another thread adds the activations of every step, 64 columns of the expert's own tokens: in phase 0 gathered from
+//     the token matrix four rows at a time (few tokens), or, once all blocks have packed the tokens in the order the
+//     tensor core wants them, one bulk copy; in phase 1 the tokens' h rows, which phase 0 stores in that order.
+//   * One thread issues the MMAs: weights are the M = 128 operand, the expert's tokens the N operand, two accumulators
+//     (g and u of the same rows, or two row blocks of y) in tensor memory, double-buffered where no expert has more
+//     than 128 tokens.
+//   * Every block works out the same routing lists for itself, and sizes its ring by the most tokens that an expert
+//     of this call has: few tokens, more stages.
 //   * Four warps read the accumulators back.  A job inside one share goes straight on.  Of a job that is cut, each
 //     block stores its partial sums; in phase 0 the block that arrives last adds them in share order and goes on, in
 //     phase 1 the combination of the experts adds them.  No atomics on values: the same bits whatever the timing.
@@ -35,11 +38,18 @@ namespace zipmoe_dev {
 constexpr uint32_t kResMaxGrid = 256;
 constexpr uint32_t kResThreads = 256;
 constexpr uint32_t kResStageA = 32768;            // weights of a step
+constexpr uint32_t kResMaxStages = 8;
+#ifndef ZIPMOE_GATHER_ROWS
+#define ZIPMOE_GATHER_ROWS 16
+#endif
+constexpr uint32_t kResGatherRows = ZIPMOE_GATHER_ROWS;   // a gather of four rows takes the copy engine about 130 ns: up to this many
+                                         // tokens per expert they are gathered in every step, beyond it packed once
 constexpr uint32_t kResMagic = 0x5A464631u;       // marks a workspace that zipmoe_expert_ffn_workspace_init prepared
 
 // The workspace starts with this: zero when no call is running (every call leaves it so).
 struct ResidentSync {
   uint32_t magic, pad0[31];
+  uint32_t x_done, pad0b[31];     // blocks that have packed their part of the tokens
   uint32_t h_done, pad1[31];      // blocks that have stored all their h
   uint32_t y_done, pad2[31];      // blocks that have stored all their y
   uint32_t exited, pad3[31];
@@ -47,17 +57,19 @@ struct ResidentSync {
 };
 
 struct ResidentArgs {
+  const uint16_t *tokens;
   const int32_t *ids;
   const float *weights;
   const uint8_t *table;
   uint16_t *out;
   ResidentSync *sync;
+  uint8_t *x;               // the experts' tokens in the same order as h, [hidden / 64] columns (where tokens are packed)
   uint8_t *h;               // per active expert: [inter / 64][rows padded to 8][64] bf16, swizzled as the operand wants it
   float *part;              // [block][2][2][T][128]: partial sums of a share's two cut jobs (0: begun by others, 1: begun here)
   float *y;                 // [choices][H]: jobs that lie inside one share
   uint32_t *status;
   uint64_t limit_ns;
-  uint32_t T, k, E, H, I, N, stages, acc_bufs, tmem_cols, extra_tx;
+  uint32_t T, k, E, H, I, ring_bytes, tmem_cols, extra_tx;
 };
 
 // How U units are shared out among P blocks: block c takes [c*U/P, (c+1)*U/P), and P <= U.
@@ -88,8 +100,13 @@ struct Active {
   uint32_t e, n, h_row, slot;   // expert; its tokens; first row of its h block; first of its choices
 };
 
-__host__ __device__ inline uint32_t resident_control_bytes(uint32_t E, uint32_t T) {
-  return E * ((T + 31) / 32) * 4 + E * (uint32_t)sizeof(Active) + ((E * 2 + 15) / 16) * 16 + 256;
+// shared memory before the ring: [token masks of the experts][active experts][expert -> active][place of every choice
+// among its expert's tokens][tokens of the active experts, padded to 8 each][barriers and words]
+__host__ __device__ inline uint32_t pad16(uint32_t bytes) { return (bytes + 15) & ~15u; }
+__host__ __device__ inline uint32_t resident_rows(uint32_t E, uint32_t choices) { return choices + 7 * (E < choices ? E : choices); }
+__host__ __device__ inline uint32_t resident_control_bytes(uint32_t E, uint32_t T, uint32_t k) {
+  return pad16(E * ((T + 31) / 32) * 4) + E * (uint32_t)sizeof(Active) + pad16(E * 2) + pad16(T * k * 2) +
+         pad16(resident_rows(E, T * k) * 2) + 256;
 }
 
 // The four reading warps give up together or not at all: their barriers count 128 threads.
@@ -109,23 +126,30 @@ __device__ __forceinline__ float silu_times(float g, float u) { return g / (1.0f
 __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __grid_constant__ CUtensorMap x_map, const ResidentArgs a) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x, G = gridDim.x;
-  const uint32_t W = (a.T + 31) / 32;
-  const uint32_t stage_bytes = kResStageA + a.N * 128;
-  // [stages, 1024-byte aligned][token masks of the experts][active experts][expert -> active][barriers ...]
-  uint8_t *stages = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  uint32_t *mask = reinterpret_cast<uint32_t *>(stages + a.stages * stage_bytes);
-  Active *act = reinterpret_cast<Active *>(mask + ((a.E * W + 3) & ~3u));
-  uint16_t *active_of = reinterpret_cast<uint16_t *>(act + a.E);
-  uint64_t *bars = reinterpret_cast<uint64_t *>(reinterpret_cast<uint8_t *>(active_of) + ((a.E * 2 + 15) / 16) * 16);
-  uint32_t *words = reinterpret_cast<uint32_t *>(bars + 2 * 8 + 4);
+  const uint32_t W = (a.T + 31) / 32, choices = a.T * a.k, n_rows_max = resident_rows(a.E, choices);
+  uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint8_t *ctl = ring + a.ring_bytes;
+  uint32_t *mask = reinterpret_cast<uint32_t *>(ctl);
+  ctl += pad16(a.E * W * 4);
+  Active *act = reinterpret_cast<Active *>(ctl);
+  ctl += a.E * sizeof(Active);
+  uint16_t *active_of = reinterpret_cast<uint16_t *>(ctl);
+  ctl += pad16(a.E * 2);
+  uint16_t *place = reinterpret_cast<uint16_t *>(ctl);
+  ctl += pad16(choices * 2);
+  uint16_t *token = reinterpret_cast<uint16_t *>(ctl);
+  ctl += pad16(n_rows_max * 2);
+  uint64_t *bars = reinterpret_cast<uint64_t *>(ctl);
+  uint32_t *words = reinterpret_cast<uint32_t *>(bars + 2 * kResMaxStages + 4);   // tmem, dead, active, last, most
   volatile uint32_t *dead = words + 1;
-  const uint32_t stage0 = smem_addr(stages);
-  const uint32_t full = smem_addr(bars), empty = full + 8 * 8, acc_full = full + 8 * 16, acc_empty = acc_full + 16;
+  const uint32_t stage0 = smem_addr(ring);
+  const uint32_t full = smem_addr(bars), empty = full + 8 * kResMaxStages, acc_full = empty + 8 * kResMaxStages, acc_empty = acc_full + 16;
   const WaitLimit lim = {dead, a.status, a.limit_ns};
 
   for (uint32_t i = tid; i < a.E * W; i += kResThreads) mask[i] = 0;
+  for (uint32_t i = tid; i < n_rows_max; i += kResThreads) token[i] = 0;   // (the rows that fill up to 8 are token 0's)
   if (tid == 0) {
-    for (uint32_t s = 0; s < a.stages; ++s) {
+    for (uint32_t s = 0; s < kResMaxStages; ++s) {
       mbar_init(full + 8 * s, 2);     // the weights' producer and the activations'
       mbar_init(empty + 8 * s, 1);
     }
@@ -156,7 +180,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
   }
   __syncthreads();
   if (warp == 0) {   // experts 8 * lane .. 8 * lane + 7
-    uint32_t cnt[8], n_act = 0, n_rows = 0, n_slots = 0;
+    uint32_t cnt[8], n_act = 0, n_rows = 0, n_slots = 0, most = 0;
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
       const uint32_t e = 8 * lane + i;
@@ -166,7 +190,9 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
       n_act += cnt[i] ? 1 : 0;
       n_rows += (cnt[i] + 7) & ~7u;
       n_slots += cnt[i];
+      most = max(most, cnt[i]);
     }
+    most = __reduce_max_sync(0xFFFFFFFFu, most);
     uint32_t at = n_act, row = n_rows, slot = n_slots;   // inclusive sums over the lanes
     for (uint32_t d = 1; d < 32; d <<= 1) {
       const uint32_t p = __shfl_up_sync(0xFFFFFFFFu, at, d), q = __shfl_up_sync(0xFFFFFFFFu, row, d), r = __shfl_up_sync(0xFFFFFFFFu, slot, d);
@@ -176,7 +202,10 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
         slot += r;
       }
     }
-    if (lane == 31) words[2] = at;
+    if (lane == 31) {
+      words[2] = at;
+      words[4] = most;
+    }
     at -= n_act;
     row -= n_rows;
     slot -= n_slots;
@@ -193,7 +222,21 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
     }
   }
   __syncthreads();
+  for (uint32_t i = tid; i < choices; i += kResThreads) {
+    const int32_t e = __ldg(a.ids + i);
+    if (e < 0 || e >= (int32_t)a.E) continue;
+    const uint32_t t = i / a.k;
+    uint32_t at = __popc(mask[(uint32_t)e * W + (t >> 5)] & ((1u << (t & 31)) - 1));
+    for (uint32_t w = 0; w < (t >> 5); ++w) at += __popc(mask[(uint32_t)e * W + w]);
+    place[i] = (uint16_t)at;
+    token[act[active_of[e]].h_row + at] = (uint16_t)t;
+  }
+  __syncthreads();
   const uint32_t n_active = prepared ? words[2] : 0;
+  const bool packed = words[4] > kResGatherRows && n_active > 0;
+  const uint32_t N = max(16u, (words[4] + 15) & ~15u);       // the widest operand of this call
+  const uint32_t stage_bytes = kResStageA + N * 128, n_stages = min(kResMaxStages, a.ring_bytes / stage_bytes);
+  const uint32_t acc_bufs = N <= 128 ? 2 : 1;                // two accumulators of N columns each, of 512 columns
   Phase ph[2];
   ph[0].KS = (a.H + 63) / 64;
   ph[0].RB = (a.I + 127) / 128;
@@ -236,43 +279,46 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
           mbar_expect_tx(bar, kResStageA + a.extra_tx);
           tma_load_2d(dst, m0, (int32_t)(s * 64), y0, bar, policy);
           tma_load_2d(dst + 16384, m1, (int32_t)(s * 64), y1, bar, policy);
-          if (++st == a.stages) {
+          if (++st == n_stages) {
             st = 0;
             ++round;
           }
         }
       }
     }
-  } else if (warp == 1 && lane == 0) {
-    // ---- activations ----
+  } else if (warp == 1 && lane < kResGatherRows / 4) {
+    // ---- activations; where tokens are not packed, lane r gathers rows 4r .. 4r + 3 of the expert's ----
+    constexpr uint32_t kLanes = (1u << (kResGatherRows / 4)) - 1;
     const uint64_t policy = policy_evict_last();
     uint32_t st = 0, round = 0;
     bool ok = true;
     for (uint32_t p = 0; p < 2 && ok; ++p) {
       uint32_t u = first(p);
       const uint32_t end = last(p);
-      if (p == 1 && u < end) {
-        ok = wait_count(&a.sync->h_done, ph[0].P, lim);
+      if (u < end && (p == 1 || packed)) {
+        ok = __all_sync(kLanes, p == 1 ? wait_count(&a.sync->h_done, ph[0].P, lim) : wait_count(&a.sync->x_done, G, lim));
         fence_async_all();       // what other blocks stored is now read by the copy engine
       }
       Piece q;
       while (ok && next_piece(ph[p], u, end, q)) {
-        const uint32_t rows = (act[q.a].n + 7) & ~7u;
-        const uint8_t *h = a.h + ((size_t)act[q.a].h_row * ph[1].KS) * 128;
+        const uint32_t rows = (act[q.a].n + 7) & ~7u, first_row = act[q.a].h_row;
+        const uint8_t *src = (p == 0 ? a.x : a.h) + ((size_t)first_row * ph[p].KS) * 128;
+        int32_t tok[4];
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) tok[i] = 4 * lane < rows ? token[first_row + 4 * lane + i] : 0;
         for (uint32_t s = q.s0; s < q.s0 + q.n; ++s) {
-          if (round > 0 && !wait_bar(empty + 8 * st, (round - 1) & 1, lim)) {
-            ok = false;
-            break;
-          }
+          ok = __all_sync(kLanes, round == 0 || wait_bar(empty + 8 * st, (round - 1) & 1, lim));
+          if (!ok) break;
           const uint32_t dst = stage0 + st * stage_bytes + kResStageA, bar = full + 8 * st;
-          if (p == 0) {
-            mbar_expect_tx(bar, a.N * 128);
-            tma_load_2d(dst, &x_map, (int32_t)(s * 64), 0, bar, policy);
-          } else {
-            mbar_expect_tx(bar, rows * 128);
-            bulk_load(dst, h + (size_t)s * rows * 128, rows * 128, bar, policy);
+          if (lane == 0) mbar_expect_tx(bar, rows * 128);
+          __syncwarp(kLanes);
+          if (p == 0 && !packed) {
+            if (4 * lane < rows)
+              tma_gather4(dst + lane * 512, &x_map, (int32_t)(s * 64), tok[0], tok[1], tok[2], tok[3], bar, policy);
+          } else if (lane == 0) {
+            bulk_load(dst, src + (size_t)s * rows * 128, rows * 128, bar, policy);
           }
-          if (++st == a.stages) {
+          if (++st == n_stages) {
             st = 0;
             ++round;
           }
@@ -288,16 +334,15 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
       const uint32_t end = last(p);
       Piece q;
       while (ok && next_piece(ph[p], u, end, q)) {
-        const uint32_t b = piece % a.acc_bufs, use = piece / a.acc_bufs;
+        const uint32_t b = piece % acc_bufs, use = piece / acc_bufs;
         if (use > 0 && !wait_bar(acc_empty + 8 * b, (use - 1) & 1, lim)) {
           ok = false;
           break;
         }
         tc_after_sync();
-        // columns: all tokens (phase 0), or the expert's own (phase 1; the rows after them hold what was there before,
-        // and give columns that nobody reads)
-        const uint32_t idesc = bf16_idesc(p == 0 ? a.N : (act[q.a].n + 15) & ~15u);
-        const uint32_t d0 = tmem + b * 2 * a.N, d1 = d0 + a.N;
+        // columns: the expert's tokens (the rows after them hold what was there before, and give columns that nobody reads)
+        const uint32_t idesc = bf16_idesc((act[q.a].n + 15) & ~15u);
+        const uint32_t d0 = tmem + b * 2 * N, d1 = d0 + N;
         for (uint32_t s = 0; s < q.n; ++s) {
           if (!wait_bar(full + 8 * st, round & 1, lim)) {
             ok = false;
@@ -312,7 +357,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
             tc_mma(d1, a1 + 2 * j, bd + 2 * j, idesc, s > 0 || j > 0);
           }
           tc_commit(empty + 8 * st);
-          if (++st == a.stages) {
+          if (++st == n_stages) {
             st = 0;
             ++round;
           }
@@ -326,12 +371,30 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
     const uint32_t w = warp - 4, row = 32 * w + lane, etid = tid - 128;
     uint32_t piece = 0;
     bool ok = true;
+    if (packed) {
+      // 16 bytes of a token's row at a time, to where the tensor core's operand has them
+      const uint32_t per_row = ph[0].KS * 8, total = choices * per_row;
+      for (uint32_t v = cta * 128 + etid; v < total; v += G * 128) {
+        const uint32_t i = v / per_row, c = v - i * per_row, t = i / a.k;
+        const int32_t e = __ldg(a.ids + i);
+        if (e < 0 || e >= (int32_t)a.E) continue;
+        const Active ex = act[active_of[e]];
+        const uint32_t r = place[i], rows = (ex.n + 7) & ~7u;
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (c * 8 < a.H) x = __ldg(reinterpret_cast<const uint4 *>(a.tokens + (size_t)t * a.H + c * 8));
+        *reinterpret_cast<uint4 *>(a.x + ((size_t)ex.h_row * ph[0].KS + (size_t)(c >> 3) * rows + r) * 128 + (((c & 7) ^ (r & 7)) << 4)) = x;
+      }
+      __threadfence();
+      fence_async_all();
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      if (etid == 0) add_release(&a.sync->x_done, 1u);
+    }
     for (uint32_t p = 0; p < 2 && ok; ++p) {
       uint32_t u = first(p);
       const uint32_t end = last(p);
       Piece q;
       while (ok && next_piece(ph[p], u, end, q)) {
-        const uint32_t b = piece % a.acc_bufs, use = piece / a.acc_bufs;
+        const uint32_t b = piece % acc_bufs, use = piece / acc_bufs;
         ++piece;
         const Active ex = act[q.a];
         const bool whole = q.n == ph[p].KS;
@@ -363,19 +426,15 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
         ok = all_agree(wait_bar(acc_full + 8 * b, use & 1, lim));
         if (!ok) break;
         tc_after_sync();
-        const uint32_t d0 = tmem + ((32 * w) << 16) + b * 2 * a.N, d1 = d0 + a.N;
-        uint32_t i = 0;
-        const uint32_t cols = p == 0 ? a.T : ex.n;
-        for (uint32_t c = 0; c < cols; c += 8) {
-          const uint32_t want = p == 0 ? (mask[ex.e * W + (c >> 5)] >> (c & 31)) & 0xFFu : (cols - c >= 8 ? 0xFFu : (1u << (cols - c)) - 1);
-          if (want == 0) continue;
+        const uint32_t d0 = tmem + ((32 * w) << 16) + b * 2 * N, d1 = d0 + N;
+        for (uint32_t c = 0; c < ex.n; c += 8) {
           uint32_t v0[8], v1[8];
           tmem_load8(d0 + c, v0);
           tmem_load8(d1 + c, v1);
           tmem_wait();
 #pragma unroll
           for (uint32_t n = 0; n < 8; ++n)
-            if ((want >> n) & 1) emit(i++, __uint_as_float(v0[n]), __uint_as_float(v1[n]));
+            if (c + n < ex.n) emit(c + n, __uint_as_float(v0[n]), __uint_as_float(v1[n]));
         }
         tc_before_sync();
         __syncwarp();
@@ -443,8 +502,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
         const int32_t e = j < a.k ? __ldg(a.ids + t * a.k + j) : -1;
         if (e >= 0 && e < (int32_t)a.E) {
           const uint32_t ai = active_of[e];
-          uint32_t i = __popc(mask[e * W + (t >> 5)] & ((1u << (t & 31)) - 1));
-          for (uint32_t w = 0; w < (t >> 5); ++w) i += __popc(mask[e * W + w]);
+          const uint32_t i = place[t * a.k + j];
           const uint32_t u0 = (ai * ph[1].RB + c / 256) * ph[1].KS;
           const uint32_t c0 = share_of(u0, ph[1].U, ph[1].P), c1 = share_of(u0 + ph[1].KS - 1, ph[1].U, ph[1].P);
           if (c0 == c1) {
@@ -487,6 +545,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
       __threadfence();
       if (atomicAdd(&a.sync->exited, 1u) == G - 1) {   // the last block leaves the counters as it found them
         for (uint32_t c = 0; c < kResMaxGrid; ++c) a.sync->cut[c] = 0;
+        a.sync->x_done = 0;
         a.sync->h_done = 0;
         a.sync->y_done = 0;
         a.sync->exited = 0;
@@ -529,25 +588,26 @@ uint32_t resident_grid() {
 }
 
 struct ResidentPlan {
-  uint32_t grid, N, stages, acc_bufs, tmem_cols, smem;
-  uint64_t off_h, off_part, off_y, total;
+  uint32_t grid, tmem_cols, ring, smem;
+  uint64_t off_x, off_h, off_part, off_y, total;
 };
 
 zipmoe_status resident_plan(uint32_t T, uint32_t k, const zipmoe_resident_experts *ex, ResidentPlan *p) {
   if (T > kResidentMaxT || k == 0 || k > kResidentMaxK || !dims_ok(ex->n_experts, ex->hidden, ex->inter))
     return ZIPMOE_ERR_UNSUPPORTED;
-  const uint64_t E = ex->n_experts, H = ex->hidden, I = ex->inter;
+  const uint64_t H = ex->hidden, I = ex->inter;
   p->grid = resident_grid();
-  p->N = std::max(16u, (T + 15) / 16 * 16);
-  p->acc_bufs = p->N <= 128 ? 2 : 1;     // two accumulators of N columns each, of the 512 there are
+  // two accumulators for as many tokens as an expert can have, twice if they fit (the kernel goes by the call's own most)
+  const uint32_t N = std::max(16u, (T + 15) / 16 * 16);
   p->tmem_cols = 32;
-  while (p->tmem_cols < p->acc_bufs * 2 * p->N) p->tmem_cols <<= 1;
-  const uint32_t control = zipmoe_dev::resident_control_bytes(ex->n_experts, T) + 1024, stage = zipmoe_dev::kResStageA + p->N * 128;
-  p->stages = std::min(8u, (227u * 1024u - control) / stage);
-  p->smem = control + p->stages * stage;
+  while (p->tmem_cols < std::min(512u, 4 * N)) p->tmem_cols <<= 1;
+  const uint32_t control = zipmoe_dev::resident_control_bytes(ex->n_experts, T, k) + 1024;
+  p->ring = (227u * 1024u - control) & ~15u;
+  p->smem = control + p->ring;
   auto up = [](uint64_t v) { return (v + 255) / 256 * 256; };
-  const uint64_t choices = (uint64_t)T * k, rows = choices + 7 * std::min(E, choices);
+  const uint64_t choices = (uint64_t)T * k, rows = zipmoe_dev::resident_rows(ex->n_experts, T * k);
   uint64_t at = up(sizeof(zipmoe_dev::ResidentSync));
+  p->off_x = at; at = up(at + rows * ((H + 63) / 64) * 128);
   p->off_h = at; at = up(at + rows * ((I + 63) / 64) * 128);
   p->off_part = at; at = up(at + (uint64_t)p->grid * 2 * 2 * T * 128 * 4);
   p->off_y = at; at = up(at + choices * H * 4);
@@ -619,7 +679,7 @@ extern "C" zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, c
     g_resident_dev[dev].ready = true;
   }
   CUtensorMap x_map;
-  if (!zipmoe_host::make_bf16_map(&x_map, tokens, T, ex->hidden, ex->hidden, p.N, false)) return ZIPMOE_ERR_CUDA;
+  if (!zipmoe_host::make_bf16_map(&x_map, tokens, T, ex->hidden, ex->hidden, 1, false)) return ZIPMOE_ERR_CUDA;
   uint8_t *ws = static_cast<uint8_t *>(workspace);
   ResidentArgs a;
   a.ids = topk_ids;
@@ -627,6 +687,8 @@ extern "C" zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, c
   a.table = static_cast<const uint8_t *>(ex->table);
   a.out = out;
   a.sync = reinterpret_cast<ResidentSync *>(ws);
+  a.tokens = tokens;
+  a.x = ws + p.off_x;
   a.h = ws + p.off_h;
   a.part = reinterpret_cast<float *>(ws + p.off_part);
   a.y = reinterpret_cast<float *>(ws + p.off_y);
@@ -639,9 +701,7 @@ extern "C" zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, c
   a.E = ex->n_experts;
   a.H = ex->hidden;
   a.I = ex->inter;
-  a.N = p.N;
-  a.stages = p.stages;
-  a.acc_bufs = p.acc_bufs;
+  a.ring_bytes = p.ring;
   a.tmem_cols = p.tmem_cols;
   cudaLaunchAttribute together;
   together.id = cudaLaunchAttributeCooperative;
