@@ -5,24 +5,26 @@
 // Bound: the active experts' weights, 6 * hidden * inter bytes each, read once.  At up to 256 tokens the products
 // are a fraction of what the tensor cores do in that time, so everything here serves one aim: that the weight stream
 // never pauses.  ONE persistent kernel, one block per SM, does the whole call:
-//   * A step is 32 KB of weights: 128 rows x 64 columns of W1 and of W3 (phase 0), or 256 rows x 64 columns of W2
-//     (phase 1), with the tokens' 64 columns.  A job is all steps of one expert and row block.  The steps of all jobs
+//   * A step is 32 KB of weights: 128 rows x 64 columns of W1 and of W3 (gate/up), or 256 rows x 64 columns of W2
+//     (down), with the tokens' 64 columns.  A job is all steps of one expert and row block.  The steps of all jobs
 //     of a phase form one sequence, cut into equal shares, so every SM streams the same number of bytes whatever the
 //     experts and their sizes.
+//   * Phases: gate/up of the first half of the active experts, gate/up of the second half, down of the first, down of
+//     the second.  What the third needs was stored before the second began, so nobody waits between them.
 //   * One thread feeds weights into a ring of shared-memory stages (TMA, 128-byte swizzle) and runs ahead as far as the
-//     ring allows, across jobs and across the phase boundary: W2 is under way while the last h is computed.
-//   * Another thread adds the activations of every step, 64 columns of the expert's own tokens: in phase 0 gathered from
+//     ring allows, across jobs and phases.
+//   * Another warp adds the activations of every step, 64 columns of the expert's own tokens: for gate/up gathered from
 //     the token matrix four rows at a time (few tokens), or, once all blocks have packed the tokens in the order the
-//     tensor core wants them, one bulk copy; in phase 1 the tokens' h rows, which phase 0 stores in that order.
+//     tensor core wants them, one bulk copy; for down the tokens' h rows, which gate/up stores in that order.
 //   * One thread issues the MMAs: weights are the M = 128 operand, the expert's tokens the N operand, two accumulators
 //     (g and u of the same rows, or two row blocks of y) in tensor memory, double-buffered where no expert has more
 //     than 128 tokens.
-//   * Every block works out the same routing lists for itself, and sizes its ring by the most tokens that an expert
+//   * Every block works out the same routing lists for itself, and sizes its rings by the most tokens that an expert
 //     of this call has: few tokens, more stages.
-//   * Four warps read the accumulators back.  A job inside one share goes straight on.  Of a job that is cut, each
-//     block stores its partial sums; in phase 0 the block that arrives last adds them in share order and goes on, in
-//     phase 1 the combination of the experts adds them.  No atomics on values: the same bits whatever the timing.
-// Blocks wait for one another twice (all h stored; all y stored), hence the cooperative launch.
+//   * Eight warps read the accumulators back.  A job inside one share goes straight on.  Of a job that is cut, each
+//     block stores its partial sums; for gate/up the block that arrives last adds them in share order and goes on, for
+//     down the combination of the experts adds them.  No atomics on values: the same bits whatever the timing.
+// Blocks wait for one another (tokens packed, h stored, y stored), hence the cooperative launch.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -36,24 +38,31 @@
 namespace zipmoe_dev {
 
 constexpr uint32_t kResMaxGrid = 256;
-constexpr uint32_t kResThreads = 256;
-constexpr uint32_t kResStageA = 32768;            // weights of a step
+constexpr uint32_t kResReaders = 8;                         // warps that read accumulators back: two per 32 lanes of tensor memory
+constexpr uint32_t kResThreads = 128 + 32 * kResReaders;
+constexpr uint32_t kResStageA = 32768;                      // weights of a step
 constexpr uint32_t kResMaxStages = 8;
-#ifndef ZIPMOE_GATHER_ROWS
-#define ZIPMOE_GATHER_ROWS 16
+#ifndef ZIPMOE_RES_DEPTH
+#define ZIPMOE_RES_DEPTH 4
 #endif
-constexpr uint32_t kResGatherRows = ZIPMOE_GATHER_ROWS;   // a gather of four rows takes the copy engine about 130 ns: up to this many
-                                         // tokens per expert they are gathered in every step, beyond it packed once
-constexpr uint32_t kResMagic = 0x5A464631u;       // marks a workspace that zipmoe_expert_ffn_workspace_init prepared
+constexpr uint32_t kResInFlight = ZIPMOE_RES_DEPTH;
+constexpr uint32_t kResMagic = 0x5A464632u;                 // marks a workspace that zipmoe_expert_ffn_workspace_init prepared
+constexpr uint32_t kResGatherRows = 16;   // a gather of four rows takes the copy engine about 130 ns: up to this many tokens
+                                          // per expert they are gathered in every step, beyond it packed once
+#ifndef ZIPMOE_RES_TWO
+#define ZIPMOE_RES_TWO 64
+#endif
+constexpr uint32_t kResTwoGroupsT = ZIPMOE_RES_TWO;   // above, a call is long enough for the wait between gate/up and down not to show,
+                                          // and the partial sums of four phases would take too much memory
 
 // The workspace starts with this: zero when no call is running (every call leaves it so).
 struct ResidentSync {
   uint32_t magic, pad0[31];
-  uint32_t x_done, pad0b[31];     // blocks that have packed their part of the tokens
-  uint32_t h_done, pad1[31];      // blocks that have stored all their h
-  uint32_t y_done, pad2[31];      // blocks that have stored all their y
-  uint32_t exited, pad3[31];
-  uint32_t cut[kResMaxGrid];      // [c]: blocks that have stored their part of the phase 0 job cut at the end of block c's share
+  uint32_t x_done, pad1[31];      // blocks that have packed their part of the tokens
+  uint32_t h_done[2], pad2[30];   // per group of experts: blocks that have stored all their h
+  uint32_t y_done, pad3[31];      // blocks that have stored all their y, one count per group
+  uint32_t exited, pad4[31];
+  uint32_t cut[2][kResMaxGrid];   // [g][c]: blocks that have stored their part of the gate/up job cut at the end of block c's share
 };
 
 struct ResidentArgs {
@@ -65,10 +74,10 @@ struct ResidentArgs {
   ResidentSync *sync;
   uint8_t *x;               // the experts' tokens in the same order as h, [hidden / 64] columns (where tokens are packed)
   uint8_t *h;               // per active expert: [inter / 64][rows padded to 8][64] bf16, swizzled as the operand wants it
-  float *part;              // [block][2][2][T][128]: partial sums of a share's two cut jobs (0: begun by others, 1: begun here)
+  float *part;              // [phase][block][2][2][T][128]: partial sums of a share's two cut jobs (0: begun by others, 1: begun here)
   float *y;                 // [choices][H]: jobs that lie inside one share
   uint32_t *status;
-  uint64_t limit_ns;
+  uint64_t limit_ns, part_phase;   // part_phase: floats between the phases' partial sums (0: one group, they follow each other)
   uint32_t T, k, E, H, I, ring_bytes, tmem_cols, extra_tx;
 };
 
@@ -78,9 +87,9 @@ __device__ __forceinline__ uint32_t share_of(uint32_t u, uint32_t U, uint32_t P)
   return (uint32_t)(((uint64_t)(u + 1) * P - 1) / U);
 }
 
-// One phase: jobs of KS steps, RB row blocks per active expert.
+// Phases 0, 1: gate/up of the two groups of experts; 2, 3: down.  Jobs of KS steps, RB row blocks per active expert.
 struct Phase {
-  uint32_t KS, RB, U, P;
+  uint32_t KS, RB, U, P, a0;   // a0: the group's first active expert
 };
 struct Piece {
   uint32_t job, a, rb, s0, n;   // steps s0 .. s0 + n of one job: active expert a, row block rb
@@ -88,8 +97,9 @@ struct Piece {
 __device__ __forceinline__ bool next_piece(const Phase &p, uint32_t &u, uint32_t end, Piece &q) {
   if (u >= end) return false;
   q.job = u / p.KS;
-  q.a = q.job / p.RB;
-  q.rb = q.job - q.a * p.RB;
+  const uint32_t ja = q.job / p.RB;
+  q.a = p.a0 + ja;
+  q.rb = q.job - ja * p.RB;
   q.s0 = u - q.job * p.KS;
   q.n = min(p.KS - q.s0, end - u);
   u += q.n;
@@ -100,33 +110,62 @@ struct Active {
   uint32_t e, n, h_row, slot;   // expert; its tokens; first row of its h block; first of its choices
 };
 
-// shared memory before the ring: [token masks of the experts][active experts][expert -> active][place of every choice
+// shared memory after the ring: [token masks of the experts][active experts][expert -> active][place of every choice
 // among its expert's tokens][tokens of the active experts, padded to 8 each][barriers and words]
 __host__ __device__ inline uint32_t pad16(uint32_t bytes) { return (bytes + 15) & ~15u; }
 __host__ __device__ inline uint32_t resident_rows(uint32_t E, uint32_t choices) { return choices + 7 * (E < choices ? E : choices); }
 __host__ __device__ inline uint32_t resident_control_bytes(uint32_t E, uint32_t T, uint32_t k) {
   return pad16(E * ((T + 31) / 32) * 4) + E * (uint32_t)sizeof(Active) + pad16(E * 2) + pad16(T * k * 2) +
-         pad16(resident_rows(E, T * k) * 2) + 256;
+         pad16(resident_rows(E, T * k) * 2) + (4 * kResMaxStages + 4) * 8 + 32;
 }
 
-// The four reading warps give up together or not at all: their barriers count 128 threads.
+// The reading warps give up together or not at all: their barriers count all of them.
 __device__ __forceinline__ bool all_agree(bool ok) {
   uint32_t r;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\t"
-      "barrier.cta.red.and.pred p, 1, 128, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      "barrier.cta.red.and.pred p, 1, %2, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
       : "=r"(r)
-      : "r"((uint32_t)ok)
+      : "r"((uint32_t)ok), "n"(32 * kResReaders)
       : "memory");
   return r != 0;
 }
+__device__ __forceinline__ void sync_readers() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kResReaders) : "memory"); }
+
+// the choice's place among its expert's tokens (in token order; a token that lists the expert twice has one place)
+__device__ __forceinline__ void place_choice(uint32_t at, int32_t e, const ResidentArgs &a, uint32_t W, const uint32_t *mask,
+                                             const Active *act, const uint16_t *active_of, uint16_t *place, uint16_t *token) {
+  const uint32_t t = at / a.k;
+  uint32_t before = __popc(mask[(uint32_t)e * W + (t >> 5)] & ((1u << (t & 31)) - 1));
+  for (uint32_t w = 0; w < (t >> 5); ++w) before += __popc(mask[(uint32_t)e * W + w]);
+  place[at] = (uint16_t)before;
+  token[act[active_of[e]].h_row + before] = (uint16_t)t;
+}
 
 __device__ __forceinline__ float silu_times(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
+
+// A place in a ring of stages and how often the ring has gone round.
+struct RingAt {
+  uint32_t st = 0, round = 0;
+  __device__ __forceinline__ void next(uint32_t n) {
+    if (++st == n) {
+      st = 0;
+      ++round;
+    }
+  }
+};
 
 __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __grid_constant__ CUtensorMap x_map, const ResidentArgs a) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x, G = gridDim.x;
   const uint32_t W = (a.T + 31) / 32, choices = a.T * a.k, n_rows_max = resident_rows(a.E, choices);
+  // every thread's ids (up to 2048 choices), asked for before anything else
+  constexpr uint32_t kIds = (256 * 8 + kResThreads - 1) / kResThreads;
+  int32_t my_id[kIds];
+#pragma unroll
+  for (uint32_t i = 0; i < kIds; ++i) my_id[i] = tid + i * kResThreads < choices ? __ldg(a.ids + tid + i * kResThreads) : -1;
+  const uint32_t magic = __ldcg(&a.sync->magic);
+
   uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t *ctl = ring + a.ring_bytes;
   uint32_t *mask = reinterpret_cast<uint32_t *>(ctl);
@@ -140,66 +179,59 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
   uint16_t *token = reinterpret_cast<uint16_t *>(ctl);
   ctl += pad16(n_rows_max * 2);
   uint64_t *bars = reinterpret_cast<uint64_t *>(ctl);
-  uint32_t *words = reinterpret_cast<uint32_t *>(bars + 2 * kResMaxStages + 4);   // tmem, dead, active, last, most
+  uint32_t *words = reinterpret_cast<uint32_t *>(bars + 4 * kResMaxStages + 4);   // tmem, dead, active, last, most
   volatile uint32_t *dead = words + 1;
-  const uint32_t stage0 = smem_addr(ring);
-  const uint32_t full = smem_addr(bars), empty = full + 8 * kResMaxStages, acc_full = empty + 8 * kResMaxStages, acc_empty = acc_full + 16;
+  // barriers: weights there / used, activations there / used, accumulators there / read
+  const uint32_t w_full = smem_addr(bars), w_empty = w_full + 8 * kResMaxStages, x_full = w_empty + 8 * kResMaxStages,
+                 x_empty = x_full + 8 * kResMaxStages, acc_full = x_empty + 8 * kResMaxStages, acc_empty = acc_full + 16;
   const WaitLimit lim = {dead, a.status, a.limit_ns};
 
   for (uint32_t i = tid; i < a.E * W; i += kResThreads) mask[i] = 0;
   for (uint32_t i = tid; i < n_rows_max; i += kResThreads) token[i] = 0;   // (the rows that fill up to 8 are token 0's)
-  if (tid == 0) {
-    for (uint32_t s = 0; s < kResMaxStages; ++s) {
-      mbar_init(full + 8 * s, 2);     // the weights' producer and the activations'
-      mbar_init(empty + 8 * s, 1);
+  if (warp == 3) {
+    for (uint32_t b = lane; b < 4 * kResMaxStages + 4; b += 32) mbar_init(w_full + 8 * b, b >= 4 * kResMaxStages + 2 ? kResReaders : 1);
+    if (lane == 0) {
+      *dead = 0;
+      prefetch_map(&x_map);
     }
-    for (uint32_t b = 0; b < 2; ++b) {
-      mbar_init(acc_full + 8 * b, 1);
-      mbar_init(acc_empty + 8 * b, 4);
-    }
-    *dead = 0;
-    prefetch_map(&x_map);
+    fence_barrier_init();
   }
-  fence_barrier_init();
   if (warp == 2) tmem_alloc(smem_addr(words), a.tmem_cols);
-  const bool prepared = a.sync->magic == kResMagic;
   tc_before_sync();
   __syncthreads();
   tc_after_sync();
   const uint32_t tmem = words[0];
 
   // ---- which tokens every expert has: the same in every block ----
-  for (uint32_t i = tid; i < a.T * a.k; i += kResThreads) {
-    const int32_t e = __ldg(a.ids + i);
-    if (e >= 0 && e < (int32_t)a.E) {
-      const uint32_t t = i / a.k;
-      atomicOr(&mask[(uint32_t)e * W + (t >> 5)], 1u << (t & 31));
-    } else if (e >= 0) {
-      report(a.status, kStatusBadDescriptor);
-    }
+#pragma unroll
+  for (uint32_t i = 0; i < kIds; ++i) {
+    const uint32_t at = tid + i * kResThreads, t = at / a.k;
+    if (at >= choices) break;
+    if (my_id[i] >= 0 && my_id[i] < (int32_t)a.E) atomicOr(&mask[(uint32_t)my_id[i] * W + (t >> 5)], 1u << (t & 31));
+    else if (my_id[i] >= 0) report(a.status, kStatusBadDescriptor);
   }
   __syncthreads();
-  if (warp == 0) {   // experts 8 * lane .. 8 * lane + 7
-    uint32_t cnt[8], n_act = 0, n_rows = 0, n_slots = 0, most = 0;
+  if (warp == 0) {   // experts per * lane .. per * lane + per - 1
+    const uint32_t per = (a.E + 31) / 32;
+    uint32_t cnt[8], n_act = 0, sums = 0, most = 0;   // sums: padded rows << 16 | choices
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
-      const uint32_t e = 8 * lane + i;
+      const uint32_t e = per * lane + i;
       cnt[i] = 0;
-      if (e < a.E)
+      if (i < per && e < a.E)
         for (uint32_t w = 0; w < W; ++w) cnt[i] += __popc(mask[e * W + w]);
       n_act += cnt[i] ? 1 : 0;
-      n_rows += (cnt[i] + 7) & ~7u;
-      n_slots += cnt[i];
+      sums += ((cnt[i] + 7) & ~7u) << 16 | cnt[i];
       most = max(most, cnt[i]);
     }
     most = __reduce_max_sync(0xFFFFFFFFu, most);
-    uint32_t at = n_act, row = n_rows, slot = n_slots;   // inclusive sums over the lanes
+    uint32_t at = n_act, sum = sums;   // inclusive sums over the lanes
+#pragma unroll
     for (uint32_t d = 1; d < 32; d <<= 1) {
-      const uint32_t p = __shfl_up_sync(0xFFFFFFFFu, at, d), q = __shfl_up_sync(0xFFFFFFFFu, row, d), r = __shfl_up_sync(0xFFFFFFFFu, slot, d);
+      const uint32_t p = __shfl_up_sync(0xFFFFFFFFu, at, d), q = __shfl_up_sync(0xFFFFFFFFu, sum, d);
       if (lane >= d) {
         at += p;
-        row += q;
-        slot += r;
+        sum += q;
       }
     }
     if (lane == 31) {
@@ -207,133 +239,170 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
       words[4] = most;
     }
     at -= n_act;
-    row -= n_rows;
-    slot -= n_slots;
+    sum -= sums;
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
-      const uint32_t e = 8 * lane + i;
-      if (e < a.E && cnt[i]) {
-        act[at] = Active{e, cnt[i], row, slot};
+      if (cnt[i]) {
+        const uint32_t e = per * lane + i;
+        act[at] = Active{e, cnt[i], sum >> 16, sum & 0xFFFFu};
         active_of[e] = (uint16_t)at;
         ++at;
-        row += (cnt[i] + 7) & ~7u;
-        slot += cnt[i];
+        sum += ((cnt[i] + 7) & ~7u) << 16 | cnt[i];
       }
     }
   }
   __syncthreads();
-  for (uint32_t i = tid; i < choices; i += kResThreads) {
-    const int32_t e = __ldg(a.ids + i);
-    if (e < 0 || e >= (int32_t)a.E) continue;
-    const uint32_t t = i / a.k;
-    uint32_t at = __popc(mask[(uint32_t)e * W + (t >> 5)] & ((1u << (t & 31)) - 1));
-    for (uint32_t w = 0; w < (t >> 5); ++w) at += __popc(mask[(uint32_t)e * W + w]);
-    place[i] = (uint16_t)at;
-    token[act[active_of[e]].h_row + at] = (uint16_t)t;
-  }
-  __syncthreads();
+  const bool prepared = magic == kResMagic;
   const uint32_t n_active = prepared ? words[2] : 0;
   const bool packed = words[4] > kResGatherRows && n_active > 0;
   const uint32_t N = max(16u, (words[4] + 15) & ~15u);       // the widest operand of this call
-  const uint32_t stage_bytes = kResStageA + N * 128, n_stages = min(kResMaxStages, a.ring_bytes / stage_bytes);
+  // as many stages of both kinds as fit; one more for weights if three are left for activations
+  const uint32_t x_stage = N * 128;
+  uint32_t n_w = min(kResMaxStages, a.ring_bytes / (kResStageA + x_stage)), n_x = n_w;
+  if (n_w < kResMaxStages && a.ring_bytes >= (n_w + 1) * kResStageA + 3 * x_stage) {
+    ++n_w;
+    n_x = min(kResMaxStages, (a.ring_bytes - n_w * kResStageA) / x_stage);
+  }
+  const uint32_t w_ring = smem_addr(ring), x_ring = w_ring + n_w * kResStageA;
   const uint32_t acc_bufs = N <= 128 ? 2 : 1;                // two accumulators of N columns each, of 512 columns
-  Phase ph[2];
-  ph[0].KS = (a.H + 63) / 64;
-  ph[0].RB = (a.I + 127) / 128;
-  ph[1].KS = (a.I + 63) / 64;
-  ph[1].RB = (a.H + 255) / 256;
+  Phase ph[4];
+  const uint32_t n_first = a.part_phase ? (n_active + 1) / 2 : n_active;
 #pragma unroll
-  for (uint32_t p = 0; p < 2; ++p) {
-    ph[p].U = n_active * ph[p].RB * ph[p].KS;
+  for (uint32_t p = 0; p < 4; ++p) {
+    ph[p].KS = p < 2 ? (a.H + 63) / 64 : (a.I + 63) / 64;
+    ph[p].RB = p < 2 ? (a.I + 127) / 128 : (a.H + 255) / 256;
+    ph[p].a0 = p & 1 ? n_first : 0;
+    ph[p].U = (p & 1 ? n_active - n_first : n_first) * ph[p].RB * ph[p].KS;
     ph[p].P = min(G, ph[p].U);
   }
   // this block's share of a phase
-  auto first = [&](uint32_t p) { return cta < ph[p].P ? share_first(cta, ph[p].U, ph[p].P) : 0u; };
-  auto last = [&](uint32_t p) { return cta < ph[p].P ? share_first(cta + 1, ph[p].U, ph[p].P) : 0u; };
+  auto first = [&](const Phase &f) { return cta < f.P ? share_first(cta, f.U, f.P) : 0u; };
+  auto last = [&](const Phase &f) { return cta < f.P ? share_first(cta + 1, f.U, f.P) : 0u; };
 
-  if (warp == 0 && lane == 0) {
+  if (warp == 0) {
     // ---- weights ----
-    const uint64_t policy = policy_evict_first();
-    uint32_t st = 0, round = 0;
-    bool ok = true;
-    for (uint32_t p = 0; p < 2 && ok; ++p) {
-      uint32_t u = first(p), seen = 0xFFFFFFFFu;
-      const uint32_t end = last(p);
-      Piece q;
-      while (ok && next_piece(ph[p], u, end, q)) {
-        const uint32_t e = act[q.a].e;
-        const uint8_t *m0 = a.table + (size_t)(3 * e + 2 * p) * ZIPMOE_RESIDENT_ENTRY_BYTES;
-        const uint8_t *m1 = p == 0 ? m0 + ZIPMOE_RESIDENT_ENTRY_BYTES : m0;
-        const int32_t y0 = (int32_t)(q.rb * (p == 0 ? 128 : 256)), y1 = p == 0 ? y0 : y0 + 128;
-        if (seen != e) {
-          acquire_map(m0);
-          if (p == 0) acquire_map(m1);
-          seen = e;
+    // the tensor maps of the share's experts, four of each phase: one lane each makes its map visible to the copies
+    constexpr uint32_t kMaps = 4;
+    {
+      const uint32_t p = lane >> 3, r = lane & 7;
+      const Phase f = p == 0 ? ph[0] : p == 1 ? ph[1] : p == 2 ? ph[2] : ph[3];
+      const uint32_t u = first(f), end = last(f);
+      if (u < end) {
+        const uint32_t per = f.KS * f.RB, ja = u / per + (r >> 1);
+        if (ja <= (end - 1) / per && (p < 2 || (r & 1) == 0)) {
+          const uint8_t *m = a.table + (size_t)(3 * act[f.a0 + ja].e + (p < 2 ? (r & 1) : 2)) * ZIPMOE_RESIDENT_ENTRY_BYTES;
+          acquire_map(m);
+          prefetch_map(m);
         }
-        for (uint32_t s = q.s0; s < q.s0 + q.n; ++s) {
-          if (round > 0 && !wait_bar(empty + 8 * st, (round - 1) & 1, lim)) {
-            ok = false;
-            break;
+      }
+    }
+    __syncwarp();
+    if (lane == 0) {
+      const uint64_t policy = policy_evict_first();
+      const uint32_t in_flight = min(kResInFlight, n_w);
+      RingAt at, behind;   // behind: the step in_flight before
+      uint32_t issued = 0;
+      bool ok = true;
+#pragma unroll 1
+      for (uint32_t p = 0; p < 4 && ok; ++p) {
+        const Phase f = p == 0 ? ph[0] : p == 1 ? ph[1] : p == 2 ? ph[2] : ph[3];
+        uint32_t u = first(f);
+        const uint32_t end = last(f), a_first = f.a0 + (u < end ? u / (f.KS * f.RB) : 0);
+        Piece q;
+        while (ok && next_piece(f, u, end, q)) {
+          const uint8_t *m0 = a.table + (size_t)(3 * act[q.a].e + (p < 2 ? 0 : 2)) * ZIPMOE_RESIDENT_ENTRY_BYTES;
+          const uint8_t *m1 = p < 2 ? m0 + ZIPMOE_RESIDENT_ENTRY_BYTES : m0;
+          const int32_t y0 = (int32_t)(q.rb * (p < 2 ? 128 : 256)), y1 = p < 2 ? y0 : y0 + 128;
+          if (q.a >= a_first + kMaps) {
+            acquire_map(m0);
+            acquire_map(m1);
           }
-          const uint32_t dst = stage0 + st * stage_bytes, bar = full + 8 * st;
-          mbar_expect_tx(bar, kResStageA + a.extra_tx);
-          tma_load_2d(dst, m0, (int32_t)(s * 64), y0, bar, policy);
-          tma_load_2d(dst + 16384, m1, (int32_t)(s * 64), y1, bar, policy);
-          if (++st == n_stages) {
-            st = 0;
-            ++round;
+          for (uint32_t s = q.s0; s < q.s0 + q.n; ++s) {
+            if (issued++ >= in_flight) {
+              ok = wait_bar(w_full + 8 * behind.st, behind.round & 1, lim);
+              behind.next(n_w);
+            }
+            if (!ok || (at.round > 0 && !wait_bar(w_empty + 8 * at.st, (at.round - 1) & 1, lim))) {
+              ok = false;
+              break;
+            }
+            const uint32_t dst = w_ring + at.st * kResStageA, bar = w_full + 8 * at.st;
+            mbar_expect_tx(bar, kResStageA + a.extra_tx);
+            tma_load_2d(dst, m0, (int32_t)(s * 64), y0, bar, policy);
+            tma_load_2d(dst + 16384, m1, (int32_t)(s * 64), y1, bar, policy);
+            at.next(n_w);
           }
         }
       }
     }
-  } else if (warp == 1 && lane < kResGatherRows / 4) {
+  } else {
+    // ---- where every choice stands among its expert's tokens (the weights are on their way already) ----
+#pragma unroll
+    for (uint32_t i = 0; i < kIds; ++i) {
+      // (warp 0's own ids are looked up again by others: it does not stop for this)
+      const uint32_t at = tid + i * kResThreads;
+      if (at < choices && my_id[i] >= 0 && my_id[i] < (int32_t)a.E) place_choice(at, my_id[i], a, W, mask, act, active_of, place, token);
+    }
+    if (warp == 1) {
+      for (uint32_t i = 0; i < kIds; ++i) {
+        const uint32_t at = lane + i * kResThreads;
+        const int32_t e = at < choices ? __ldg(a.ids + at) : -1;
+        if (e >= 0 && e < (int32_t)a.E) place_choice(at, e, a, W, mask, act, active_of, place, token);
+      }
+    }
+    asm volatile("bar.sync 2, %0;" ::"n"(kResThreads - 32) : "memory");
+  }
+
+  if (warp == 1 && lane < kResGatherRows / 4) {
     // ---- activations; where tokens are not packed, lane r gathers rows 4r .. 4r + 3 of the expert's ----
     constexpr uint32_t kLanes = (1u << (kResGatherRows / 4)) - 1;
     const uint64_t policy = policy_evict_last();
-    uint32_t st = 0, round = 0;
+    RingAt at;
     bool ok = true;
-    for (uint32_t p = 0; p < 2 && ok; ++p) {
-      uint32_t u = first(p);
-      const uint32_t end = last(p);
-      if (u < end && (p == 1 || packed)) {
-        ok = __all_sync(kLanes, p == 1 ? wait_count(&a.sync->h_done, ph[0].P, lim) : wait_count(&a.sync->x_done, G, lim));
+#pragma unroll 1
+    for (uint32_t p = 0; p < 4 && ok; ++p) {
+      const Phase f = p == 0 ? ph[0] : p == 1 ? ph[1] : p == 2 ? ph[2] : ph[3];
+      uint32_t u = first(f);
+      const uint32_t end = last(f);
+      if (u < end && (p >= 2 || packed)) {
+        ok = __all_sync(kLanes, p < 2 ? wait_count(&a.sync->x_done, G, lim) : wait_count(&a.sync->h_done[p - 2], p == 2 ? ph[0].P : ph[1].P, lim));
         fence_async_all();       // what other blocks stored is now read by the copy engine
       }
       Piece q;
-      while (ok && next_piece(ph[p], u, end, q)) {
+      while (ok && next_piece(f, u, end, q)) {
         const uint32_t rows = (act[q.a].n + 7) & ~7u, first_row = act[q.a].h_row;
-        const uint8_t *src = (p == 0 ? a.x : a.h) + ((size_t)first_row * ph[p].KS) * 128;
+        const uint8_t *src = (p < 2 ? a.x : a.h) + ((size_t)first_row * f.KS) * 128;
         int32_t tok[4];
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i) tok[i] = 4 * lane < rows ? token[first_row + 4 * lane + i] : 0;
         for (uint32_t s = q.s0; s < q.s0 + q.n; ++s) {
-          ok = __all_sync(kLanes, round == 0 || wait_bar(empty + 8 * st, (round - 1) & 1, lim));
+          ok = __all_sync(kLanes, at.round == 0 || wait_bar(x_empty + 8 * at.st, (at.round - 1) & 1, lim));
           if (!ok) break;
-          const uint32_t dst = stage0 + st * stage_bytes + kResStageA, bar = full + 8 * st;
+          const uint32_t dst = x_ring + at.st * x_stage, bar = x_full + 8 * at.st;
           if (lane == 0) mbar_expect_tx(bar, rows * 128);
           __syncwarp(kLanes);
-          if (p == 0 && !packed) {
+          if (p < 2 && !packed) {
             if (4 * lane < rows)
               tma_gather4(dst + lane * 512, &x_map, (int32_t)(s * 64), tok[0], tok[1], tok[2], tok[3], bar, policy);
           } else if (lane == 0) {
             bulk_load(dst, src + (size_t)s * rows * 128, rows * 128, bar, policy);
           }
-          if (++st == n_stages) {
-            st = 0;
-            ++round;
-          }
+          at.next(n_x);
         }
       }
     }
   } else if (warp == 2 && lane == 0) {
     // ---- MMAs ----
-    uint32_t st = 0, round = 0, piece = 0;
+    RingAt wa, xa;
+    uint32_t piece = 0;
     bool ok = true;
-    for (uint32_t p = 0; p < 2 && ok; ++p) {
-      uint32_t u = first(p);
-      const uint32_t end = last(p);
+#pragma unroll 1
+    for (uint32_t p = 0; p < 4 && ok; ++p) {
+      const Phase f = p == 0 ? ph[0] : p == 1 ? ph[1] : p == 2 ? ph[2] : ph[3];
+      uint32_t u = first(f);
+      const uint32_t end = last(f);
       Piece q;
-      while (ok && next_piece(ph[p], u, end, q)) {
+      while (ok && next_piece(f, u, end, q)) {
         const uint32_t b = piece % acc_bufs, use = piece / acc_bufs;
         if (use > 0 && !wait_bar(acc_empty + 8 * b, (use - 1) & 1, lim)) {
           ok = false;
@@ -344,68 +413,81 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
         const uint32_t idesc = bf16_idesc((act[q.a].n + 15) & ~15u);
         const uint32_t d0 = tmem + b * 2 * N, d1 = d0 + N;
         for (uint32_t s = 0; s < q.n; ++s) {
-          if (!wait_bar(full + 8 * st, round & 1, lim)) {
+          if (!wait_bar(w_full + 8 * wa.st, wa.round & 1, lim) || !wait_bar(x_full + 8 * xa.st, xa.round & 1, lim)) {
             ok = false;
             break;
           }
           tc_after_sync();
-          const uint32_t at = stage0 + st * stage_bytes;
-          const uint64_t a0 = swizzled_desc(at), a1 = swizzled_desc(at + 16384), bd = swizzled_desc(at + kResStageA);
+          const uint32_t at = w_ring + wa.st * kResStageA;
+          const uint64_t a0 = swizzled_desc(at), a1 = swizzled_desc(at + 16384), bd = swizzled_desc(x_ring + xa.st * x_stage);
 #pragma unroll
           for (uint32_t j = 0; j < 4; ++j) {
             tc_mma(d0, a0 + 2 * j, bd + 2 * j, idesc, s > 0 || j > 0);
             tc_mma(d1, a1 + 2 * j, bd + 2 * j, idesc, s > 0 || j > 0);
           }
-          tc_commit(empty + 8 * st);
-          if (++st == n_stages) {
-            st = 0;
-            ++round;
-          }
+          tc_commit(w_empty + 8 * wa.st);
+          tc_commit(x_empty + 8 * xa.st);
+          wa.next(n_w);
+          xa.next(n_x);
         }
         if (ok) tc_commit(acc_full + 8 * b);
         ++piece;
       }
     }
   } else if (warp >= 4) {
-    // ---- accumulators back; thread = one row of the job's 128 (twice) ----
-    const uint32_t w = warp - 4, row = 32 * w + lane, etid = tid - 128;
+    // ---- accumulators back; a thread has one row of the job's 128 (twice), and every second group of 8 tokens ----
+    const uint32_t w = warp & 3, half = (warp - 4) >> 2, row = 32 * w + lane, rtid = tid - 128;
     uint32_t piece = 0;
     bool ok = true;
     if (packed) {
-      // 16 bytes of a token's row at a time, to where the tensor core's operand has them
-      const uint32_t per_row = ph[0].KS * 8, total = choices * per_row;
-      for (uint32_t v = cta * 128 + etid; v < total; v += G * 128) {
-        const uint32_t i = v / per_row, c = v - i * per_row, t = i / a.k;
+      // a warp per choice: the token's row, 16 bytes per lane at a time, to where the tensor core's operand has them
+      const uint32_t chunks = ph[0].KS * 8;
+      for (uint32_t i = cta * kResReaders + (warp - 4); i < choices; i += G * kResReaders) {
         const int32_t e = __ldg(a.ids + i);
         if (e < 0 || e >= (int32_t)a.E) continue;
         const Active ex = act[active_of[e]];
         const uint32_t r = place[i], rows = (ex.n + 7) & ~7u;
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (c * 8 < a.H) x = __ldg(reinterpret_cast<const uint4 *>(a.tokens + (size_t)t * a.H + c * 8));
-        *reinterpret_cast<uint4 *>(a.x + ((size_t)ex.h_row * ph[0].KS + (size_t)(c >> 3) * rows + r) * 128 + (((c & 7) ^ (r & 7)) << 4)) = x;
+        const uint16_t *src = a.tokens + (size_t)(i / a.k) * a.H;
+        uint8_t *dst = a.x + ((size_t)ex.h_row * ph[0].KS + r) * 128;
+        for (uint32_t c0 = lane; c0 < chunks; c0 += 256) {
+          uint4 x[8];
+#pragma unroll
+          for (uint32_t v = 0; v < 8; ++v) {
+            const uint32_t c = c0 + 32 * v;
+            x[v] = c * 8 < a.H ? __ldg(reinterpret_cast<const uint4 *>(src + c * 8)) : make_uint4(0, 0, 0, 0);
+          }
+#pragma unroll
+          for (uint32_t v = 0; v < 8; ++v) {
+            const uint32_t c = c0 + 32 * v;
+            if (c < chunks) *reinterpret_cast<uint4 *>(dst + (size_t)(c >> 3) * rows * 128 + (((c & 7) ^ (r & 7)) << 4)) = x[v];
+          }
+        }
       }
       __threadfence();
       fence_async_all();
-      asm volatile("bar.sync 1, 128;" ::: "memory");
-      if (etid == 0) add_release(&a.sync->x_done, 1u);
+      sync_readers();
+      if (rtid == 0) add_release(&a.sync->x_done, 1u);
     }
-    for (uint32_t p = 0; p < 2 && ok; ++p) {
-      uint32_t u = first(p);
-      const uint32_t end = last(p);
+#pragma unroll 1
+    for (uint32_t p = 0; p < 4 && ok; ++p) {
+      const Phase f = p == 0 ? ph[0] : p == 1 ? ph[1] : p == 2 ? ph[2] : ph[3];
+      uint32_t u = first(f);
+      const uint32_t end = last(f);
+      float *part = a.part + p * a.part_phase;
       Piece q;
-      while (ok && next_piece(ph[p], u, end, q)) {
+      while (ok && next_piece(f, u, end, q)) {
         const uint32_t b = piece % acc_bufs, use = piece / acc_bufs;
         ++piece;
         const Active ex = act[q.a];
-        const bool whole = q.n == ph[p].KS;
-        float *mine = a.part + ((size_t)cta * 2 + (q.s0 > 0 ? 0 : 1)) * (2 * a.T * 128) + row;
+        const bool whole = q.n == f.KS;
+        float *mine = part + ((size_t)cta * 2 + (q.s0 > 0 ? 0 : 1)) * (2 * a.T * 128) + row;
         // a finished pair of sums of the expert's i-th token
         const uint32_t rows = (ex.n + 7) & ~7u, ir = q.rb * 128 + row;
-        uint8_t *h = a.h + ((size_t)ex.h_row * ph[1].KS + (size_t)(ir >> 6) * rows) * 128 + (ir & 7) * 2;
+        uint8_t *h = a.h + ((size_t)ex.h_row * ph[2].KS + (size_t)(ir >> 6) * rows) * 128 + (ir & 7) * 2;
         const uint32_t chunk = (ir & 63) >> 3;
         auto finish = [&](uint32_t i, float v0, float v1) {
-          if (p == 0) {
-            if (ir < ph[1].KS * 64)     // (rows between inter and the next multiple of 64 are zeros: W2 has no columns there)
+          if (p < 2) {
+            if (ir < ph[2].KS * 64)     // (rows between inter and the next multiple of 64 are zeros: W2 has no columns there)
               *reinterpret_cast<uint16_t *>(h + i * 128 + ((chunk ^ (i & 7)) << 4)) =
                   ir < a.I ? __bfloat16_as_ushort(__float2bfloat16_rn(silu_times(v0, v1))) : (uint16_t)0;
           } else {
@@ -427,7 +509,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
         if (!ok) break;
         tc_after_sync();
         const uint32_t d0 = tmem + ((32 * w) << 16) + b * 2 * N, d1 = d0 + N;
-        for (uint32_t c = 0; c < ex.n; c += 8) {
+        for (uint32_t c = 8 * half; c < ex.n; c += 16) {
           uint32_t v0[8], v1[8];
           tmem_load8(d0 + c, v0);
           tmem_load8(d1 + c, v1);
@@ -439,27 +521,26 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
         tc_before_sync();
         __syncwarp();
         if (lane == 0) arrive(acc_empty + 8 * b);
-        if (whole || p == 1) continue;
-        // a job of phase 0 that is cut: the block that stores its part last adds all parts, in share order
-        const uint32_t c0 = share_of(q.job * ph[0].KS, ph[0].U, ph[0].P);
-        const uint32_t c1 = share_of(q.job * ph[0].KS + ph[0].KS - 1, ph[0].U, ph[0].P);
+        if (whole || p >= 2) continue;
+        // a gate/up job that is cut: the block that stores its part last adds all parts, in share order
+        const uint32_t c0 = share_of(q.job * f.KS, f.U, f.P), c1 = share_of(q.job * f.KS + f.KS - 1, f.U, f.P);
         __threadfence();
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        if (etid == 0) {
-          words[3] = atomicAdd(&a.sync->cut[c0], 1u) == c1 - c0;
+        sync_readers();
+        if (rtid == 0) {
+          words[3] = atomicAdd(&a.sync->cut[p][c0], 1u) == c1 - c0;
           __threadfence();
         }
-        asm volatile("bar.sync 1, 128;" ::: "memory");
+        sync_readers();
         if (words[3]) {
-          for (uint32_t n0 = 0; n0 < ex.n; n0 += 4) {
+          for (uint32_t n0 = 4 * half; n0 < ex.n; n0 += 8) {
             float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
             for (uint32_t c = c0; c <= c1; ++c) {
-              const float *part = a.part + ((size_t)c * 2 + (c == c0 ? 1 : 0)) * (2 * a.T * 128) + row;
+              const float *from = part + ((size_t)c * 2 + (c == c0 ? 1 : 0)) * (2 * a.T * 128) + row;
 #pragma unroll
               for (uint32_t n = 0; n < 4; ++n)
                 if (n0 + n < ex.n) {
-                  s0[n] += __ldcg(part + (size_t)(n0 + n) * 128);
-                  s1[n] += __ldcg(part + (size_t)(a.T + n0 + n) * 128);
+                  s0[n] += __ldcg(from + (size_t)(n0 + n) * 128);
+                  s1[n] += __ldcg(from + (size_t)(a.T + n0 + n) * 128);
                 }
             }
 #pragma unroll
@@ -469,11 +550,11 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
         }
       }
       // everything this block stores in the phase is out: tell the others
-      if (ok && cta < ph[p].P) {
+      if (ok && cta < f.P) {
         __threadfence();
-        if (p == 0) fence_async_all();
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        if (etid == 0) add_release(p == 0 ? &a.sync->h_done : &a.sync->y_done, 1u);
+        if (p < 2) fence_async_all();
+        sync_readers();
+        if (rtid == 0) add_release(p < 2 ? &a.sync->h_done[p] : &a.sync->y_done, 1u);
       }
     }
   }
@@ -484,54 +565,63 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
   if (*dead)   // let the copies and MMAs that this block has under way end before its memory goes to somebody else
     for (uint32_t i = 0; i < 200; ++i) __nanosleep(1000);
   if (warp == 2) tmem_free(tmem, a.tmem_cols);
-  if (tid == 0 && !*dead) wait_count(&a.sync->y_done, ph[1].P, lim);
+  if (tid == 0 && !*dead) wait_count(&a.sync->y_done, ph[2].P + ph[3].P, lim);
   __syncthreads();
 
-  // ---- out[t] = sum over the token's choices; 8 lanes per 4 columns, one per choice ----
+  // ---- out[t] = sum over the token's choices: 4 columns per item, 1 to 8 lanes per item (as many as there are threads for) ----
   if (!*dead && prepared) {
-    const uint32_t j = lane & 7, vecs = a.H / 4;
-    const uint64_t items = (uint64_t)a.T * vecs;
-    const uint32_t per_block = kResThreads / 8;
-    for (uint64_t it0 = (uint64_t)cta * per_block; it0 < items; it0 += (uint64_t)G * per_block) {
-      const uint64_t it = it0 + (tid >> 3);
+    const uint32_t vecs = a.H / 4, items = a.T * vecs;
+    uint32_t lanes = 8;
+    while (lanes > 1 && (items * lanes > G * kResThreads || lanes >= 2 * a.k)) lanes >>= 1;
+    const uint32_t per_block = kResThreads / lanes, l = tid % lanes;
+    for (uint32_t it0 = cta * per_block; it0 < items; it0 += G * per_block) {
+      const uint32_t it = it0 + tid / lanes;
       float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-      uint32_t t = 0, c = 0;
+      const uint32_t t = it / vecs, c = (it - t * vecs) * 4;
       if (it < items) {
-        t = (uint32_t)(it / vecs);
-        c = (uint32_t)(it - (uint64_t)t * vecs) * 4;
-        const int32_t e = j < a.k ? __ldg(a.ids + t * a.k + j) : -1;
-        if (e >= 0 && e < (int32_t)a.E) {
-          const uint32_t ai = active_of[e];
-          const uint32_t i = place[t * a.k + j];
-          const uint32_t u0 = (ai * ph[1].RB + c / 256) * ph[1].KS;
-          const uint32_t c0 = share_of(u0, ph[1].U, ph[1].P), c1 = share_of(u0 + ph[1].KS - 1, ph[1].U, ph[1].P);
+#pragma unroll 2
+        for (uint32_t j = l; j < a.k; j += lanes) {
+          const int32_t e = __ldg(a.ids + t * a.k + j);
+          if (e < 0 || e >= (int32_t)a.E) continue;
+          const uint32_t ai = active_of[e], i = place[t * a.k + j];
+          const uint32_t p = ai < n_first ? 2 : 3;
+          const Phase f = p == 2 ? ph[2] : ph[3];
+          const uint32_t u0 = ((ai - f.a0) * f.RB + c / 256) * f.KS;
+          const uint32_t c0 = share_of(u0, f.U, f.P), c1 = share_of(u0 + f.KS - 1, f.U, f.P);
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
           if (c0 == c1) {
-            s = __ldcg(reinterpret_cast<const float4 *>(a.y + (size_t)(act[ai].slot + i) * a.H + c));
+            v = __ldcg(reinterpret_cast<const float4 *>(a.y + (size_t)(act[ai].slot + i) * a.H + c));
           } else {
-            for (uint32_t b = c0; b <= c1; ++b) {
-              const float4 v = __ldcg(reinterpret_cast<const float4 *>(
-                  a.part + ((size_t)b * 2 + (b == c0 ? 1 : 0)) * (2 * a.T * 128) + (size_t)(((c >> 7) & 1) * a.T + i) * 128 + (c & 127)));
-              s.x += v.x;
-              s.y += v.y;
-              s.z += v.z;
-              s.w += v.w;
+            const float *from = a.part + p * a.part_phase + (size_t)(((c >> 7) & 1) * a.T + i) * 128 + (c & 127);
+            for (uint32_t b = c0; b <= c1; b += 4) {
+              float4 r[4];
+#pragma unroll
+              for (uint32_t n = 0; n < 4; ++n)
+                r[n] = b + n <= c1 ? __ldcg(reinterpret_cast<const float4 *>(from + ((size_t)(b + n) * 2 + (b + n == c0 ? 1 : 0)) * (2 * a.T * 128)))
+                                   : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+              for (uint32_t n = 0; n < 4; ++n) {
+                v.x += r[n].x;
+                v.y += r[n].y;
+                v.z += r[n].z;
+                v.w += r[n].w;
+              }
             }
           }
           const float wt = a.weights ? __ldg(a.weights + t * a.k + j) : 1.0f;
-          s.x *= wt;
-          s.y *= wt;
-          s.z *= wt;
-          s.w *= wt;
+          s.x += wt * v.x;
+          s.y += wt * v.y;
+          s.z += wt * v.z;
+          s.w += wt * v.w;
         }
       }
-#pragma unroll
-      for (int d = 4; d > 0; d >>= 1) {
+      for (uint32_t d = lanes >> 1; d > 0; d >>= 1) {
         s.x += __shfl_xor_sync(0xFFFFFFFFu, s.x, d);
         s.y += __shfl_xor_sync(0xFFFFFFFFu, s.y, d);
         s.z += __shfl_xor_sync(0xFFFFFFFFu, s.z, d);
         s.w += __shfl_xor_sync(0xFFFFFFFFu, s.w, d);
       }
-      if (it < items && j == 0) {
+      if (it < items && l == 0) {
         const __nv_bfloat162 lo = __floats2bfloat162_rn(s.x, s.y), hi = __floats2bfloat162_rn(s.z, s.w);
         *reinterpret_cast<uint2 *>(a.out + (size_t)t * a.H + c) =
             make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
@@ -544,9 +634,9 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
     if (prepared) {
       __threadfence();
       if (atomicAdd(&a.sync->exited, 1u) == G - 1) {   // the last block leaves the counters as it found them
-        for (uint32_t c = 0; c < kResMaxGrid; ++c) a.sync->cut[c] = 0;
+        for (uint32_t c = 0; c < kResMaxGrid; ++c) a.sync->cut[0][c] = a.sync->cut[1][c] = 0;
         a.sync->x_done = 0;
-        a.sync->h_done = 0;
+        a.sync->h_done[0] = a.sync->h_done[1] = 0;
         a.sync->y_done = 0;
         a.sync->exited = 0;
       }
@@ -589,7 +679,7 @@ uint32_t resident_grid() {
 
 struct ResidentPlan {
   uint32_t grid, tmem_cols, ring, smem;
-  uint64_t off_x, off_h, off_part, off_y, total;
+  uint64_t part_phase, off_x, off_h, off_part, off_y, total;
 };
 
 zipmoe_status resident_plan(uint32_t T, uint32_t k, const zipmoe_resident_experts *ex, ResidentPlan *p) {
@@ -609,7 +699,10 @@ zipmoe_status resident_plan(uint32_t T, uint32_t k, const zipmoe_resident_expert
   uint64_t at = up(sizeof(zipmoe_dev::ResidentSync));
   p->off_x = at; at = up(at + rows * ((H + 63) / 64) * 128);
   p->off_h = at; at = up(at + rows * ((I + 63) / 64) * 128);
-  p->off_part = at; at = up(at + (uint64_t)p->grid * 2 * 2 * T * 128 * 4);
+  // (a workspace for more tokens always serves fewer: up to kResTwoGroupsT tokens four phases have partial sums of their own)
+  const uint64_t per_token = (uint64_t)p->grid * 2 * 2 * 128, few = std::min(T, zipmoe_dev::kResTwoGroupsT);
+  p->part_phase = T == few ? few * per_token : 0;
+  p->off_part = at; at = up(at + std::max(4 * few, (uint64_t)T) * per_token * 4);
   p->off_y = at; at = up(at + choices * H * 4);
   p->total = at;
   return ZIPMOE_OK;
@@ -701,6 +794,7 @@ extern "C" zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, c
   a.E = ex->n_experts;
   a.H = ex->hidden;
   a.I = ex->inter;
+  a.part_phase = p.part_phase;
   a.ring_bytes = p.ring;
   a.tmem_cols = p.tmem_cols;
   cudaLaunchAttribute together;
