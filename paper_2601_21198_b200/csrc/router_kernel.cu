@@ -1,24 +1,34 @@
-// The router: logits = tokens x gate^T + bias, the k largest per token, and their softmax weights.
-// One block per token: every warp takes experts in turn (each lane sums 8 columns of every 256), then the first warp
-// picks the k largest.  A logit is compared through a 32-bit key that orders as the number does, with NaN on top.
+// The router: logits = tokens x gate^T + bias, the k largest per token, and their softmax weights, in one launch.
+// Bound: the tokens' bytes for a long prompt (the gate stays in the second-level cache), latency for a few tokens.
+//   * A cluster of 1 to 8 blocks takes 128 tokens (the M operand of a tcgen05 MMA; N = all experts, padded to 16) and
+//     splits the hidden dimension among its blocks.  Each block streams its columns of tokens and gate through a ring of
+//     TMA stages and accumulates [128 x N] in tensor memory.  Rows and columns past the matrices come in as zeros, so no
+//     size needs a path of its own; a single token reads one row.
+//   * Every block leaves its partial logits in its shared memory; after a cluster barrier the block of rank r adds, in
+//     rank order, the parts of tokens r, r + S, ... straight from its neighbours' shared memory.
+//   * One warp picks a token's k experts: a logit becomes a 32-bit key that orders as the number does (NaN on top),
+//     every lane holds the keys of experts lane, lane + 32, ..., and each choice is one maximum over the warp and one
+//     minimum over the indices that reach it.
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 
 #include "zipmoe.h"
-#include "decode_device.cuh"
+#include "tensor_core.cuh"
 
 namespace zipmoe_dev {
 
 constexpr uint32_t kMaxExperts = 256, kMaxTopK = 8;
+constexpr uint32_t kRouterRows = 128, kRouterThreads = 256, kRouterMaxStages = 8;
 
 struct RouterArgs {
-  const uint16_t *tokens, *gate;
   const float *bias;
   int32_t *ids;
   float *weights, *logits;
-  uint64_t token_pitch;
-  uint32_t T, E, H, k, flags;
+  uint32_t *status;
+  uint64_t limit_ns;
+  uint32_t T, E, H, k, flags, N, stages, tmem_cols, extra_tx;
 };
 
 // A key that orders as the logit does: NaN above all, then +infinity down to -infinity; 0 for -infinity, so that it
@@ -30,43 +40,47 @@ __device__ __forceinline__ uint32_t logit_key(float l) {
   if (b == 0x80000000u) return 0x80000000u;                  // -0 equals +0
   return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
+__device__ __forceinline__ float key_logit(uint32_t key) {   // (NaN's key gives a NaN)
+  return __uint_as_float((key & 0x80000000u) ? (key & 0x7FFFFFFFu) : ~key);
+}
 
-// One warp picks the k largest of the logits l[0..E) (shared memory) of token t and writes ids and weights.
-__device__ __forceinline__ void pick_experts(const float *l, uint32_t E, uint32_t k, uint32_t flags, uint32_t lane,
-                                             int32_t *ids, float *weights) {
-  uint32_t key[kMaxExperts / 32];
+// One warp picks the k largest of a token's logits (l[i] is expert lane + 32 i; -infinity past the last) and writes ids
+// and weights.
+template <int kPer>
+__device__ __forceinline__ void pick_experts(const float (&l)[kPer], uint32_t k, uint32_t flags, uint32_t lane, int32_t *ids,
+                                             float *weights) {
+  uint32_t key[kPer];
 #pragma unroll
-  for (uint32_t i = 0; i < kMaxExperts / 32; ++i) {
-    const uint32_t e = lane + 32 * i;
-    key[i] = e < E ? logit_key(l[e]) : 0u;
-  }
+  for (int i = 0; i < kPer; ++i) key[i] = logit_key(l[i]);
   int32_t my_id = -1;       // lane j keeps choice j
-  float my_logit = -INFINITY, top = -INFINITY;
+  uint32_t my_key = 0, top_key = 0;
   for (uint32_t j = 0; j < k; ++j) {
     uint32_t best = 0, at = 0;
 #pragma unroll
-    for (uint32_t i = 0; i < kMaxExperts / 32; ++i)
+    for (int i = 0; i < kPer; ++i)
       if (key[i] > best) {
         best = key[i];
-        at = lane + 32 * i;
+        at = i;
       }
     const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, best);
     if (most == 0) break;
-    const uint32_t e = __reduce_min_sync(0xFFFFFFFFu, best == most ? at : 0xFFFFFFFFu);
-    const float v = l[e];
-    if (j == 0) top = v;
+    const uint32_t e = __reduce_min_sync(0xFFFFFFFFu, best == most ? at * 32 + lane : 0xFFFFFFFFu);
+    if (j == 0) top_key = most;
     if (lane == j) {
       my_id = (int32_t)e;
-      my_logit = v;
+      my_key = most;
     }
 #pragma unroll
-    for (uint32_t i = 0; i < kMaxExperts / 32; ++i)
+    for (int i = 0; i < kPer; ++i)
       if (e == lane + 32 * i) key[i] = 0;
   }
-  float p = my_id >= 0 ? __expf(my_logit - top) : 0.f, sum = p;
+  const float top = key_logit(top_key);
+  const float p = my_id >= 0 ? __expf(key_logit(my_key) - top) : 0.f;
+  float sum = p;
   if (flags & ZIPMOE_ROUTE_SOFTMAX_ALL) {
     sum = 0.f;
-    for (uint32_t e = lane; e < E; e += 32) sum += l[e] == -INFINITY ? 0.f : __expf(l[e] - top);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) sum += l[i] == -INFINITY ? 0.f : __expf(l[i] - top);
   }
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
@@ -76,44 +90,195 @@ __device__ __forceinline__ void pick_experts(const float *l, uint32_t E, uint32_
   }
 }
 
-__global__ void __launch_bounds__(256) router_kernel(const RouterArgs a) {
-  __shared__ float s_logit[kMaxExperts];
-  const uint32_t t = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const uint16_t *x = a.tokens + t * a.token_pitch;
-  for (uint32_t e = warp; e < a.E; e += 8) {
-    const uint16_t *g = a.gate + (uint64_t)e * a.H;
-    float sum = 0.f;
-    for (uint32_t c = lane * 8; c < a.H; c += 256) {
-      const uint4 xv = __ldg(reinterpret_cast<const uint4 *>(x + c)), gv = __ldg(reinterpret_cast<const uint4 *>(g + c));
-      const uint32_t xw[4] = {xv.x, xv.y, xv.z, xv.w}, gw[4] = {gv.x, gv.y, gv.z, gv.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        sum = fmaf(__uint_as_float(xw[i] << 16), __uint_as_float(gw[i] << 16), sum);
-        sum = fmaf(__uint_as_float(xw[i] & 0xFFFF0000u), __uint_as_float(gw[i] & 0xFFFF0000u), sum);
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %cluster_nctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank) {   // the same place in another block's shared memory
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float load_cluster(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+template <int kPer>
+__global__ void __launch_bounds__(kRouterThreads) router_kernel(const __grid_constant__ CUtensorMap x_map,
+                                                               const __grid_constant__ CUtensorMap gate_map, const RouterArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t bars[2 * kRouterMaxStages + 1];
+  __shared__ uint32_t words[2];   // tmem, dead
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, rank = cluster_rank(), S = cluster_size();
+  uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  const uint32_t ring0 = smem_addr(ring), stage_bytes = (kRouterRows + a.N) * 128, pitch = a.N + 1;
+  const uint32_t full = smem_addr(bars), empty = full + 8 * kRouterMaxStages, done = empty + 8 * kRouterMaxStages;
+  volatile uint32_t *dead = words + 1;
+  const WaitLimit lim = {dead, a.status, a.limit_ns};
+  const uint32_t t0 = (blockIdx.x / S) * kRouterRows, rows = min(kRouterRows, a.T - t0);
+  const uint32_t steps = (a.H + 63) / 64, s0 = rank * steps / S, s1 = (rank + 1) * steps / S;
+
+  if (tid == 0) {
+    for (uint32_t s = 0; s < a.stages; ++s) {
+      mbar_init(full + 8 * s, 1);
+      mbar_init(empty + 8 * s, 1);
+    }
+    mbar_init(done, 1);
+    *dead = 0;
+    prefetch_map(&x_map);
+    prefetch_map(&gate_map);
+    fence_barrier_init();
+  }
+  if (warp == 1) tmem_alloc(smem_addr(words), a.tmem_cols);
+  tc_before_sync();
+  __syncthreads();
+  tc_after_sync();
+  const uint32_t tmem = words[0];
+
+  if (warp == 0 && lane == 0) {
+    const uint64_t once = policy_evict_first(), keep = policy_evict_last();
+    uint32_t st = 0, round = 0;
+    for (uint32_t s = s0; s < s1; ++s) {
+      if (round > 0 && !wait_bar(empty + 8 * st, (round - 1) & 1, lim)) break;
+      const uint32_t dst = ring0 + st * stage_bytes, bar = full + 8 * st;
+      mbar_expect_tx(bar, stage_bytes + a.extra_tx);
+      tma_load_2d(dst, &x_map, (int32_t)(s * 64), (int32_t)t0, bar, once);
+      tma_load_2d(dst + kRouterRows * 128, &gate_map, (int32_t)(s * 64), 0, bar, keep);
+      if (++st == a.stages) {
+        st = 0;
+        ++round;
       }
     }
+  } else if (warp == 1 && lane == 0) {
+    const uint32_t idesc = bf16_idesc(a.N);
+    uint32_t st = 0, round = 0;
+    bool ok = true;
+    for (uint32_t s = s0; s < s1; ++s) {
+      ok = wait_bar(full + 8 * st, round & 1, lim);
+      if (!ok) break;
+      tc_after_sync();
+      const uint64_t xd = swizzled_desc(ring0 + st * stage_bytes), gd = swizzled_desc(ring0 + st * stage_bytes + kRouterRows * 128);
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-    if (lane == 0) {
-      if (a.bias) sum += a.bias[e];
-      s_logit[e] = sum;
-      if (a.logits) a.logits[(uint64_t)t * a.E + e] = sum;
+      for (uint32_t j = 0; j < 4; ++j) tc_mma(tmem, xd + 2 * j, gd + 2 * j, idesc, s > s0 || j > 0);
+      tc_commit(empty + 8 * st);
+      if (++st == a.stages) {
+        st = 0;
+        ++round;
+      }
+    }
+    if (ok) tc_commit(done);
+  }
+  __syncwarp();
+
+  // ---- partial logits into shared memory, over the ring (every MMA has read it); row = token ----
+  float *part = reinterpret_cast<float *>(ring);
+  const bool ok = __all_sync(0xFFFFFFFFu, wait_bar(done, 0, lim));
+  tc_after_sync();
+  const uint32_t row = 32 * (warp & 3) + lane;
+  if (ok && 32 * (warp & 3) < rows) {
+    for (uint32_t c = 8 * (warp >> 2); c < a.N; c += 16) {
+      uint32_t v[8];
+      if (s1 > s0) {
+        tmem_load8(tmem + ((32 * (warp & 3)) << 16) + c, v);
+        tmem_wait();
+      }
+#pragma unroll
+      for (uint32_t n = 0; n < 8; ++n) part[row * pitch + c + n] = s1 > s0 ? __uint_as_float(v[n]) : 0.f;
     }
   }
-  __syncthreads();
-  if (warp == 0) pick_experts(s_logit, a.E, a.k, a.flags, lane, a.ids + (uint64_t)t * a.k, a.weights + (uint64_t)t * a.k);
+  __syncwarp();
+  tc_before_sync();
+  cluster_sync();
+  tc_after_sync();
+  if (*dead)   // let the copies and MMAs that this block has under way end before its memory goes to somebody else
+    for (uint32_t i = 0; i < 200; ++i) __nanosleep(1000);
+  if (warp == 1) tmem_free(tmem, a.tmem_cols);
+
+  // ---- the tokens of this rank ----
+  if (!*dead) {
+    uint32_t base[8];
+#pragma unroll
+    for (uint32_t r = 0; r < 8; ++r) base[r] = in_block(ring0, r < S ? r : 0);
+    for (uint32_t m = rank + S * warp; m < rows; m += S * (kRouterThreads / 32)) {
+      const uint64_t t = t0 + m;
+      float l[kPer];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) l[i] = 0.f;
+#pragma unroll
+      for (uint32_t r = 0; r < 8; ++r)
+        if (r < S) {
+#pragma unroll
+          for (int i = 0; i < kPer; ++i)
+            if (lane + 32 * i < a.E) l[i] += load_cluster(base[r] + (m * pitch + lane + 32 * i) * 4);
+        }
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const uint32_t e = lane + 32 * i;
+        if (e < a.E) {
+          if (a.bias) l[i] += __ldg(a.bias + e);
+          if (a.logits) a.logits[t * a.E + e] = l[i];
+        } else {
+          l[i] = -INFINITY;
+        }
+      }
+      pick_experts<kPer>(l, a.k, a.flags, lane, a.ids + t * a.k, a.weights + t * a.k);
+    }
+  }
+  __syncwarp();
+  cluster_sync();   // nobody leaves while a neighbour may still read its shared memory
 }
 
 }  // namespace zipmoe_dev
+
+namespace {
+
+bool g_router_ready[64];
+
+template <int kPer>
+zipmoe_status launch_router(int dev, const CUtensorMap &x_map, const CUtensorMap &gate_map, const zipmoe_dev::RouterArgs &a, uint32_t S,
+                            uint32_t smem, cudaStream_t stream) {
+  using namespace zipmoe_dev;
+  static bool ready[64];
+  if (!ready[dev]) {
+    if (cudaFuncSetAttribute(router_kernel<kPer>, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024) != cudaSuccess)
+      return ZIPMOE_ERR_CUDA;
+    ready[dev] = true;
+  }
+  cudaLaunchAttribute cluster;
+  cluster.id = cudaLaunchAttributeClusterDimension;
+  cluster.val.clusterDim.x = S;
+  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.stream = stream;
+  cfg.attrs = &cluster;
+  cfg.numAttrs = 1;
+  cfg.gridDim = dim3((a.T + kRouterRows - 1) / kRouterRows * S);
+  cfg.blockDim = dim3(kRouterThreads);
+  cfg.dynamicSmemBytes = smem;
+  return cudaLaunchKernelEx(&cfg, router_kernel<kPer>, x_map, gate_map, a) == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
+}
+
+}  // namespace
 
 extern "C" zipmoe_status zipmoe_route(const uint16_t *tokens, uint32_t T, uint64_t token_pitch, const uint16_t *gate,
                                       uint32_t n_experts, uint32_t hidden, const float *bias, uint32_t k, uint32_t flags,
                                       int32_t *topk_ids, float *topk_weights, float *logits, uint32_t *status_word,
                                       zipmoe_stream stream) {
+  using namespace zipmoe_dev;
   zipmoe_host::TraceRange trace("zipmoe_route");
-  (void)status_word;
-  if (n_experts == 0 || n_experts > zipmoe_dev::kMaxExperts || k == 0 || k > zipmoe_dev::kMaxTopK || k > n_experts ||
-      hidden == 0 || hidden > 32768 || hidden % 8 || token_pitch % 8)
+  if (n_experts == 0 || n_experts > kMaxExperts || k == 0 || k > kMaxTopK || k > n_experts || hidden == 0 || hidden > 32768 ||
+      hidden % 8 || token_pitch % 8)
     return ZIPMOE_ERR_UNSUPPORTED;
   if (flags & ~ZIPMOE_ROUTE_SOFTMAX_ALL) return ZIPMOE_ERR_INVALID_ARG;
   if (T == 0) return ZIPMOE_OK;
@@ -122,19 +287,47 @@ extern "C" zipmoe_status zipmoe_route(const uint16_t *tokens, uint32_t T, uint64
       ((reinterpret_cast<uintptr_t>(bias) | reinterpret_cast<uintptr_t>(topk_ids) | reinterpret_cast<uintptr_t>(topk_weights) |
         reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(status_word)) & 3))
     return ZIPMOE_ERR_INVALID_ARG;
-  zipmoe_dev::RouterArgs a;
-  a.tokens = tokens;
-  a.gate = gate;
+  if (token_pitch >= 1ull << 39 || T > 1u << 30) return ZIPMOE_ERR_UNSUPPORTED;   // (what a tensor map and a grid can hold)
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return ZIPMOE_ERR_CUDA;
+  if (!g_router_ready[dev]) {
+    int major = 0;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) return ZIPMOE_ERR_CUDA;
+    if (major != 10) return ZIPMOE_ERR_UNSUPPORTED;
+    g_router_ready[dev] = true;
+  }
+  RouterArgs a;
   a.bias = bias;
   a.ids = topk_ids;
   a.weights = topk_weights;
   a.logits = logits;
-  a.token_pitch = token_pitch;
+  a.status = status_word;
+  uint32_t tries = 0;
+  zipmoe_host::wait_fault_setting(&a.extra_tx, &tries);
+  a.limit_ns = tries < zipmoe_host::kWaitTries ? 1000000ull : 1000000000ull;   // (1 ms in the tests of the limit)
   a.T = T;
   a.E = n_experts;
   a.H = hidden;
   a.k = k;
   a.flags = flags;
-  zipmoe_dev::router_kernel<<<T, 256, 0, reinterpret_cast<cudaStream_t>(stream)>>>(a);
-  return cudaGetLastError() == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
+  a.N = (n_experts + 15) / 16 * 16;
+  a.tmem_cols = 32;
+  while (a.tmem_cols < a.N) a.tmem_cols <<= 1;
+  // two blocks per SM up to 128 experts, so that one streams while the other picks; then as many blocks per 128 tokens as
+  // the device runs at once
+  const uint32_t tiles = (T + kRouterRows - 1) / kRouterRows, steps = (hidden + 63) / 64, stage = (kRouterRows + a.N) * 128;
+  const uint32_t per_sm = a.N <= 128 ? 2 : 1;
+  a.stages = std::min(kRouterMaxStages, (per_sm == 2 ? 108u : 216u) * 1024 / stage);
+  uint32_t S = 8;
+  while (S > 1 && (S > steps || tiles * S > 148 * per_sm)) S >>= 1;
+  const uint32_t smem = 1024 + std::max(a.stages * stage, kRouterRows * (a.N + 1) * 4);
+  CUtensorMap x_map, gate_map;
+  if (!zipmoe_host::make_bf16_map(&x_map, tokens, T, hidden, token_pitch, kRouterRows, true) ||
+      !zipmoe_host::make_bf16_map(&gate_map, gate, n_experts, hidden, hidden, a.N, true))
+    return ZIPMOE_ERR_CUDA;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (n_experts <= 32) return launch_router<1>(dev, x_map, gate_map, a, S, smem, s);
+  if (n_experts <= 64) return launch_router<2>(dev, x_map, gate_map, a, S, smem, s);
+  if (n_experts <= 128) return launch_router<4>(dev, x_map, gate_map, a, S, smem, s);
+  return launch_router<8>(dev, x_map, gate_map, a, S, smem, s);
 }

@@ -23,7 +23,7 @@ struct WaitLimit {
   uint32_t *status;
   uint64_t limit_ns;
 };
-__device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, const WaitLimit &w) {
+static __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, const WaitLimit &w) {
   const uint64_t t0 = global_ns();
   for (;;) {
     if (mbar_try_wait(bar, parity)) return true;
