@@ -319,6 +319,25 @@ zipmoe_status zipmoe_decode_expert_ffn_noalloc(const uint16_t *tokens, uint32_t 
 
 #define ZIPMOE_NORM_RESIDUAL_F32 1u /* residual and residual_out are fp32 (else bf16 patterns) */
 
+/* One call of zipmoe_add_rmsnorm.  A HOST struct holding DEVICE pointers; pitches in elements between rows. */
+typedef struct {
+  const uint16_t *x;           /* in: [rows] of cols bf16 patterns, x_pitch apart                                   */
+  uint64_t x_pitch;
+  const void *residual;        /* in: residual_pitch apart, bf16 patterns or fp32; may be NULL                      */
+  uint64_t residual_pitch;
+  void *residual_out;          /* out: residual_out_pitch apart; may be NULL; may be `residual` itself with the same
+                                  pitch, may not overlap anything else                                             */
+  uint64_t residual_out_pitch;
+  const uint16_t *weight;      /* in: [cols] bf16 patterns                                                          */
+  uint16_t *out;               /* out: out_pitch apart, bf16 patterns; may be NULL; may be x with the same pitch    */
+  uint8_t *out_q;              /* out: out_pitch apart, e4m3 bytes; may be NULL (one of out and out_q is needed)    */
+  uint64_t out_pitch;
+  float *scales;               /* out: [rows][ceil(cols / group)] dense; NULL exactly if out_q is                   */
+  uint32_t rows, cols, group, flags;
+  float eps;
+  uint32_t reserved;           /* zero                                                                              */
+} zipmoe_norm_args;
+
 /* Residual addition and root-mean-square norm of `rows` rows of `cols` elements:
  *     h = x + residual                       (h = x where residual is NULL)
  *     residual_out = h                       (rounded to bf16 unless ZIPMOE_NORM_RESIDUAL_F32)
@@ -328,20 +347,27 @@ zipmoe_status zipmoe_decode_expert_ffn_noalloc(const uint16_t *tokens, uint32_t 
  * A group of zeros has scale 0 and zeros; q * scale gives the row back.  One launch on `stream`, asynchronous;
  * every input is read once.  A row whose sum of squares exceeds fp32 (elements of about 1e19) gives zeros, as the
  * formula in fp32 does; NaN and infinities come out as NaN.
- * device in : x (rows x_pitch elements apart), residual (rows residual_pitch apart; may be NULL), weight[cols] bf16
- * device out: residual_out (rows residual_out_pitch apart; may be NULL, may be `residual` itself with the same pitch,
- *             may not overlap anything else), out (rows out_pitch apart; may be NULL, may be x itself with the same pitch), out_q
- *             (e4m3 bytes, rows out_pitch apart; may be NULL), scales[rows][ceil(cols / group)] dense (NULL exactly
- *             if out_q is).  One of out and out_q must be given.
  * group     : 32, 64, 128 or 256 columns; 0, or any value >= cols, is the whole row.
- * Pitches are in elements, at least cols.  Any element alignment; rows and weight that start on 16-byte boundaries
- * are faster.  rows = 0 does nothing.  Limits: cols <= 32768 (ZIPMOE_ERR_UNSUPPORTED otherwise). */
-zipmoe_status zipmoe_add_rmsnorm(const uint16_t *x, uint64_t x_pitch, const void *residual, uint64_t residual_pitch,
-                                 void *residual_out, uint64_t residual_out_pitch, const uint16_t *weight, uint32_t rows,
-                                 uint32_t cols, float eps, uint16_t *out, uint8_t *out_q, uint64_t out_pitch, float *scales,
-                                 uint32_t group, uint32_t flags, zipmoe_stream stream);
+ * Pitches are at least cols.  Any element alignment; rows and weight that start on 16-byte boundaries are faster.
+ * rows = 0 does nothing.  Limits: cols <= 32768 (ZIPMOE_ERR_UNSUPPORTED otherwise). */
+zipmoe_status zipmoe_add_rmsnorm(const zipmoe_norm_args *args, zipmoe_stream stream);
 
 #define ZIPMOE_ROUTE_SOFTMAX_ALL 1u /* weights are the softmax over all experts, not renormalised over the chosen */
+
+/* One call of zipmoe_route.  A HOST struct holding DEVICE pointers. */
+typedef struct {
+  const uint16_t *tokens;      /* in: [T] rows of `hidden` bf16 patterns, token_pitch elements apart (a multiple of 8);
+                                  16-byte aligned                                                                  */
+  uint64_t token_pitch;
+  const uint16_t *gate;        /* in: [n_experts, hidden] bf16 patterns, 16-byte aligned                            */
+  const float *bias;           /* in: [n_experts]; may be NULL                                                      */
+  int32_t *topk_ids;           /* out: [T, k]                                                                       */
+  float *topk_weights;         /* out: [T, k]                                                                       */
+  float *logits;               /* out: [T, n_experts]; may be NULL                                                  */
+  uint32_t *status_word;       /* as for zipmoe_decode: code 3 when a wait ran out; may be NULL                     */
+  uint32_t T, n_experts, hidden, k, flags;
+  uint32_t reserved;           /* zero                                                                              */
+} zipmoe_route_args;
 
 /* The router: which experts every token goes to, and with what weights.
  *     logit[t, e] = sum_h tokens[t, h] * gate[e, h] + bias[e]        (fp32 accumulation)
@@ -350,16 +376,9 @@ zipmoe_status zipmoe_add_rmsnorm(const uint16_t *x, uint64_t x_pitch, const void
  * An expert whose logit is -infinity (a bias of -infinity switches it off) is never chosen: where fewer than k are
  * left, the remaining ids are -1 with weight 0.  A NaN logit counts as larger than every number, and makes the
  * token's weights NaN.  One launch on `stream`, asynchronous.
- * device in : tokens (T rows of `hidden`, token_pitch elements apart), gate [n_experts, hidden] bf16 patterns (both
- *             16-byte aligned, hidden and token_pitch multiples of 8), bias[n_experts] fp32 or NULL
- * device out: topk_ids [T, k], topk_weights [T, k], logits [T, n_experts] fp32 (may be NULL); status_word (nullable)
- *             as for zipmoe_decode: code 3 when a wait ran out.
- * Limits: n_experts <= 256, k <= 8, k <= n_experts, hidden <= 32768 (ZIPMOE_ERR_UNSUPPORTED otherwise).  T = 0 does
- * nothing. */
-zipmoe_status zipmoe_route(const uint16_t *tokens, uint32_t T, uint64_t token_pitch, const uint16_t *gate,
-                           uint32_t n_experts, uint32_t hidden, const float *bias, uint32_t k, uint32_t flags,
-                           int32_t *topk_ids, float *topk_weights, float *logits, uint32_t *status_word,
-                           zipmoe_stream stream);
+ * Limits: n_experts <= 256, k <= 8, k <= n_experts, hidden a multiple of 8 and <= 32768 (ZIPMOE_ERR_UNSUPPORTED
+ * otherwise).  T = 0 does nothing. */
+zipmoe_status zipmoe_route(const zipmoe_route_args *args, zipmoe_stream stream);
 
 /* The recovered experts of one MoE layer.  A HOST struct; `table` is DEVICE memory holding what
  * zipmoe_resident_experts_plan wrote. */

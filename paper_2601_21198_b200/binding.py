@@ -10,6 +10,7 @@ module raises.
 """
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -349,9 +350,12 @@ class ResidentExpertsStruct(ctypes.Structure):
     _fields_ = [("n_experts", _u32), ("hidden", _u32), ("inter", _u32), ("reserved", _u32), ("table", _vp)]
 
 
-_lib.zipmoe_add_rmsnorm.argtypes = [_vp, _u64, _vp, _u64, _vp, _u64, _vp, _u32, _u32, ctypes.c_float, _vp, _vp, _u64, _vp,
-                                    _u32, _u32, _vp]
-_lib.zipmoe_route.argtypes = [_vp, _u32, _u64, _vp, _u32, _u32, _vp, _u32, _u32, _vp, _vp, _vp, _vp, _vp]
+# zipmoe_norm_args and zipmoe_route_args, packed in one go (a call with one pointer costs a sixth of one with 17 arguments)
+_NORM_ARGS = struct.Struct("<11Q4IfI")
+_ROUTE_ARGS = struct.Struct("<8Q6I")
+assert _NORM_ARGS.size == 112 and _ROUTE_ARGS.size == 88
+_lib.zipmoe_add_rmsnorm.argtypes = [ctypes.c_char_p, _vp]
+_lib.zipmoe_route.argtypes = [ctypes.c_char_p, _vp]
 _lib.zipmoe_resident_experts_plan.argtypes = [ctypes.POINTER(_vp), _u32, _u32, _u32, _vp]
 _lib.zipmoe_expert_ffn_workspace_bytes.argtypes = [_u32, _u32, ctypes.POINTER(ResidentExpertsStruct), ctypes.POINTER(_u64)]
 _lib.zipmoe_expert_ffn_workspace_init.argtypes = [_vp, _u64, _vp]
@@ -365,18 +369,18 @@ for _f in ("zipmoe_add_rmsnorm", "zipmoe_route", "zipmoe_resident_experts_plan",
 def zipmoe_add_rmsnorm(x, x_pitch, residual, residual_pitch, residual_out, residual_out_pitch, weight, rows, cols, eps, out,
                        out_q, out_pitch, scales=None, group=0, flags=0, stream=None):
     """Pointer arguments are device tensors (or raw device addresses, or None); pitches in elements."""
-    _check("zipmoe_add_rmsnorm",
-           _lib.zipmoe_add_rmsnorm(_ptr(x), x_pitch, _ptr(residual), residual_pitch, _ptr(residual_out), residual_out_pitch,
-                                   _ptr(weight), rows, cols, eps, _ptr(out), _ptr(out_q), out_pitch, _ptr(scales), group,
-                                   flags, _ptr(stream)))
+    args = _NORM_ARGS.pack(_ptr(x) or 0, x_pitch, _ptr(residual) or 0, residual_pitch, _ptr(residual_out) or 0,
+                           residual_out_pitch, _ptr(weight) or 0, _ptr(out) or 0, _ptr(out_q) or 0, out_pitch,
+                           _ptr(scales) or 0, rows, cols, group, flags, eps, 0)
+    _check("zipmoe_add_rmsnorm", _lib.zipmoe_add_rmsnorm(args, _ptr(stream)))
 
 
 def zipmoe_route(tokens, T, token_pitch, gate, n_experts, hidden, bias, k, flags, topk_ids, topk_weights, logits=None,
                  status_word=None, stream=None):
     """Pointer arguments are device tensors (or raw device addresses, or None)."""
-    _check("zipmoe_route",
-           _lib.zipmoe_route(_ptr(tokens), T, token_pitch, _ptr(gate), n_experts, hidden, _ptr(bias), k, flags,
-                             _ptr(topk_ids), _ptr(topk_weights), _ptr(logits), _ptr(status_word), _ptr(stream)))
+    args = _ROUTE_ARGS.pack(_ptr(tokens) or 0, token_pitch, _ptr(gate) or 0, _ptr(bias) or 0, _ptr(topk_ids) or 0,
+                            _ptr(topk_weights) or 0, _ptr(logits) or 0, _ptr(status_word) or 0, T, n_experts, hidden, k, flags, 0)
+    _check("zipmoe_route", _lib.zipmoe_route(args, _ptr(stream)))
 
 
 def zipmoe_resident_experts_plan(tensors, n_experts, hidden, inter):
@@ -556,11 +560,11 @@ def _kind(name):
     return _KINDS[name]
 
 
-def _stream_of(device, stream):
-    """The handle of a torch stream, of the device's current one where none is given."""
+def _stream_of(index, stream):
+    """The handle of a torch stream, of the current one of device `index` where none is given."""
+    import torch
     if stream is None:
-        import torch
-        stream = torch.cuda.current_stream(device)
+        return torch._C._cuda_getCurrentRawStream(index)
     return stream.cuda_stream
 
 
@@ -574,21 +578,21 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _rows(name, t, rows, cols, kind):
-    """Row pitch, in elements, of a [rows, cols] device tensor whose rows are dense."""
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError("%s: shape %s, wanted (%d, %d)" % (name, tuple(t.shape), rows, cols))
-    if t.dtype not in _kind(kind) or not t.is_cuda:
-        raise ValueError("%s: a device tensor of %s is wanted, not %s on %s" % (name, kind, t.dtype, t.device))
-    if cols > 1 and t.stride(1) != 1:
+def _rows(name, t, shape, kinds, index):
+    """Row pitch, in elements, of a tensor of this shape on device `index` whose rows are dense."""
+    stride = t.stride()
+    if t.shape != shape or t.dtype not in kinds or t.get_device() != index or index < 0:
+        raise ValueError("%s: a tensor %s of %s on device %d is wanted, not %s of %s on %s" %
+                         (name, shape, kinds[0], index, tuple(t.shape), t.dtype, t.device))
+    if stride[1] != 1 and shape[1] > 1:
         raise ValueError("%s: the elements of a row are not next to each other" % name)
-    return t.stride(0) if rows > 1 else cols
+    return stride[0] if shape[0] > 1 else shape[1]
 
 
-def _dense(name, t, shape, kind):
-    if tuple(t.shape) != shape or t.dtype not in _kind(kind) or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError("%s: a contiguous device tensor %s of %s is wanted, not %s of %s on %s" %
-                         (name, shape, kind, tuple(t.shape), t.dtype, t.device))
+def _dense(name, t, shape, kinds, index):
+    if t.shape != shape or t.dtype not in kinds or t.get_device() != index or index < 0 or not t.is_contiguous():
+        raise ValueError("%s: a contiguous tensor %s of %s on device %d is wanted, not %s of %s on %s" %
+                         (name, shape, kinds[0], index, tuple(t.shape), t.dtype, t.device))
 
 
 class RmsNorm:
@@ -596,36 +600,38 @@ class RmsNorm:
     bf16 tensors or int16 patterns [rows, cols] whose rows may lie apart; the residual stream is of that kind or fp32."""
 
     def __init__(self, weight, eps=1e-6):
-        _dense("weight", weight, (weight.numel(),), "bf16")
+        self.index = weight.get_device()
+        _dense("weight", weight, (weight.numel(),), _kind("bf16"), self.index)
         self.weight, self.eps, self.cols = weight, float(eps), weight.numel()
 
     def n_groups(self, group):
         return 1 if group <= 0 or group >= self.cols else -(-self.cols // group)
 
     def _call(self, x, residual, residual_out, out, out_q, scales, group, stream):
-        rows, cols = x.shape[0], self.cols
-        x_pitch = _rows("x", x, rows, cols, "bf16")
-        res_pitch = res_out_pitch = cols
-        flags = 0
+        shape, index, bf16 = (x.shape[0], self.cols), self.index, _kind("bf16")
+        x_pitch = _rows("x", x, shape, bf16, index)
+        res = res_out = res_pitch = res_out_pitch = flags = 0
         if residual is not None:
-            kind = "fp32" if residual.element_size() == 4 else "bf16"
-            flags = NORM_RESIDUAL_F32 if kind == "fp32" else 0
-            res_pitch = _rows("residual", residual, rows, cols, kind)
+            kinds = bf16 if residual.dtype in bf16 else _kind("fp32")
+            flags = 0 if kinds is bf16 else NORM_RESIDUAL_F32
+            res_pitch, res = _rows("residual", residual, shape, kinds, index), residual.data_ptr()
             if residual_out is not None:
-                res_out_pitch = _rows("residual_out", residual_out, rows, cols, kind)
+                res_out_pitch, res_out = _rows("residual_out", residual_out, shape, kinds, index), residual_out.data_ptr()
         elif residual_out is not None:
             raise ValueError("residual_out without a residual")
-        out_pitch = cols
+        out_at = q_at = scales_at = 0
         if out is not None:
-            out_pitch = _rows("out", out, rows, cols, "bf16")
+            out_pitch, out_at = _rows("out", out, shape, bf16, index), out.data_ptr()
         if out_q is not None:
-            q_pitch = _rows("out_q", out_q, rows, cols, "e4m3")
+            q_pitch, q_at = _rows("out_q", out_q, shape, _kind("e4m3"), index), out_q.data_ptr()
             if out is not None and out_pitch != q_pitch:
                 raise ValueError("out and out_q have rows %d and %d apart" % (out_pitch, q_pitch))
             out_pitch = q_pitch
-            _dense("scales", scales, (rows, self.n_groups(group)), "fp32")
-        zipmoe_add_rmsnorm(x, x_pitch, residual, res_pitch, residual_out, res_out_pitch, self.weight, rows, cols, self.eps,
-                           out, out_q, out_pitch, scales, group, flags, _stream_of(x.device, stream))
+            _dense("scales", scales, (shape[0], self.n_groups(group)), _kind("fp32"), index)
+            scales_at = scales.data_ptr()
+        args = _NORM_ARGS.pack(x.data_ptr(), x_pitch, res, res_pitch, res_out, res_out_pitch, self.weight.data_ptr(), out_at, q_at,
+                               out_pitch, scales_at, shape[0], shape[1], max(group, 0), flags, self.eps, 0)
+        _check("zipmoe_add_rmsnorm", _lib.zipmoe_add_rmsnorm(args, _stream_of(index, stream)))
 
     def add_norm(self, x, residual=None, residual_out=None, out=None, stream=None):
         """Returns out [rows, cols] (bf16); residual_out (may be `residual` itself) gets x + residual."""
@@ -649,30 +655,34 @@ class Router:
 
     def __init__(self, gate, k, bias=None, renormalise=True):
         import torch
+        self.index = gate.get_device()
         self.n_experts, self.hidden = gate.shape
-        _dense("gate", gate, (self.n_experts, self.hidden), "bf16")
+        _dense("gate", gate, (self.n_experts, self.hidden), _kind("bf16"), self.index)
         if bias is not None:
-            _dense("bias", bias, (self.n_experts,), "fp32")
+            _dense("bias", bias, (self.n_experts,), _kind("fp32"), self.index)
         self.gate, self.bias, self.k = gate, bias, int(k)
         self.flags = 0 if renormalise else ROUTE_SOFTMAX_ALL
         self.status = torch.zeros(1, dtype=torch.int32, device=gate.device)
 
     def route(self, tokens, ids=None, weights=None, logits=None, stream=None):
         """tokens [T, hidden] -> ids [T, k] int32, weights [T, k] fp32; logits, if given, gets [T, n_experts] fp32."""
-        T = tokens.shape[0]
-        pitch = _rows("tokens", tokens, T, self.hidden, "bf16")
+        T, index = tokens.shape[0], self.index
+        pitch = _rows("tokens", tokens, (T, self.hidden), _kind("bf16"), index)
+        chosen = (T, self.k)
         if ids is None:
-            ids = _empty((T, self.k), _kind("int32")[0], tokens.device, stream)
+            ids = _empty(chosen, _kind("int32")[0], tokens.device, stream)
         else:
-            _dense("ids", ids, (T, self.k), "int32")
+            _dense("ids", ids, chosen, _kind("int32"), index)
         if weights is None:
-            weights = _empty((T, self.k), _kind("fp32")[0], tokens.device, stream)
+            weights = _empty(chosen, _kind("fp32")[0], tokens.device, stream)
         else:
-            _dense("weights", weights, (T, self.k), "fp32")
+            _dense("weights", weights, chosen, _kind("fp32"), index)
         if logits is not None:
-            _dense("logits", logits, (T, self.n_experts), "fp32")
-        zipmoe_route(tokens, T, pitch, self.gate, self.n_experts, self.hidden, self.bias, self.k, self.flags, ids, weights,
-                     logits, self.status, _stream_of(tokens.device, stream))
+            _dense("logits", logits, (T, self.n_experts), _kind("fp32"), index)
+        args = _ROUTE_ARGS.pack(tokens.data_ptr(), pitch, self.gate.data_ptr(), 0 if self.bias is None else self.bias.data_ptr(),
+                                ids.data_ptr(), weights.data_ptr(), 0 if logits is None else logits.data_ptr(),
+                                self.status.data_ptr(), T, self.n_experts, self.hidden, self.k, self.flags, 0)
+        _check("zipmoe_route", _lib.zipmoe_route(args, _stream_of(index, stream)))
         return ids, weights
 
 
@@ -684,41 +694,55 @@ class ResidentExperts:
         import torch
         if len(tensors) % 3 or not tensors:
             raise ValueError("three tensors per expert are wanted")
+        self.index = tensors[0].get_device()
         for i, t in enumerate(tensors):
             if t.numel() != hidden * inter:
                 raise ValueError("tensor %d: %d elements, wanted %d x %d" % (i, t.numel(), hidden, inter))
-            _dense("tensor %d" % i, t, tuple(t.shape), "bf16")
+            _dense("tensor %d" % i, t, t.shape, _kind("bf16"), self.index)
         self.tensors = list(tensors)      # the experts' memory is theirs: keep it while the table points at it
         self.device = tensors[0].device
         self.hidden, self.inter = hidden, inter
         self.table = torch.from_numpy(zipmoe_resident_experts_plan(self.tensors, len(tensors) // 3, hidden, inter)).to(self.device)
         self.struct = ResidentExpertsStruct(len(tensors) // 3, hidden, inter, 0, self.table.data_ptr())
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
-        self._ws = {}
+        self._struct_at = ctypes.byref(self.struct)
+        self._ws, self._need = {}, {}
 
     @classmethod
     def from_decode(cls, plan, out, hidden, inter):
         """The experts that one decode launch recovered: `plan` a DecodePlan over 3 * n_experts blobs, `out` its output."""
         return cls([plan.tensor_slice(out, i) for i in range(len(plan.infos))], hidden, inter)
 
+    def _workspace(self, T, k, handle, stream):
+        """The stream's workspace, large enough for T tokens with k experts each.  One that has become too small is kept: a
+        captured graph may still use it."""
+        need = self._need.get((T, k))
+        if need is None:
+            fits = T if T > 128 else 1 << max(T - 1, 15).bit_length()      # some more tokens than asked for: it seldom grows
+            need = self._need[(T, k)] = zipmoe_expert_ffn_workspace_bytes(min(fits, 256) if T <= 256 else T, k, self.struct)
+        held = self._ws.setdefault(handle, [])
+        if not held or held[-1].numel() < need:
+            held.append(_empty(need, _kind("e4m3")[1], self.device, stream))
+            zipmoe_expert_ffn_workspace_init(held[-1], need, handle)
+        return held[-1]
+
     def ffn(self, tokens, topk_ids, topk_weights, out=None, stream=None):
         """tokens [T, hidden] bf16 (or int16 patterns), topk_ids [T, k] int32, topk_weights [T, k] float32 or None: device
-        tensors.  Returns out [T, hidden].  The workspace is kept per size and stream, so calls on different streams may
+        tensors.  Returns out [T, hidden].  Every stream has a workspace of its own, so calls on different streams may
         overlap."""
         T, k = topk_ids.shape
-        _dense("tokens", tokens, (T, self.hidden), "bf16")
-        _dense("topk_ids", topk_ids, (T, k), "int32")
+        index, shape = self.index, (T, self.hidden)
+        _dense("tokens", tokens, shape, _kind("bf16"), index)
+        _dense("topk_ids", topk_ids, (T, k), _kind("int32"), index)
         if topk_weights is not None:
-            _dense("topk_weights", topk_weights, (T, k), "fp32")
-        s = _stream_of(self.device, stream)
-        ws = self._ws.get((T, k, s))
-        if ws is None:
-            n = zipmoe_expert_ffn_workspace_bytes(T, k, self.struct)
-            ws = self._ws[(T, k, s)] = _empty(n, _kind("e4m3")[1], self.device, stream)
-            zipmoe_expert_ffn_workspace_init(ws, n, s)
+            _dense("topk_weights", topk_weights, (T, k), _kind("fp32"), index)
         if out is None:
-            out = _empty((T, self.hidden), tokens.dtype, self.device, stream)
+            out = _empty(shape, tokens.dtype, self.device, stream)
         else:
-            _dense("out", out, (T, self.hidden), "bf16")
-        zipmoe_expert_ffn(tokens, T, topk_ids, topk_weights, k, self.struct, out, ws, ws.numel(), self.status, s)
+            _dense("out", out, shape, _kind("bf16"), index)
+        handle = _stream_of(index, stream)
+        ws = self._workspace(T, k, handle, stream)
+        _check("zipmoe_expert_ffn",
+               _lib.zipmoe_expert_ffn(tokens.data_ptr(), T, topk_ids.data_ptr(), None if topk_weights is None else topk_weights.data_ptr(),
+                                      k, self._struct_at, out.data_ptr(), ws.data_ptr(), ws.numel(), self.status.data_ptr(), handle))
         return out

@@ -192,47 +192,44 @@ void launch_norm(const zipmoe_dev::NormArgs &a, cudaStream_t stream) {
 
 }  // namespace
 
-extern "C" zipmoe_status zipmoe_add_rmsnorm(const uint16_t *x, uint64_t x_pitch, const void *residual,
-                                            uint64_t residual_pitch, void *residual_out, uint64_t residual_out_pitch,
-                                            const uint16_t *weight, uint32_t rows, uint32_t cols, float eps, uint16_t *out,
-                                            uint8_t *out_q, uint64_t out_pitch, float *scales, uint32_t group,
-                                            uint32_t flags, zipmoe_stream stream_) {
+extern "C" zipmoe_status zipmoe_add_rmsnorm(const zipmoe_norm_args *n, zipmoe_stream stream_) {
   zipmoe_host::TraceRange trace("zipmoe_add_rmsnorm");
-  if (cols == 0 || (flags & ~ZIPMOE_NORM_RESIDUAL_F32) || !(eps >= 0.f)) return ZIPMOE_ERR_INVALID_ARG;
-  if (cols > 32768) return ZIPMOE_ERR_UNSUPPORTED;
-  if (rows == 0) return ZIPMOE_OK;
-  if (!x || !weight || (!out && !out_q) || (out_q != nullptr) != (scales != nullptr) || (residual_out && !residual))
+  if (!n || n->cols == 0 || (n->flags & ~ZIPMOE_NORM_RESIDUAL_F32) || !(n->eps >= 0.f) || n->reserved) return ZIPMOE_ERR_INVALID_ARG;
+  if (n->cols > 32768) return ZIPMOE_ERR_UNSUPPORTED;
+  if (n->rows == 0) return ZIPMOE_OK;
+  if (!n->x || !n->weight || (!n->out && !n->out_q) || (n->out_q != nullptr) != (n->scales != nullptr) || (n->residual_out && !n->residual))
     return ZIPMOE_ERR_INVALID_ARG;
-  if (x_pitch < cols || out_pitch < cols || (residual && residual_pitch < cols) ||
-      (residual_out && residual_out_pitch < cols)) return ZIPMOE_ERR_INVALID_ARG;
-  if (group >= cols) group = 0;
+  if (n->x_pitch < n->cols || n->out_pitch < n->cols || (n->residual && n->residual_pitch < n->cols) ||
+      (n->residual_out && n->residual_out_pitch < n->cols))
+    return ZIPMOE_ERR_INVALID_ARG;
+  const uint32_t group = n->group >= n->cols ? 0 : n->group;
   if (group && group != 32 && group != 64 && group != 128 && group != 256) return ZIPMOE_ERR_UNSUPPORTED;
-  const bool f32 = flags & ZIPMOE_NORM_RESIDUAL_F32;
+  const bool f32 = n->flags & ZIPMOE_NORM_RESIDUAL_F32;
   auto bits = [](const void *p) { return reinterpret_cast<uintptr_t>(p); };
-  if (((bits(x) | bits(weight) | bits(out)) & 1) || ((bits(residual) | bits(residual_out)) & (f32 ? 3 : 1)) || (bits(scales) & 3))
-    return ZIPMOE_ERR_INVALID_ARG;
+  const uintptr_t bf16_bits = bits(n->x) | bits(n->weight) | bits(n->out), residual_bits = bits(n->residual) | bits(n->residual_out);
+  if ((bf16_bits & 1) || (residual_bits & (f32 ? 3 : 1)) || (bits(n->scales) & 3)) return ZIPMOE_ERR_INVALID_ARG;
   zipmoe_dev::NormArgs a;
-  a.x = x;
-  a.residual = residual;
-  a.residual_out = residual_out;
-  a.weight = weight;
-  a.out = out;
-  a.out_q = out_q;
-  a.scales = scales;
-  a.x_pitch = x_pitch;
-  a.residual_pitch = residual_pitch;
-  a.residual_out_pitch = residual_out_pitch;
-  a.out_pitch = out_pitch;
-  a.rows = rows;
-  a.cols = cols;
+  a.x = n->x;
+  a.residual = n->residual;
+  a.residual_out = n->residual_out;
+  a.weight = n->weight;
+  a.out = n->out;
+  a.out_q = n->out_q;
+  a.scales = n->scales;
+  a.x_pitch = n->x_pitch;
+  a.residual_pitch = n->residual_pitch;
+  a.residual_out_pitch = n->residual_out_pitch;
+  a.out_pitch = n->out_pitch;
+  a.rows = n->rows;
+  a.cols = n->cols;
   a.group = group;
-  a.groups = group ? (cols + group - 1) / group : 1;
-  a.eps = eps;
-  const bool aligned = cols % 8 == 0 && x_pitch % 8 == 0 && out_pitch % 8 == 0 && (!residual || residual_pitch % 8 == 0) &&
-                       (!residual_out || residual_out_pitch % 8 == 0) &&
-                       ((bits(x) | bits(weight) | bits(residual) | bits(residual_out) | bits(out)) & 15) == 0 && (bits(out_q) & 7) == 0;
+  a.groups = group ? (n->cols + group - 1) / group : 1;
+  a.eps = n->eps;
+  const bool aligned = (n->cols | n->x_pitch | n->out_pitch | (n->residual ? n->residual_pitch : 0) |
+                        (n->residual_out ? n->residual_out_pitch : 0)) % 8 == 0 &&
+                       ((bf16_bits | residual_bits) & 15) == 0 && (bits(n->out_q) & 7) == 0;
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
-  if (!residual) aligned ? launch_norm<void, true>(a, stream) : launch_norm<void, false>(a, stream);
+  if (!n->residual) aligned ? launch_norm<void, true>(a, stream) : launch_norm<void, false>(a, stream);
   else if (f32) aligned ? launch_norm<float, true>(a, stream) : launch_norm<float, false>(a, stream);
   else aligned ? launch_norm<uint16_t, true>(a, stream) : launch_norm<uint16_t, false>(a, stream);
   return cudaGetLastError() == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;

@@ -271,23 +271,22 @@ zipmoe_status launch_router(int dev, const CUtensorMap &x_map, const CUtensorMap
 
 }  // namespace
 
-extern "C" zipmoe_status zipmoe_route(const uint16_t *tokens, uint32_t T, uint64_t token_pitch, const uint16_t *gate,
-                                      uint32_t n_experts, uint32_t hidden, const float *bias, uint32_t k, uint32_t flags,
-                                      int32_t *topk_ids, float *topk_weights, float *logits, uint32_t *status_word,
-                                      zipmoe_stream stream) {
+extern "C" zipmoe_status zipmoe_route(const zipmoe_route_args *r, zipmoe_stream stream) {
   using namespace zipmoe_dev;
   zipmoe_host::TraceRange trace("zipmoe_route");
-  if (n_experts == 0 || n_experts > kMaxExperts || k == 0 || k > kMaxTopK || k > n_experts || hidden == 0 || hidden > 32768 ||
-      hidden % 8 || token_pitch % 8)
+  if (!r) return ZIPMOE_ERR_INVALID_ARG;
+  const uint32_t T = r->T, n_experts = r->n_experts, hidden = r->hidden;
+  if (n_experts == 0 || n_experts > kMaxExperts || r->k == 0 || r->k > kMaxTopK || r->k > n_experts || hidden == 0 || hidden > 32768 ||
+      hidden % 8 || r->token_pitch % 8)
     return ZIPMOE_ERR_UNSUPPORTED;
-  if (flags & ~ZIPMOE_ROUTE_SOFTMAX_ALL) return ZIPMOE_ERR_INVALID_ARG;
+  if ((r->flags & ~ZIPMOE_ROUTE_SOFTMAX_ALL) || r->reserved) return ZIPMOE_ERR_INVALID_ARG;
   if (T == 0) return ZIPMOE_OK;
-  if (!tokens || !gate || !topk_ids || !topk_weights || token_pitch < hidden) return ZIPMOE_ERR_INVALID_ARG;
-  if (((reinterpret_cast<uintptr_t>(tokens) | reinterpret_cast<uintptr_t>(gate)) & 15) ||
-      ((reinterpret_cast<uintptr_t>(bias) | reinterpret_cast<uintptr_t>(topk_ids) | reinterpret_cast<uintptr_t>(topk_weights) |
-        reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(status_word)) & 3))
+  if (!r->tokens || !r->gate || !r->topk_ids || !r->topk_weights || r->token_pitch < hidden) return ZIPMOE_ERR_INVALID_ARG;
+  auto bits = [](const void *p) { return reinterpret_cast<uintptr_t>(p); };
+  if (((bits(r->tokens) | bits(r->gate)) & 15) ||
+      ((bits(r->bias) | bits(r->topk_ids) | bits(r->topk_weights) | bits(r->logits) | bits(r->status_word)) & 3))
     return ZIPMOE_ERR_INVALID_ARG;
-  if (token_pitch >= 1ull << 39 || T > 1u << 30) return ZIPMOE_ERR_UNSUPPORTED;   // (what a tensor map and a grid can hold)
+  if (r->token_pitch >= 1ull << 39 || T > 1u << 30) return ZIPMOE_ERR_UNSUPPORTED;   // (what a tensor map and a grid can hold)
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return ZIPMOE_ERR_CUDA;
   if (!g_router_ready[dev]) {
@@ -297,19 +296,19 @@ extern "C" zipmoe_status zipmoe_route(const uint16_t *tokens, uint32_t T, uint64
     g_router_ready[dev] = true;
   }
   RouterArgs a;
-  a.bias = bias;
-  a.ids = topk_ids;
-  a.weights = topk_weights;
-  a.logits = logits;
-  a.status = status_word;
+  a.bias = r->bias;
+  a.ids = r->topk_ids;
+  a.weights = r->topk_weights;
+  a.logits = r->logits;
+  a.status = r->status_word;
   uint32_t tries = 0;
   zipmoe_host::wait_fault_setting(&a.extra_tx, &tries);
   a.limit_ns = tries < zipmoe_host::kWaitTries ? 1000000ull : 1000000000ull;   // (1 ms in the tests of the limit)
   a.T = T;
   a.E = n_experts;
   a.H = hidden;
-  a.k = k;
-  a.flags = flags;
+  a.k = r->k;
+  a.flags = r->flags;
   a.N = (n_experts + 15) / 16 * 16;
   a.tmem_cols = 32;
   while (a.tmem_cols < a.N) a.tmem_cols <<= 1;
@@ -322,8 +321,8 @@ extern "C" zipmoe_status zipmoe_route(const uint16_t *tokens, uint32_t T, uint64
   while (S > 1 && (S > steps || tiles * S > 148 * per_sm)) S >>= 1;
   const uint32_t smem = 1024 + std::max(a.stages * stage, kRouterRows * (a.N + 1) * 4);
   CUtensorMap x_map, gate_map;
-  if (!zipmoe_host::make_bf16_map(&x_map, tokens, T, hidden, token_pitch, kRouterRows, true) ||
-      !zipmoe_host::make_bf16_map(&gate_map, gate, n_experts, hidden, hidden, a.N, true))
+  if (!zipmoe_host::make_bf16_map(&x_map, r->tokens, T, hidden, r->token_pitch, kRouterRows, true) ||
+      !zipmoe_host::make_bf16_map(&gate_map, r->gate, n_experts, hidden, hidden, a.N, true))
     return ZIPMOE_ERR_CUDA;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (n_experts <= 32) return launch_router<1>(dev, x_map, gate_map, a, S, smem, s);
