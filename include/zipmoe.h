@@ -387,7 +387,7 @@ typedef struct {
   uint32_t n_experts, hidden, inter, reserved; /* hidden, inter: multiples of 8                                   */
   const void *table;                           /* device [3 * n_experts * ZIPMOE_RESIDENT_ENTRY_BYTES], 64-byte aligned */
 } zipmoe_resident_experts;
-#define ZIPMOE_RESIDENT_ENTRY_BYTES 128u
+#define ZIPMOE_RESIDENT_ENTRY_BYTES 256u
 
 /* Describes recovered experts to zipmoe_expert_ffn: one opaque entry per tensor, which the caller copies to the
  * device as it is.  Written once per layer (and again for an expert whose tensors move).

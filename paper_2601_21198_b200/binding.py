@@ -342,7 +342,7 @@ def zipmoe_decode_expert_ffn_noalloc(tokens, T, topk_ids, topk_weights, k, exper
 # ---- the rest of the expert sublayer: norm, router, experts that are already recovered --------------------
 NORM_RESIDUAL_F32 = 1       # zipmoe_add_rmsnorm flag: residual and residual_out are fp32
 ROUTE_SOFTMAX_ALL = 1       # zipmoe_route flag: weights are not renormalised over the chosen experts
-RESIDENT_ENTRY_BYTES = 128
+RESIDENT_ENTRY_BYTES = 256
 
 
 class ResidentExpertsStruct(ctypes.Structure):

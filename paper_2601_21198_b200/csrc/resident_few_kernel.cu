@@ -1,0 +1,419 @@
+// The resident experts for at most 8 tokens, where a call is short enough for every hand-over between blocks to show.
+//     g = W1 x,  u = W3 x,  h = bf16(SiLU(g) * u),  y = W2 h,  out[t] = bf16(sum_j w[t, j] * y)
+// Bound: the active experts' weights, 6 * hidden * inter bytes each, read once; beyond that the latency of a call.
+//
+// Every block owns a slice of rows - inter / SMs rows of every W1 and W3, hidden / SMs rows of every W2 - and all of their
+// columns.  So every sum is finished inside one block: no partial sums cross memory, the experts' combination happens in
+// the block that owns the output rows, and blocks wait for one another once, for h.
+//   * A chunk is 512 columns of up to 16 rows of W1 and of W3, or of up to 32 rows of W2.  One thread brings it into a ring
+//     of stages: a tensor map that sees the matrix as [columns / 64][rows][64] delivers a box of 8 x rows x 64 in one copy,
+//     each 64 columns a tile in the 128-byte swizzle.  (One bulk copy per row and 1 KB was tried: the copy engine takes
+//     38 ns for each, 4 TB/s.  Loads into registers were tried: 12 warps with 16 loads in flight each, 4.8 TB/s.)
+//     It runs ahead across experts, and asks the first chunks of W2 into the second-level cache before h is there.
+//   * Another warp adds the same columns of the expert's tokens (x, then h).
+//   * Eight warps take the chunk's 16-column steps in turn: ldmatrix, mma.sync m16n8k16 (weights the 16 rows, tokens the 8
+//     columns; fp32 sums in registers).  With so few tokens these need a tenth of the issue slots of the time that the
+//     bytes take; a tcgen05 operand of 128 rows would be nine tenths empty with 10 to 28 rows per block.
+//   * At the end of a job (one expert's set of rows) they leave their partial sums in shared memory and go on; four more
+//     warps add them and finish the job.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "zipmoe.h"
+#include "resident.cuh"
+
+namespace zipmoe_dev {
+
+constexpr uint32_t kFewThreads = 64 + 256 + 128;       // weights, activations, eight warps of products, four of sums
+constexpr uint32_t kFewCols = 512, kFewRowBytes = kFewCols * 2;
+constexpr uint32_t kFewPitch = kFewRowBytes + 16;      // of a token's columns: eight tokens' words fall into different banks
+constexpr uint32_t kFewTokenBytes = 9 * 1024;          // eight of them
+constexpr uint32_t kFewAheadBytes = 192 * 1024;        // of W2 that a block asks into the cache before h is there
+constexpr uint32_t kFewSumPitch = 20;                  // floats between the columns of a warp's 16 rows of sums: no bank conflicts
+
+struct FewArgs {
+  const uint16_t *tokens;
+  const int32_t *ids;
+  const float *weights;
+  const uint8_t *table;
+  uint16_t *out;
+  ResidentSync *sync;
+  uint16_t *h;              // [choices][I]
+  uint32_t *status;
+  uint64_t limit_ns;
+  uint32_t T, k, E, H, I;
+  uint32_t R1, S1, R2, S2;  // rows of a block, rows of a set: of W1 and W3, of W2
+  uint32_t stages, w_bytes, extra_tx;
+};
+
+// shared memory: [ring][sums, two sets][outputs][active experts][masks][ids, weights][barriers, words]
+constexpr uint32_t kFewSumBytes = 8 * 2 * 8 * kFewSumPitch * 4;
+__host__ __device__ inline uint32_t few_control_bytes(uint32_t E, uint32_t T, uint32_t k) {
+  return 2 * kFewSumBytes + T * 32 * 4 + 64 * (uint32_t)sizeof(Active) + pad16(E * 4) + 2 * pad16(T * k * 4) + (2 * kResMaxStages + 4) * 8 + 32;
+}
+
+__device__ __forceinline__ void load_a(uint32_t addr, uint32_t *r) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ void mma_16816(float *d, const uint32_t *a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t load_b(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t nth_bit(uint32_t mask, uint32_t n) {   // place of the n-th set bit (counted from 0)
+  for (; n > 0; --n) mask &= mask - 1;
+  return __ffs(mask) - 1;
+}
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void *map, int32_t x, int32_t y, int32_t z, uint32_t bar, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4}], "
+      "[%5], %6;" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar), "l"(policy)
+      : "memory");
+}
+__device__ __forceinline__ void tma_prefetch_3d(const void *map, int32_t x, int32_t y, int32_t z) {
+  asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(map), "r"(x), "r"(y), "r"(z) : "memory");
+}
+
+__global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const FewArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x, G = gridDim.x, choices = a.T * a.k;
+  const uint32_t stage_bytes = a.w_bytes + kFewTokenBytes;
+  uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint8_t *ctl = smem + a.stages * stage_bytes;
+  float *sums = reinterpret_cast<float *>(ctl);                       // [2][8 warps][2][8][kFewSumPitch]
+  ctl += 2 * kFewSumBytes;
+  float *outs = reinterpret_cast<float *>(ctl);                       // [T][32]
+  ctl += a.T * 32 * 4;
+  Active *act = reinterpret_cast<Active *>(ctl);
+  ctl += 64 * sizeof(Active);                                        // at most 8 * 8 choices
+  uint32_t *mask = reinterpret_cast<uint32_t *>(ctl);
+  ctl += pad16(a.E * 4);
+  int32_t *ids = reinterpret_cast<int32_t *>(ctl);
+  ctl += pad16(choices * 4);
+  float *wts = reinterpret_cast<float *>(ctl);
+  ctl += pad16(choices * 4);
+  uint64_t *bars = reinterpret_cast<uint64_t *>(ctl);
+  uint32_t *words = reinterpret_cast<uint32_t *>(bars + 2 * kResMaxStages + 4);   // unused, dead, active
+  volatile uint32_t *dead = words + 1;
+  const uint32_t ring = smem_addr(smem), full = smem_addr(bars), empty = full + 8 * kResMaxStages, sums_full = empty + 8 * kResMaxStages, sums_empty = sums_full + 16;
+  const WaitLimit lim = {dead, a.status, a.limit_ns};
+
+  // ---- everything that has to come from memory first, at once ----
+  const uint32_t magic = __ldcg(&a.sync->magic);
+  const int32_t my_id = tid < choices ? __ldg(a.ids + tid) : -1;
+  const float my_wt = tid < choices && a.weights ? __ldg(a.weights + tid) : 1.0f;
+  prefetch_table(a.table, a.E, cta * kFewThreads + tid, G * kFewThreads);
+  for (uint32_t i = tid; i < a.E; i += kFewThreads) mask[i] = 0;
+  if (tid == 0) {
+    for (uint32_t s = 0; s < a.stages; ++s) {
+      mbar_init(full + 8 * s, 2);
+      mbar_init(empty + 8 * s, 8);
+    }
+    for (uint32_t b = 0; b < 2; ++b) {
+      mbar_init(sums_full + 8 * b, 8);
+      mbar_init(sums_empty + 8 * b, 4);
+    }
+    *dead = 0;
+    fence_barrier_init();
+  }
+  __syncthreads();
+  if (tid < choices) {
+    ids[tid] = my_id;
+    wts[tid] = my_wt;
+    if (my_id >= 0 && my_id < (int32_t)a.E) atomicOr(&mask[my_id], 1u << (tid / a.k));
+    else if (my_id >= 0) report(a.status, kStatusBadDescriptor);
+  }
+  __syncthreads();
+  if (warp == 0) {   // experts per * lane .. per * lane + per - 1
+    const uint32_t per = (a.E + 31) / 32;
+    uint32_t cnt[8], sum = 0;   // active experts << 16 | choices
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+      cnt[i] = i < per && per * lane + i < a.E ? __popc(mask[per * lane + i]) : 0;
+      sum += (cnt[i] ? 1u << 16 : 0) + cnt[i];
+    }
+    uint32_t at = sum;
+#pragma unroll
+    for (uint32_t d = 1; d < 32; d <<= 1) {
+      const uint32_t p = __shfl_up_sync(0xFFFFFFFFu, at, d);
+      if (lane >= d) at += p;
+    }
+    if (lane == 31) words[2] = at >> 16;
+    at -= sum;
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i)
+      if (cnt[i]) {
+        act[at >> 16] = Active{per * lane + i, cnt[i], 0, at & 0xFFFFu};
+        at += (1u << 16) + cnt[i];
+      }
+  }
+  __syncthreads();
+  const bool prepared = magic == kResMagic;
+  const uint32_t n_active = prepared ? words[2] : 0;
+  // this block's rows, in sets; a phase's chunks run over experts, sets and columns (gate/up) or sets, experts and columns
+  const uint32_t row0[2] = {min(a.I, cta * a.R1), min(a.H, cta * a.R2)}, row1[2] = {min(a.I, (cta + 1) * a.R1), min(a.H, (cta + 1) * a.R2)};
+  const uint32_t sets[2] = {(row1[0] - row0[0] + a.S1 - 1) / a.S1, (row1[1] - row0[1] + a.S2 - 1) / a.S2};
+  const uint32_t h_blocks = n_active ? (a.I + a.R1 - 1) / a.R1 : 0;   // blocks that have rows of W1
+
+  if (warp == 0) {
+    // ---- weights ----
+    for (uint32_t i = lane; i < 3 * n_active; i += 32) {   // the experts' maps, W1 and W3 first
+      const uint32_t down = i >= 2 * n_active, ai = down ? i - 2 * n_active : i >> 1;
+      const uint8_t *m = sliced_map(a.table, act[ai].e, down ? 2 : i & 1);
+      acquire_map(m);
+      prefetch_map(m);
+    }
+    __syncwarp();
+    if (lane == 0) {
+      const uint64_t policy = policy_evict_first();
+      RingAt at;
+      bool ok = true;
+      for (uint32_t p = 0; p < 2 && ok; ++p) {
+        const uint32_t K = p == 0 ? a.H : a.I, per_set = p == 0 ? a.S1 : a.S2, jobs = n_active * sets[p];
+        for (uint32_t j = 0; j < jobs && ok; ++j) {
+          const uint32_t ai = p == 0 ? j / sets[0] : j % n_active, s = p == 0 ? j - ai * sets[0] : j / n_active;
+          const int32_t r0 = (int32_t)(row0[p] + s * per_set);
+          const uint8_t *m0 = sliced_map(a.table, act[ai].e, p == 0 ? 0 : 2), *m1 = sliced_map(a.table, act[ai].e, 1);
+          for (uint32_t c = 0; c < K; c += kFewCols) {
+            if (at.round > 0 && !wait_bar(empty + 8 * at.st, (at.round - 1) & 1, lim)) {
+              ok = false;
+              break;
+            }
+            const uint32_t dst = ring + at.st * stage_bytes, bar = full + 8 * at.st;
+            mbar_expect_tx(bar, (p == 0 ? 2 : 1) * per_set * kFewRowBytes + a.extra_tx);
+            tma_load_3d(dst, m0, 0, r0, (int32_t)(c / 64), bar, policy);
+            if (p == 0) tma_load_3d(dst + per_set * kFewRowBytes, m1, 0, r0, (int32_t)(c / 64), bar, policy);
+            at.next(a.stages);
+          }
+        }
+        if (p == 0 && ok) {   // the beginning of W2, in the order in which it will be wanted
+          uint32_t left = kFewAheadBytes / (a.S2 * kFewRowBytes);
+          for (uint32_t j = 0; j < n_active * sets[1] && left > 0; ++j)
+            for (uint32_t c = 0; c < a.I && left > 0; c += kFewCols, --left)
+              tma_prefetch_3d(sliced_map(a.table, act[j % n_active].e, 2), 0, (int32_t)(row0[1] + j / n_active * a.S2), (int32_t)(c / 64));
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ---- activations: lane r copies the columns of the expert's r-th token ----
+    const uint64_t policy = policy_evict_last();
+    RingAt at;
+    bool ok = true;
+    for (uint32_t p = 0; p < 2 && ok; ++p) {
+      const uint32_t K = p == 0 ? a.H : a.I, jobs = n_active * sets[p];
+      if (p == 1 && jobs > 0) {
+        ok = __all_sync(0xFFFFFFFFu, wait_count(&a.sync->h_done[0], h_blocks, lim));
+        fence_async_all();       // what other blocks stored is now read by the copy engine
+      }
+      for (uint32_t j = 0; j < jobs && ok; ++j) {
+        const uint32_t ai = p == 0 ? j / sets[0] : j % n_active;
+        const Active ex = act[ai];
+        const uint16_t *src = a.tokens;
+        if (lane < ex.n)
+          src = p == 0 ? a.tokens + (size_t)nth_bit(mask[ex.e], lane) * K : a.h + (size_t)(ex.slot + lane) * K;
+        for (uint32_t c = 0; c < K; c += kFewCols) {
+          ok = __all_sync(0xFFFFFFFFu, at.round == 0 || wait_bar(empty + 8 * at.st, (at.round - 1) & 1, lim));
+          if (!ok) break;
+          const uint32_t bytes = min(kFewCols, K - c) * 2, bar = full + 8 * at.st;
+          if (lane == 0) mbar_expect_tx(bar, ex.n * bytes);
+          __syncwarp();
+          if (lane < ex.n) bulk_load(ring + at.st * stage_bytes + a.w_bytes + lane * kFewPitch, src + c, bytes, bar, policy);
+          at.next(a.stages);
+        }
+      }
+    }
+  } else if (warp < 10) {
+    // ---- products ----
+    const uint32_t cw = warp - 2;
+    const uint32_t a_row = lane & 15, a_half = lane >> 4;   // ldmatrix: this lane's row and half of 16 columns
+    const uint32_t b_at = a.w_bytes + (lane >> 2) * kFewPitch + (lane & 3) * 4;
+    RingAt at;
+    uint32_t job = 0;
+    bool ok = true;
+    for (uint32_t p = 0; p < 2 && ok; ++p) {
+      const uint32_t K = p == 0 ? a.H : a.I, per_set = p == 0 ? a.S1 : a.S2, jobs = n_active * sets[p];
+      const bool two = p == 0 || per_set > 16;
+      for (uint32_t j = 0; j < jobs && ok; ++j, ++job) {
+        float d[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        for (uint32_t c = 0; c < K; c += kFewCols) {
+          ok = __all_sync(0xFFFFFFFFu, wait_bar(full + 8 * at.st, at.round & 1, lim));
+          if (!ok) break;
+          const uint32_t left = min(kFewCols, K - c), base = ring + at.st * stage_bytes;
+#pragma unroll 4
+          for (uint32_t q = cw * 16; q < left; q += 128) {
+            // 64 columns are per_set lines of 128 bytes; the second 16 rows are W3's box, or the lines after the first
+            const uint32_t line = (q >> 6) * per_set + a_row, chunk = ((q & 63) >> 3) + a_half;
+            uint32_t w0[4], w1[4];
+            load_a(base + line * 128 + ((chunk ^ (line & 7)) << 4), w0);
+            if (p == 0) load_a(base + per_set * kFewRowBytes + line * 128 + ((chunk ^ (line & 7)) << 4), w1);
+            else if (two) load_a(base + (line + 16) * 128 + ((chunk ^ (line & 7)) << 4), w1);
+            const uint32_t b0 = load_b(base + b_at + q * 2), b1 = load_b(base + b_at + q * 2 + 16);
+            mma_16816(d[0], w0, b0, b1);
+            if (two) mma_16816(d[1], w1, b0, b1);
+          }
+          __syncwarp();
+          if (lane == 0) arrive(empty + 8 * at.st);
+          at.next(a.stages);
+        }
+        const uint32_t buf = job & 1;
+        ok = ok && __all_sync(0xFFFFFFFFu, job < 2 || wait_bar(sums_empty + 8 * buf, ((job >> 1) - 1) & 1, lim));
+        if (!ok) break;
+        float *own = sums + buf * (kFewSumBytes / 4) + cw * (2 * 8 * kFewSumPitch);
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) own[(m * 8 + (lane & 3) * 2 + (i & 1)) * kFewSumPitch + (lane >> 2) + (i >> 1) * 8] = d[m][i];
+        __syncwarp();
+        if (lane == 0) arrive(sums_full + 8 * buf);
+      }
+    }
+  } else {
+    // ---- sums ----
+    const uint32_t ct = tid - 320;
+    uint32_t job = 0;
+    bool ok = true;
+    for (uint32_t p = 0; p < 2 && ok; ++p) {
+      const uint32_t per_set = p == 0 ? a.S1 : a.S2, jobs = n_active * sets[p];
+      for (uint32_t j = 0; j < jobs && ok; ++j, ++job) {
+        const uint32_t ai = p == 0 ? j / sets[0] : j % n_active, s = p == 0 ? j - ai * sets[0] : j / n_active;
+        const uint32_t r0 = row0[p] + s * per_set, rows = min(per_set, row1[p] - r0);
+        const Active ex = act[ai];
+        if (p == 1 && ai == 0) {   // a new set of output rows
+          for (uint32_t i = ct; i < a.T * 32; i += 128) outs[i] = 0.f;
+        }
+        const uint32_t buf = job & 1;
+        ok = all_agree<128>(wait_bar(sums_full + 8 * buf, (job >> 1) & 1, lim));
+        if (!ok) break;
+        const float *mine = sums + buf * (kFewSumBytes / 4);
+        const uint32_t span = p == 0 ? 16 : 32;
+        for (uint32_t i = ct; i < span * ex.n; i += 128) {
+          const uint32_t r = i % span, n = i / span;
+          if (r >= rows) continue;
+          float v[2] = {0.f, 0.f};
+#pragma unroll
+          for (uint32_t w = 0; w < 8; ++w) {
+            const float *from = mine + w * (2 * 8 * kFewSumPitch) + n * kFewSumPitch;
+            if (p == 0) {
+              v[0] += from[r];
+              v[1] += from[8 * kFewSumPitch + r];
+            } else {
+              v[0] += from[(r >> 4) * 8 * kFewSumPitch + (r & 15)];
+            }
+          }
+          if (p == 0) {
+            a.h[(size_t)(ex.slot + n) * a.I + r0 + r] = __bfloat16_as_ushort(__float2bfloat16_rn(silu_times(v[0], v[1])));
+          } else {
+            const uint32_t t = nth_bit(mask[ex.e], n);
+            float wt = 0.f;
+            for (uint32_t c = 0; c < a.k; ++c)
+              if (ids[t * a.k + c] == (int32_t)ex.e) wt += wts[t * a.k + c];
+            outs[t * 32 + r] += wt * v[0];
+          }
+        }
+        __syncwarp();
+        if (lane == 0) arrive(sums_empty + 8 * buf);
+        if (p == 1 && ai + 1 == n_active) {
+          sync_group<128>();
+          for (uint32_t i = ct; i < a.T * 32; i += 128) {
+            const uint32_t r = i & 31, t = i >> 5;
+            if (r < rows) a.out[(size_t)t * a.H + r0 + r] = __bfloat16_as_ushort(__float2bfloat16_rn(outs[i]));
+          }
+          sync_group<128>();   // (the next set begins by clearing what was just read)
+        }
+      }
+      if (p == 0 && ok && jobs > 0) {   // all of this block's h is out: tell the others
+        __threadfence();
+        fence_async_all();
+        sync_group<128>();
+        if (ct == 0) add_release(&a.sync->h_done[0], 1u);
+      }
+    }
+    if (prepared && n_active == 0)      // no token has an expert
+      for (uint32_t i = ct; i < a.T * (row1[1] - row0[1]); i += 128) {
+        const uint32_t t = i / (row1[1] - row0[1]), r = i - t * (row1[1] - row0[1]);
+        a.out[(size_t)t * a.H + row0[1] + r] = 0;
+      }
+  }
+  __syncwarp();
+  __syncthreads();
+  if (*dead)   // let the copies that this block has under way end before its memory goes to somebody else
+    for (uint32_t i = 0; i < 200; ++i) __nanosleep(1000);
+  if (tid == 0) {
+    if (!prepared) {
+      report(a.status, kStatusBadDescriptor);
+    } else {
+      __threadfence();
+      if (atomicAdd(&a.sync->exited, 1u) == G - 1) {   // the last block leaves the counters as it found them
+        a.sync->h_done[0] = 0;
+        a.sync->exited = 0;
+      }
+    }
+  }
+}
+
+}  // namespace zipmoe_dev
+
+namespace zipmoe_host {
+
+void resident_few_rows(uint32_t H, uint32_t I, uint32_t grid, uint32_t *R1, uint32_t *S1, uint32_t *R2, uint32_t *S2) {
+  auto up = [](uint32_t v, uint32_t d) { return (v + d - 1) / d; };
+  *R1 = up(I, grid);
+  *S1 = up(*R1, up(*R1, 16));
+  *R2 = up(H, grid);
+  *S2 = up(*R2, up(*R2, 32));
+}
+
+zipmoe_status launch_resident_few(const ResidentCall &c, cudaStream_t stream) {
+  using namespace zipmoe_dev;
+  FewArgs a;
+  a.tokens = c.tokens;
+  a.ids = c.ids;
+  a.weights = c.weights;
+  a.table = c.table;
+  a.out = c.out;
+  a.sync = c.sync;
+  a.h = reinterpret_cast<uint16_t *>(c.h);
+  a.status = c.status;
+  a.limit_ns = c.limit_ns;
+  a.extra_tx = c.extra_tx;
+  a.T = c.T;
+  a.k = c.k;
+  a.E = c.E;
+  a.H = c.H;
+  a.I = c.I;
+  resident_few_rows(c.H, c.I, c.grid, &a.R1, &a.S1, &a.R2, &a.S2);
+  a.w_bytes = (2 * a.S1 > a.S2 ? 2 * a.S1 : a.S2) * kFewRowBytes;
+  const uint32_t control = few_control_bytes(c.E, c.T, c.k) + 1024, room = 227 * 1024 - control, stage = a.w_bytes + kFewTokenBytes;
+  a.stages = room / stage < kResMaxStages ? room / stage : kResMaxStages;
+  static bool ready[64];
+  if (!ready[c.device]) {
+    if (cudaFuncSetAttribute(resident_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024) != cudaSuccess)
+      return ZIPMOE_ERR_CUDA;
+    ready[c.device] = true;
+  }
+  cudaLaunchAttribute together;
+  together.id = cudaLaunchAttributeCooperative;
+  together.val.cooperative = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.stream = stream;
+  cfg.attrs = &together;
+  cfg.numAttrs = 1;
+  cfg.gridDim = dim3(c.grid);
+  cfg.blockDim = dim3(kFewThreads);
+  cfg.dynamicSmemBytes = control + a.stages * stage;
+  return cudaLaunchKernelEx(&cfg, resident_few_kernel, a) == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
+}
+
+}  // namespace zipmoe_host

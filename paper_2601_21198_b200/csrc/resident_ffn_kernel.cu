@@ -33,20 +33,21 @@
 #include <cstring>
 
 #include "zipmoe.h"
-#include "tensor_core.cuh"
+#include "resident.cuh"
 
 namespace zipmoe_dev {
 
-constexpr uint32_t kResMaxGrid = 256;
 constexpr uint32_t kResReaders = 8;                         // warps that read accumulators back: two per 32 lanes of tensor memory
 constexpr uint32_t kResThreads = 128 + 32 * kResReaders;
 constexpr uint32_t kResStageA = 32768;                      // weights of a step
-constexpr uint32_t kResMaxStages = 8;
 #ifndef ZIPMOE_RES_DEPTH
 #define ZIPMOE_RES_DEPTH 4
 #endif
 constexpr uint32_t kResInFlight = ZIPMOE_RES_DEPTH;
-constexpr uint32_t kResMagic = 0x5A464632u;                 // marks a workspace that zipmoe_expert_ffn_workspace_init prepared
+#ifndef ZIPMOE_RES_FEW
+#define ZIPMOE_RES_FEW 8
+#endif
+constexpr uint32_t kResFewT = ZIPMOE_RES_FEW;   // up to this many tokens the kernel that gives every block whole rows runs instead
 constexpr uint32_t kResGatherRows = 16;   // a gather of four rows takes the copy engine about 130 ns: up to this many tokens
                                           // per expert they are gathered in every step, beyond it packed once
 #ifndef ZIPMOE_RES_TWO
@@ -54,16 +55,6 @@ constexpr uint32_t kResGatherRows = 16;   // a gather of four rows takes the cop
 #endif
 constexpr uint32_t kResTwoGroupsT = ZIPMOE_RES_TWO;   // above, a call is long enough for the wait between gate/up and down not to show,
                                           // and the partial sums of four phases would take too much memory
-
-// The workspace starts with this: zero when no call is running (every call leaves it so).
-struct ResidentSync {
-  uint32_t magic, pad0[31];
-  uint32_t x_done, pad1[31];      // blocks that have packed their part of the tokens
-  uint32_t h_done[2], pad2[30];   // per group of experts: blocks that have stored all their h
-  uint32_t y_done, pad3[31];      // blocks that have stored all their y, one count per group
-  uint32_t exited, pad4[31];
-  uint32_t cut[2][kResMaxGrid];   // [g][c]: blocks that have stored their part of the gate/up job cut at the end of block c's share
-};
 
 struct ResidentArgs {
   const uint16_t *tokens;
@@ -106,31 +97,13 @@ __device__ __forceinline__ bool next_piece(const Phase &p, uint32_t &u, uint32_t
   return true;
 }
 
-struct Active {
-  uint32_t e, n, h_row, slot;   // expert; its tokens; first row of its h block; first of its choices
-};
-
 // shared memory after the ring: [token masks of the experts][active experts][expert -> active][place of every choice
 // among its expert's tokens][tokens of the active experts, padded to 8 each][barriers and words]
-__host__ __device__ inline uint32_t pad16(uint32_t bytes) { return (bytes + 15) & ~15u; }
 __host__ __device__ inline uint32_t resident_rows(uint32_t E, uint32_t choices) { return choices + 7 * (E < choices ? E : choices); }
 __host__ __device__ inline uint32_t resident_control_bytes(uint32_t E, uint32_t T, uint32_t k) {
   return pad16(E * ((T + 31) / 32) * 4) + E * (uint32_t)sizeof(Active) + pad16(E * 2) + pad16(T * k * 2) +
          pad16(resident_rows(E, T * k) * 2) + (4 * kResMaxStages + 4) * 8 + 32;
 }
-
-// The reading warps give up together or not at all: their barriers count all of them.
-__device__ __forceinline__ bool all_agree(bool ok) {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\t"
-      "barrier.cta.red.and.pred p, 1, %2, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(r)
-      : "r"((uint32_t)ok), "n"(32 * kResReaders)
-      : "memory");
-  return r != 0;
-}
-__device__ __forceinline__ void sync_readers() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kResReaders) : "memory"); }
 
 // the choice's place among its expert's tokens (in token order; a token that lists the expert twice has one place)
 __device__ __forceinline__ void place_choice(uint32_t at, int32_t e, const ResidentArgs &a, uint32_t W, const uint32_t *mask,
@@ -142,19 +115,6 @@ __device__ __forceinline__ void place_choice(uint32_t at, int32_t e, const Resid
   token[act[active_of[e]].h_row + before] = (uint16_t)t;
 }
 
-__device__ __forceinline__ float silu_times(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
-
-// A place in a ring of stages and how often the ring has gone round.
-struct RingAt {
-  uint32_t st = 0, round = 0;
-  __device__ __forceinline__ void next(uint32_t n) {
-    if (++st == n) {
-      st = 0;
-      ++round;
-    }
-  }
-};
-
 __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __grid_constant__ CUtensorMap x_map, const ResidentArgs a) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x, G = gridDim.x;
@@ -165,6 +125,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
 #pragma unroll
   for (uint32_t i = 0; i < kIds; ++i) my_id[i] = tid + i * kResThreads < choices ? __ldg(a.ids + tid + i * kResThreads) : -1;
   const uint32_t magic = __ldcg(&a.sync->magic);
+  prefetch_table(a.table, a.E, cta * kResThreads + tid, G * kResThreads);
 
   uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t *ctl = ring + a.ring_bytes;
@@ -290,7 +251,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
       if (u < end) {
         const uint32_t per = f.KS * f.RB, ja = u / per + (r >> 1);
         if (ja <= (end - 1) / per && (p < 2 || (r & 1) == 0)) {
-          const uint8_t *m = a.table + (size_t)(3 * act[f.a0 + ja].e + (p < 2 ? (r & 1) : 2)) * ZIPMOE_RESIDENT_ENTRY_BYTES;
+          const uint8_t *m = wide_map(a.table, act[f.a0 + ja].e, p < 2 ? (r & 1) : 2);
           acquire_map(m);
           prefetch_map(m);
         }
@@ -310,7 +271,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
         const uint32_t end = last(f), a_first = f.a0 + (u < end ? u / (f.KS * f.RB) : 0);
         Piece q;
         while (ok && next_piece(f, u, end, q)) {
-          const uint8_t *m0 = a.table + (size_t)(3 * act[q.a].e + (p < 2 ? 0 : 2)) * ZIPMOE_RESIDENT_ENTRY_BYTES;
+          const uint8_t *m0 = wide_map(a.table, act[q.a].e, p < 2 ? 0 : 2);
           const uint8_t *m1 = p < 2 ? m0 + ZIPMOE_RESIDENT_ENTRY_BYTES : m0;
           const int32_t y0 = (int32_t)(q.rb * (p < 2 ? 128 : 256)), y1 = p < 2 ? y0 : y0 + 128;
           if (q.a >= a_first + kMaps) {
@@ -465,7 +426,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
       }
       __threadfence();
       fence_async_all();
-      sync_readers();
+      sync_group<32 * kResReaders>();
       if (rtid == 0) add_release(&a.sync->x_done, 1u);
     }
 #pragma unroll 1
@@ -505,7 +466,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
             mine[(size_t)(a.T + i) * 128] = v1;
           }
         };
-        ok = all_agree(wait_bar(acc_full + 8 * b, use & 1, lim));
+        ok = all_agree<32 * kResReaders>(wait_bar(acc_full + 8 * b, use & 1, lim));
         if (!ok) break;
         tc_after_sync();
         const uint32_t d0 = tmem + ((32 * w) << 16) + b * 2 * N, d1 = d0 + N;
@@ -525,12 +486,12 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
         // a gate/up job that is cut: the block that stores its part last adds all parts, in share order
         const uint32_t c0 = share_of(q.job * f.KS, f.U, f.P), c1 = share_of(q.job * f.KS + f.KS - 1, f.U, f.P);
         __threadfence();
-        sync_readers();
+        sync_group<32 * kResReaders>();
         if (rtid == 0) {
           words[3] = atomicAdd(&a.sync->cut[p][c0], 1u) == c1 - c0;
           __threadfence();
         }
-        sync_readers();
+        sync_group<32 * kResReaders>();
         if (words[3]) {
           for (uint32_t n0 = 4 * half; n0 < ex.n; n0 += 8) {
             float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
@@ -553,7 +514,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
       if (ok && cta < f.P) {
         __threadfence();
         if (p < 2) fence_async_all();
-        sync_readers();
+        sync_group<32 * kResReaders>();
         if (rtid == 0) add_release(p < 2 ? &a.sync->h_done[p] : &a.sync->y_done, 1u);
       }
     }
@@ -659,6 +620,9 @@ bool dims_ok(uint32_t E, uint32_t H, uint32_t I) {
          I <= kResidentMaxDim;
 }
 
+// the sizes that a block's slices of rows can be described for
+bool sliced_sizes(uint32_t H, uint32_t I) { return H % 64 == 0 && I % 64 == 0; }
+
 struct ResidentDevice {
   int sms = 0;
   bool ready = false;
@@ -716,12 +680,21 @@ extern "C" zipmoe_status zipmoe_resident_experts_plan(const uint16_t *const *ten
   if (!tensors || !table) return ZIPMOE_ERR_INVALID_ARG;
   for (uint32_t i = 0; i < 3 * n_experts; ++i)
     if (!tensors[i] || (reinterpret_cast<uintptr_t>(tensors[i]) & 15)) return ZIPMOE_ERR_INVALID_ARG;
-  static_assert(sizeof(CUtensorMap) == ZIPMOE_RESIDENT_ENTRY_BYTES, "an entry is a tensor map");
+  static_assert(sizeof(CUtensorMap) == zipmoe_dev::kSlicedMap && 2 * sizeof(CUtensorMap) == ZIPMOE_RESIDENT_ENTRY_BYTES,
+                "an entry is two tensor maps");
+  uint32_t R1, S1, R2, S2;
+  zipmoe_host::resident_few_rows(hidden, inter, resident_grid(), &R1, &S1, &R2, &S2);
   for (uint32_t i = 0; i < 3 * n_experts; ++i) {
     CUtensorMap map;
     const uint32_t rows = i % 3 < 2 ? inter : hidden, cols = i % 3 < 2 ? hidden : inter;
     if (!zipmoe_host::make_bf16_map(&map, tensors[i], rows, cols, cols, 128, true)) return ZIPMOE_ERR_CUDA;
-    std::memcpy(static_cast<uint8_t *>(table) + (size_t)i * ZIPMOE_RESIDENT_ENTRY_BYTES, &map, sizeof(map));
+    uint8_t *entry = static_cast<uint8_t *>(table) + (size_t)i * ZIPMOE_RESIDENT_ENTRY_BYTES;
+    std::memset(entry, 0, ZIPMOE_RESIDENT_ENTRY_BYTES);
+    std::memcpy(entry, &map, sizeof(map));
+    if (sliced_sizes(hidden, inter)) {
+      if (!zipmoe_host::make_sliced_map(&map, tensors[i], rows, cols, i % 3 < 2 ? S1 : S2)) return ZIPMOE_ERR_CUDA;
+      std::memcpy(entry + zipmoe_dev::kSlicedMap, &map, sizeof(map));
+    }
   }
   return ZIPMOE_OK;
 }
@@ -771,9 +744,33 @@ extern "C" zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, c
       return ZIPMOE_ERR_CUDA;
     g_resident_dev[dev].ready = true;
   }
+  uint8_t *ws = static_cast<uint8_t *>(workspace);
+  uint32_t tries = 0, extra_tx = 0;
+  zipmoe_host::wait_fault_setting(&extra_tx, &tries);
+  const uint64_t limit_ns = tries < zipmoe_host::kWaitTries ? 1000000ull : 1000000000ull;   // (1 ms in the tests of the limit)
+  if (T <= kResFewT && sliced_sizes(ex->hidden, ex->inter)) {
+    zipmoe_host::ResidentCall c;
+    c.tokens = tokens;
+    c.ids = topk_ids;
+    c.weights = topk_weights;
+    c.table = static_cast<const uint8_t *>(ex->table);
+    c.out = out;
+    c.sync = reinterpret_cast<ResidentSync *>(ws);
+    c.h = ws + p.off_h;
+    c.status = status_word;
+    c.limit_ns = limit_ns;
+    c.T = T;
+    c.k = k;
+    c.E = ex->n_experts;
+    c.H = ex->hidden;
+    c.I = ex->inter;
+    c.grid = p.grid;
+    c.extra_tx = extra_tx;
+    c.device = dev;
+    return zipmoe_host::launch_resident_few(c, reinterpret_cast<cudaStream_t>(stream_));
+  }
   CUtensorMap x_map;
   if (!zipmoe_host::make_bf16_map(&x_map, tokens, T, ex->hidden, ex->hidden, 1, false)) return ZIPMOE_ERR_CUDA;
-  uint8_t *ws = static_cast<uint8_t *>(workspace);
   ResidentArgs a;
   a.ids = topk_ids;
   a.weights = topk_weights;
@@ -786,9 +783,8 @@ extern "C" zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, c
   a.part = reinterpret_cast<float *>(ws + p.off_part);
   a.y = reinterpret_cast<float *>(ws + p.off_y);
   a.status = status_word;
-  uint32_t tries = 0;
-  zipmoe_host::wait_fault_setting(&a.extra_tx, &tries);
-  a.limit_ns = tries < zipmoe_host::kWaitTries ? 1000000ull : 1000000000ull;   // (1 ms in the tests of the limit)
+  a.extra_tx = extra_tx;
+  a.limit_ns = limit_ns;
   a.T = T;
   a.k = k;
   a.E = ex->n_experts;

@@ -148,28 +148,45 @@ __device__ __forceinline__ void arrive(uint32_t bar) {
 
 namespace zipmoe_host {
 
-// Describes a dense row-major bf16 matrix to the copy engine: boxes of 64 columns x box_rows rows, written to shared
-// memory in the 128-byte swizzle, zeros outside the matrix.  False if the driver does not offer the call or refuses it.
-inline bool make_bf16_map(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint64_t pitch_elems, uint32_t box_rows,
-                          bool wide_fetch) {
-  using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                              const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-  static const Encode encode = [] {
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+// The driver's call that writes tensor maps; null if it does not offer one.
+inline EncodeTiled encode_tiled() {
+  static const EncodeTiled encode = [] {
     void *fn = nullptr;
     cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
     if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess ||
         found != cudaDriverEntryPointSuccess)
       fn = nullptr;
     (void)cudaGetLastError();
-    return reinterpret_cast<Encode>(fn);
+    return reinterpret_cast<EncodeTiled>(fn);
   }();
+  return encode;
+}
+
+// Describes a dense row-major bf16 matrix to the copy engine: boxes of 64 columns x box_rows rows, written to shared
+// memory in the 128-byte swizzle, zeros outside the matrix.  False if the driver does not offer the call or refuses it.
+inline bool make_bf16_map(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint64_t pitch_elems, uint32_t box_rows,
+                          bool wide_fetch) {
+  const EncodeTiled encode = encode_tiled();
   if (!encode) return false;
   const cuuint64_t dims[2] = {cols, rows}, strides[1] = {pitch_elems * 2};
   const cuuint32_t box[2] = {64, box_rows}, step[2] = {1, 1};
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims, strides, box, step,
                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                 wide_fetch ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// The same matrix, cols a multiple of 64, seen as [cols / 64][rows][64]: a box of 8 x box_rows x 64 is 512 columns of
+// box_rows rows.
+inline bool make_sliced_map(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
+  const EncodeTiled encode = encode_tiled();
+  if (!encode) return false;
+  const cuuint64_t dims[3] = {64, rows, cols / 64}, strides[2] = {cols * 2, 128};
+  const cuuint32_t box[3] = {64, box_rows, 8}, step[3] = {1, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, step,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
