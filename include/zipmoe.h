@@ -381,23 +381,27 @@ typedef struct {
  * otherwise).  T = 0 does nothing. */
 zipmoe_status zipmoe_route(const zipmoe_route_args *args, zipmoe_stream stream);
 
-/* The recovered experts of one MoE layer.  A HOST struct; `table` is DEVICE memory holding what
- * zipmoe_resident_experts_plan wrote. */
+/* The recovered experts of one MoE layer.  A HOST struct that zipmoe_resident_experts_plan fills; the caller then sets
+ * `table` to where it has copied the table on the device. */
 typedef struct {
-  uint32_t n_experts, hidden, inter, reserved; /* hidden, inter: multiples of 8                                   */
-  const void *table;                           /* device [3 * n_experts * ZIPMOE_RESIDENT_ENTRY_BYTES], 64-byte aligned */
+  uint32_t n_experts, hidden, inter;  /* hidden, inter: multiples of 8                                              */
+  uint32_t even;                      /* 1: every kind of tensor lies at equal distances from expert to expert      */
+  const void *table;                  /* device [3 * n_experts * ZIPMOE_RESIDENT_ENTRY_BYTES], 64-byte aligned      */
+  uint8_t maps[6 * 128];              /* opaque: the tensors of evenly spaced experts                               */
 } zipmoe_resident_experts;
 #define ZIPMOE_RESIDENT_ENTRY_BYTES 256u
 
 /* Describes recovered experts to zipmoe_expert_ffn: one opaque entry per tensor, which the caller copies to the
- * device as it is.  Written once per layer (and again for an expert whose tensors move).
+ * device as it is, and the struct that the call takes.  Once per layer, and again when an expert's tensors move.
+ * Experts whose w1 lie at equal distances, in ascending order, and their w3 and w2 too (one array per kind, or one
+ * decode launch's output) are found faster: about 3 us per call.
  * host in : tensors[3 * n_experts] DEVICE addresses, tensors[3e+0] = w1 (gate) [inter, hidden], 3e+1 = w3 (up)
  *           [inter, hidden], 3e+2 = w2 (down) [hidden, inter]: dense row-major bf16, 16-byte aligned, for example
  *           where zipmoe_decode put them.  The memory itself is not touched.
- * host out: table[3 * n_experts * ZIPMOE_RESIDENT_ENTRY_BYTES]
+ * host out: table[3 * n_experts * ZIPMOE_RESIDENT_ENTRY_BYTES]; *experts, but for its `table`
  * Limits: n_experts <= 256, hidden and inter multiples of 8, at most 32768 (ZIPMOE_ERR_UNSUPPORTED otherwise). */
 zipmoe_status zipmoe_resident_experts_plan(const uint16_t *const *tensors, uint32_t n_experts, uint32_t hidden,
-                                           uint32_t inter, void *table);
+                                           uint32_t inter, void *table, zipmoe_resident_experts *experts);
 
 /* Scratch zipmoe_expert_ffn needs for T tokens with k experts each.  Host only. */
 zipmoe_status zipmoe_expert_ffn_workspace_bytes(uint32_t T, uint32_t k, const zipmoe_resident_experts *experts,

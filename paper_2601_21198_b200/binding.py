@@ -347,7 +347,7 @@ RESIDENT_ENTRY_BYTES = 256
 
 class ResidentExpertsStruct(ctypes.Structure):
     """zipmoe_resident_experts."""
-    _fields_ = [("n_experts", _u32), ("hidden", _u32), ("inter", _u32), ("reserved", _u32), ("table", _vp)]
+    _fields_ = [("n_experts", _u32), ("hidden", _u32), ("inter", _u32), ("even", _u32), ("table", _vp), ("maps", ctypes.c_uint8 * 768)]
 
 
 # zipmoe_norm_args and zipmoe_route_args, packed in one go (a call with one pointer costs a sixth of one with 17 arguments)
@@ -356,7 +356,7 @@ _ROUTE_ARGS = struct.Struct("<8Q6I")
 assert _NORM_ARGS.size == 112 and _ROUTE_ARGS.size == 88
 _lib.zipmoe_add_rmsnorm.argtypes = [ctypes.c_char_p, _vp]
 _lib.zipmoe_route.argtypes = [ctypes.c_char_p, _vp]
-_lib.zipmoe_resident_experts_plan.argtypes = [ctypes.POINTER(_vp), _u32, _u32, _u32, _vp]
+_lib.zipmoe_resident_experts_plan.argtypes = [ctypes.POINTER(_vp), _u32, _u32, _u32, _vp, ctypes.POINTER(ResidentExpertsStruct)]
 _lib.zipmoe_expert_ffn_workspace_bytes.argtypes = [_u32, _u32, ctypes.POINTER(ResidentExpertsStruct), ctypes.POINTER(_u64)]
 _lib.zipmoe_expert_ffn_workspace_init.argtypes = [_vp, _u64, _vp]
 _lib.zipmoe_expert_ffn_workspace_init.restype = _int
@@ -384,13 +384,16 @@ def zipmoe_route(tokens, T, token_pitch, gate, n_experts, hidden, bias, k, flags
 
 
 def zipmoe_resident_experts_plan(tensors, n_experts, hidden, inter):
-    """tensors: 3 * n_experts device tensors (or addresses).  Returns the table (numpy uint8), to be copied to the device."""
-    ptrs = (_vp * max(len(tensors), 1))(*[_ptr(t) for t in tensors])
+    """tensors: 3 * n_experts device tensors (or addresses).  Returns (table: numpy uint8, to be copied to the device;
+    ResidentExpertsStruct, whose `table` is then to be set to that copy's address)."""
     if len(tensors) != 3 * n_experts:
         raise ValueError("three tensors per expert are wanted")
+    ptrs = (_vp * max(len(tensors), 1))(*[_ptr(t) for t in tensors])
     table = np.zeros(3 * n_experts * RESIDENT_ENTRY_BYTES, np.uint8)
-    _check("zipmoe_resident_experts_plan", _lib.zipmoe_resident_experts_plan(ptrs, n_experts, hidden, inter, _ptr(table)))
-    return table
+    experts = ResidentExpertsStruct()
+    _check("zipmoe_resident_experts_plan",
+           _lib.zipmoe_resident_experts_plan(ptrs, n_experts, hidden, inter, _ptr(table), ctypes.byref(experts)))
+    return table, experts
 
 
 def zipmoe_expert_ffn_workspace_bytes(T, k, experts):
@@ -702,8 +705,9 @@ class ResidentExperts:
         self.tensors = list(tensors)      # the experts' memory is theirs: keep it while the table points at it
         self.device = tensors[0].device
         self.hidden, self.inter = hidden, inter
-        self.table = torch.from_numpy(zipmoe_resident_experts_plan(self.tensors, len(tensors) // 3, hidden, inter)).to(self.device)
-        self.struct = ResidentExpertsStruct(len(tensors) // 3, hidden, inter, 0, self.table.data_ptr())
+        table, self.struct = zipmoe_resident_experts_plan(self.tensors, len(tensors) // 3, hidden, inter)
+        self.table = torch.from_numpy(table).to(self.device)
+        self.struct.table = self.table.data_ptr()
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._struct_at = ctypes.byref(self.struct)
         self._ws, self._need = {}, {}

@@ -12,6 +12,11 @@ constexpr uint32_t kResMaxStages = 8;
 constexpr uint32_t kResMagic = 0x5A464632u;                 // marks a workspace that zipmoe_expert_ffn_workspace_init prepared
 constexpr uint32_t kSlicedMap = 128;   // an entry of the table: the map of 128-row boxes, then that of a block's slices of rows
 
+// Maps of all experts' W1, W3 and W2 at once, where they lie at equal distances.
+struct EvenMaps {
+  CUtensorMap w[3];
+};
+
 // The workspace starts with this: zero when no call is running (every call leaves it so).
 struct ResidentSync {
   uint32_t magic, pad0[31];
@@ -45,8 +50,9 @@ __device__ __forceinline__ void sync_group() { asm volatile("bar.sync 1, %0;" ::
 
 __device__ __forceinline__ float silu_times(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
 
-// The maps of expert e's tensor j, and all maps into the second-level cache: which ones a call needs is known only once
-// its ids are there, and a map that the copy engine has to fetch from memory holds it up for more than 2 us.
+// Expert e's tensor j in its own map of the table.  Which of those a call needs is known only once its ids are there, so
+// all are asked into the second-level cache at the start: a map that the copy engine has to fetch from memory holds it up
+// for more than 2 us.
 __device__ __forceinline__ const uint8_t *wide_map(const uint8_t *table, uint32_t e, uint32_t j) {
   return table + (size_t)(3 * e + j) * ZIPMOE_RESIDENT_ENTRY_BYTES;
 }
@@ -77,6 +83,7 @@ struct ResidentCall {
   const int32_t *ids;
   const float *weights;
   const uint8_t *table;
+  const uint8_t *even_maps;   // host: the three sliced maps, or null
   uint16_t *out;
   zipmoe_dev::ResidentSync *sync;
   uint8_t *h;

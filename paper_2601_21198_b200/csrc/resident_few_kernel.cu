@@ -20,6 +20,7 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <cstring>
 
 #include "zipmoe.h"
 #include "resident.cuh"
@@ -43,7 +44,7 @@ struct FewArgs {
   uint16_t *h;              // [choices][I]
   uint32_t *status;
   uint64_t limit_ns;
-  uint32_t T, k, E, H, I;
+  uint32_t T, k, E, H, I, even;
   uint32_t R1, S1, R2, S2;  // rows of a block, rows of a set: of W1 and W3, of W2
   uint32_t stages, w_bytes, extra_tx;
 };
@@ -75,18 +76,7 @@ __device__ __forceinline__ uint32_t nth_bit(uint32_t mask, uint32_t n) {   // pl
   return __ffs(mask) - 1;
 }
 
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void *map, int32_t x, int32_t y, int32_t z, uint32_t bar, uint64_t policy) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4}], "
-      "[%5], %6;" ::"r"(dst),
-      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar), "l"(policy)
-      : "memory");
-}
-__device__ __forceinline__ void tma_prefetch_3d(const void *map, int32_t x, int32_t y, int32_t z) {
-  asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(map), "r"(x), "r"(y), "r"(z) : "memory");
-}
-
-__global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const FewArgs a) {
+__global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __grid_constant__ EvenMaps even, const FewArgs a) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x, G = gridDim.x, choices = a.T * a.k;
   const uint32_t stage_bytes = a.w_bytes + kFewTokenBytes;
@@ -114,7 +104,8 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const FewA
   const uint32_t magic = __ldcg(&a.sync->magic);
   const int32_t my_id = tid < choices ? __ldg(a.ids + tid) : -1;
   const float my_wt = tid < choices && a.weights ? __ldg(a.weights + tid) : 1.0f;
-  prefetch_table(a.table, a.E, cta * kFewThreads + tid, G * kFewThreads);
+  if (!a.even) prefetch_table(a.table, a.E, cta * kFewThreads + tid, G * kFewThreads);
+  else if (tid >= 64 && tid < 67) prefetch_map(&even.w[tid - 64]);
   for (uint32_t i = tid; i < a.E; i += kFewThreads) mask[i] = 0;
   if (tid == 0) {
     for (uint32_t s = 0; s < a.stages; ++s) {
@@ -169,23 +160,34 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const FewA
 
   if (warp == 0) {
     // ---- weights ----
-    for (uint32_t i = lane; i < 3 * n_active; i += 32) {   // the experts' maps, W1 and W3 first
-      const uint32_t down = i >= 2 * n_active, ai = down ? i - 2 * n_active : i >> 1;
-      const uint8_t *m = sliced_map(a.table, act[ai].e, down ? 2 : i & 1);
-      acquire_map(m);
-      prefetch_map(m);
-    }
+    if (!a.even)
+      for (uint32_t i = lane; i < 3 * n_active; i += 32) {   // the experts' maps, W1 and W3 first
+        const uint32_t down = i >= 2 * n_active, ai = down ? i - 2 * n_active : i >> 1;
+        const uint8_t *m = sliced_map(a.table, act[ai].e, down ? 2 : i & 1);
+        acquire_map(m);
+        if (i < 2) prefetch_map(m);
+      }
     __syncwarp();
     if (lane == 0) {
       const uint64_t policy = policy_evict_first();
+      auto map_of = [&](uint32_t e, uint32_t j) -> const void * { return a.even ? static_cast<const void *>(&even.w[j]) : sliced_map(a.table, e, j); };
       RingAt at;
       bool ok = true;
       for (uint32_t p = 0; p < 2 && ok; ++p) {
         const uint32_t K = p == 0 ? a.H : a.I, per_set = p == 0 ? a.S1 : a.S2, jobs = n_active * sets[p];
         for (uint32_t j = 0; j < jobs && ok; ++j) {
-          const uint32_t ai = p == 0 ? j / sets[0] : j % n_active, s = p == 0 ? j - ai * sets[0] : j / n_active;
-          const int32_t r0 = (int32_t)(row0[p] + s * per_set);
-          const uint8_t *m0 = sliced_map(a.table, act[ai].e, p == 0 ? 0 : 2), *m1 = sliced_map(a.table, act[ai].e, 1);
+          const uint32_t ai = p == 0 ? j / sets[0] : j % n_active, s = p == 0 ? j - ai * sets[0] : j / n_active, e = act[ai].e;
+          const int32_t r0 = (int32_t)(row0[p] + s * per_set), z = a.even ? (int32_t)e : 0;
+          const void *m0 = map_of(e, p == 0 ? 0 : 2), *m1 = map_of(e, 1);
+          if (!a.even && s == 0) {   // the next expert's maps
+            const uint32_t next = ai + 1 < n_active ? act[ai + 1].e : act[0].e;
+            if (p == 0 && ai + 1 < n_active) {
+              prefetch_map(map_of(next, 0));
+              prefetch_map(map_of(next, 1));
+            } else {
+              prefetch_map(map_of(next, 2));
+            }
+          }
           for (uint32_t c = 0; c < K; c += kFewCols) {
             if (at.round > 0 && !wait_bar(empty + 8 * at.st, (at.round - 1) & 1, lim)) {
               ok = false;
@@ -193,16 +195,18 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const FewA
             }
             const uint32_t dst = ring + at.st * stage_bytes, bar = full + 8 * at.st;
             mbar_expect_tx(bar, (p == 0 ? 2 : 1) * per_set * kFewRowBytes + a.extra_tx);
-            tma_load_3d(dst, m0, 0, r0, (int32_t)(c / 64), bar, policy);
-            if (p == 0) tma_load_3d(dst + per_set * kFewRowBytes, m1, 0, r0, (int32_t)(c / 64), bar, policy);
+            tma_load_4d(dst, m0, 0, r0, (int32_t)(c / 64), z, bar, policy);
+            if (p == 0) tma_load_4d(dst + per_set * kFewRowBytes, m1, 0, r0, (int32_t)(c / 64), z, bar, policy);
             at.next(a.stages);
           }
         }
         if (p == 0 && ok) {   // the beginning of W2, in the order in which it will be wanted
           uint32_t left = kFewAheadBytes / (a.S2 * kFewRowBytes);
-          for (uint32_t j = 0; j < n_active * sets[1] && left > 0; ++j)
+          for (uint32_t j = 0; j < n_active * sets[1] && left > 0; ++j) {
+            const uint32_t e = act[j % n_active].e;
             for (uint32_t c = 0; c < a.I && left > 0; c += kFewCols, --left)
-              tma_prefetch_3d(sliced_map(a.table, act[j % n_active].e, 2), 0, (int32_t)(row0[1] + j / n_active * a.S2), (int32_t)(c / 64));
+              tma_prefetch_4d(map_of(e, 2), 0, (int32_t)(row0[1] + j / n_active * a.S2), (int32_t)(c / 64), a.even ? (int32_t)e : 0);
+          }
         }
       }
     }
@@ -382,6 +386,9 @@ zipmoe_status launch_resident_few(const ResidentCall &c, cudaStream_t stream) {
   a.ids = c.ids;
   a.weights = c.weights;
   a.table = c.table;
+  a.even = c.even_maps != nullptr;
+  EvenMaps even = {};
+  if (a.even) std::memcpy(&even, c.even_maps, sizeof(even));
   a.out = c.out;
   a.sync = c.sync;
   a.h = reinterpret_cast<uint16_t *>(c.h);
@@ -413,7 +420,7 @@ zipmoe_status launch_resident_few(const ResidentCall &c, cudaStream_t stream) {
   cfg.gridDim = dim3(c.grid);
   cfg.blockDim = dim3(kFewThreads);
   cfg.dynamicSmemBytes = control + a.stages * stage;
-  return cudaLaunchKernelEx(&cfg, resident_few_kernel, a) == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, resident_few_kernel, even, a) == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
 }
 
 }  // namespace zipmoe_host

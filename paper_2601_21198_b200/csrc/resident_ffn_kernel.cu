@@ -40,20 +40,12 @@ namespace zipmoe_dev {
 constexpr uint32_t kResReaders = 8;                         // warps that read accumulators back: two per 32 lanes of tensor memory
 constexpr uint32_t kResThreads = 128 + 32 * kResReaders;
 constexpr uint32_t kResStageA = 32768;                      // weights of a step
-#ifndef ZIPMOE_RES_DEPTH
-#define ZIPMOE_RES_DEPTH 4
-#endif
-constexpr uint32_t kResInFlight = ZIPMOE_RES_DEPTH;
-#ifndef ZIPMOE_RES_FEW
-#define ZIPMOE_RES_FEW 8
-#endif
-constexpr uint32_t kResFewT = ZIPMOE_RES_FEW;   // up to this many tokens the kernel that gives every block whole rows runs instead
+constexpr uint32_t kResInFlight = 4;                        // steps asked for and not there yet (2: 473 us, 3: 447, 4: 442 for 64
+                                                            // tokens through 8 large experts); more only delays everybody else
+constexpr uint32_t kResFewT = 8;   // up to this many tokens the kernel that gives every block whole rows may run instead
 constexpr uint32_t kResGatherRows = 16;   // a gather of four rows takes the copy engine about 130 ns: up to this many tokens
                                           // per expert they are gathered in every step, beyond it packed once
-#ifndef ZIPMOE_RES_TWO
-#define ZIPMOE_RES_TWO 64
-#endif
-constexpr uint32_t kResTwoGroupsT = ZIPMOE_RES_TWO;   // above, a call is long enough for the wait between gate/up and down not to show,
+constexpr uint32_t kResTwoGroupsT = 64;   // above, a call is long enough for the wait between gate/up and down not to show,
                                           // and the partial sums of four phases would take too much memory
 
 struct ResidentArgs {
@@ -69,7 +61,7 @@ struct ResidentArgs {
   float *y;                 // [choices][H]: jobs that lie inside one share
   uint32_t *status;
   uint64_t limit_ns, part_phase;   // part_phase: floats between the phases' partial sums (0: one group, they follow each other)
-  uint32_t T, k, E, H, I, ring_bytes, tmem_cols, extra_tx;
+  uint32_t T, k, E, H, I, even, ring_bytes, tmem_cols, extra_tx;
 };
 
 // How U units are shared out among P blocks: block c takes [c*U/P, (c+1)*U/P), and P <= U.
@@ -115,7 +107,8 @@ __device__ __forceinline__ void place_choice(uint32_t at, int32_t e, const Resid
   token[act[active_of[e]].h_row + before] = (uint16_t)t;
 }
 
-__global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __grid_constant__ CUtensorMap x_map, const ResidentArgs a) {
+__global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ EvenMaps even,
+                                                                      const ResidentArgs a) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x, G = gridDim.x;
   const uint32_t W = (a.T + 31) / 32, choices = a.T * a.k, n_rows_max = resident_rows(a.E, choices);
@@ -125,7 +118,8 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
 #pragma unroll
   for (uint32_t i = 0; i < kIds; ++i) my_id[i] = tid + i * kResThreads < choices ? __ldg(a.ids + tid + i * kResThreads) : -1;
   const uint32_t magic = __ldcg(&a.sync->magic);
-  prefetch_table(a.table, a.E, cta * kResThreads + tid, G * kResThreads);
+  if (!a.even) prefetch_table(a.table, a.E, cta * kResThreads + tid, G * kResThreads);
+  else if (tid < 3) prefetch_map(&even.w[tid]);
 
   uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t *ctl = ring + a.ring_bytes;
@@ -244,7 +238,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
     // ---- weights ----
     // the tensor maps of the share's experts, four of each phase: one lane each makes its map visible to the copies
     constexpr uint32_t kMaps = 4;
-    {
+    if (!a.even) {
       const uint32_t p = lane >> 3, r = lane & 7;
       const Phase f = p == 0 ? ph[0] : p == 1 ? ph[1] : p == 2 ? ph[2] : ph[3];
       const uint32_t u = first(f), end = last(f);
@@ -271,10 +265,15 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
         const uint32_t end = last(f), a_first = f.a0 + (u < end ? u / (f.KS * f.RB) : 0);
         Piece q;
         while (ok && next_piece(f, u, end, q)) {
-          const uint8_t *m0 = wide_map(a.table, act[q.a].e, p < 2 ? 0 : 2);
-          const uint8_t *m1 = p < 2 ? m0 + ZIPMOE_RESIDENT_ENTRY_BYTES : m0;
+          const uint32_t e = act[q.a].e;
+          const int32_t z = a.even ? (int32_t)e : 0;
+          const void *m0 = wide_map(a.table, e, p < 2 ? 0 : 2), *m1 = p < 2 ? wide_map(a.table, e, 1) : m0;
+          if (a.even) {
+            m0 = &even.w[p < 2 ? 0 : 2];
+            m1 = &even.w[p < 2 ? 1 : 2];
+          }
           const int32_t y0 = (int32_t)(q.rb * (p < 2 ? 128 : 256)), y1 = p < 2 ? y0 : y0 + 128;
-          if (q.a >= a_first + kMaps) {
+          if (!a.even && q.a >= a_first + kMaps) {
             acquire_map(m0);
             acquire_map(m1);
           }
@@ -289,8 +288,8 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
             }
             const uint32_t dst = w_ring + at.st * kResStageA, bar = w_full + 8 * at.st;
             mbar_expect_tx(bar, kResStageA + a.extra_tx);
-            tma_load_2d(dst, m0, (int32_t)(s * 64), y0, bar, policy);
-            tma_load_2d(dst + 16384, m1, (int32_t)(s * 64), y1, bar, policy);
+            tma_load_3d(dst, m0, (int32_t)(s * 64), y0, z, bar, policy);
+            tma_load_3d(dst + 16384, m1, (int32_t)(s * 64), y1, z, bar, policy);
             at.next(n_w);
           }
         }
@@ -623,6 +622,13 @@ bool dims_ok(uint32_t E, uint32_t H, uint32_t I) {
 // the sizes that a block's slices of rows can be described for
 bool sliced_sizes(uint32_t H, uint32_t I) { return H % 64 == 0 && I % 64 == 0; }
 
+// Whether a block's whole rows are the faster way for few tokens.  They save about 9 us of a call (one token, 6 experts of
+// 2048 x 1408: 27 us against 35 to 40), and stream as fast (8 tokens, 7 experts of 4096 x 14336: 347 against 369 us) as
+// long as a block has a dozen rows of W2: with 7 (16 experts of 1024 x 4096, 400 MB) 90 against 76 us.
+bool whole_rows_pay(uint32_t choices, uint32_t E, uint32_t H, uint32_t I, uint32_t grid) {
+  return H >= 11 * grid || (uint64_t)std::min(choices, E) * 6 * H * I < (100u << 20);
+}
+
 struct ResidentDevice {
   int sms = 0;
   bool ready = false;
@@ -675,27 +681,52 @@ zipmoe_status resident_plan(uint32_t T, uint32_t k, const zipmoe_resident_expert
 }  // namespace
 
 extern "C" zipmoe_status zipmoe_resident_experts_plan(const uint16_t *const *tensors, uint32_t n_experts, uint32_t hidden,
-                                                      uint32_t inter, void *table) {
+                                                      uint32_t inter, void *table, zipmoe_resident_experts *experts) {
+  using zipmoe_dev::kSlicedMap;
   if (!dims_ok(n_experts, hidden, inter)) return ZIPMOE_ERR_UNSUPPORTED;
-  if (!tensors || !table) return ZIPMOE_ERR_INVALID_ARG;
+  if (!tensors || !table || !experts) return ZIPMOE_ERR_INVALID_ARG;
   for (uint32_t i = 0; i < 3 * n_experts; ++i)
     if (!tensors[i] || (reinterpret_cast<uintptr_t>(tensors[i]) & 15)) return ZIPMOE_ERR_INVALID_ARG;
-  static_assert(sizeof(CUtensorMap) == zipmoe_dev::kSlicedMap && 2 * sizeof(CUtensorMap) == ZIPMOE_RESIDENT_ENTRY_BYTES,
-                "an entry is two tensor maps");
+  static_assert(sizeof(CUtensorMap) == kSlicedMap && 2 * sizeof(CUtensorMap) == ZIPMOE_RESIDENT_ENTRY_BYTES, "an entry is two tensor maps");
+  const uint64_t bytes = 2ull * hidden * inter;
   uint32_t R1, S1, R2, S2;
   zipmoe_host::resident_few_rows(hidden, inter, resident_grid(), &R1, &S1, &R2, &S2);
-  for (uint32_t i = 0; i < 3 * n_experts; ++i) {
+  // both maps of n tensors of kind j (0 w1, 1 w3, 2 w2), `distance` bytes apart
+  auto describe = [&](uint8_t *to, const uint16_t *base, uint32_t j, uint64_t n, uint64_t distance) {
+    const uint32_t rows = j < 2 ? inter : hidden, cols = j < 2 ? hidden : inter;
     CUtensorMap map;
-    const uint32_t rows = i % 3 < 2 ? inter : hidden, cols = i % 3 < 2 ? hidden : inter;
-    if (!zipmoe_host::make_bf16_map(&map, tensors[i], rows, cols, cols, 128, true)) return ZIPMOE_ERR_CUDA;
-    uint8_t *entry = static_cast<uint8_t *>(table) + (size_t)i * ZIPMOE_RESIDENT_ENTRY_BYTES;
-    std::memset(entry, 0, ZIPMOE_RESIDENT_ENTRY_BYTES);
-    std::memcpy(entry, &map, sizeof(map));
-    if (sliced_sizes(hidden, inter)) {
-      if (!zipmoe_host::make_sliced_map(&map, tensors[i], rows, cols, i % 3 < 2 ? S1 : S2)) return ZIPMOE_ERR_CUDA;
-      std::memcpy(entry + zipmoe_dev::kSlicedMap, &map, sizeof(map));
-    }
+    if (!zipmoe_host::make_wide_map(&map, base, rows, cols, n, distance)) return false;
+    std::memset(to, 0, ZIPMOE_RESIDENT_ENTRY_BYTES);
+    std::memcpy(to, &map, sizeof(map));
+    if (!sliced_sizes(hidden, inter)) return true;
+    if (!zipmoe_host::make_sliced_map(&map, base, rows, cols, j < 2 ? S1 : S2, n, distance)) return false;
+    std::memcpy(to + kSlicedMap, &map, sizeof(map));
+    return true;
+  };
+  for (uint32_t i = 0; i < 3 * n_experts; ++i)
+    if (!describe(static_cast<uint8_t *>(table) + (size_t)i * ZIPMOE_RESIDENT_ENTRY_BYTES, tensors[i], i % 3, 1, bytes)) return ZIPMOE_ERR_CUDA;
+  std::memset(experts, 0, sizeof(*experts));
+  experts->n_experts = n_experts;
+  experts->hidden = hidden;
+  experts->inter = inter;
+  // evenly spaced experts: one map per kind of tensor serves them all (distances that a map can hold)
+  uint64_t distance[3];
+  bool even = true;
+  for (uint32_t j = 0; j < 3; ++j) {
+    const uintptr_t first = reinterpret_cast<uintptr_t>(tensors[j]);
+    const uintptr_t second = n_experts > 1 ? reinterpret_cast<uintptr_t>(tensors[3 + j]) : first + bytes;
+    distance[j] = second - first;
+    even = even && second > first && distance[j] >= bytes && distance[j] < (1ull << 40);
+    for (uint32_t e = 2; e < n_experts && even; ++e)
+      even = reinterpret_cast<uintptr_t>(tensors[3 * e + j]) == first + e * distance[j];
   }
+  for (uint32_t j = 0; j < 3 && even; ++j) {
+    uint8_t both[ZIPMOE_RESIDENT_ENTRY_BYTES];
+    if (!describe(both, tensors[j], j, n_experts, distance[j])) return ZIPMOE_ERR_CUDA;
+    std::memcpy(experts->maps + 128 * j, both, 128);
+    std::memcpy(experts->maps + 128 * (3 + j), both + kSlicedMap, 128);
+  }
+  experts->even = even;
   return ZIPMOE_OK;
 }
 
@@ -728,7 +759,7 @@ extern "C" zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, c
   const zipmoe_status rc = resident_plan(T, k, ex, &p);
   if (rc != ZIPMOE_OK) return rc;
   if (T == 0) return ZIPMOE_OK;
-  if (!tokens || !topk_ids || !out || !workspace || !ex->table) return ZIPMOE_ERR_INVALID_ARG;
+  if (!tokens || !topk_ids || !out || !workspace || !ex->table || ex->even > 1) return ZIPMOE_ERR_INVALID_ARG;
   if (((reinterpret_cast<uintptr_t>(tokens) | reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(workspace)) & 15) ||
       (reinterpret_cast<uintptr_t>(ex->table) & 63) ||
       ((reinterpret_cast<uintptr_t>(topk_ids) | reinterpret_cast<uintptr_t>(topk_weights) | reinterpret_cast<uintptr_t>(status_word)) & 3))
@@ -748,12 +779,13 @@ extern "C" zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, c
   uint32_t tries = 0, extra_tx = 0;
   zipmoe_host::wait_fault_setting(&extra_tx, &tries);
   const uint64_t limit_ns = tries < zipmoe_host::kWaitTries ? 1000000ull : 1000000000ull;   // (1 ms in the tests of the limit)
-  if (T <= kResFewT && sliced_sizes(ex->hidden, ex->inter)) {
+  if (T <= kResFewT && sliced_sizes(ex->hidden, ex->inter) && whole_rows_pay(T * k, ex->n_experts, ex->hidden, ex->inter, p.grid)) {
     zipmoe_host::ResidentCall c;
     c.tokens = tokens;
     c.ids = topk_ids;
     c.weights = topk_weights;
     c.table = static_cast<const uint8_t *>(ex->table);
+    c.even_maps = ex->even ? ex->maps + 3 * 128 : nullptr;
     c.out = out;
     c.sync = reinterpret_cast<ResidentSync *>(ws);
     c.h = ws + p.off_h;
@@ -775,6 +807,9 @@ extern "C" zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, c
   a.ids = topk_ids;
   a.weights = topk_weights;
   a.table = static_cast<const uint8_t *>(ex->table);
+  a.even = ex->even;
+  EvenMaps even = {};
+  if (ex->even) std::memcpy(&even, ex->maps, sizeof(even));
   a.out = out;
   a.sync = reinterpret_cast<ResidentSync *>(ws);
   a.tokens = tokens;
@@ -803,5 +838,5 @@ extern "C" zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, c
   cfg.gridDim = dim3(p.grid);
   cfg.blockDim = dim3(kResThreads);
   cfg.dynamicSmemBytes = p.smem;
-  return cudaLaunchKernelEx(&cfg, resident_ffn_kernel, x_map, a) == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, resident_ffn_kernel, x_map, even, a) == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
 }

@@ -72,13 +72,32 @@ __device__ __forceinline__ uint64_t policy_evict_last() {
   asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
   return p;
 }
-// one box of a 2-D tensor map into shared memory; x in elements, x * element size a multiple of 16 bytes
+// one box of a tensor map into shared memory; x in elements, x * element size a multiple of 16 bytes
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const void *map, int32_t x, int32_t y, uint32_t bar, uint64_t policy) {
   asm volatile(
       "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3}], "
       "[%4], %5;" ::"r"(dst),
       "l"(map), "r"(x), "r"(y), "r"(bar), "l"(policy)
       : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void *map, int32_t x, int32_t y, int32_t z, uint32_t bar, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4}], "
+      "[%5], %6;" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar), "l"(policy)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const void *map, int32_t x, int32_t y, int32_t z, int32_t w, uint32_t bar,
+                                            uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5}], "
+      "[%6], %7;" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar), "l"(policy)
+      : "memory");
+}
+__device__ __forceinline__ void tma_prefetch_4d(const void *map, int32_t x, int32_t y, int32_t z, int32_t w) {
+  asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];" ::"l"(map), "r"(x), "r"(y), "r"(z), "r"(w)
+               : "memory");
 }
 // four rows of a 2-D tensor map whose box is 64 columns x 1 row: the rows land one after the other
 __device__ __forceinline__ void tma_gather4(uint32_t dst, const void *map, int32_t x, int32_t r0, int32_t r1, int32_t r2, int32_t r3,
@@ -165,29 +184,36 @@ inline EncodeTiled encode_tiled() {
   return encode;
 }
 
-// Describes a dense row-major bf16 matrix to the copy engine: boxes of 64 columns x box_rows rows, written to shared
-// memory in the 128-byte swizzle, zeros outside the matrix.  False if the driver does not offer the call or refuses it.
+// What the maps below have in common: bf16, boxes whose rows are 64 columns in the 128-byte swizzle, zeros outside.
+inline bool encode_bf16(CUtensorMap *map, uint32_t rank, const void *base, const cuuint64_t *dims, const cuuint64_t *strides,
+                        const cuuint32_t *box, bool wide_fetch) {
+  const EncodeTiled encode = encode_tiled();
+  const cuuint32_t step[4] = {1, 1, 1, 1};
+  return encode && encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void *>(base), dims, strides, box, step,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                          wide_fetch ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// A row-major matrix: boxes of 64 columns x box_rows rows.  False if the driver does not offer the call or refuses it.
 inline bool make_bf16_map(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint64_t pitch_elems, uint32_t box_rows,
                           bool wide_fetch) {
-  const EncodeTiled encode = encode_tiled();
-  if (!encode) return false;
   const cuuint64_t dims[2] = {cols, rows}, strides[1] = {pitch_elems * 2};
-  const cuuint32_t box[2] = {64, box_rows}, step[2] = {1, 1};
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims, strides, box, step,
-                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                wide_fetch ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const cuuint32_t box[2] = {64, box_rows};
+  return encode_bf16(map, 2, base, dims, strides, box, wide_fetch);
 }
-// The same matrix, cols a multiple of 64, seen as [cols / 64][rows][64]: a box of 8 x box_rows x 64 is 512 columns of
-// box_rows rows.
-inline bool make_sliced_map(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
-  const EncodeTiled encode = encode_tiled();
-  if (!encode) return false;
-  const cuuint64_t dims[3] = {64, rows, cols / 64}, strides[2] = {cols * 2, 128};
-  const cuuint32_t box[3] = {64, box_rows, 8}, step[3] = {1, 1, 1};
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, step,
-                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+// n dense row-major matrices `distance` bytes apart: boxes of 64 columns x 128 rows of one of them.
+inline bool make_wide_map(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint64_t n, uint64_t distance) {
+  const cuuint64_t dims[3] = {cols, rows, n}, strides[2] = {cols * 2, distance};
+  const cuuint32_t box[3] = {64, 128, 1};
+  return encode_bf16(map, 3, base, dims, strides, box, true);
+}
+// The same, cols a multiple of 64, seen as [n][cols / 64][rows][64]: a box of 8 x box_rows x 64 is 512 columns of box_rows
+// rows.
+inline bool make_sliced_map(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint32_t box_rows, uint64_t n,
+                            uint64_t distance) {
+  const cuuint64_t dims[4] = {64, rows, cols / 64, n}, strides[3] = {cols * 2, 128, distance};
+  const cuuint32_t box[4] = {64, box_rows, 8, 1};
+  return encode_bf16(map, 4, base, dims, strides, box, true);
 }
 
 }  // namespace zipmoe_host

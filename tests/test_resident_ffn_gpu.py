@@ -229,3 +229,30 @@ def test_binding_refuses_what_the_kernel_would_misread(zb):
         zb.ResidentExperts(ws[:4], 64, 64)
     with pytest.raises(ValueError):
         zb.ResidentExperts(ws, 64, 72)
+
+
+@pytest.mark.parametrize("E,H,I,k", [(5, 512, 384, 2), (4, 264, 200, 3), (1, 128, 64, 1)])
+@pytest.mark.parametrize("T", [3, 40])
+def test_evenly_spaced_and_scattered_experts_give_the_same_bits(zb, E, H, I, k, T):
+    """Tensors at equal distances are found through one map per kind, others through the table."""
+    import torch
+    ws = layer(E, H, I, 77)
+    tok, (ids, wts) = inputs.tokens(T, H, seed=4), inputs.routing(T, n_experts=E, k=k, seed=4)
+    stacked = [torch.stack([dev(ws[3 * e + j]) for e in range(E)]) for j in range(3)]
+    even = zb.ResidentExperts([stacked[j][e] for e in range(E) for j in range(3)], H, I)
+    assert even.struct.even == 1
+    a = even.ffn(dev(tok), dev(ids), dev(wts))
+    check(a, ws, tok, ids, wts)
+    if E == 1:
+        return
+    room = torch.zeros(3 * E * (H * I + 8) + 8, dtype=torch.int16, device="cuda")
+    at = {int(s): 8 * i + i * H * I for i, s in enumerate(np.random.default_rng(1).permutation(3 * E)[::-1])}
+    scattered = []
+    for s in range(3 * E):
+        view = room[at[s]:at[s] + H * I].view(ws[s].shape)
+        view.copy_(dev(ws[s]))
+        scattered.append(view)
+    apart = zb.ResidentExperts(scattered, H, I)
+    assert apart.struct.even == 0
+    b = apart.ffn(dev(tok), dev(ids), dev(wts))
+    assert torch.equal(a, b) and int(apart.status.item()) == 0 and int(even.status.item()) == 0

@@ -82,7 +82,8 @@ def test_resident_plan_refusals(zb):
 
     def plan(addresses, E=2, H=64, I=128, out=table):
         ptrs = (ctypes.c_void_p * len(addresses))(*addresses)
-        return lib.zipmoe_resident_experts_plan(ptrs, E, H, I, None if out is None else out.ctypes.data)
+        experts = ctypes.byref(zb.ResidentExpertsStruct())
+        return lib.zipmoe_resident_experts_plan(ptrs, E, H, I, None if out is None else out.ctypes.data, experts)
 
     assert plan([A] * 5 + [None]) == zb.ERR_INVALID_ARG
     assert plan([A] * 5 + [A + 8]) == zb.ERR_INVALID_ARG
