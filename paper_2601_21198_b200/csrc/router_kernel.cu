@@ -5,10 +5,11 @@
 //     TMA stages and accumulates [128 x N] in tensor memory.  Rows and columns past the matrices come in as zeros, so no
 //     size needs a path of its own; a single token reads one row.
 //   * Every block leaves its partial logits in its shared memory; after a cluster barrier the block of rank r adds, in
-//     rank order, the parts of tokens r, r + S, ... straight from its neighbours' shared memory.
-//   * One warp picks a token's k experts: a logit becomes a 32-bit key that orders as the number does (NaN on top),
-//     every lane holds the keys of experts lane, lane + 32, ..., and each choice is one maximum over the warp and one
-//     minimum over the indices that reach it.
+//     rank order, the parts of tokens r, r + S, ... straight from its neighbours' shared memory.  (Sent there by their
+//     owners instead they need a second barrier, before the rings may be written over: 2 us slower for 8192 tokens.)
+//   * Eight lanes pick a token's k experts, four tokens to a warp: a logit becomes a 32-bit key that orders as the number
+//     does (NaN on top), every lane holds an eighth of them, and each choice is the lanes' own best and three exchanges.
+//     (A whole warp per token spends most of its instructions on two experts per lane: 450 per token, 6 of 16 us for 8192.)
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -44,35 +45,56 @@ __device__ __forceinline__ float key_logit(uint32_t key) {   // (NaN's key gives
   return __uint_as_float((key & 0x80000000u) ? (key & 0x7FFFFFFFu) : ~key);
 }
 
-// One warp picks the k largest of a token's logits (l[i] is expert lane + 32 i; -infinity past the last) and writes ids
-// and weights.
+// The expert of a lane's i-th value: eight lanes hold four neighbouring ones each, then the next 32.
+__device__ __forceinline__ uint32_t expert_of(uint32_t q, uint32_t i) { return (i >> 2) * 32 + q * 4 + (i & 3); }
+
+// Eight lanes (q = 0..7) pick the k largest of their token's logits (l[i] is expert_of(q, i); -infinity past the last) and
+// write ids and weights, unless `there` is false.  The four groups of a warp work in step.
 template <int kPer>
-__device__ __forceinline__ void pick_experts(const float (&l)[kPer], uint32_t k, uint32_t flags, uint32_t lane, int32_t *ids,
+__device__ __forceinline__ void pick_experts(const float (&l)[kPer], uint32_t k, uint32_t flags, uint32_t q, bool there, int32_t *ids,
                                              float *weights) {
   uint32_t key[kPer];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) key[i] = logit_key(l[i]);
   int32_t my_id = -1;       // lane j keeps choice j
   uint32_t my_key = 0, top_key = 0;
+#pragma unroll 1
   for (uint32_t j = 0; j < k; ++j) {
-    uint32_t best = 0, at = 0;
+    // the lane's best, pair by pair (equal keys: the first, which is the lowest expert)
+    uint32_t top_of[kPer], place[kPer];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (key[i] > best) {
-        best = key[i];
-        at = i;
+    for (int i = 0; i < kPer; ++i) {
+      top_of[i] = key[i];
+      place[i] = i;
+    }
+#pragma unroll
+    for (int d = 1; d < kPer; d *= 2)
+#pragma unroll
+      for (int i = 0; i < kPer; i += 2 * d)
+        if (top_of[i + d] > top_of[i]) {
+          top_of[i] = top_of[i + d];
+          place[i] = place[i + d];
+        }
+    uint32_t best = top_of[0];
+    const uint32_t at = place[0];
+    uint32_t e = expert_of(q, at);
+    const uint32_t own = e;
+#pragma unroll
+    for (uint32_t d = 1; d < 8; d <<= 1) {
+      const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, best, d), other_e = __shfl_xor_sync(0xFFFFFFFFu, e, d);
+      if (other > best || (other == best && other_e < e)) {
+        best = other;
+        e = other_e;
       }
-    const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, best);
-    if (most == 0) break;
-    const uint32_t e = __reduce_min_sync(0xFFFFFFFFu, best == most ? at * 32 + lane : 0xFFFFFFFFu);
-    if (j == 0) top_key = most;
-    if (lane == j) {
+    }
+    if (j == 0) top_key = best;
+    if (q == j && best != 0) {
       my_id = (int32_t)e;
-      my_key = most;
+      my_key = best;
     }
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
-      if (e == lane + 32 * i) key[i] = 0;
+      if (own == e && at == (uint32_t)i) key[i] = 0;
   }
   const float top = key_logit(top_key);
   const float p = my_id >= 0 ? __expf(key_logit(my_key) - top) : 0.f;
@@ -83,10 +105,10 @@ __device__ __forceinline__ void pick_experts(const float (&l)[kPer], uint32_t k,
     for (int i = 0; i < kPer; ++i) sum += l[i] == -INFINITY ? 0.f : __expf(l[i] - top);
   }
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-  if (lane < k) {
-    ids[lane] = my_id;
-    weights[lane] = my_id >= 0 ? __fdiv_rn(p, sum) : 0.f;
+  for (uint32_t d = 1; d < 8; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+  if (there && q < k) {
+    ids[q] = my_id;
+    weights[q] = my_id >= 0 ? __fdiv_rn(p, sum) : 0.f;
   }
 }
 
@@ -108,12 +130,14 @@ __device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank) {   /
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
   return r;
 }
-__device__ __forceinline__ float load_cluster(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+// four neighbouring floats of another block's shared memory.  Volatile: it stays behind the cluster's barrier.
+__device__ __forceinline__ float4 load_cluster(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
   return v;
 }
 
+// kPer: experts per lane, E <= 8 * kPer
 template <int kPer>
 __global__ void __launch_bounds__(kRouterThreads) router_kernel(const __grid_constant__ CUtensorMap x_map,
                                                                const __grid_constant__ CUtensorMap gate_map, const RouterArgs a) {
@@ -122,7 +146,8 @@ __global__ void __launch_bounds__(kRouterThreads) router_kernel(const __grid_con
   __shared__ uint32_t words[2];   // tmem, dead
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, rank = cluster_rank(), S = cluster_size();
   uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  const uint32_t ring0 = smem_addr(ring), stage_bytes = (kRouterRows + a.N) * 128, pitch = a.N + 1;
+  const uint32_t ring0 = smem_addr(ring), stage_bytes = (kRouterRows + a.N) * 128;
+  const uint32_t pitch = a.N + 4;   // floats between tokens: the 16-byte pieces of eight of them fall into different banks
   const uint32_t full = smem_addr(bars), empty = full + 8 * kRouterMaxStages, done = empty + 8 * kRouterMaxStages;
   volatile uint32_t *dead = words + 1;
   const WaitLimit lim = {dead, a.status, a.limit_ns};
@@ -181,6 +206,12 @@ __global__ void __launch_bounds__(kRouterThreads) router_kernel(const __grid_con
   }
   __syncwarp();
 
+  // (wanted at the end, asked for now)
+  const uint32_t q = lane & 7;
+  float bias[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) bias[i] = a.bias && expert_of(q, i) < a.E ? __ldg(a.bias + expert_of(q, i)) : 0.f;
+
   // ---- partial logits into shared memory, over the ring (every MMA has read it); row = token ----
   float *part = reinterpret_cast<float *>(ring);
   const bool ok = __all_sync(0xFFFFFFFFu, wait_bar(done, 0, lim));
@@ -188,13 +219,15 @@ __global__ void __launch_bounds__(kRouterThreads) router_kernel(const __grid_con
   const uint32_t row = 32 * (warp & 3) + lane;
   if (ok && 32 * (warp & 3) < rows) {
     for (uint32_t c = 8 * (warp >> 2); c < a.N; c += 16) {
-      uint32_t v[8];
+      uint32_t v[8] = {};
       if (s1 > s0) {
         tmem_load8(tmem + ((32 * (warp & 3)) << 16) + c, v);
         tmem_wait();
       }
-#pragma unroll
-      for (uint32_t n = 0; n < 8; ++n) part[row * pitch + c + n] = s1 > s0 ? __uint_as_float(v[n]) : 0.f;
+      float4 *to = reinterpret_cast<float4 *>(part + row * pitch + c);
+      const bool any = s1 > s0;
+      to[0] = any ? make_float4(__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]), __uint_as_float(v[3])) : make_float4(0.f, 0.f, 0.f, 0.f);
+      to[1] = any ? make_float4(__uint_as_float(v[4]), __uint_as_float(v[5]), __uint_as_float(v[6]), __uint_as_float(v[7])) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
   }
   __syncwarp();
@@ -210,29 +243,47 @@ __global__ void __launch_bounds__(kRouterThreads) router_kernel(const __grid_con
     uint32_t base[8];
 #pragma unroll
     for (uint32_t r = 0; r < 8; ++r) base[r] = in_block(ring0, r < S ? r : 0);
-    for (uint32_t m = rank + S * warp; m < rows; m += S * (kRouterThreads / 32)) {
+    const bool wide_logits = a.logits && a.E % 4 == 0 && (reinterpret_cast<uintptr_t>(a.logits) & 15) == 0;
+    // token rank + S * n for n = warp * 4 + lane / 8, then the next 32
+    for (uint32_t n0 = warp * 4; rank + S * n0 < rows; n0 += kRouterThreads / 8) {
+      const uint32_t m = rank + S * (n0 + (lane >> 3));
+      const bool there = m < rows;
       const uint64_t t = t0 + m;
       float l[kPer];
 #pragma unroll
       for (int i = 0; i < kPer; ++i) l[i] = 0.f;
+      const uint32_t at = ((there ? m : rank) * pitch + q * 4) * 4;
 #pragma unroll
-      for (uint32_t r = 0; r < 8; ++r)
-        if (r < S) {
+      for (uint32_t i = 0; i < kPer; i += 4) {
+        if (i * 8 >= a.N) break;
+        const bool in = i * 8 + q * 4 < a.N;   // (the operand's columns up to N are there, zeros past the experts)
+        float4 v[8];
 #pragma unroll
-          for (int i = 0; i < kPer; ++i)
-            if (lane + 32 * i < a.E) l[i] += load_cluster(base[r] + (m * pitch + lane + 32 * i) * 4);
-        }
+        for (uint32_t r = 0; r < 8; ++r)
+          if (r < S) v[r] = load_cluster(base[r] + (in ? at + i * 32 : 0));
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const uint32_t e = lane + 32 * i;
-        if (e < a.E) {
-          if (a.bias) l[i] += __ldg(a.bias + e);
-          if (a.logits) a.logits[t * a.E + e] = l[i];
-        } else {
-          l[i] = -INFINITY;
+        for (uint32_t r = 0; r < 8; ++r)
+          if (r < S) {
+            l[i] += v[r].x;
+            l[i + 1] += v[r].y;
+            l[i + 2] += v[r].z;
+            l[i + 3] += v[r].w;
+          }
+      }
+#pragma unroll
+      for (uint32_t i = 0; i < kPer; i += 4) {
+        const uint32_t e = expert_of(q, i);
+#pragma unroll
+        for (uint32_t c = 0; c < 4; ++c) l[i + c] = e + c < a.E ? l[i + c] + bias[i + c] : -INFINITY;
+        if (there && wide_logits) {
+          if (e < a.E) *reinterpret_cast<float4 *>(a.logits + t * a.E + e) = make_float4(l[i], l[i + 1], l[i + 2], l[i + 3]);
+        } else if (there && a.logits) {
+#pragma unroll
+          for (uint32_t c = 0; c < 4; ++c)
+            if (e + c < a.E) a.logits[t * a.E + e + c] = l[i + c];
         }
       }
-      pick_experts<kPer>(l, a.k, a.flags, lane, a.ids + t * a.k, a.weights + t * a.k);
+      pick_experts<kPer>(l, a.k, a.flags, q, there, a.ids + t * a.k, a.weights + t * a.k);
     }
   }
   __syncwarp();
@@ -319,14 +370,14 @@ extern "C" zipmoe_status zipmoe_route(const zipmoe_route_args *r, zipmoe_stream 
   a.stages = std::min(kRouterMaxStages, (per_sm == 2 ? 108u : 216u) * 1024 / stage);
   uint32_t S = 8;
   while (S > 1 && (S > steps || tiles * S > 148 * per_sm)) S >>= 1;
-  const uint32_t smem = 1024 + std::max(a.stages * stage, kRouterRows * (a.N + 1) * 4);
+  const uint32_t smem = 1024 + std::max(a.stages * stage, kRouterRows * (a.N + 4) * 4);
   CUtensorMap x_map, gate_map;
   if (!zipmoe_host::make_bf16_map(&x_map, r->tokens, T, hidden, r->token_pitch, kRouterRows, true) ||
       !zipmoe_host::make_bf16_map(&gate_map, r->gate, n_experts, hidden, hidden, a.N, true))
     return ZIPMOE_ERR_CUDA;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  if (n_experts <= 32) return launch_router<1>(dev, x_map, gate_map, a, S, smem, s);
-  if (n_experts <= 64) return launch_router<2>(dev, x_map, gate_map, a, S, smem, s);
-  if (n_experts <= 128) return launch_router<4>(dev, x_map, gate_map, a, S, smem, s);
-  return launch_router<8>(dev, x_map, gate_map, a, S, smem, s);
+  if (n_experts <= 32) return launch_router<4>(dev, x_map, gate_map, a, S, smem, s);
+  if (n_experts <= 64) return launch_router<8>(dev, x_map, gate_map, a, S, smem, s);
+  if (n_experts <= 128) return launch_router<16>(dev, x_map, gate_map, a, S, smem, s);
+  return launch_router<32>(dev, x_map, gate_map, a, S, smem, s);
 }
