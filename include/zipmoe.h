@@ -535,7 +535,8 @@ zipmoe_status zipmoe_plan_schedule(const zipmoe_sched_task *tasks, uint32_t n_ta
  * still terminates.  That path cannot be reached with sound inputs, so this switch provokes it without a fault:
  * from now on zipmoe_decode and zipmoe_decode_expert_ffn arm the barrier of every tile-record copy for
  * extra_tx_bytes more than the copy delivers (so that the barrier never completes although the copy does) and give
- * up after `tries` tries.  (0, 0) restores normal operation.  Process-wide; not for concurrent use. */
+ * up after `tries` tries; zipmoe_route and zipmoe_expert_ffn do the same with the barriers of their weights, and give
+ * up after a millisecond.  (0, 0) restores normal operation.  Process-wide; not for concurrent use. */
 void zipmoe_test_wait_fault(uint32_t extra_tx_bytes, uint32_t tries);
 
 /* For the library's own tests (the paper has no counterpart).  A launch that hands its tiles out dynamically owns
