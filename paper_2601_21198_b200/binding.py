@@ -551,24 +551,26 @@ class DeviceExperts:
         return out
 
 
-_KINDS = {}
-
-
-def _kind(name):
+class _Kinds:
     """The torch types that hold a kind of element: bf16 values may come as int16 bit patterns, e4m3 as bytes."""
-    if not _KINDS:
+
+    def __init__(self):
         import torch
-        _KINDS.update({"bf16": (torch.bfloat16, torch.int16, torch.uint16), "e4m3": (torch.float8_e4m3fn, torch.uint8),
-                       "fp32": (torch.float32,), "int32": (torch.int32,)})
-    return _KINDS[name]
+        self.bf16 = (torch.bfloat16, torch.int16, torch.uint16)
+        self.e4m3 = (torch.float8_e4m3fn, torch.uint8)
+        self.fp32 = (torch.float32,)
+        self.int32 = (torch.int32,)
+        self.current_stream = torch._C._cuda_getCurrentRawStream   # handle of a device's current stream
 
 
-def _stream_of(index, stream):
-    """The handle of a torch stream, of the current one of device `index` where none is given."""
-    import torch
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(index)
-    return stream.cuda_stream
+_kinds = None
+
+
+def _get_kinds():
+    global _kinds
+    if _kinds is None:
+        _kinds = _Kinds()
+    return _kinds
 
 
 def _empty(shape, dtype, device, stream):
@@ -581,21 +583,31 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _refuse(name, t, shape, kinds, index, what):
+    raise ValueError("%s: a %s tensor %s of %s on CUDA device %d is wanted, not %s of %s on %s (strides %s)" %
+                     (name, what, shape, kinds[0], index, tuple(t.shape), t.dtype, t.device, t.stride()))
+
+
 def _rows(name, t, shape, kinds, index):
-    """Row pitch, in elements, of a tensor of this shape on device `index` whose rows are dense."""
+    """Address and row pitch, in elements, of a tensor of this shape on device `index` whose rows are dense."""
     stride = t.stride()
-    if t.shape != shape or t.dtype not in kinds or t.get_device() != index or index < 0:
-        raise ValueError("%s: a tensor %s of %s on device %d is wanted, not %s of %s on %s" %
-                         (name, shape, kinds[0], index, tuple(t.shape), t.dtype, t.device))
-    if stride[1] != 1 and shape[1] > 1:
-        raise ValueError("%s: the elements of a row are not next to each other" % name)
-    return stride[0] if shape[0] > 1 else shape[1]
+    if t.shape != shape or t.dtype not in kinds or t.get_device() != index or (stride[1] != 1 and shape[1] > 1):
+        _refuse(name, t, shape, kinds, index, "row by row dense")
+    return t.data_ptr(), (stride[0] if shape[0] > 1 else shape[1])
 
 
 def _dense(name, t, shape, kinds, index):
-    if t.shape != shape or t.dtype not in kinds or t.get_device() != index or index < 0 or not t.is_contiguous():
-        raise ValueError("%s: a contiguous tensor %s of %s on device %d is wanted, not %s of %s on %s" %
-                         (name, shape, kinds[0], index, tuple(t.shape), t.dtype, t.device))
+    """Address of a contiguous tensor of this shape on device `index`."""
+    if t.shape != shape or t.dtype not in kinds or t.get_device() != index or not t.is_contiguous():
+        _refuse(name, t, shape, kinds, index, "contiguous")
+    return t.data_ptr()
+
+
+def _device_of(name, t):
+    index = t.get_device()
+    if index < 0:
+        raise ValueError("%s: a tensor on a CUDA device is wanted, not on %s" % (name, t.device))
+    return index
 
 
 class RmsNorm:
@@ -603,38 +615,42 @@ class RmsNorm:
     bf16 tensors or int16 patterns [rows, cols] whose rows may lie apart; the residual stream is of that kind or fp32."""
 
     def __init__(self, weight, eps=1e-6):
-        self.index = weight.get_device()
-        _dense("weight", weight, (weight.numel(),), _kind("bf16"), self.index)
+        self.kinds = _get_kinds()
+        self.index = _device_of("weight", weight)
         self.weight, self.eps, self.cols = weight, float(eps), weight.numel()
+        self.weight_at = _dense("weight", weight, (self.cols,), self.kinds.bf16, self.index)
 
     def n_groups(self, group):
         return 1 if group <= 0 or group >= self.cols else -(-self.cols // group)
 
     def _call(self, x, residual, residual_out, out, out_q, scales, group, stream):
-        shape, index, bf16 = (x.shape[0], self.cols), self.index, _kind("bf16")
-        x_pitch = _rows("x", x, shape, bf16, index)
+        kinds, index, rows, cols = self.kinds, self.index, x.shape[0], self.cols
+        shape, bf16 = (rows, cols), kinds.bf16
+        x_at, x_pitch = _rows("x", x, shape, bf16, index)
         res = res_out = res_pitch = res_out_pitch = flags = 0
         if residual is not None:
-            kinds = bf16 if residual.dtype in bf16 else _kind("fp32")
-            flags = 0 if kinds is bf16 else NORM_RESIDUAL_F32
-            res_pitch, res = _rows("residual", residual, shape, kinds, index), residual.data_ptr()
+            of = bf16
+            if residual.dtype not in bf16:
+                of, flags = kinds.fp32, NORM_RESIDUAL_F32
+            res, res_pitch = _rows("residual", residual, shape, of, index)
             if residual_out is not None:
-                res_out_pitch, res_out = _rows("residual_out", residual_out, shape, kinds, index), residual_out.data_ptr()
+                res_out, res_out_pitch = _rows("residual_out", residual_out, shape, of, index)
         elif residual_out is not None:
             raise ValueError("residual_out without a residual")
         out_at = q_at = scales_at = 0
         if out is not None:
-            out_pitch, out_at = _rows("out", out, shape, bf16, index), out.data_ptr()
+            out_at, out_pitch = _rows("out", out, shape, bf16, index)
         if out_q is not None:
-            q_pitch, q_at = _rows("out_q", out_q, shape, _kind("e4m3"), index), out_q.data_ptr()
+            q_at, q_pitch = _rows("out_q", out_q, shape, kinds.e4m3, index)
             if out is not None and out_pitch != q_pitch:
                 raise ValueError("out and out_q have rows %d and %d apart" % (out_pitch, q_pitch))
             out_pitch = q_pitch
-            _dense("scales", scales, (shape[0], self.n_groups(group)), _kind("fp32"), index)
-            scales_at = scales.data_ptr()
-        args = _NORM_ARGS.pack(x.data_ptr(), x_pitch, res, res_pitch, res_out, res_out_pitch, self.weight.data_ptr(), out_at, q_at,
-                               out_pitch, scales_at, shape[0], shape[1], max(group, 0), flags, self.eps, 0)
-        _check("zipmoe_add_rmsnorm", _lib.zipmoe_add_rmsnorm(args, _stream_of(index, stream)))
+            scales_at = _dense("scales", scales, (rows, self.n_groups(group)), kinds.fp32, index)
+        args = _NORM_ARGS.pack(x_at, x_pitch, res, res_pitch, res_out, res_out_pitch, self.weight_at, out_at, q_at, out_pitch, scales_at,
+                               rows, cols, group if group > 0 else 0, flags, self.eps, 0)
+        status = _lib.zipmoe_add_rmsnorm(args, kinds.current_stream(index) if stream is None else stream.cuda_stream)
+        if status:
+            raise ZipMoEError("zipmoe_add_rmsnorm", status)
 
     def add_norm(self, x, residual=None, residual_out=None, out=None, stream=None):
         """Returns out [rows, cols] (bf16); residual_out (may be `residual` itself) gets x + residual."""
@@ -646,9 +662,9 @@ class RmsNorm:
     def add_norm_8bit(self, x, residual=None, residual_out=None, out_q=None, scales=None, group=0, out=None, stream=None):
         """Returns (out_q [rows, cols] e4m3, scales [rows, groups] fp32); `out`, if given, gets the bf16 rows as well."""
         if out_q is None:
-            out_q = _empty(x.shape, _kind("e4m3")[0], x.device, stream)
+            out_q = _empty(x.shape, self.kinds.e4m3[0], x.device, stream)
         if scales is None:
-            scales = _empty((x.shape[0], self.n_groups(group)), _kind("fp32")[0], x.device, stream)
+            scales = _empty((x.shape[0], self.n_groups(group)), self.kinds.fp32[0], x.device, stream)
         self._call(x, residual, residual_out, out, out_q, scales, group, stream)
         return out_q, scales
 
@@ -658,34 +674,33 @@ class Router:
 
     def __init__(self, gate, k, bias=None, renormalise=True):
         import torch
-        self.index = gate.get_device()
+        self.kinds = _get_kinds()
+        self.index = _device_of("gate", gate)
         self.n_experts, self.hidden = gate.shape
-        _dense("gate", gate, (self.n_experts, self.hidden), _kind("bf16"), self.index)
-        if bias is not None:
-            _dense("bias", bias, (self.n_experts,), _kind("fp32"), self.index)
         self.gate, self.bias, self.k = gate, bias, int(k)
+        self.gate_at = _dense("gate", gate, (self.n_experts, self.hidden), self.kinds.bf16, self.index)
+        self.bias_at = 0 if bias is None else _dense("bias", bias, (self.n_experts,), self.kinds.fp32, self.index)
         self.flags = 0 if renormalise else ROUTE_SOFTMAX_ALL
         self.status = torch.zeros(1, dtype=torch.int32, device=gate.device)
+        self.status_at = self.status.data_ptr()
 
     def route(self, tokens, ids=None, weights=None, logits=None, stream=None):
         """tokens [T, hidden] -> ids [T, k] int32, weights [T, k] fp32; logits, if given, gets [T, n_experts] fp32."""
-        T, index = tokens.shape[0], self.index
-        pitch = _rows("tokens", tokens, (T, self.hidden), _kind("bf16"), index)
+        kinds, index, T = self.kinds, self.index, tokens.shape[0]
         chosen = (T, self.k)
+        tokens_at, pitch = _rows("tokens", tokens, (T, self.hidden), kinds.bf16, index)
         if ids is None:
-            ids = _empty(chosen, _kind("int32")[0], tokens.device, stream)
-        else:
-            _dense("ids", ids, chosen, _kind("int32"), index)
+            ids = _empty(chosen, kinds.int32[0], tokens.device, stream)
         if weights is None:
-            weights = _empty(chosen, _kind("fp32")[0], tokens.device, stream)
-        else:
-            _dense("weights", weights, chosen, _kind("fp32"), index)
-        if logits is not None:
-            _dense("logits", logits, (T, self.n_experts), _kind("fp32"), index)
-        args = _ROUTE_ARGS.pack(tokens.data_ptr(), pitch, self.gate.data_ptr(), 0 if self.bias is None else self.bias.data_ptr(),
-                                ids.data_ptr(), weights.data_ptr(), 0 if logits is None else logits.data_ptr(),
-                                self.status.data_ptr(), T, self.n_experts, self.hidden, self.k, self.flags, 0)
-        _check("zipmoe_route", _lib.zipmoe_route(args, _stream_of(index, stream)))
+            weights = _empty(chosen, kinds.fp32[0], tokens.device, stream)
+        ids_at = _dense("ids", ids, chosen, kinds.int32, index)
+        weights_at = _dense("weights", weights, chosen, kinds.fp32, index)
+        logits_at = 0 if logits is None else _dense("logits", logits, (T, self.n_experts), kinds.fp32, index)
+        args = _ROUTE_ARGS.pack(tokens_at, pitch, self.gate_at, self.bias_at, ids_at, weights_at, logits_at, self.status_at, T,
+                                self.n_experts, self.hidden, self.k, self.flags, 0)
+        status = _lib.zipmoe_route(args, kinds.current_stream(index) if stream is None else stream.cuda_stream)
+        if status:
+            raise ZipMoEError("zipmoe_route", status)
         return ids, weights
 
 
@@ -697,18 +712,21 @@ class ResidentExperts:
         import torch
         if len(tensors) % 3 or not tensors:
             raise ValueError("three tensors per expert are wanted")
-        self.index = tensors[0].get_device()
+        self.kinds = _get_kinds()
+        self.index = _device_of("tensor 0", tensors[0])
+        addresses = []
         for i, t in enumerate(tensors):
             if t.numel() != hidden * inter:
                 raise ValueError("tensor %d: %d elements, wanted %d x %d" % (i, t.numel(), hidden, inter))
-            _dense("tensor %d" % i, t, t.shape, _kind("bf16"), self.index)
+            addresses.append(_dense("a weight", t, t.shape, self.kinds.bf16, self.index))
         self.tensors = list(tensors)      # the experts' memory is theirs: keep it while the table points at it
         self.device = tensors[0].device
         self.hidden, self.inter = hidden, inter
-        table, self.struct = zipmoe_resident_experts_plan(self.tensors, len(tensors) // 3, hidden, inter)
+        table, self.struct = zipmoe_resident_experts_plan(addresses, len(tensors) // 3, hidden, inter)
         self.table = torch.from_numpy(table).to(self.device)
         self.struct.table = self.table.data_ptr()
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self.status_at = self.status.data_ptr()
         self._struct_at = ctypes.byref(self.struct)
         self._ws, self._need = {}, {}
 
@@ -726,7 +744,7 @@ class ResidentExperts:
             need = self._need[(T, k)] = zipmoe_expert_ffn_workspace_bytes(min(fits, 256) if T <= 256 else T, k, self.struct)
         held = self._ws.setdefault(handle, [])
         if not held or held[-1].numel() < need:
-            held.append(_empty(need, _kind("e4m3")[1], self.device, stream))
+            held.append(_empty(need, self.kinds.e4m3[1], self.device, stream))
             zipmoe_expert_ffn_workspace_init(held[-1], need, handle)
         return held[-1]
 
@@ -734,19 +752,19 @@ class ResidentExperts:
         """tokens [T, hidden] bf16 (or int16 patterns), topk_ids [T, k] int32, topk_weights [T, k] float32 or None: device
         tensors.  Returns out [T, hidden].  Every stream has a workspace of its own, so calls on different streams may
         overlap."""
-        T, k = topk_ids.shape
-        index, shape = self.index, (T, self.hidden)
-        _dense("tokens", tokens, shape, _kind("bf16"), index)
-        _dense("topk_ids", topk_ids, (T, k), _kind("int32"), index)
-        if topk_weights is not None:
-            _dense("topk_weights", topk_weights, (T, k), _kind("fp32"), index)
+        kinds, index = self.kinds, self.index
+        T, k = chosen = topk_ids.shape
+        shape = (T, self.hidden)
+        tokens_at = _dense("tokens", tokens, shape, kinds.bf16, index)
+        ids_at = _dense("topk_ids", topk_ids, chosen, kinds.int32, index)
+        weights_at = None if topk_weights is None else _dense("topk_weights", topk_weights, chosen, kinds.fp32, index)
         if out is None:
             out = _empty(shape, tokens.dtype, self.device, stream)
-        else:
-            _dense("out", out, shape, _kind("bf16"), index)
-        handle = _stream_of(index, stream)
+        out_at = _dense("out", out, shape, kinds.bf16, index)
+        handle = kinds.current_stream(index) if stream is None else stream.cuda_stream
         ws = self._workspace(T, k, handle, stream)
-        _check("zipmoe_expert_ffn",
-               _lib.zipmoe_expert_ffn(tokens.data_ptr(), T, topk_ids.data_ptr(), None if topk_weights is None else topk_weights.data_ptr(),
-                                      k, self._struct_at, out.data_ptr(), ws.data_ptr(), ws.numel(), self.status.data_ptr(), handle))
+        status = _lib.zipmoe_expert_ffn(tokens_at, T, ids_at, weights_at, k, self._struct_at, out_at, ws.data_ptr(), ws.numel(),
+                                        self.status_at, handle)
+        if status:
+            raise ZipMoEError("zipmoe_expert_ffn", status)
         return out
