@@ -315,7 +315,9 @@ zipmoe_status zipmoe_decode_expert_ffn_noalloc(const uint16_t *tokens, uint32_t 
 /* ---- the rest of the expert sublayer (device) ---------------------------------
  * What surrounds the experts in a decode step: the residual's addition with the norm, the router whose choice
  * decides which experts are needed, and the experts that are already recovered (the planner's pool F).  (The paper
- * takes these from the host framework; its scheduler only sees the router's choice and the time p_n.) */
+ * takes these from the host framework; its scheduler only sees the router's choice and the time p_n.)  The kernels of
+ * the norm and the router are launched with programmatic stream serialization: each is set up while its predecessor on
+ * the stream drains and waits for it before it reads or writes anything, so the stream's order holds as for any kernel. */
 
 #define ZIPMOE_NORM_RESIDUAL_F32 1u /* residual and residual_out are fp32 (else bf16 patterns) */
 

@@ -19,7 +19,7 @@
 #include <type_traits>
 
 #include "zipmoe.h"
-#include "decode_device.cuh"
+#include "tensor_core.cuh"
 
 namespace zipmoe_dev {
 
@@ -266,6 +266,7 @@ __global__ void __launch_bounds__(1024) add_rmsnorm_kernel(const NormArgs a) {
         if (kHasRes) r[i].load(static_cast<const R *>(a.residual) + row * a.residual_pitch + column(i), a.cols - column(i), lane);
       }
   };
+  after_predecessor();
   uint64_t row = blockIdx.x;
   fetch(row);
 #pragma unroll
@@ -350,6 +351,7 @@ __global__ void __launch_bounds__(512, 2) add_rmsnorm_wide_kernel(const NormArgs
       for (int j = 0; j < 4; ++j) h[j] = add2(h[j], rf[j]);
     }
   };
+  after_predecessor();
   uint32_t turn = 0;
   for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x, ++turn) {
     float2 sums = make_float2(0.f, 0.f);
@@ -400,32 +402,41 @@ int norm_sms() {
   return sms[dev];
 }
 
+cudaError_t launch(void (*kernel)(zipmoe_dev::NormArgs), uint32_t blocks, uint32_t warps, const zipmoe_dev::NormArgs &a, cudaStream_t stream) {
+  const cudaLaunchAttribute overlapped = zipmoe_host::overlapped();
+  cudaLaunchConfig_t cfg = {};
+  cfg.stream = stream;
+  cfg.attrs = const_cast<cudaLaunchAttribute *>(&overlapped);
+  cfg.numAttrs = 1;
+  cfg.gridDim = dim3(blocks);
+  cfg.blockDim = dim3(32 * warps);
+  return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
 // A row to a block of as many warps as it has segments of 256 columns, up to 32.  Where that is not
 // enough, or there are many rows for every SM, a warp takes two segments: half the instructions of the reductions.
 template <typename Res, bool kAligned, int kScales>
-void launch_sizes(const zipmoe_dev::NormArgs &a, cudaStream_t stream) {
+cudaError_t launch_sizes(const zipmoe_dev::NormArgs &a, cudaStream_t stream) {
   using namespace zipmoe_dev;
   const uint32_t segments = (a.cols + 255) / 256, sms = norm_sms();
   auto grid = [&](uint32_t warps) { return (uint32_t)std::min<uint64_t>(a.rows, (uint64_t)sms * std::min(32u, 32 / warps)); };
   if (segments > (kAligned ? 64 : 32)) {
     const uint32_t per_warp = (segments + 15) / 16, warps = (segments + per_warp - 1) / per_warp;
-    add_rmsnorm_wide_kernel<Res, kAligned, kScales><<<grid(warps), warps * 32, 0, stream>>>(a);
-    return;
+    return launch(add_rmsnorm_wide_kernel<Res, kAligned, kScales>, grid(warps), warps, a, stream);
   }
   if constexpr (kAligned) {
     if (segments > 32 || (segments >= 2 && a.rows >= 16 * sms)) {
       const uint32_t warps = (segments + 1) / 2;
-      add_rmsnorm_kernel<Res, 2, kAligned, kScales><<<grid(warps), warps * 32, 0, stream>>>(a);
-      return;
+      return launch(add_rmsnorm_kernel<Res, 2, kAligned, kScales>, grid(warps), warps, a, stream);
     }
   }
-  add_rmsnorm_kernel<Res, 1, kAligned, kScales><<<grid(segments), segments * 32, 0, stream>>>(a);
+  return launch(add_rmsnorm_kernel<Res, 1, kAligned, kScales>, grid(segments), segments, a, stream);
 }
 template <typename Res, bool kAligned>
-void launch_norm(const zipmoe_dev::NormArgs &a, cudaStream_t stream) {
-  if (!a.out_q) launch_sizes<Res, kAligned, zipmoe_dev::kNoScales>(a, stream);
-  else if (a.group_log2 == 0) launch_sizes<Res, kAligned, zipmoe_dev::kRowScales>(a, stream);
-  else launch_sizes<Res, kAligned, zipmoe_dev::kGroupScales>(a, stream);
+cudaError_t launch_norm(const zipmoe_dev::NormArgs &a, cudaStream_t stream) {
+  if (!a.out_q) return launch_sizes<Res, kAligned, zipmoe_dev::kNoScales>(a, stream);
+  if (a.group_log2 == 0) return launch_sizes<Res, kAligned, zipmoe_dev::kRowScales>(a, stream);
+  return launch_sizes<Res, kAligned, zipmoe_dev::kGroupScales>(a, stream);
 }
 
 }  // namespace
@@ -467,8 +478,8 @@ extern "C" zipmoe_status zipmoe_add_rmsnorm(const zipmoe_norm_args *n, zipmoe_st
                         (n->residual_out ? n->residual_out_pitch : 0)) % 8 == 0 &&
                        ((bf16_bits | residual_bits) & 15) == 0 && (bits(n->out_q) & 7) == 0;
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
-  if (!n->residual) aligned ? launch_norm<void, true>(a, stream) : launch_norm<void, false>(a, stream);
-  else if (f32) aligned ? launch_norm<float, true>(a, stream) : launch_norm<float, false>(a, stream);
-  else aligned ? launch_norm<uint16_t, true>(a, stream) : launch_norm<uint16_t, false>(a, stream);
-  return cudaGetLastError() == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
+  const cudaError_t rc = !n->residual ? (aligned ? launch_norm<void, true>(a, stream) : launch_norm<void, false>(a, stream))
+                         : f32        ? (aligned ? launch_norm<float, true>(a, stream) : launch_norm<float, false>(a, stream))
+                                      : (aligned ? launch_norm<uint16_t, true>(a, stream) : launch_norm<uint16_t, false>(a, stream));
+  return rc == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
 }

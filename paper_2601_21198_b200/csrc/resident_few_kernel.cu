@@ -100,6 +100,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
   const uint32_t ring = smem_addr(smem), full = smem_addr(bars), empty = full + 8 * kResMaxStages, sums_full = empty + 8 * kResMaxStages, sums_empty = sums_full + 16;
   const WaitLimit lim = {dead, a.status, a.limit_ns};
 
+  after_predecessor();
   // ---- everything that has to come from memory first, at once ----
   const uint32_t magic = __ldcg(&a.sync->magic);
   const int32_t my_id = tid < choices ? __ldg(a.ids + tid) : -1;

@@ -112,6 +112,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
   extern __shared__ uint8_t smem_raw[];
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x, G = gridDim.x;
   const uint32_t W = (a.T + 31) / 32, choices = a.T * a.k, n_rows_max = resident_rows(a.E, choices);
+  after_predecessor();
   // every thread's ids (up to 2048 choices), asked for before anything else
   constexpr uint32_t kIds = (256 * 8 + kResThreads - 1) / kResThreads;
   int32_t my_id[kIds];

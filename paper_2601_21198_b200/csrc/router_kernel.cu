@@ -166,6 +166,7 @@ __global__ void __launch_bounds__(kRouterThreads) router_kernel(const __grid_con
     fence_barrier_init();
   }
   if (warp == 1) tmem_alloc(smem_addr(words), a.tmem_cols);
+  after_predecessor();
   tc_before_sync();
   __syncthreads();
   tc_after_sync();
@@ -306,14 +307,15 @@ zipmoe_status launch_router(int dev, const CUtensorMap &x_map, const CUtensorMap
       return ZIPMOE_ERR_CUDA;
     ready[dev] = true;
   }
-  cudaLaunchAttribute cluster;
-  cluster.id = cudaLaunchAttributeClusterDimension;
-  cluster.val.clusterDim.x = S;
-  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+  cudaLaunchAttribute attrs[2];
+  attrs[0].id = cudaLaunchAttributeClusterDimension;
+  attrs[0].val.clusterDim.x = S;
+  attrs[0].val.clusterDim.y = attrs[0].val.clusterDim.z = 1;
+  attrs[1] = zipmoe_host::overlapped();
   cudaLaunchConfig_t cfg = {};
   cfg.stream = stream;
-  cfg.attrs = &cluster;
-  cfg.numAttrs = 1;
+  cfg.attrs = attrs;
+  cfg.numAttrs = 2;
   cfg.gridDim = dim3((a.T + kRouterRows - 1) / kRouterRows * S);
   cfg.blockDim = dim3(kRouterThreads);
   cfg.dynamicSmemBytes = smem;

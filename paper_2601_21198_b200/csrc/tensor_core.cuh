@@ -62,6 +62,13 @@ __device__ __forceinline__ bool wait_count(const uint32_t *p, uint32_t want, con
   }
 }
 
+// A kernel launched with programmatic stream serialization is set up while its predecessor drains: it waits here before it
+// reads or writes anything, and lets its own successor do the same.  (Launched the ordinary way, the wait returns at once.)
+__device__ __forceinline__ void after_predecessor() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 __device__ __forceinline__ uint64_t policy_evict_first() {
   uint64_t p;
   asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
@@ -166,6 +173,13 @@ __device__ __forceinline__ void arrive(uint32_t bar) {
 }  // namespace zipmoe_dev
 
 namespace zipmoe_host {
+
+inline cudaLaunchAttribute overlapped() {
+  cudaLaunchAttribute a;
+  a.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  a.val.programmaticStreamSerializationAllowed = 1;
+  return a;
+}
 
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
