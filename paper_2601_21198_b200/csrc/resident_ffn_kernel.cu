@@ -8,7 +8,7 @@
 //   * A step is 32 KB of weights: 128 rows x 64 columns of W1 and of W3 (gate/up), or 256 rows x 64 columns of W2
 //     (down), with the tokens' 64 columns.  A job is all steps of one expert and row block.  The steps of all jobs
 //     of a phase form one sequence, cut into equal shares, so every SM streams the same number of bytes whatever the
-//     experts and their sizes.
+//     experts and their sizes (steps of experts with very many tokens weigh more).
 //   * Phases: gate/up of the first half of the active experts, gate/up of the second half, down of the first, down of
 //     the second.  What the third needs was stored before the second began, so nobody waits between them.
 //   * One thread feeds weights into a ring of shared-memory stages (TMA, 128-byte swizzle) and runs ahead as far as the
@@ -64,16 +64,38 @@ struct ResidentArgs {
   uint32_t T, k, E, H, I, even, ring_bytes, tmem_cols, extra_tx;
 };
 
-// How U units are shared out among P blocks: block c takes [c*U/P, (c+1)*U/P), and P <= U.
-__device__ __forceinline__ uint32_t share_first(uint32_t c, uint32_t U, uint32_t P) { return (uint32_t)((uint64_t)c * U / P); }
-__device__ __forceinline__ uint32_t share_of(uint32_t u, uint32_t U, uint32_t P) {
-  return (uint32_t)(((uint64_t)(u + 1) * P - 1) / U);
-}
-
 // Phases 0, 1: gate/up of the two groups of experts; 2, 3: down.  Jobs of KS steps, RB row blocks per active expert.
+// The steps (units) are shared out among P blocks by weight: a unit at position p of W belongs to block floor(p * P / W), so
+// block c begins with the first unit at or behind c * W / P.  A step costs what its bytes take: 32 KB from memory at the
+// SM's share of its bandwidth, or, with many tokens, 32 KB + 128 bytes per token into shared memory at 56 GB/s - the same
+// up to 72 tokens.  Weights are in KB of the latter, and all 1 where no expert has more tokens.
 struct Phase {
   uint32_t KS, RB, U, P, a0;   // a0: the group's first active expert
+  uint64_t W;
+  const uint16_t *weight;      // sums of the active experts' weights before each of them; null: all 1
+  __device__ __forceinline__ uint64_t position(uint32_t u) const {
+    if (!weight) return u;
+    const uint32_t per = KS * RB, ja = u / per, a = a0 + ja;
+    return (uint64_t)per * (weight[a] - weight[a0]) + (uint64_t)(u - ja * per) * (weight[a + 1] - weight[a]);
+  }
+  __device__ __forceinline__ uint32_t owner(uint32_t u) const { return (uint32_t)(position(u) * P / W); }
+  // first unit of block c; P gives the end
+  __device__ __forceinline__ uint32_t begin(uint32_t c) const {
+    const uint64_t x = ((uint64_t)c * W + P - 1) / P;
+    if (!weight) return (uint32_t)x;
+    const uint32_t per = KS * RB;
+    uint32_t lo = 0, hi = U / per;   // the last expert whose units begin at or before x
+    while (hi - lo > 1) {
+      const uint32_t mid = (lo + hi) / 2;
+      if ((uint64_t)per * (weight[a0 + mid] - weight[a0]) <= x) lo = mid;
+      else hi = mid;
+    }
+    const uint32_t w = weight[a0 + lo + 1] - weight[a0 + lo];
+    return lo * per + (uint32_t)((x - (uint64_t)per * (weight[a0 + lo] - weight[a0]) + w - 1) / w);
+  }
 };
+__device__ __forceinline__ uint32_t step_weight(uint32_t tokens) { return max(41u, 32 + (tokens + 7) / 8); }
+constexpr uint32_t kResEvenTokens = 72;   // up to here all steps weigh the same
 struct Piece {
   uint32_t job, a, rb, s0, n;   // steps s0 .. s0 + n of one job: active expert a, row block rb
 };
@@ -89,11 +111,11 @@ __device__ __forceinline__ bool next_piece(const Phase &p, uint32_t &u, uint32_t
   return true;
 }
 
-// shared memory after the ring: [token masks of the experts][active experts][expert -> active][place of every choice
+// shared memory after the ring: [token masks of the experts][active experts][expert -> active][sums of weights][place of every choice
 // among its expert's tokens][tokens of the active experts, padded to 8 each][barriers and words]
 __host__ __device__ inline uint32_t resident_rows(uint32_t E, uint32_t choices) { return choices + 7 * (E < choices ? E : choices); }
 __host__ __device__ inline uint32_t resident_control_bytes(uint32_t E, uint32_t T, uint32_t k) {
-  return pad16(E * ((T + 31) / 32) * 4) + E * (uint32_t)sizeof(Active) + pad16(E * 2) + pad16(T * k * 2) +
+  return pad16(E * ((T + 31) / 32) * 4) + E * (uint32_t)sizeof(Active) + pad16(E * 2) + pad16((E + 1) * 2) + pad16(T * k * 2) +
          pad16(resident_rows(E, T * k) * 2) + (4 * kResMaxStages + 4) * 8 + 32;
 }
 
@@ -130,6 +152,8 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
   ctl += a.E * sizeof(Active);
   uint16_t *active_of = reinterpret_cast<uint16_t *>(ctl);
   ctl += pad16(a.E * 2);
+  uint16_t *weight = reinterpret_cast<uint16_t *>(ctl);
+  ctl += pad16((a.E + 1) * 2);
   uint16_t *place = reinterpret_cast<uint16_t *>(ctl);
   ctl += pad16(choices * 2);
   uint16_t *token = reinterpret_cast<uint16_t *>(ctl);
@@ -169,7 +193,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
   __syncthreads();
   if (warp == 0) {   // experts per * lane .. per * lane + per - 1
     const uint32_t per = (a.E + 31) / 32;
-    uint32_t cnt[8], n_act = 0, sums = 0, most = 0;   // sums: padded rows << 16 | choices
+    uint32_t cnt[8], n_act = 0, sums = 0, most = 0, heavy = 0;   // sums: padded rows << 16 | choices; heavy: weights
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
       const uint32_t e = per * lane + i;
@@ -177,32 +201,38 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
       if (i < per && e < a.E)
         for (uint32_t w = 0; w < W; ++w) cnt[i] += __popc(mask[e * W + w]);
       n_act += cnt[i] ? 1 : 0;
+      heavy += cnt[i] ? step_weight(cnt[i]) : 0;
       sums += ((cnt[i] + 7) & ~7u) << 16 | cnt[i];
       most = max(most, cnt[i]);
     }
     most = __reduce_max_sync(0xFFFFFFFFu, most);
-    uint32_t at = n_act, sum = sums;   // inclusive sums over the lanes
+    uint32_t at = n_act, sum = sums, before = heavy;   // inclusive sums over the lanes
 #pragma unroll
     for (uint32_t d = 1; d < 32; d <<= 1) {
-      const uint32_t p = __shfl_up_sync(0xFFFFFFFFu, at, d), q = __shfl_up_sync(0xFFFFFFFFu, sum, d);
+      const uint32_t p = __shfl_up_sync(0xFFFFFFFFu, at, d), q = __shfl_up_sync(0xFFFFFFFFu, sum, d), r = __shfl_up_sync(0xFFFFFFFFu, before, d);
       if (lane >= d) {
         at += p;
         sum += q;
+        before += r;
       }
     }
     if (lane == 31) {
       words[2] = at;
       words[4] = most;
+      weight[at] = (uint16_t)before;
     }
     at -= n_act;
     sum -= sums;
+    before -= heavy;
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
       if (cnt[i]) {
         const uint32_t e = per * lane + i;
         act[at] = Active{e, cnt[i], sum >> 16, sum & 0xFFFFu};
         active_of[e] = (uint16_t)at;
+        weight[at] = (uint16_t)before;
         ++at;
+        before += step_weight(cnt[i]);
         sum += ((cnt[i] + 7) & ~7u) << 16 | cnt[i];
       }
     }
@@ -230,10 +260,19 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
     ph[p].a0 = p & 1 ? n_first : 0;
     ph[p].U = (p & 1 ? n_active - n_first : n_first) * ph[p].RB * ph[p].KS;
     ph[p].P = min(G, ph[p].U);
+    ph[p].W = ph[p].U;
+    ph[p].weight = nullptr;
+    if (words[4] > kResEvenTokens && ph[p].U > 0) {
+      const uint64_t total = (uint64_t)ph[p].KS * ph[p].RB * (weight[p & 1 ? n_active : n_first] - weight[ph[p].a0]);
+      if (total >= (uint64_t)step_weight(words[4]) * ph[p].P) {   // (every block gets a unit)
+        ph[p].W = total;
+        ph[p].weight = weight;
+      }
+    }
   }
   // this block's share of a phase
-  auto first = [&](const Phase &f) { return cta < f.P ? share_first(cta, f.U, f.P) : 0u; };
-  auto last = [&](const Phase &f) { return cta < f.P ? share_first(cta + 1, f.U, f.P) : 0u; };
+  auto first = [&](const Phase &f) { return cta < f.P ? f.begin(cta) : 0u; };
+  auto last = [&](const Phase &f) { return cta < f.P ? f.begin(cta + 1) : 0u; };
 
   if (warp == 0) {
     // ---- weights ----
@@ -484,7 +523,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
         if (lane == 0) arrive(acc_empty + 8 * b);
         if (whole || p >= 2) continue;
         // a gate/up job that is cut: the block that stores its part last adds all parts, in share order
-        const uint32_t c0 = share_of(q.job * f.KS, f.U, f.P), c1 = share_of(q.job * f.KS + f.KS - 1, f.U, f.P);
+        const uint32_t c0 = f.owner(q.job * f.KS), c1 = f.owner(q.job * f.KS + f.KS - 1);
         __threadfence();
         sync_group<32 * kResReaders>();
         if (rtid == 0) {
@@ -548,7 +587,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
           const uint32_t p = ai < n_first ? 2 : 3;
           const Phase f = p == 2 ? ph[2] : ph[3];
           const uint32_t u0 = ((ai - f.a0) * f.RB + c / 256) * f.KS;
-          const uint32_t c0 = share_of(u0, f.U, f.P), c1 = share_of(u0 + f.KS - 1, f.U, f.P);
+          const uint32_t c0 = f.owner(u0), c1 = f.owner(u0 + f.KS - 1);
           float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
           if (c0 == c1) {
             v = __ldcg(reinterpret_cast<const float4 *>(a.y + (size_t)(act[ai].slot + i) * a.H + c));
