@@ -532,20 +532,39 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
         }
         sync_group<32 * kResReaders>();
         if (words[3]) {
-          for (uint32_t n0 = 4 * half; n0 < ex.n; n0 += 8) {
-            float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
-            for (uint32_t c = c0; c <= c1; ++c) {
-              const float *from = part + ((size_t)c * 2 + (c == c0 ? 1 : 0)) * (2 * a.T * 128) + row;
+          // a warp per token, four rows per lane; four tokens' parts are asked for at a time
+          const uint32_t row4 = 4 * lane, ir4 = q.rb * 128 + row4, h_rows = ph[2].KS * 64;
+          uint8_t *to = a.h + ((size_t)ex.h_row * ph[2].KS + (size_t)(ir4 >> 6) * rows) * 128 + (ir4 & 7) * 2;
+          const uint32_t chunk4 = (ir4 & 63) >> 3;
+          for (uint32_t n0 = warp - 4; n0 < ex.n; n0 += 4 * kResReaders) {
+            float4 g[4], v[4];
 #pragma unroll
-              for (uint32_t n = 0; n < 4; ++n)
-                if (n0 + n < ex.n) {
-                  s0[n] += __ldcg(from + (size_t)(n0 + n) * 128);
-                  s1[n] += __ldcg(from + (size_t)(a.T + n0 + n) * 128);
-                }
+            for (uint32_t n = 0; n < 4; ++n) g[n] = v[n] = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (uint32_t c = c0; c <= c1; ++c) {
+              const float *from = part + ((size_t)c * 2 + (c == c0 ? 1 : 0)) * (2 * a.T * 128) + row4;
+              float4 x[4], y[4];
+#pragma unroll
+              for (uint32_t n = 0; n < 4; ++n) {
+                const uint32_t i = min(n0 + n * kResReaders, ex.n - 1);
+                x[n] = __ldcg(reinterpret_cast<const float4 *>(from + (size_t)i * 128));
+                y[n] = __ldcg(reinterpret_cast<const float4 *>(from + (size_t)(a.T + i) * 128));
+              }
+#pragma unroll
+              for (uint32_t n = 0; n < 4; ++n) {
+                g[n] = make_float4(g[n].x + x[n].x, g[n].y + x[n].y, g[n].z + x[n].z, g[n].w + x[n].w);
+                v[n] = make_float4(v[n].x + y[n].x, v[n].y + y[n].y, v[n].z + y[n].z, v[n].w + y[n].w);
+              }
             }
 #pragma unroll
-            for (uint32_t n = 0; n < 4; ++n)
-              if (n0 + n < ex.n) finish(n0 + n, s0[n], s1[n]);
+            for (uint32_t n = 0; n < 4; ++n) {
+              const uint32_t i = n0 + n * kResReaders;
+              if (i >= ex.n || ir4 >= h_rows) continue;
+              // (inter is a multiple of 8: four rows are all inside it or all behind it)
+              const __nv_bfloat162 lo = __floats2bfloat162_rn(silu_times(g[n].x, v[n].x), silu_times(g[n].y, v[n].y));
+              const __nv_bfloat162 hi = __floats2bfloat162_rn(silu_times(g[n].z, v[n].z), silu_times(g[n].w, v[n].w));
+              const uint2 packed4 = make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
+              *reinterpret_cast<uint2 *>(to + i * 128 + ((chunk4 ^ (i & 7)) << 4)) = ir4 < a.I ? packed4 : make_uint2(0, 0);
+            }
           }
         }
       }
@@ -568,64 +587,73 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
   if (tid == 0 && !*dead) wait_count(&a.sync->y_done, ph[2].P + ph[3].P, lim);
   __syncthreads();
 
-  // ---- out[t] = sum over the token's choices: 4 columns per item, 1 to 8 lanes per item (as many as there are threads for) ----
+  // ---- out[t] = sum over the token's choices.  A turn is 256 columns (a row block of down) of six tokens; 64 threads have
+  // a token's columns, four each.  Which blocks have parts of an expert's job is worked out once per row block. ----
   if (!*dead && prepared) {
-    const uint32_t vecs = a.H / 4, items = a.T * vecs;
-    uint32_t lanes = 8;
-    while (lanes > 1 && (items * lanes > G * kResThreads || lanes >= 2 * a.k)) lanes >>= 1;
-    const uint32_t per_block = kResThreads / lanes, l = tid % lanes;
-    for (uint32_t it0 = cta * per_block; it0 < items; it0 += G * per_block) {
-      const uint32_t it = it0 + tid / lanes;
+    uint32_t *owners = reinterpret_cast<uint32_t *>(ring);   // [active experts]: first and last block (the ring is done with)
+    constexpr uint32_t kTokens = kResThreads / 64;
+    const uint32_t RB = ph[2].RB, groups = (a.T + kTokens - 1) / kTokens, turns = RB * groups;
+    uint32_t rb_now = 0xFFFFFFFFu;
+    for (uint32_t turn = cta * turns / G; turn < (cta + 1) * turns / G; ++turn) {
+      const uint32_t rb = turn / groups, t = (turn - rb * groups) * kTokens + (tid >> 6), v4 = tid & 63, c = rb * 256 + v4 * 4;
+      if (rb != rb_now) {
+        __syncthreads();
+        for (uint32_t ai = tid; ai < n_active; ai += kResThreads) {
+          const Phase f = ai < n_first ? ph[2] : ph[3];
+          const uint32_t u0 = ((ai - f.a0) * RB + rb) * f.KS;
+          owners[ai] = f.owner(u0) | f.owner(u0 + f.KS - 1) << 16;
+        }
+        __syncthreads();
+        rb_now = rb;
+      }
+      if (t >= a.T || c >= a.H) continue;
+      // every choice's sum, or the first part of it, is asked for before the first is used
+      const uint32_t in_part = ((v4 >> 5) * a.T) * 128 + (v4 & 31) * 4;
+      float4 y[8];
+      uint32_t more[8];
+#pragma unroll
+      for (uint32_t j = 0; j < 8; ++j) {
+        y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        more[j] = 0;
+        if (j >= a.k) continue;
+        const int32_t e = __ldg(a.ids + t * a.k + j);
+        if (e < 0 || e >= (int32_t)a.E) continue;
+        const uint32_t ai = active_of[e], i = place[t * a.k + j], c0 = owners[ai] & 0xFFFFu, c1 = owners[ai] >> 16;
+        const float *from = a.y + (size_t)(act[ai].slot + i) * a.H + c;
+        if (c0 != c1) {
+          from = a.part + (ai < n_first ? 2 : 3) * a.part_phase + ((size_t)c0 * 2 + 1) * (2 * a.T * 128) + in_part + (size_t)i * 128;
+          more[j] = c1 - c0;
+        }
+        y[j] = __ldcg(reinterpret_cast<const float4 *>(from));
+      }
       float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-      const uint32_t t = it / vecs, c = (it - t * vecs) * 4;
-      if (it < items) {
-#pragma unroll 2
-        for (uint32_t j = l; j < a.k; j += lanes) {
-          const int32_t e = __ldg(a.ids + t * a.k + j);
-          if (e < 0 || e >= (int32_t)a.E) continue;
-          const uint32_t ai = active_of[e], i = place[t * a.k + j];
-          const uint32_t p = ai < n_first ? 2 : 3;
-          const Phase f = p == 2 ? ph[2] : ph[3];
-          const uint32_t u0 = ((ai - f.a0) * f.RB + c / 256) * f.KS;
-          const uint32_t c0 = f.owner(u0), c1 = f.owner(u0 + f.KS - 1);
-          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (c0 == c1) {
-            v = __ldcg(reinterpret_cast<const float4 *>(a.y + (size_t)(act[ai].slot + i) * a.H + c));
-          } else {
-            const float *from = a.part + p * a.part_phase + (size_t)(((c >> 7) & 1) * a.T + i) * 128 + (c & 127);
-            for (uint32_t b = c0; b <= c1; b += 4) {
-              float4 r[4];
 #pragma unroll
-              for (uint32_t n = 0; n < 4; ++n)
-                r[n] = b + n <= c1 ? __ldcg(reinterpret_cast<const float4 *>(from + ((size_t)(b + n) * 2 + (b + n == c0 ? 1 : 0)) * (2 * a.T * 128)))
-                                   : make_float4(0.f, 0.f, 0.f, 0.f);
+      for (uint32_t j = 0; j < 8; ++j) {
+        if (j >= a.k) continue;
+        if (more[j]) {
+          const uint32_t ai = active_of[__ldg(a.ids + t * a.k + j)], i = place[t * a.k + j], c0 = owners[ai] & 0xFFFFu;
+          const float *from = a.part + (ai < n_first ? 2 : 3) * a.part_phase + (size_t)c0 * 2 * (2 * a.T * 128) + in_part + (size_t)i * 128;
+          for (uint32_t b = 1; b <= more[j]; b += 4) {
+            float4 r[4];
 #pragma unroll
-              for (uint32_t n = 0; n < 4; ++n) {
-                v.x += r[n].x;
-                v.y += r[n].y;
-                v.z += r[n].z;
-                v.w += r[n].w;
-              }
-            }
+            for (uint32_t n = 0; n < 4; ++n)
+              r[n] = b + n <= more[j] ? __ldcg(reinterpret_cast<const float4 *>(from + (size_t)(b + n) * 2 * (2 * a.T * 128))) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (uint32_t n = 0; n < 4; ++n) y[j] = make_float4(y[j].x + r[n].x, y[j].y + r[n].y, y[j].z + r[n].z, y[j].w + r[n].w);
           }
-          const float wt = a.weights ? __ldg(a.weights + t * a.k + j) : 1.0f;
-          s.x += wt * v.x;
-          s.y += wt * v.y;
-          s.z += wt * v.z;
-          s.w += wt * v.w;
+        }
+        const float wt = a.weights ? __ldg(a.weights + t * a.k + j) : 1.0f;
+        // (a choice that is no expert adds nothing, whatever its weight is)
+        if (__ldg(a.ids + t * a.k + j) >= 0 && __ldg(a.ids + t * a.k + j) < (int32_t)a.E) {
+          s.x += wt * y[j].x;
+          s.y += wt * y[j].y;
+          s.z += wt * y[j].z;
+          s.w += wt * y[j].w;
         }
       }
-      for (uint32_t d = lanes >> 1; d > 0; d >>= 1) {
-        s.x += __shfl_xor_sync(0xFFFFFFFFu, s.x, d);
-        s.y += __shfl_xor_sync(0xFFFFFFFFu, s.y, d);
-        s.z += __shfl_xor_sync(0xFFFFFFFFu, s.z, d);
-        s.w += __shfl_xor_sync(0xFFFFFFFFu, s.w, d);
-      }
-      if (it < items && l == 0) {
-        const __nv_bfloat162 lo = __floats2bfloat162_rn(s.x, s.y), hi = __floats2bfloat162_rn(s.z, s.w);
-        *reinterpret_cast<uint2 *>(a.out + (size_t)t * a.H + c) =
-            make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
-      }
+      const __nv_bfloat162 lo = __floats2bfloat162_rn(s.x, s.y), hi = __floats2bfloat162_rn(s.z, s.w);
+      *reinterpret_cast<uint2 *>(a.out + (size_t)t * a.H + c) =
+          make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
     }
   }
   __syncthreads();
