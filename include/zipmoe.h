@@ -389,9 +389,9 @@ typedef struct {
   uint32_t n_experts, hidden, inter;  /* hidden, inter: multiples of 8                                              */
   uint32_t even;                      /* 1: every kind of tensor lies at equal distances from expert to expert      */
   const void *table;                  /* device [3 * n_experts * ZIPMOE_RESIDENT_ENTRY_BYTES], 64-byte aligned      */
-  uint8_t maps[6 * 128];              /* opaque: the tensors of evenly spaced experts                               */
+  uint8_t maps[9 * 128];              /* opaque: the tensors of evenly spaced experts                               */
 } zipmoe_resident_experts;
-#define ZIPMOE_RESIDENT_ENTRY_BYTES 256u
+#define ZIPMOE_RESIDENT_ENTRY_BYTES 384u
 
 /* Describes recovered experts to zipmoe_expert_ffn: one opaque entry per tensor, which the caller copies to the
  * device as it is, and the struct that the call takes.  Once per layer, and again when an expert's tensors move.

@@ -342,12 +342,12 @@ def zipmoe_decode_expert_ffn_noalloc(tokens, T, topk_ids, topk_weights, k, exper
 # ---- the rest of the expert sublayer: norm, router, experts that are already recovered --------------------
 NORM_RESIDUAL_F32 = 1       # zipmoe_add_rmsnorm flag: residual and residual_out are fp32
 ROUTE_SOFTMAX_ALL = 1       # zipmoe_route flag: weights are not renormalised over the chosen experts
-RESIDENT_ENTRY_BYTES = 256
+RESIDENT_ENTRY_BYTES = 384
 
 
 class ResidentExpertsStruct(ctypes.Structure):
     """zipmoe_resident_experts."""
-    _fields_ = [("n_experts", _u32), ("hidden", _u32), ("inter", _u32), ("even", _u32), ("table", _vp), ("maps", ctypes.c_uint8 * 768)]
+    _fields_ = [("n_experts", _u32), ("hidden", _u32), ("inter", _u32), ("even", _u32), ("table", _vp), ("maps", ctypes.c_uint8 * 1152)]
 
 
 # zipmoe_norm_args and zipmoe_route_args, packed in one go (a call with one pointer costs a sixth of one with 17 arguments)

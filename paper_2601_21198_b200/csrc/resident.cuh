@@ -10,7 +10,9 @@ namespace zipmoe_dev {
 constexpr uint32_t kResMaxGrid = 256;
 constexpr uint32_t kResMaxStages = 8;
 constexpr uint32_t kResMagic = 0x5A464632u;                 // marks a workspace that zipmoe_expert_ffn_workspace_init prepared
-constexpr uint32_t kSlicedMap = 128;   // an entry of the table: the map of 128-row boxes, then that of a block's slices of rows
+// An entry of the table: the map of 128-row boxes, that of a block's slices of rows, that of the columns behind a row's last
+// whole 64.
+constexpr uint32_t kSlicedMap = 128, kRestMap = 256;
 
 // Maps of all experts' W1, W3 and W2 at once, where they lie at equal distances.
 struct EvenMaps {
@@ -83,7 +85,7 @@ struct ResidentCall {
   const int32_t *ids;
   const float *weights;
   const uint8_t *table;
-  const uint8_t *even_maps;   // host: the three sliced maps, or null
+  const uint8_t *even_maps;   // host: the three sliced maps and the three of the rests, or null
   uint16_t *out;
   zipmoe_dev::ResidentSync *sync;
   uint8_t *h;

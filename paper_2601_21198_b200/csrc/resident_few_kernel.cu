@@ -7,7 +7,8 @@
 // the block that owns the output rows, and blocks wait for one another once, for h.
 //   * A chunk is 512 columns of up to 16 rows of W1 and of W3, or of up to 32 rows of W2.  One thread brings it into a ring
 //     of stages: a tensor map that sees the matrix as [columns / 64][rows][64] delivers a box of 8 x rows x 64 in one copy,
-//     each 64 columns a tile in the 128-byte swizzle.  (One bulk copy per row and 1 KB was tried: the copy engine takes
+//     each 64 columns a tile in the 128-byte swizzle.  What is left of a row behind its last whole 64 columns is a chunk of
+//     its own, through an ordinary map.  (One bulk copy per row and 1 KB was tried: the copy engine takes
 //     38 ns for each, 4 TB/s.  Loads into registers were tried: 12 warps with 16 loads in flight each, 4.8 TB/s.)
 //     It runs ahead across experts, and asks the first chunks of W2 into the second-level cache before h is there.
 //   * Another warp adds the same columns of the expert's tokens (x, then h).
@@ -76,7 +77,8 @@ __device__ __forceinline__ uint32_t nth_bit(uint32_t mask, uint32_t n) {   // pl
   return __ffs(mask) - 1;
 }
 
-__global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __grid_constant__ EvenMaps even, const FewArgs a) {
+__global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __grid_constant__ EvenMaps even, const __grid_constant__ EvenMaps rests,
+                                                                      const FewArgs a) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x, G = gridDim.x, choices = a.T * a.k;
   const uint32_t stage_bytes = a.w_bytes + kFewTokenBytes;
@@ -107,6 +109,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
   const float my_wt = tid < choices && a.weights ? __ldg(a.weights + tid) : 1.0f;
   if (!a.even) prefetch_table(a.table, a.E, cta * kFewThreads + tid, G * kFewThreads);
   else if (tid >= 64 && tid < 67) prefetch_map(&even.w[tid - 64]);
+  else if (tid >= 96 && tid < 99 && ((tid < 98 ? a.H : a.I) & 63) != 0) prefetch_map(&rests.w[tid - 96]);
   for (uint32_t i = tid; i < a.E; i += kFewThreads) mask[i] = 0;
   if (tid == 0) {
     for (uint32_t s = 0; s < a.stages; ++s) {
@@ -166,16 +169,20 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
         const uint32_t down = i >= 2 * n_active, ai = down ? i - 2 * n_active : i >> 1;
         const uint8_t *m = sliced_map(a.table, act[ai].e, down ? 2 : i & 1);
         acquire_map(m);
+        if (((down ? a.I : a.H) & 63) != 0) acquire_map(m + (kRestMap - kSlicedMap));
         if (i < 2) prefetch_map(m);
       }
     __syncwarp();
     if (lane == 0) {
       const uint64_t policy = policy_evict_first();
       auto map_of = [&](uint32_t e, uint32_t j) -> const void * { return a.even ? static_cast<const void *>(&even.w[j]) : sliced_map(a.table, e, j); };
+      auto rest_of = [&](uint32_t e, uint32_t j) -> const void * {
+        return a.even ? static_cast<const void *>(&rests.w[j]) : sliced_map(a.table, e, j) + (kRestMap - kSlicedMap);
+      };
       RingAt at;
       bool ok = true;
       for (uint32_t p = 0; p < 2 && ok; ++p) {
-        const uint32_t K = p == 0 ? a.H : a.I, per_set = p == 0 ? a.S1 : a.S2, jobs = n_active * sets[p];
+        const uint32_t K = p == 0 ? a.H : a.I, whole = K & ~63u, per_set = p == 0 ? a.S1 : a.S2, jobs = n_active * sets[p];
         for (uint32_t j = 0; j < jobs && ok; ++j) {
           const uint32_t ai = p == 0 ? j / sets[0] : j % n_active, s = p == 0 ? j - ai * sets[0] : j / n_active, e = act[ai].e;
           const int32_t r0 = (int32_t)(row0[p] + s * per_set), z = a.even ? (int32_t)e : 0;
@@ -189,7 +196,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
               prefetch_map(map_of(next, 2));
             }
           }
-          for (uint32_t c = 0; c < K; c += kFewCols) {
+          for (uint32_t c = 0; c < whole; c += kFewCols) {
             if (at.round > 0 && !wait_bar(empty + 8 * at.st, (at.round - 1) & 1, lim)) {
               ok = false;
               break;
@@ -200,12 +207,23 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
             if (p == 0) tma_load_4d(dst + per_set * kFewRowBytes, m1, 0, r0, (int32_t)(c / 64), z, bar, policy);
             at.next(a.stages);
           }
+          if (whole < K && ok) {
+            if (at.round > 0 && !wait_bar(empty + 8 * at.st, (at.round - 1) & 1, lim)) {
+              ok = false;
+              break;
+            }
+            const uint32_t dst = ring + at.st * stage_bytes, bar = full + 8 * at.st;
+            mbar_expect_tx(bar, (p == 0 ? 2 : 1) * per_set * 128 + a.extra_tx);
+            tma_load_3d(dst, rest_of(e, p == 0 ? 0 : 2), (int32_t)whole, r0, z, bar, policy);
+            if (p == 0) tma_load_3d(dst + per_set * kFewRowBytes, rest_of(e, 1), (int32_t)whole, r0, z, bar, policy);
+            at.next(a.stages);
+          }
         }
         if (p == 0 && ok) {   // the beginning of W2, in the order in which it will be wanted
           uint32_t left = kFewAheadBytes / (a.S2 * kFewRowBytes);
           for (uint32_t j = 0; j < n_active * sets[1] && left > 0; ++j) {
             const uint32_t e = act[j % n_active].e;
-            for (uint32_t c = 0; c < a.I && left > 0; c += kFewCols, --left)
+            for (uint32_t c = 0; c < (a.I & ~63u) && left > 0; c += kFewCols, --left)
               tma_prefetch_4d(map_of(e, 2), 0, (int32_t)(row0[1] + j / n_active * a.S2), (int32_t)(c / 64), a.even ? (int32_t)e : 0);
           }
         }
@@ -217,7 +235,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
     RingAt at;
     bool ok = true;
     for (uint32_t p = 0; p < 2 && ok; ++p) {
-      const uint32_t K = p == 0 ? a.H : a.I, jobs = n_active * sets[p];
+      const uint32_t K = p == 0 ? a.H : a.I, whole = K & ~63u, jobs = n_active * sets[p];
       if (p == 1 && jobs > 0) {
         ok = __all_sync(0xFFFFFFFFu, wait_count(&a.sync->h_done[0], h_blocks, lim));
         fence_async_all();       // what other blocks stored is now read by the copy engine
@@ -228,10 +246,11 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
         const uint16_t *src = a.tokens;
         if (lane < ex.n)
           src = p == 0 ? a.tokens + (size_t)nth_bit(mask[ex.e], lane) * K : a.h + (size_t)(ex.slot + lane) * K;
-        for (uint32_t c = 0; c < K; c += kFewCols) {
+        for (uint32_t c = 0, cols; c < K; c += cols) {
+          cols = c < whole ? min(kFewCols, whole - c) : K - c;
           ok = __all_sync(0xFFFFFFFFu, at.round == 0 || wait_bar(empty + 8 * at.st, (at.round - 1) & 1, lim));
           if (!ok) break;
-          const uint32_t bytes = min(kFewCols, K - c) * 2, bar = full + 8 * at.st;
+          const uint32_t bytes = cols * 2, bar = full + 8 * at.st;
           if (lane == 0) mbar_expect_tx(bar, ex.n * bytes);
           __syncwarp();
           if (lane < ex.n) bulk_load(ring + at.st * stage_bytes + a.w_bytes + lane * kFewPitch, src + c, bytes, bar, policy);
@@ -248,14 +267,14 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
     uint32_t job = 0;
     bool ok = true;
     for (uint32_t p = 0; p < 2 && ok; ++p) {
-      const uint32_t K = p == 0 ? a.H : a.I, per_set = p == 0 ? a.S1 : a.S2, jobs = n_active * sets[p];
+      const uint32_t K = p == 0 ? a.H : a.I, whole = K & ~63u, per_set = p == 0 ? a.S1 : a.S2, jobs = n_active * sets[p];
       const bool two = p == 0 || per_set > 16;
       for (uint32_t j = 0; j < jobs && ok; ++j, ++job) {
         float d[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-        for (uint32_t c = 0; c < K; c += kFewCols) {
+        for (uint32_t c = 0; c < whole; c += kFewCols) {
           ok = __all_sync(0xFFFFFFFFu, wait_bar(full + 8 * at.st, at.round & 1, lim));
           if (!ok) break;
-          const uint32_t left = min(kFewCols, K - c), base = ring + at.st * stage_bytes;
+          const uint32_t left = min(kFewCols, whole - c), base = ring + at.st * stage_bytes;
 #pragma unroll 4
           for (uint32_t q = cw * 16; q < left; q += 128) {
             // 64 columns are per_set lines of 128 bytes; the second 16 rows are W3's box, or the lines after the first
@@ -265,6 +284,24 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
             if (p == 0) load_a(base + per_set * kFewRowBytes + line * 128 + ((chunk ^ (line & 7)) << 4), w1);
             else if (two) load_a(base + (line + 16) * 128 + ((chunk ^ (line & 7)) << 4), w1);
             const uint32_t b0 = load_b(base + b_at + q * 2), b1 = load_b(base + b_at + q * 2 + 16);
+            mma_16816(d[0], w0, b0, b1);
+            if (two) mma_16816(d[1], w1, b0, b1);
+          }
+          __syncwarp();
+          if (lane == 0) arrive(empty + 8 * at.st);
+          at.next(a.stages);
+        }
+        if (whole < K && ok) {   // up to 64 columns more: a step for each of the first warps
+          ok = __all_sync(0xFFFFFFFFu, wait_bar(full + 8 * at.st, at.round & 1, lim));
+          if (!ok) break;
+          const uint32_t left = K - whole, base = ring + at.st * stage_bytes, q = cw * 16;
+          if (q < left) {
+            const uint32_t place = a_row * 128 + (((q >> 3) + a_half) ^ (a_row & 7)) * 16;
+            uint32_t w0[4], w1[4];
+            load_a(base + place, w0);
+            if (two) load_a(base + place + (p == 0 ? per_set * kFewRowBytes : 16 * 128), w1);
+            // (the last 8 of 16 columns may lie behind the row: weights are zero there, tokens have to be)
+            const uint32_t b0 = load_b(base + b_at + q * 2), behind = load_b(base + b_at + q * 2 + 16), b1 = q + 8 < left ? behind : 0u;
             mma_16816(d[0], w0, b0, b1);
             if (two) mma_16816(d[1], w1, b0, b1);
           }
@@ -388,8 +425,11 @@ zipmoe_status launch_resident_few(const ResidentCall &c, cudaStream_t stream) {
   a.weights = c.weights;
   a.table = c.table;
   a.even = c.even_maps != nullptr;
-  EvenMaps even = {};
-  if (a.even) std::memcpy(&even, c.even_maps, sizeof(even));
+  EvenMaps even = {}, rests = {};
+  if (a.even) {
+    std::memcpy(&even, c.even_maps, sizeof(even));
+    std::memcpy(&rests, c.even_maps + sizeof(even), sizeof(rests));
+  }
   a.out = c.out;
   a.sync = c.sync;
   a.h = reinterpret_cast<uint16_t *>(c.h);
@@ -421,7 +461,7 @@ zipmoe_status launch_resident_few(const ResidentCall &c, cudaStream_t stream) {
   cfg.gridDim = dim3(c.grid);
   cfg.blockDim = dim3(kFewThreads);
   cfg.dynamicSmemBytes = control + a.stages * stage;
-  return cudaLaunchKernelEx(&cfg, resident_few_kernel, even, a) == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, resident_few_kernel, even, rests, a) == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
 }
 
 }  // namespace zipmoe_host

@@ -71,27 +71,39 @@ struct ResidentArgs {
 // up to 72 tokens.  Weights are in KB of the latter, and all 1 where no expert has more tokens.
 struct Phase {
   uint32_t KS, RB, U, P, a0;   // a0: the group's first active expert
-  uint64_t W;
+  uint32_t W, each, left;      // each, left: W / P, W % P   (W < 2^31: at most 2^25 units of weight 64)
   const uint16_t *weight;      // sums of the active experts' weights before each of them; null: all 1
-  __device__ __forceinline__ uint64_t position(uint32_t u) const {
+  __device__ __forceinline__ void share(uint32_t total) {
+    W = total;
+    each = P ? W / P : 0;
+    left = P ? W - each * P : 0;
+  }
+  __device__ __forceinline__ uint32_t position(uint32_t u) const {
     if (!weight) return u;
     const uint32_t per = KS * RB, ja = u / per, a = a0 + ja;
-    return (uint64_t)per * (weight[a] - weight[a0]) + (uint64_t)(u - ja * per) * (weight[a + 1] - weight[a]);
+    return per * (weight[a] - weight[a0]) + (u - ja * per) * (weight[a + 1] - weight[a]);
   }
-  __device__ __forceinline__ uint32_t owner(uint32_t u) const { return (uint32_t)(position(u) * P / W); }
+  __device__ __forceinline__ uint32_t begin_position(uint32_t c) const { return c * each + (c * left + P - 1) / P; }   // ceil(c * W / P)
+  __device__ __forceinline__ uint32_t owner(uint32_t u) const {   // the last block that begins at or before the unit
+    const uint32_t pos = position(u);
+    uint32_t c = min(P - 1, (uint32_t)((float)pos * ((float)P / (float)W)));
+    while (begin_position(c) > pos) --c;
+    while (c + 1 < P && begin_position(c + 1) <= pos) ++c;
+    return c;
+  }
   // first unit of block c; P gives the end
   __device__ __forceinline__ uint32_t begin(uint32_t c) const {
-    const uint64_t x = ((uint64_t)c * W + P - 1) / P;
-    if (!weight) return (uint32_t)x;
+    const uint32_t x = begin_position(c);
+    if (!weight) return x;
     const uint32_t per = KS * RB;
     uint32_t lo = 0, hi = U / per;   // the last expert whose units begin at or before x
     while (hi - lo > 1) {
       const uint32_t mid = (lo + hi) / 2;
-      if ((uint64_t)per * (weight[a0 + mid] - weight[a0]) <= x) lo = mid;
+      if (per * (weight[a0 + mid] - weight[a0]) <= x) lo = mid;
       else hi = mid;
     }
     const uint32_t w = weight[a0 + lo + 1] - weight[a0 + lo];
-    return lo * per + (uint32_t)((x - (uint64_t)per * (weight[a0 + lo] - weight[a0]) + w - 1) / w);
+    return lo * per + (x - per * (weight[a0 + lo] - weight[a0]) + w - 1) / w;
   }
 };
 __device__ __forceinline__ uint32_t step_weight(uint32_t tokens) { return max(41u, 32 + (tokens + 7) / 8); }
@@ -260,13 +272,13 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
     ph[p].a0 = p & 1 ? n_first : 0;
     ph[p].U = (p & 1 ? n_active - n_first : n_first) * ph[p].RB * ph[p].KS;
     ph[p].P = min(G, ph[p].U);
-    ph[p].W = ph[p].U;
     ph[p].weight = nullptr;
+    ph[p].share(ph[p].U);
     if (words[4] > kResEvenTokens && ph[p].U > 0) {
-      const uint64_t total = (uint64_t)ph[p].KS * ph[p].RB * (weight[p & 1 ? n_active : n_first] - weight[ph[p].a0]);
-      if (total >= (uint64_t)step_weight(words[4]) * ph[p].P) {   // (every block gets a unit)
-        ph[p].W = total;
+      const uint32_t total = ph[p].KS * ph[p].RB * (weight[p & 1 ? n_active : n_first] - weight[ph[p].a0]);
+      if (total >= step_weight(words[4]) * ph[p].P) {   // (every block gets a unit)
         ph[p].weight = weight;
+        ph[p].share(total);
       }
     }
   }
@@ -532,7 +544,26 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
         }
         sync_group<32 * kResReaders>();
         if (words[3]) {
-          // a warp per token, four rows per lane; four tokens' parts are asked for at a time
+          if (ex.n <= 16) {
+            for (uint32_t n0 = 4 * half; n0 < ex.n; n0 += 8) {
+              float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
+              for (uint32_t c = c0; c <= c1; ++c) {
+                const float *from = part + ((size_t)c * 2 + (c == c0 ? 1 : 0)) * (2 * a.T * 128) + row;
+#pragma unroll
+                for (uint32_t n = 0; n < 4; ++n)
+                  if (n0 + n < ex.n) {
+                    s0[n] += __ldcg(from + (size_t)(n0 + n) * 128);
+                    s1[n] += __ldcg(from + (size_t)(a.T + n0 + n) * 128);
+                  }
+              }
+#pragma unroll
+              for (uint32_t n = 0; n < 4; ++n)
+                if (n0 + n < ex.n) finish(n0 + n, s0[n], s1[n]);
+            }
+            continue;
+          }
+          // many tokens: a warp per token, four rows per lane; four tokens' parts are asked for at a time (10 us less for 231
+          // tokens of one expert, 3 us more for one)
           const uint32_t row4 = 4 * lane, ir4 = q.rb * 128 + row4, h_rows = ph[2].KS * 64;
           uint8_t *to = a.h + ((size_t)ex.h_row * ph[2].KS + (size_t)(ir4 >> 6) * rows) * 128 + (ir4 & 7) * 2;
           const uint32_t chunk4 = (ir4 & 63) >> 3;
@@ -587,9 +618,70 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
   if (tid == 0 && !*dead) wait_count(&a.sync->y_done, ph[2].P + ph[3].P, lim);
   __syncthreads();
 
-  // ---- out[t] = sum over the token's choices.  A turn is 256 columns (a row block of down) of six tokens; 64 threads have
-  // a token's columns, four each.  Which blocks have parts of an expert's job is worked out once per row block. ----
-  if (!*dead && prepared) {
+  // ---- out[t] = sum over the token's choices ----
+  const uint32_t vecs = a.H / 4, items = a.T * vecs;   // four columns of a token each
+  if (!*dead && prepared && items * 8 <= 2 * G * kResThreads) {
+    // few outputs: up to 8 lanes share the choices of an item (64 threads per token and all its choices in each: 5 to 10 us
+    // longer for one token)
+    uint32_t lanes = 8;
+    while (lanes > 1 && (items * lanes > G * kResThreads || lanes >= 2 * a.k)) lanes >>= 1;
+    const uint32_t per_block = kResThreads / lanes, l = tid % lanes;
+    for (uint32_t it0 = cta * per_block; it0 < items; it0 += G * per_block) {
+      const uint32_t it = it0 + tid / lanes;
+      float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+      const uint32_t t = it / vecs, c = (it - t * vecs) * 4;
+      if (it < items) {
+#pragma unroll 2
+        for (uint32_t j = l; j < a.k; j += lanes) {
+          const int32_t e = __ldg(a.ids + t * a.k + j);
+          if (e < 0 || e >= (int32_t)a.E) continue;
+          const uint32_t ai = active_of[e], i = place[t * a.k + j];
+          const uint32_t p = ai < n_first ? 2 : 3;
+          const Phase f = p == 2 ? ph[2] : ph[3];
+          const uint32_t u0 = ((ai - f.a0) * f.RB + c / 256) * f.KS;
+          const uint32_t c0 = f.owner(u0), c1 = f.owner(u0 + f.KS - 1);
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (c0 == c1) {
+            v = __ldcg(reinterpret_cast<const float4 *>(a.y + (size_t)(act[ai].slot + i) * a.H + c));
+          } else {
+            const float *from = a.part + p * a.part_phase + (size_t)(((c >> 7) & 1) * a.T + i) * 128 + (c & 127);
+            for (uint32_t b = c0; b <= c1; b += 4) {
+              float4 r[4];
+#pragma unroll
+              for (uint32_t n = 0; n < 4; ++n)
+                r[n] = b + n <= c1 ? __ldcg(reinterpret_cast<const float4 *>(from + ((size_t)(b + n) * 2 + (b + n == c0 ? 1 : 0)) * (2 * a.T * 128)))
+                                   : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+              for (uint32_t n = 0; n < 4; ++n) {
+                v.x += r[n].x;
+                v.y += r[n].y;
+                v.z += r[n].z;
+                v.w += r[n].w;
+              }
+            }
+          }
+          const float wt = a.weights ? __ldg(a.weights + t * a.k + j) : 1.0f;
+          s.x += wt * v.x;
+          s.y += wt * v.y;
+          s.z += wt * v.z;
+          s.w += wt * v.w;
+        }
+      }
+      for (uint32_t d = lanes >> 1; d > 0; d >>= 1) {
+        s.x += __shfl_xor_sync(0xFFFFFFFFu, s.x, d);
+        s.y += __shfl_xor_sync(0xFFFFFFFFu, s.y, d);
+        s.z += __shfl_xor_sync(0xFFFFFFFFu, s.z, d);
+        s.w += __shfl_xor_sync(0xFFFFFFFFu, s.w, d);
+      }
+      if (it < items && l == 0) {
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(s.x, s.y), hi = __floats2bfloat162_rn(s.z, s.w);
+        *reinterpret_cast<uint2 *>(a.out + (size_t)t * a.H + c) =
+            make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
+      }
+    }
+  } else if (!*dead && prepared) {
+    // many: a turn is 256 columns (a row block of down) of six tokens; 64 threads have a token's columns, four each.  Which
+    // blocks have parts of an expert's job is worked out once per row block.  (As above: 9 us longer for 256 tokens.)
     uint32_t *owners = reinterpret_cast<uint32_t *>(ring);   // [active experts]: first and last block (the ring is done with)
     constexpr uint32_t kTokens = kResThreads / 64;
     const uint32_t RB = ph[2].RB, groups = (a.T + kTokens - 1) / kTokens, turns = RB * groups;
@@ -687,12 +779,10 @@ bool dims_ok(uint32_t E, uint32_t H, uint32_t I) {
          I <= kResidentMaxDim;
 }
 
-// the sizes that a block's slices of rows can be described for
-bool sliced_sizes(uint32_t H, uint32_t I) { return H % 64 == 0 && I % 64 == 0; }
-
-// Whether a block's whole rows are the faster way for few tokens.  They save about 9 us of a call (one token, 6 experts of
-// 2048 x 1408: 27 us against 35 to 40), and stream as fast (8 tokens, 7 experts of 4096 x 14336: 347 against 369 us) as
-// long as a block has a dozen rows of W2: with 7 (16 experts of 1024 x 4096, 400 MB) 90 against 76 us.
+// Whether a block's whole rows are the faster way for few tokens.  They save 10 us of a call (one token, 6 experts of
+// 2048 x 1408: 28 us against 42), and stream as fast (8 tokens, 7 experts of 4096 x 14336: 347 against 369 us) as long as a
+// block has a dozen rows of W2: with 7 (16 experts of 1024 x 4096, 400 MB) 90 against 76 us.  (A second column of eight
+// tokens was built and taken out: 16 tokens, 16 experts of 1096 x 904: 60 us against 44.)
 bool whole_rows_pay(uint32_t choices, uint32_t E, uint32_t H, uint32_t I, uint32_t grid) {
   return H >= 11 * grid || (uint64_t)std::min(choices, E) * 6 * H * I < (100u << 20);
 }
@@ -750,12 +840,13 @@ zipmoe_status resident_plan(uint32_t T, uint32_t k, const zipmoe_resident_expert
 
 extern "C" zipmoe_status zipmoe_resident_experts_plan(const uint16_t *const *tensors, uint32_t n_experts, uint32_t hidden,
                                                       uint32_t inter, void *table, zipmoe_resident_experts *experts) {
+  using zipmoe_dev::kRestMap;
   using zipmoe_dev::kSlicedMap;
   if (!dims_ok(n_experts, hidden, inter)) return ZIPMOE_ERR_UNSUPPORTED;
   if (!tensors || !table || !experts) return ZIPMOE_ERR_INVALID_ARG;
   for (uint32_t i = 0; i < 3 * n_experts; ++i)
     if (!tensors[i] || (reinterpret_cast<uintptr_t>(tensors[i]) & 15)) return ZIPMOE_ERR_INVALID_ARG;
-  static_assert(sizeof(CUtensorMap) == kSlicedMap && 2 * sizeof(CUtensorMap) == ZIPMOE_RESIDENT_ENTRY_BYTES, "an entry is two tensor maps");
+  static_assert(sizeof(CUtensorMap) == kSlicedMap && 3 * sizeof(CUtensorMap) == ZIPMOE_RESIDENT_ENTRY_BYTES, "an entry is three tensor maps");
   const uint64_t bytes = 2ull * hidden * inter;
   uint32_t R1, S1, R2, S2;
   zipmoe_host::resident_few_rows(hidden, inter, resident_grid(), &R1, &S1, &R2, &S2);
@@ -763,12 +854,16 @@ extern "C" zipmoe_status zipmoe_resident_experts_plan(const uint16_t *const *ten
   auto describe = [&](uint8_t *to, const uint16_t *base, uint32_t j, uint64_t n, uint64_t distance) {
     const uint32_t rows = j < 2 ? inter : hidden, cols = j < 2 ? hidden : inter;
     CUtensorMap map;
-    if (!zipmoe_host::make_wide_map(&map, base, rows, cols, n, distance)) return false;
+    if (!zipmoe_host::make_wide_map(&map, base, rows, cols, 128, n, distance)) return false;
     std::memset(to, 0, ZIPMOE_RESIDENT_ENTRY_BYTES);
     std::memcpy(to, &map, sizeof(map));
-    if (!sliced_sizes(hidden, inter)) return true;
-    if (!zipmoe_host::make_sliced_map(&map, base, rows, cols, j < 2 ? S1 : S2, n, distance)) return false;
-    std::memcpy(to + kSlicedMap, &map, sizeof(map));
+    const uint32_t box_rows = j < 2 ? S1 : S2;
+    if (cols >= 64 && !zipmoe_host::make_sliced_map(&map, base, rows, cols, box_rows, n, distance)) return false;
+    std::memcpy(to + kSlicedMap, &map, sizeof(map));   // (fewer columns: nothing is loaded through it)
+    if (cols % 64) {
+      if (!zipmoe_host::make_wide_map(&map, base, rows, cols, box_rows, n, distance)) return false;
+      std::memcpy(to + kRestMap, &map, sizeof(map));
+    }
     return true;
   };
   for (uint32_t i = 0; i < 3 * n_experts; ++i)
@@ -789,10 +884,11 @@ extern "C" zipmoe_status zipmoe_resident_experts_plan(const uint16_t *const *ten
       even = reinterpret_cast<uintptr_t>(tensors[3 * e + j]) == first + e * distance[j];
   }
   for (uint32_t j = 0; j < 3 && even; ++j) {
-    uint8_t both[ZIPMOE_RESIDENT_ENTRY_BYTES];
-    if (!describe(both, tensors[j], j, n_experts, distance[j])) return ZIPMOE_ERR_CUDA;
-    std::memcpy(experts->maps + 128 * j, both, 128);
-    std::memcpy(experts->maps + 128 * (3 + j), both + kSlicedMap, 128);
+    uint8_t all[ZIPMOE_RESIDENT_ENTRY_BYTES];
+    if (!describe(all, tensors[j], j, n_experts, distance[j])) return ZIPMOE_ERR_CUDA;
+    std::memcpy(experts->maps + 128 * j, all, 128);
+    std::memcpy(experts->maps + 128 * (3 + j), all + kSlicedMap, 128);
+    std::memcpy(experts->maps + 128 * (6 + j), all + kRestMap, 128);
   }
   experts->even = even;
   return ZIPMOE_OK;
@@ -847,7 +943,7 @@ extern "C" zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, c
   uint32_t tries = 0, extra_tx = 0;
   zipmoe_host::wait_fault_setting(&extra_tx, &tries);
   const uint64_t limit_ns = tries < zipmoe_host::kWaitTries ? 1000000ull : 1000000000ull;   // (1 ms in the tests of the limit)
-  if (T <= kResFewT && sliced_sizes(ex->hidden, ex->inter) && whole_rows_pay(T * k, ex->n_experts, ex->hidden, ex->inter, p.grid)) {
+  if (T <= kResFewT && whole_rows_pay(T * k, ex->n_experts, ex->hidden, ex->inter, p.grid)) {
     zipmoe_host::ResidentCall c;
     c.tokens = tokens;
     c.ids = topk_ids;

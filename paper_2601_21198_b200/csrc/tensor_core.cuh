@@ -215,14 +215,15 @@ inline bool make_bf16_map(CUtensorMap *map, const void *base, uint64_t rows, uin
   const cuuint32_t box[2] = {64, box_rows};
   return encode_bf16(map, 2, base, dims, strides, box, wide_fetch);
 }
-// n dense row-major matrices `distance` bytes apart: boxes of 64 columns x 128 rows of one of them.
-inline bool make_wide_map(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint64_t n, uint64_t distance) {
+// n dense row-major matrices `distance` bytes apart: boxes of 64 columns x box_rows rows of one of them.
+inline bool make_wide_map(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint32_t box_rows, uint64_t n,
+                          uint64_t distance) {
   const cuuint64_t dims[3] = {cols, rows, n}, strides[2] = {cols * 2, distance};
-  const cuuint32_t box[3] = {64, 128, 1};
+  const cuuint32_t box[3] = {64, box_rows, 1};
   return encode_bf16(map, 3, base, dims, strides, box, true);
 }
-// The same, cols a multiple of 64, seen as [n][cols / 64][rows][64]: a box of 8 x box_rows x 64 is 512 columns of box_rows
-// rows.
+// The same without the columns behind the last whole 64, seen as [n][cols / 64][rows][64]: a box of 8 x box_rows x 64 is
+// 512 columns of box_rows rows.
 inline bool make_sliced_map(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint32_t box_rows, uint64_t n,
                             uint64_t distance) {
   const cuuint64_t dims[4] = {64, rows, cols / 64, n}, strides[3] = {cols * 2, 128, distance};
