@@ -10,7 +10,8 @@
 //     of a phase form one sequence, cut into equal shares, so every SM streams the same number of bytes whatever the
 //     experts and their sizes (steps of experts with very many tokens weigh more).
 //   * Phases: gate/up of the first half of the active experts, gate/up of the second half, down of the first, down of
-//     the second.  What the third needs was stored before the second began, so nobody waits between them.
+//     the second.  What the third needs was stored before the second began, so nobody waits between them.  Short calls
+//     take all experts as one group: fewer jobs are cut.
 //   * One thread feeds weights into a ring of shared-memory stages (TMA, 128-byte swizzle) and runs ahead as far as the
 //     ring allows, across jobs and phases.
 //   * Another warp adds the activations of every step, 64 columns of the expert's own tokens: for gate/up gathered from
@@ -31,6 +32,7 @@
 #include <algorithm>
 #include <cstdint>
 #include <cstring>
+#include <type_traits>
 
 #include "zipmoe.h"
 #include "resident.cuh"
@@ -45,8 +47,13 @@ constexpr uint32_t kResInFlight = 4;                        // steps asked for a
 constexpr uint32_t kResFewT = 8;   // up to this many tokens the kernel that gives every block whole rows may run instead
 constexpr uint32_t kResGatherRows = 16;   // a gather of four rows takes the copy engine about 130 ns: up to this many tokens
                                           // per expert they are gathered in every step, beyond it packed once
-constexpr uint32_t kResTwoGroupsT = 64;   // above, a call is long enough for the wait between gate/up and down not to show,
-                                          // and the partial sums of four phases would take too much memory
+
+// Bytes of weights from which on the experts are taken in two groups.  One group waits between gate/up and down, two cut
+// more jobs.  One against two: 16 experts of 1024 x 512, 32 tokens (50 MB) 32 against 41 us; 8 of 2048 x 1408, 12 tokens
+// (138 MB) 42 against 47; 24 of them, 12 tokens (415 MB) 80 against 81; 40 of 2048 x 1000, 16 tokens (490 MB) 94 against 90; 60
+// of 2048 x 1408, 32 tokens (1.04 GB) 176 against 170.  Where experts have many tokens a cut costs more: 8 of 4096 x 3584, 256
+// tokens (705 MB) 167 against 173; 60 of 2048 x 1408, 256 tokens 226 against 216.
+constexpr uint64_t kResTwoGroups = 450000000, kResTwoGroupsMany = 1000000000;
 
 struct ResidentArgs {
   const uint16_t *tokens;
@@ -57,10 +64,11 @@ struct ResidentArgs {
   ResidentSync *sync;
   uint8_t *x;               // the experts' tokens in the same order as h, [hidden / 64] columns (where tokens are packed)
   uint8_t *h;               // per active expert: [inter / 64][rows padded to 8][64] bf16, swizzled as the operand wants it
-  float *part;              // [phase][block][2][2][T][128]: partial sums of a share's two cut jobs (0: begun by others, 1: begun here)
+  float *part;              // [group][block][2][2][T][128]: partial sums of a share's two cut jobs (0: begun by others, 1: begun here);
+                            // gate/up's have been read when down begins, and down's are stored over them
   float *y;                 // [choices][H]: jobs that lie inside one share
   uint32_t *status;
-  uint64_t limit_ns, part_phase;   // part_phase: floats between the phases' partial sums (0: one group, they follow each other)
+  uint64_t limit_ns, part_phase;   // part_phase: floats of a group's partial sums
   uint32_t T, k, E, H, I, even, ring_bytes, tmem_cols, extra_tx;
 };
 
@@ -264,7 +272,8 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
   const uint32_t w_ring = smem_addr(ring), x_ring = w_ring + n_w * kResStageA;
   const uint32_t acc_bufs = N <= 128 ? 2 : 1;                // two accumulators of N columns each, of 512 columns
   Phase ph[4];
-  const uint32_t n_first = a.part_phase ? (n_active + 1) / 2 : n_active;
+    const bool two_groups = (uint64_t)n_active * a.H * a.I * 6 >= (words[4] > kResEvenTokens ? kResTwoGroupsMany : kResTwoGroups);
+  const uint32_t n_first = two_groups ? (n_active + 1) / 2 : n_active;
 #pragma unroll
   for (uint32_t p = 0; p < 4; ++p) {
     ph[p].KS = p < 2 ? (a.H + 63) / 64 : (a.I + 63) / 64;
@@ -485,7 +494,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
       const Phase f = p == 0 ? ph[0] : p == 1 ? ph[1] : p == 2 ? ph[2] : ph[3];
       uint32_t u = first(f);
       const uint32_t end = last(f);
-      float *part = a.part + p * a.part_phase;
+      float *part = a.part + (p & 1) * a.part_phase;
       Piece q;
       while (ok && next_piece(f, u, end, q)) {
         const uint32_t b = piece % acc_bufs, use = piece / acc_bufs;
@@ -644,7 +653,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
           if (c0 == c1) {
             v = __ldcg(reinterpret_cast<const float4 *>(a.y + (size_t)(act[ai].slot + i) * a.H + c));
           } else {
-            const float *from = a.part + p * a.part_phase + (size_t)(((c >> 7) & 1) * a.T + i) * 128 + (c & 127);
+            const float *from = a.part + (p & 1) * a.part_phase + (size_t)(((c >> 7) & 1) * a.T + i) * 128 + (c & 127);
             for (uint32_t b = c0; b <= c1; b += 4) {
               float4 r[4];
 #pragma unroll
@@ -680,73 +689,83 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
       }
     }
   } else if (!*dead && prepared) {
-    // many: a turn is 256 columns (a row block of down) of six tokens; 64 threads have a token's columns, four each.  Which
-    // blocks have parts of an expert's job is worked out once per row block.  (As above: 9 us longer for 256 tokens.)
+    // many: a turn is 256 columns (a row block of down) of six tokens, or twelve with up to four choices each; 64 threads have
+    // a token's columns, four each.  Which blocks have parts of an expert's job is worked out once per row block.  (As above:
+    // 9 us longer for 256 tokens.)
     uint32_t *owners = reinterpret_cast<uint32_t *>(ring);   // [active experts]: first and last block (the ring is done with)
-    constexpr uint32_t kTokens = kResThreads / 64;
-    const uint32_t RB = ph[2].RB, groups = (a.T + kTokens - 1) / kTokens, turns = RB * groups;
-    uint32_t rb_now = 0xFFFFFFFFu;
-    for (uint32_t turn = cta * turns / G; turn < (cta + 1) * turns / G; ++turn) {
-      const uint32_t rb = turn / groups, t = (turn - rb * groups) * kTokens + (tid >> 6), v4 = tid & 63, c = rb * 256 + v4 * 4;
-      if (rb != rb_now) {
-        __syncthreads();
-        for (uint32_t ai = tid; ai < n_active; ai += kResThreads) {
-          const Phase f = ai < n_first ? ph[2] : ph[3];
-          const uint32_t u0 = ((ai - f.a0) * RB + rb) * f.KS;
-          owners[ai] = f.owner(u0) | f.owner(u0 + f.KS - 1) << 16;
+    auto combine = [&](auto most_choices) {
+      constexpr uint32_t kK = decltype(most_choices)::value, kN = 8 / kK, kTokens = kResThreads / 64 * kN;
+      const uint32_t RB = ph[2].RB, groups = (a.T + kTokens - 1) / kTokens, turns = RB * groups;
+      uint32_t rb_now = 0xFFFFFFFFu;
+      for (uint32_t turn = cta * turns / G; turn < (cta + 1) * turns / G; ++turn) {
+        const uint32_t rb = turn / groups, t0 = (turn - rb * groups) * kTokens + (tid >> 6), v4 = tid & 63, c = rb * 256 + v4 * 4;
+        if (rb != rb_now) {
+          __syncthreads();
+          for (uint32_t ai = tid; ai < n_active; ai += kResThreads) {
+            const Phase f = ai < n_first ? ph[2] : ph[3];
+            const uint32_t u0 = ((ai - f.a0) * RB + rb) * f.KS;
+            owners[ai] = f.owner(u0) | f.owner(u0 + f.KS - 1) << 16;
+          }
+          __syncthreads();
+          rb_now = rb;
         }
-        __syncthreads();
-        rb_now = rb;
-      }
-      if (t >= a.T || c >= a.H) continue;
-      // every choice's sum, or the first part of it, is asked for before the first is used
-      const uint32_t in_part = ((v4 >> 5) * a.T) * 128 + (v4 & 31) * 4;
-      float4 y[8];
-      uint32_t more[8];
+        if (c >= a.H) continue;
+        // every choice's sum, or the first two parts of it, are asked for before the first is used
+        const uint32_t in_part = ((v4 >> 5) * a.T) * 128 + (v4 & 31) * 4;
+        const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+        const size_t next_block = 2 * (2 * a.T * 128);
+        float4 y[8], z[8];
+        const float *from[8];
+        uint32_t more[8];
+        float wt[8];
 #pragma unroll
-      for (uint32_t j = 0; j < 8; ++j) {
-        y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-        more[j] = 0;
-        if (j >= a.k) continue;
-        const int32_t e = __ldg(a.ids + t * a.k + j);
-        if (e < 0 || e >= (int32_t)a.E) continue;
-        const uint32_t ai = active_of[e], i = place[t * a.k + j], c0 = owners[ai] & 0xFFFFu, c1 = owners[ai] >> 16;
-        const float *from = a.y + (size_t)(act[ai].slot + i) * a.H + c;
-        if (c0 != c1) {
-          from = a.part + (ai < n_first ? 2 : 3) * a.part_phase + ((size_t)c0 * 2 + 1) * (2 * a.T * 128) + in_part + (size_t)i * 128;
-          more[j] = c1 - c0;
+        for (uint32_t i = 0; i < 8; ++i) {
+          const uint32_t t = t0 + i / kK * (kResThreads / 64), j = i % kK, at = t * a.k + j;
+          y[i] = z[i] = zero;
+          more[i] = 0;
+          wt[i] = 0.f;
+          if (t >= a.T || j >= a.k) continue;
+          const int32_t e = __ldg(a.ids + at);
+          if (e < 0 || e >= (int32_t)a.E) continue;   // (adds nothing, whatever its weight is)
+          wt[i] = a.weights ? __ldg(a.weights + at) : 1.0f;
+          const uint32_t ai = active_of[e], r = place[at], c0 = owners[ai] & 0xFFFFu, c1 = owners[ai] >> 16;
+          if (c0 == c1) {
+            y[i] = __ldcg(reinterpret_cast<const float4 *>(a.y + (size_t)(act[ai].slot + r) * a.H + c));
+          } else {
+            from[i] = a.part + (ai < n_first ? 0 : 1) * a.part_phase + c0 * next_block + in_part + (size_t)r * 128;
+            more[i] = c1 - c0;
+            y[i] = __ldcg(reinterpret_cast<const float4 *>(from[i] + next_block / 2));
+            z[i] = __ldcg(reinterpret_cast<const float4 *>(from[i] + next_block));
+          }
         }
-        y[j] = __ldcg(reinterpret_cast<const float4 *>(from));
-      }
-      float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (uint32_t j = 0; j < 8; ++j) {
-        if (j >= a.k) continue;
-        if (more[j]) {
-          const uint32_t ai = active_of[__ldg(a.ids + t * a.k + j)], i = place[t * a.k + j], c0 = owners[ai] & 0xFFFFu;
-          const float *from = a.part + (ai < n_first ? 2 : 3) * a.part_phase + (size_t)c0 * 2 * (2 * a.T * 128) + in_part + (size_t)i * 128;
-          for (uint32_t b = 1; b <= more[j]; b += 4) {
+        for (uint32_t i = 0; i < 8; ++i) {
+          y[i] = make_float4(y[i].x + z[i].x, y[i].y + z[i].y, y[i].z + z[i].z, y[i].w + z[i].w);
+          for (uint32_t b = 2; b <= more[i]; b += 4) {
             float4 r[4];
 #pragma unroll
             for (uint32_t n = 0; n < 4; ++n)
-              r[n] = b + n <= more[j] ? __ldcg(reinterpret_cast<const float4 *>(from + (size_t)(b + n) * 2 * (2 * a.T * 128))) : make_float4(0.f, 0.f, 0.f, 0.f);
+              r[n] = b + n <= more[i] ? __ldcg(reinterpret_cast<const float4 *>(from[i] + (b + n) * next_block)) : zero;
 #pragma unroll
-            for (uint32_t n = 0; n < 4; ++n) y[j] = make_float4(y[j].x + r[n].x, y[j].y + r[n].y, y[j].z + r[n].z, y[j].w + r[n].w);
+            for (uint32_t n = 0; n < 4; ++n) y[i] = make_float4(y[i].x + r[n].x, y[i].y + r[n].y, y[i].z + r[n].z, y[i].w + r[n].w);
           }
         }
-        const float wt = a.weights ? __ldg(a.weights + t * a.k + j) : 1.0f;
-        // (a choice that is no expert adds nothing, whatever its weight is)
-        if (__ldg(a.ids + t * a.k + j) >= 0 && __ldg(a.ids + t * a.k + j) < (int32_t)a.E) {
-          s.x += wt * y[j].x;
-          s.y += wt * y[j].y;
-          s.z += wt * y[j].z;
-          s.w += wt * y[j].w;
+#pragma unroll
+        for (uint32_t n = 0; n < kN; ++n) {
+          const uint32_t t = t0 + n * (kResThreads / 64);
+          if (t >= a.T) continue;
+          float4 s = zero;
+#pragma unroll
+          for (uint32_t i = n * kK; i < (n + 1) * kK; ++i)
+            s = make_float4(s.x + wt[i] * y[i].x, s.y + wt[i] * y[i].y, s.z + wt[i] * y[i].z, s.w + wt[i] * y[i].w);
+          const __nv_bfloat162 lo = __floats2bfloat162_rn(s.x, s.y), hi = __floats2bfloat162_rn(s.z, s.w);
+          *reinterpret_cast<uint2 *>(a.out + (size_t)t * a.H + c) =
+              make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
         }
       }
-      const __nv_bfloat162 lo = __floats2bfloat162_rn(s.x, s.y), hi = __floats2bfloat162_rn(s.z, s.w);
-      *reinterpret_cast<uint2 *>(a.out + (size_t)t * a.H + c) =
-          make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
-    }
+    };
+    if (a.k <= 4) combine(std::integral_constant<uint32_t, 4>());
+    else combine(std::integral_constant<uint32_t, 8>());
   }
   __syncthreads();
   if (tid == 0) {
@@ -827,10 +846,8 @@ zipmoe_status resident_plan(uint32_t T, uint32_t k, const zipmoe_resident_expert
   uint64_t at = up(sizeof(zipmoe_dev::ResidentSync));
   p->off_x = at; at = up(at + rows * ((H + 63) / 64) * 128);
   p->off_h = at; at = up(at + rows * ((I + 63) / 64) * 128);
-  // (a workspace for more tokens always serves fewer: up to kResTwoGroupsT tokens four phases have partial sums of their own)
-  const uint64_t per_token = (uint64_t)p->grid * 2 * 2 * 128, few = std::min(T, zipmoe_dev::kResTwoGroupsT);
-  p->part_phase = T == few ? few * per_token : 0;
-  p->off_part = at; at = up(at + std::max(4 * few, (uint64_t)T) * per_token * 4);
+  p->part_phase = (uint64_t)T * p->grid * 2 * 2 * 128;
+  p->off_part = at; at = up(at + 2 * p->part_phase * 4);
   p->off_y = at; at = up(at + choices * H * 4);
   p->total = at;
   return ZIPMOE_OK;
