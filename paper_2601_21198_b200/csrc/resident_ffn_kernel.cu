@@ -23,7 +23,7 @@
 //   * Every block works out the same routing lists for itself, and sizes its rings by the most tokens that an expert
 //     of this call has: few tokens, more stages.
 //   * Eight warps read the accumulators back.  A job inside one share goes straight on.  Of a job that is cut, each
-//     block stores its partial sums; for gate/up the block that arrives last adds them in share order and goes on, for
+//     block stores its partial sums; for gate/up the block that is done last adds them in share order and goes on, for
 //     down the combination of the experts adds them.  No atomics on values: the same bits whatever the timing.
 // Blocks wait for one another (tokens packed, h stored, y stored), hence the cooperative launch.
 #include <cuda_bf16.h>
@@ -526,10 +526,59 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
             mine[(size_t)(a.T + i) * 128] = v1;
           }
         };
-        ok = all_agree<32 * kResReaders>(wait_bar(acc_full + 8 * b, use & 1, lim));
+        // a gate/up job that is cut: the block that is done with its part last adds all parts, in share order.  That is
+        // mostly the one that began the job, at the end of its share, and finds the others' parts there: its own never leave
+        // the tensor memory.
+        const bool join = !whole && p < 2;
+        const uint32_t c0 = join ? f.owner(q.job * f.KS) : 0, c1 = join ? f.owner(q.job * f.KS + f.KS - 1) : 0;
+        volatile uint32_t *others_there = words + 5 + (piece & 1);
+        ok = wait_bar(acc_full + 8 * b, use & 1, lim);
+        if (rtid == 0) *others_there = join && q.s0 == 0 && load_acquire(&a.sync->cut[p][c0]) == c1 - c0;
+        ok = all_agree<32 * kResReaders>(ok);
         if (!ok) break;
         tc_after_sync();
         const uint32_t d0 = tmem + ((32 * w) << 16) + b * 2 * N, d1 = d0 + N;
+        if (*others_there) {
+          const size_t next_block = 2 * (2 * a.T * 128);
+          const float *from = part + (c0 + 1) * next_block + row;
+          for (uint32_t c = 8 * half; c < ex.n; c += 32) {
+            float g[2][8], v[2][8];   // the next block's part: of 16 tokens at a time
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i) {
+              const uint32_t t = min(c + 16 * (i >> 3) + (i & 7), ex.n - 1);
+              g[i >> 3][i & 7] = __ldcg(from + (size_t)t * 128);
+              v[i >> 3][i & 7] = __ldcg(from + (size_t)(a.T + t) * 128);
+            }
+#pragma unroll
+            for (uint32_t m = 0; m < 2; ++m) {
+              const uint32_t t0 = c + 16 * m;
+              if (t0 >= ex.n) continue;
+              uint32_t v0[8], v1[8];
+              tmem_load8(d0 + t0, v0);
+              tmem_load8(d1 + t0, v1);
+              tmem_wait();
+#pragma unroll
+              for (uint32_t n = 0; n < 8; ++n) {   // (from zero, as below: the same bits for either way)
+                g[m][n] = 0.f + __uint_as_float(v0[n]) + g[m][n];
+                v[m][n] = 0.f + __uint_as_float(v1[n]) + v[m][n];
+              }
+              for (uint32_t o = 1; o < c1 - c0; ++o)
+#pragma unroll
+                for (uint32_t n = 0; n < 8; ++n) {
+                  const uint32_t t = min(t0 + n, ex.n - 1);
+                  g[m][n] += __ldcg(from + o * next_block + (size_t)t * 128);
+                  v[m][n] += __ldcg(from + o * next_block + (size_t)(a.T + t) * 128);
+                }
+#pragma unroll
+              for (uint32_t n = 0; n < 8; ++n)
+                if (t0 + n < ex.n) finish(t0 + n, g[m][n], v[m][n]);
+            }
+          }
+          tc_before_sync();
+          __syncwarp();
+          if (lane == 0) arrive(acc_empty + 8 * b);
+          continue;
+        }
         for (uint32_t c = 8 * half; c < ex.n; c += 16) {
           uint32_t v0[8], v1[8];
           tmem_load8(d0 + c, v0);
@@ -542,9 +591,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
         tc_before_sync();
         __syncwarp();
         if (lane == 0) arrive(acc_empty + 8 * b);
-        if (whole || p >= 2) continue;
-        // a gate/up job that is cut: the block that stores its part last adds all parts, in share order
-        const uint32_t c0 = f.owner(q.job * f.KS), c1 = f.owner(q.job * f.KS + f.KS - 1);
+        if (!join) continue;
         __threadfence();
         sync_group<32 * kResReaders>();
         if (rtid == 0) {
