@@ -847,12 +847,18 @@ bool dims_ok(uint32_t E, uint32_t H, uint32_t I) {
          I <= kResidentMaxDim;
 }
 
-// Whether a block's whole rows are the faster way for few tokens.  They save 10 us of a call (one token, 6 experts of
-// 2048 x 1408: 28 us against 42), and stream as fast (8 tokens, 7 experts of 4096 x 14336: 347 against 369 us) as long as a
-// block has a dozen rows of W2: with 7 (16 experts of 1024 x 4096, 400 MB) 90 against 76 us.  (A second column of eight
-// tokens was built and taken out: 16 tokens, 16 experts of 1096 x 904: 60 us against 44.)
+// Whether a block's whole rows are the faster way for few tokens.  They save 10 us of a call, but a chunk of 512 columns takes
+// a block 0.43 us however few rows it has; where that is longer than its bytes take, experts cost what is over.  8 tokens,
+// whole rows against shares: 8 experts of 2048 x 1408 34 against 41 us, 30 of them 96 against 90; 30 of 3008 x 1536 126 against
+// 137; 30 of 4096 x 256 118 against 50; 60 of 1024 x 512 111 against 47, but 8 of them (one token) 23 against 26.  (A second
+// column of eight tokens was built and taken out: 16 tokens, 16 experts of 1096 x 904: 60 us against 44.)
 bool whole_rows_pay(uint32_t choices, uint32_t E, uint32_t H, uint32_t I, uint32_t grid) {
-  return H >= 11 * grid || (uint64_t)std::min(choices, E) * 6 * H * I < (100u << 20);
+  uint32_t R1, S1, R2, S2;
+  zipmoe_host::resident_few_rows(H, I, grid, &R1, &S1, &R2, &S2);
+  const uint64_t chunks = (uint64_t)((R1 + S1 - 1) / S1) * std::max(1u, (H / 64 + 7) / 8) +
+                          (uint64_t)((R2 + S2 - 1) / S2) * std::max(1u, (I / 64 + 7) / 8);
+  const uint64_t chunk_ns = 430 * chunks, byte_ns = 6ull * H * I / 6464;   // of an expert
+  return chunk_ns <= byte_ns || std::min(choices, E) * (chunk_ns - byte_ns) <= 10000;
 }
 
 struct ResidentDevice {

@@ -81,6 +81,18 @@ def test_shapes(zb, E, H, I, k, T):
     assert int(ex.status.item()) == 0
 
 
+@pytest.mark.parametrize("E,H,I,k,T", [(1, 8192, 1024, 1, 3), (1, 16384, 512, 1, 2), (1, 8200, 1032, 1, 8), (2, 4096, 4104, 2, 8),
+                                       (2, 5120, 1536, 1, 5)])
+def test_few_tokens_through_several_sets_of_rows(zb, E, H, I, k, T):
+    """A block's rows of W1 and W3 beyond 16, of W2 beyond 32, come in several sets."""
+    ws = layer(E, H, I, 60 + E, std=1.0 / np.sqrt(max(H, I)))
+    ex = zb.ResidentExperts([dev(w) for w in ws], H, I)
+    tok = inputs.tokens(T, H, seed=E)
+    ids, wts = inputs.routing(T, n_experts=E, k=k, seed=I)
+    check(ex.ffn(dev(tok), dev(ids), dev(wts)), ws, tok, ids, wts)
+    assert int(ex.status.item()) == 0
+
+
 def test_empty_rows_and_repeated_experts(zb):
     """Ids of -1 (a router with experts switched off), tokens without any expert, an expert listed twice."""
     E, H, I, T, k = 5, 256, 320, 40, 4
