@@ -410,9 +410,15 @@ zipmoe_status zipmoe_expert_ffn_workspace_bytes(uint32_t T, uint32_t k, const zi
                                                 uint64_t *workspace_bytes);
 
 /* Prepares a new workspace for zipmoe_expert_ffn (one small kernel on `stream`): once, before its first use.  Every
- * call leaves the workspace ready for the next one, whatever the sizes of either.
+ * call leaves the workspace ready for the next one, whatever the sizes of either.  On a stream that is being captured
+ * the kernel becomes a node of the graph: the workspace is then prepared by that graph's replays and by nothing else, so
+ * it is for calls captured into that graph only.
  * device out: workspace (16-byte aligned). */
 zipmoe_status zipmoe_expert_ffn_workspace_init(void *workspace, uint64_t workspace_bytes, zipmoe_stream stream);
+
+/* Which capture `stream` takes part in: a number of that capture's own, or 0 while the stream is not being captured.  For
+ * callers that keep workspaces: what is prepared or allocated in a capture belongs to its graph. */
+zipmoe_status zipmoe_stream_capture_id(zipmoe_stream stream, uint64_t *capture_id);
 
 /* Expert execution on recovered weights (Section 3.3: the GPU work p_n of the tokens routed to expert n, for experts
  * found in pool F): what zipmoe_decode_expert_ffn computes, from bf16 tensors.  For every token t and choice j with

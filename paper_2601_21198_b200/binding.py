@@ -11,6 +11,7 @@ module raises.
 import ctypes
 import os
 import struct
+import threading
 
 import numpy as np
 
@@ -360,6 +361,8 @@ _lib.zipmoe_resident_experts_plan.argtypes = [ctypes.POINTER(_vp), _u32, _u32, _
 _lib.zipmoe_expert_ffn_workspace_bytes.argtypes = [_u32, _u32, ctypes.POINTER(ResidentExpertsStruct), ctypes.POINTER(_u64)]
 _lib.zipmoe_expert_ffn_workspace_init.argtypes = [_vp, _u64, _vp]
 _lib.zipmoe_expert_ffn_workspace_init.restype = _int
+_lib.zipmoe_stream_capture_id.argtypes = [_vp, ctypes.POINTER(_u64)]
+_lib.zipmoe_stream_capture_id.restype = _int
 _lib.zipmoe_expert_ffn.argtypes = [_vp, _u32, _vp, _vp, _u32, ctypes.POINTER(ResidentExpertsStruct), _vp, _vp, _u64, _vp, _vp]
 for _f in ("zipmoe_add_rmsnorm", "zipmoe_route", "zipmoe_resident_experts_plan", "zipmoe_expert_ffn_workspace_bytes",
            "zipmoe_expert_ffn"):
@@ -407,6 +410,13 @@ def zipmoe_expert_ffn_workspace_init(workspace, workspace_bytes, stream=None):
     """Prepares a new device workspace; once, before its first zipmoe_expert_ffn."""
     _check("zipmoe_expert_ffn_workspace_init",
            _lib.zipmoe_expert_ffn_workspace_init(_ptr(workspace), workspace_bytes, _ptr(stream)))
+
+
+def zipmoe_stream_capture_id(stream):
+    """0, or the number of the capture that `stream` (a raw handle) takes part in."""
+    out = _u64(0)
+    _check("zipmoe_stream_capture_id", _lib.zipmoe_stream_capture_id(_ptr(stream), ctypes.byref(out)))
+    return out.value
 
 
 def zipmoe_expert_ffn(tokens, T, topk_ids, topk_weights, k, experts, out, workspace, workspace_bytes, status_word=None,
@@ -561,6 +571,7 @@ class _Kinds:
         self.fp32 = (torch.float32,)
         self.int32 = (torch.int32,)
         self.current_stream = torch._C._cuda_getCurrentRawStream   # handle of a device's current stream
+        self.capturing = torch._C._cuda_isCurrentStreamCapturing
 
 
 _kinds = None
@@ -728,7 +739,8 @@ class ResidentExperts:
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self.status_at = self.status.data_ptr()
         self._struct_at = ctypes.byref(self.struct)
-        self._ws, self._need = {}, {}
+        self._ws, self._captured, self._need = {}, {}, {}
+        self._lock = threading.Lock()
 
     @classmethod
     def from_decode(cls, plan, out, hidden, inter):
@@ -736,17 +748,34 @@ class ResidentExperts:
         return cls([plan.tensor_slice(out, i) for i in range(len(plan.infos))], hidden, inter)
 
     def _workspace(self, T, k, handle, stream):
-        """The stream's workspace, large enough for T tokens with k experts each.  One that has become too small is kept: a
-        captured graph may still use it."""
+        """A workspace large enough for T tokens with k experts each: the stream's own, or, while the stream is being
+        captured, one that belongs to that capture alone: only the graph's replays prepare it.  Its memory comes from the
+        graph's pool, which lives as long as the graph, so it is kept here for the rest of the capture only."""
         need = self._need.get((T, k))
         if need is None:
             fits = T if T > 128 else 1 << max(T - 1, 15).bit_length()      # some more tokens than asked for: it seldom grows
             need = self._need[(T, k)] = zipmoe_expert_ffn_workspace_bytes(min(fits, 256) if T <= 256 else T, k, self.struct)
-        held = self._ws.setdefault(handle, [])
-        if not held or held[-1].numel() < need:
-            held.append(_empty(need, self.kinds.e4m3[1], self.device, stream))
-            zipmoe_expert_ffn_workspace_init(held[-1], need, handle)
+        capture = 0
+        if stream is not None or self.kinds.capturing():
+            capture = zipmoe_stream_capture_id(handle)
+        if capture:
+            of, held = self._captured.get(handle, (0, None))
+            if of != capture or held.numel() < need:
+                held = self._prepared(need, handle, stream)
+                self._captured[handle] = capture, held
+            return held
+        held = self._ws.get(handle)
+        if held is None or held[-1].numel() < need:
+            with self._lock:
+                held = self._ws.get(handle, [])
+                if not held or held[-1].numel() < need:
+                    held = self._ws[handle] = held + [self._prepared(need, handle, stream)]
         return held[-1]
+
+    def _prepared(self, need, handle, stream):
+        ws = _empty(need, self.kinds.e4m3[1], self.device, stream)
+        zipmoe_expert_ffn_workspace_init(ws, need, handle)
+        return ws
 
     def ffn(self, tokens, topk_ids, topk_weights, out=None, stream=None):
         """tokens [T, hidden] bf16 (or int16 patterns), topk_ids [T, k] int32, topk_weights [T, k] float32 or None: device

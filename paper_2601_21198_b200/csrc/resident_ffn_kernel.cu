@@ -984,6 +984,19 @@ extern "C" zipmoe_status zipmoe_expert_ffn_workspace_init(void *workspace, uint6
   return cudaGetLastError() == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
 }
 
+extern "C" zipmoe_status zipmoe_stream_capture_id(zipmoe_stream stream, uint64_t *capture_id) {
+  if (!capture_id) return ZIPMOE_ERR_INVALID_ARG;
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  unsigned long long id = 0;
+  if (cudaStreamGetCaptureInfo(reinterpret_cast<cudaStream_t>(stream), &capture, &id) != cudaSuccess ||
+      capture == cudaStreamCaptureStatusInvalidated) {
+    (void)cudaGetLastError();
+    return ZIPMOE_ERR_CUDA;
+  }
+  *capture_id = capture == cudaStreamCaptureStatusActive ? id : 0;
+  return ZIPMOE_OK;
+}
+
 extern "C" zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, const int32_t *topk_ids,
                                            const float *topk_weights, uint32_t k, const zipmoe_resident_experts *ex,
                                            uint16_t *out, void *workspace, uint64_t workspace_bytes,

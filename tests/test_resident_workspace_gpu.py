@@ -1,0 +1,137 @@
+"""The scratch that ResidentExperts keeps for zipmoe_expert_ffn: calls captured into graphs, on several streams and by
+several layers never share a workspace that is not theirs, nor meet one that was not prepared.  Every output is compared bit
+for bit with the same call outside of any graph (the kernels give the same bits whatever the timing)."""
+import numpy as np
+import pytest
+
+from paper_2601_21198_b200 import build, inputs
+
+pytestmark = pytest.mark.gpu
+E, H, I, K = 6, 512, 384, 3
+
+
+@pytest.fixture(scope="module")
+def zb():
+    build.build()
+    from paper_2601_21198_b200 import binding
+    return binding
+
+
+def dev(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a.view(np.int16) if a.dtype == np.uint16 else a)).cuda()
+
+
+@pytest.fixture(scope="module")
+def weights():
+    return [dev(inputs.gaussian((I, H) if j % 3 < 2 else (H, I), 0.05, 300 + j)) for j in range(3 * E)]
+
+
+def call(T):
+    """Inputs of one call and an output that holds what no call writes."""
+    import torch
+    ids, wts = inputs.routing(T, n_experts=E, k=K, seed=T)
+    return dev(inputs.tokens(T, H, seed=T)), dev(ids), dev(wts), torch.full((T, H), 0x5555, dtype=torch.int16, device="cuda")
+
+
+def capture(ex, args, stream=None):
+    import torch
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        ex.ffn(*args)
+    return graph
+
+
+@pytest.mark.parametrize("sizes", [(1, 2), (40, 3), (2, 200), (200, 40)])     # both kernels, tokens gathered and packed
+def test_graphs_without_a_call_before_them_replayed_in_any_order(zb, weights, sizes):
+    import torch
+    ex = zb.ResidentExperts(weights, H, I)
+    calls = [call(T) for T in sizes]
+    graphs = [capture(ex, c) for c in calls]
+    graphs[1].replay()
+    graphs[0].replay()
+    graphs[1].replay()
+    torch.cuda.synchronize()
+    assert int(ex.status.item()) == 0
+    other = zb.ResidentExperts(weights, H, I)
+    for c in calls:
+        assert torch.equal(c[3], other.ffn(*c[:3]))
+
+
+def test_a_call_on_the_capturing_stream_before_the_first_replay(zb, weights):
+    import torch
+    ex = zb.ResidentExperts(weights, H, I)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph_args, args = call(20), call(20)
+    graph = capture(ex, graph_args, side)
+    ex.ffn(*args, stream=side)
+    side.synchronize()
+    assert int(ex.status.item()) == 0
+    graph.replay()
+    torch.cuda.synchronize()
+    want = zb.ResidentExperts(weights, H, I).ffn(*args[:3])
+    assert torch.equal(args[3], want) and torch.equal(graph_args[3], want) and int(ex.status.item()) == 0
+    del graph            # its memory may go to somebody else: the stream's own workspace must not be in it
+    torch.cuda.empty_cache()
+    junk = [torch.full((1 << 20,), 0x77777777, dtype=torch.int32, device="cuda") for _ in range(64)]
+    args[3].fill_(0x5555)
+    side.wait_stream(torch.cuda.current_stream())
+    ex.ffn(*args, stream=side)
+    side.synchronize()
+    assert torch.equal(args[3], want) and int(ex.status.item()) == 0
+    del junk
+
+
+def test_more_tokens_within_one_capture(zb, weights):
+    """A capture whose later call wants a larger workspace than its first, the stream having one of its own already."""
+    import torch
+    ex = zb.ResidentExperts(weights, H, I)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    calls = [call(T) for T in (5, 129, 40)]
+    with torch.cuda.stream(side):
+        ex.ffn(*calls[0][:3])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        for c in calls:
+            ex.ffn(*c)
+    with torch.cuda.stream(side):       # between the capture and its replay, with more tokens than before
+        between = ex.ffn(*calls[1][:3])
+    graph.replay()
+    torch.cuda.synchronize()
+    assert int(ex.status.item()) == 0
+    other = zb.ResidentExperts(weights, H, I)
+    assert torch.equal(between, other.ffn(*calls[1][:3]))
+    for c in calls:
+        assert torch.equal(c[3], other.ffn(*c[:3]))
+    for _ in range(3):
+        for c in calls:
+            c[3].fill_(0x5555)
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(c[3], other.ffn(*c[:3])) for c in calls) and int(ex.status.item()) == 0
+
+
+def test_graphs_replayed_on_two_streams_do_not_meet(zb, weights):
+    """Two graphs captured one after the other on one stream, then replayed with no order between them, beside calls
+    outside of any graph: each has a workspace of its own."""
+    import torch
+    ex = zb.ResidentExperts(weights, H, I)
+    calls = [call(T) for T in (3, 60, 130)]
+    graphs = [capture(ex, c) for c in calls[:2]]
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    want = [zb.ResidentExperts(weights, H, I).ffn(*c[:3]) for c in calls]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c in calls:
+            c[3].fill_(0x5555)
+        for s, g in zip(sides, graphs):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                for _ in range(5):
+                    g.replay()
+        ex.ffn(*calls[2])
+        torch.cuda.synchronize()
+        assert all(torch.equal(c[3], w) for c, w in zip(calls, want))
+    assert int(ex.status.item()) == 0
