@@ -20,7 +20,8 @@
  *   - Plain C, no exceptions, no aborts: the return value is a zipmoe_status.
  *   - The library never allocates or frees device memory and never
  *     synchronises a stream, except where an entry point says otherwise.
- *     Device buffers and streams belong to the caller.
+ *     Device buffers and streams belong to the caller.  Kernels are launched on the
+ *     current device, which has to be the one of the stream and of the buffers.
  *   - "host" / "device" in an argument's comment says where the pointer must
  *     point.  Sizes are in the unit named in the comment.
  *   - The container ("blob") produced by zipmoe_encode is self-describing,

@@ -572,6 +572,7 @@ class _Kinds:
         self.int32 = (torch.int32,)
         self.current_stream = torch._C._cuda_getCurrentRawStream   # handle of a device's current stream
         self.capturing = torch._C._cuda_isCurrentStreamCapturing
+        self.current_device = torch._C._cuda_getDevice
 
 
 _kinds = None
@@ -621,6 +622,22 @@ def _device_of(name, t):
     return index
 
 
+def _on_device(index):
+    """Context in which the tensors' device is the current one: the library launches on the current device, and the
+    default stream has the same handle on all of them."""
+    import torch
+    return torch.cuda.device(index)
+
+
+def _handle(kinds, index, stream):
+    """Raw handle of a torch stream of device `index` (None: its current one)."""
+    if stream is None:
+        return kinds.current_stream(index)
+    if stream.device_index != index:
+        raise ValueError("a stream of CUDA device %d is wanted, not of device %d" % (index, stream.device_index))
+    return stream.cuda_stream
+
+
 class RmsNorm:
     """Residual addition and root-mean-square norm with one weight vector (bf16, or int16 bf16 patterns).  x and out are
     bf16 tensors or int16 patterns [rows, cols] whose rows may lie apart; the residual stream is of that kind or fp32."""
@@ -636,6 +653,9 @@ class RmsNorm:
 
     def _call(self, x, residual, residual_out, out, out_q, scales, group, stream):
         kinds, index, rows, cols = self.kinds, self.index, x.shape[0], self.cols
+        if kinds.current_device() != index:
+            with _on_device(index):
+                return self._call(x, residual, residual_out, out, out_q, scales, group, stream)
         shape, bf16 = (rows, cols), kinds.bf16
         x_at, x_pitch = _rows("x", x, shape, bf16, index)
         res = res_out = res_pitch = res_out_pitch = flags = 0
@@ -659,7 +679,7 @@ class RmsNorm:
             scales_at = _dense("scales", scales, (rows, self.n_groups(group)), kinds.fp32, index)
         args = _NORM_ARGS.pack(x_at, x_pitch, res, res_pitch, res_out, res_out_pitch, self.weight_at, out_at, q_at, out_pitch, scales_at,
                                rows, cols, group if group > 0 else 0, flags, self.eps, 0)
-        status = _lib.zipmoe_add_rmsnorm(args, kinds.current_stream(index) if stream is None else stream.cuda_stream)
+        status = _lib.zipmoe_add_rmsnorm(args, _handle(kinds, index, stream))
         if status:
             raise ZipMoEError("zipmoe_add_rmsnorm", status)
 
@@ -698,6 +718,9 @@ class Router:
     def route(self, tokens, ids=None, weights=None, logits=None, stream=None):
         """tokens [T, hidden] -> ids [T, k] int32, weights [T, k] fp32; logits, if given, gets [T, n_experts] fp32."""
         kinds, index, T = self.kinds, self.index, tokens.shape[0]
+        if kinds.current_device() != index:
+            with _on_device(index):
+                return self.route(tokens, ids, weights, logits, stream)
         chosen = (T, self.k)
         tokens_at, pitch = _rows("tokens", tokens, (T, self.hidden), kinds.bf16, index)
         if ids is None:
@@ -709,7 +732,7 @@ class Router:
         logits_at = 0 if logits is None else _dense("logits", logits, (T, self.n_experts), kinds.fp32, index)
         args = _ROUTE_ARGS.pack(tokens_at, pitch, self.gate_at, self.bias_at, ids_at, weights_at, logits_at, self.status_at, T,
                                 self.n_experts, self.hidden, self.k, self.flags, 0)
-        status = _lib.zipmoe_route(args, kinds.current_stream(index) if stream is None else stream.cuda_stream)
+        status = _lib.zipmoe_route(args, _handle(kinds, index, stream))
         if status:
             raise ZipMoEError("zipmoe_route", status)
         return ids, weights
@@ -733,7 +756,8 @@ class ResidentExperts:
         self.tensors = list(tensors)      # the experts' memory is theirs: keep it while the table points at it
         self.device = tensors[0].device
         self.hidden, self.inter = hidden, inter
-        table, self.struct = zipmoe_resident_experts_plan(addresses, len(tensors) // 3, hidden, inter)
+        with _on_device(self.index):
+            table, self.struct = zipmoe_resident_experts_plan(addresses, len(tensors) // 3, hidden, inter)
         self.table = torch.from_numpy(table).to(self.device)
         self.struct.table = self.table.data_ptr()
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
@@ -779,9 +803,13 @@ class ResidentExperts:
 
     def ffn(self, tokens, topk_ids, topk_weights, out=None, stream=None):
         """tokens [T, hidden] bf16 (or int16 patterns), topk_ids [T, k] int32, topk_weights [T, k] float32 or None: device
-        tensors.  Returns out [T, hidden].  Every stream has a workspace of its own, so calls on different streams may
-        overlap."""
+        tensors.  Returns out [T, hidden].  Every stream has a workspace of its own, and so has every capture of a stream by
+        torch.cuda.graph: calls on different streams, replays of different graphs and both may overlap, and no call has to
+        come before a capture."""
         kinds, index = self.kinds, self.index
+        if kinds.current_device() != index:
+            with _on_device(index):
+                return self.ffn(tokens, topk_ids, topk_weights, out, stream)
         T, k = chosen = topk_ids.shape
         shape = (T, self.hidden)
         tokens_at = _dense("tokens", tokens, shape, kinds.bf16, index)
@@ -790,7 +818,7 @@ class ResidentExperts:
         if out is None:
             out = _empty(shape, tokens.dtype, self.device, stream)
         out_at = _dense("out", out, shape, kinds.bf16, index)
-        handle = kinds.current_stream(index) if stream is None else stream.cuda_stream
+        handle = _handle(kinds, index, stream)
         ws = self._workspace(T, k, handle, stream)
         status = _lib.zipmoe_expert_ffn(tokens_at, T, ids_at, weights_at, k, self._struct_at, out_at, ws.data_ptr(), ws.numel(),
                                         self.status_at, handle)
