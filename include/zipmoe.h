@@ -391,11 +391,15 @@ typedef struct {
   uint32_t even;                      /* 1: every kind of tensor lies at equal distances from expert to expert      */
   const void *table;                  /* device [3 * n_experts * ZIPMOE_RESIDENT_ENTRY_BYTES], 64-byte aligned      */
   uint8_t maps[9 * 128];              /* opaque: the tensors of evenly spaced experts                               */
+  uint32_t grid;                      /* blocks of a call on the device planned for: the maps' boxes go by it        */
+  uint32_t reserved;                  /* zero                                                                       */
 } zipmoe_resident_experts;
 #define ZIPMOE_RESIDENT_ENTRY_BYTES 384u
 
 /* Describes recovered experts to zipmoe_expert_ffn: one opaque entry per tensor, which the caller copies to the
  * device as it is, and the struct that the call takes.  Once per layer, and again when an expert's tensors move.
+ * The current device is the one that will run the calls: zipmoe_expert_ffn refuses (ZIPMOE_ERR_INVALID_ARG) a struct
+ * that was planned for a device with another number of SMs.
  * Experts whose w1 lie at equal distances, in ascending order, and their w3 and w2 too (one array per kind, or one
  * decode launch's output) are found faster: about 3 us per call.
  * host in : tensors[3 * n_experts] DEVICE addresses, tensors[3e+0] = w1 (gate) [inter, hidden], 3e+1 = w3 (up)

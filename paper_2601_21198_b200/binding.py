@@ -348,7 +348,8 @@ RESIDENT_ENTRY_BYTES = 384
 
 class ResidentExpertsStruct(ctypes.Structure):
     """zipmoe_resident_experts."""
-    _fields_ = [("n_experts", _u32), ("hidden", _u32), ("inter", _u32), ("even", _u32), ("table", _vp), ("maps", ctypes.c_uint8 * 1152)]
+    _fields_ = [("n_experts", _u32), ("hidden", _u32), ("inter", _u32), ("even", _u32), ("table", _vp), ("maps", ctypes.c_uint8 * 1152),
+                ("grid", _u32), ("reserved", _u32)]
 
 
 # zipmoe_norm_args and zipmoe_route_args, packed in one go (a call with one pointer costs a sixth of one with 17 arguments)

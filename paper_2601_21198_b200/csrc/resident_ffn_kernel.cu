@@ -921,7 +921,8 @@ extern "C" zipmoe_status zipmoe_resident_experts_plan(const uint16_t *const *ten
   static_assert(sizeof(CUtensorMap) == kSlicedMap && 3 * sizeof(CUtensorMap) == ZIPMOE_RESIDENT_ENTRY_BYTES, "an entry is three tensor maps");
   const uint64_t bytes = 2ull * hidden * inter;
   uint32_t R1, S1, R2, S2;
-  zipmoe_host::resident_few_rows(hidden, inter, resident_grid(), &R1, &S1, &R2, &S2);
+  const uint32_t grid = resident_grid();
+  zipmoe_host::resident_few_rows(hidden, inter, grid, &R1, &S1, &R2, &S2);
   // both maps of n tensors of kind j (0 w1, 1 w3, 2 w2), `distance` bytes apart
   auto describe = [&](uint8_t *to, const uint16_t *base, uint32_t j, uint64_t n, uint64_t distance) {
     const uint32_t rows = j < 2 ? inter : hidden, cols = j < 2 ? hidden : inter;
@@ -944,6 +945,7 @@ extern "C" zipmoe_status zipmoe_resident_experts_plan(const uint16_t *const *ten
   experts->n_experts = n_experts;
   experts->hidden = hidden;
   experts->inter = inter;
+  experts->grid = grid;
   // evenly spaced experts: one map per kind of tensor serves them all (distances that a map can hold)
   uint64_t distance[3];
   bool even = true;
@@ -1014,6 +1016,8 @@ extern "C" zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, c
       ((reinterpret_cast<uintptr_t>(topk_ids) | reinterpret_cast<uintptr_t>(topk_weights) | reinterpret_cast<uintptr_t>(status_word)) & 3))
     return ZIPMOE_ERR_INVALID_ARG;
   if (workspace_bytes < p.total) return ZIPMOE_ERR_BUFFER_TOO_SMALL;
+  // (other boxes than those of the plan's maps: the barriers would wait for bytes that never come)
+  if (ex->grid != p.grid || ex->reserved) return ZIPMOE_ERR_INVALID_ARG;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return ZIPMOE_ERR_CUDA;
   if (!g_resident_dev[dev].ready) {

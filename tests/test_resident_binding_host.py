@@ -116,3 +116,17 @@ def test_streams_of_another_device_are_refused(zb, monkeypatch):
         with pytest.raises(ValueError):
             call(stream=FakeStream(0))
     assert not devices.seen
+
+
+@pytest.mark.parametrize("grid", [0, 1, 1 << 30])
+def test_a_plan_for_a_device_of_another_size_is_refused(zb, grid):
+    """The boxes that a plan's tensor maps bring in follow the number of SMs: a call that takes other boxes would wait for
+    bytes that never come.  (No device has one SM or none of them, so nothing is launched here, wherever this runs.)"""
+    A = 1 << 20
+    for T in (4, 40):
+        ex = zb.ResidentExpertsStruct(4, 64, 128, 0, A)
+        ex.grid = grid
+        n = zb.zipmoe_expert_ffn_workspace_bytes(T, 2, ex)
+        with pytest.raises(zb.ZipMoEError) as err:
+            zb.zipmoe_expert_ffn(A, T, A, A, 2, ex, A, A, n)
+        assert err.value.status == zb.ERR_INVALID_ARG
