@@ -12,6 +12,7 @@ import ctypes
 import os
 import struct
 import threading
+import weakref
 
 import numpy as np
 
@@ -739,6 +740,53 @@ class Router:
         return ids, weights
 
 
+class _Scratch:
+    """The workspaces of zipmoe_expert_ffn on one device, shared by all layers there: one per stream, as large as the
+    largest call so far (a call leaves its workspace ready for the next one, whatever the sizes of either), and, while a
+    stream is being captured, one for that capture alone, which only the graph's replays prepare."""
+
+    def __init__(self, device):
+        self.kinds, self.device, self.lock = _get_kinds(), device, threading.Lock()
+        self.own, self.captured = {}, {}      # stream handle -> workspace; stream handle -> (capture, workspace)
+
+    def get(self, need, handle, stream):
+        if (stream is not None or self.kinds.capturing()) and (capture := zipmoe_stream_capture_id(handle)):
+            # its memory comes from the graph's pool, which lives as long as the graph: it is kept here for the rest of
+            # the capture only
+            with self.lock:
+                of, ws = self.captured.get(handle, (0, None))
+                if of != capture or ws.numel() < need:
+                    ws = self._prepared(need, handle, stream)
+                    self.captured[handle] = capture, ws
+                return ws
+        ws = self.own.get(handle)
+        if ws is None or ws.numel() < need:
+            with self.lock:
+                ws = self.own.get(handle)
+                if ws is None or ws.numel() < need:
+                    self.own.pop(handle, None)      # back to the stream's pool: what is queued there comes before its next use
+                    del ws
+                    ws = self.own[handle] = self._prepared(need, handle, stream)
+        return ws
+
+    def _prepared(self, need, handle, stream):
+        ws = _empty(need, self.kinds.e4m3[1], self.device, stream)
+        zipmoe_expert_ffn_workspace_init(ws, need, handle)
+        return ws
+
+
+_scratch, _scratch_lock = weakref.WeakValueDictionary(), threading.Lock()
+
+
+def _scratch_of(device, index):
+    """The device's workspaces; they go with the last layer that holds them."""
+    with _scratch_lock:
+        found = _scratch.get(index)
+        if found is None:
+            found = _scratch[index] = _Scratch(device)
+        return found
+
+
 class ResidentExperts:
     """Recovered experts of one layer: tensors[3*e + j] (j: 0 w1 [inter, hidden], 1 w3, 2 w2 [hidden, inter]) are dense
     bf16 (or int16 pattern) device tensors, for example the slices of a DevicePlan.decode output."""
@@ -764,8 +812,7 @@ class ResidentExperts:
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self.status_at = self.status.data_ptr()
         self._struct_at = ctypes.byref(self.struct)
-        self._ws, self._captured, self._need = {}, {}, {}
-        self._lock = threading.Lock()
+        self._scratch, self._need = _scratch_of(self.device, self.index), {}
 
     @classmethod
     def from_decode(cls, plan, out, hidden, inter):
@@ -773,34 +820,13 @@ class ResidentExperts:
         return cls([plan.tensor_slice(out, i) for i in range(len(plan.infos))], hidden, inter)
 
     def _workspace(self, T, k, handle, stream):
-        """A workspace large enough for T tokens with k experts each: the stream's own, or, while the stream is being
-        captured, one that belongs to that capture alone: only the graph's replays prepare it.  Its memory comes from the
-        graph's pool, which lives as long as the graph, so it is kept here for the rest of the capture only."""
+        """A workspace large enough for T tokens with k experts each."""
         need = self._need.get((T, k))
         if need is None:
-            fits = T if T > 128 else 1 << max(T - 1, 15).bit_length()      # some more tokens than asked for: it seldom grows
-            need = self._need[(T, k)] = zipmoe_expert_ffn_workspace_bytes(min(fits, 256) if T <= 256 else T, k, self.struct)
-        capture = 0
-        if stream is not None or self.kinds.capturing():
-            capture = zipmoe_stream_capture_id(handle)
-        if capture:
-            of, held = self._captured.get(handle, (0, None))
-            if of != capture or held.numel() < need:
-                held = self._prepared(need, handle, stream)
-                self._captured[handle] = capture, held
-            return held
-        held = self._ws.get(handle)
-        if held is None or held[-1].numel() < need:
-            with self._lock:
-                held = self._ws.get(handle, [])
-                if not held or held[-1].numel() < need:
-                    held = self._ws[handle] = held + [self._prepared(need, handle, stream)]
-        return held[-1]
-
-    def _prepared(self, need, handle, stream):
-        ws = _empty(need, self.kinds.e4m3[1], self.device, stream)
-        zipmoe_expert_ffn_workspace_init(ws, need, handle)
-        return ws
+            # some more tokens than asked for, in few steps: a workspace seldom grows
+            fits = T if T > 256 else 256 if T > 128 else 1 << max(T - 1, 15).bit_length()
+            need = self._need[(T, k)] = zipmoe_expert_ffn_workspace_bytes(fits, k, self.struct)
+        return self._scratch.get(need, handle, stream)
 
     def ffn(self, tokens, topk_ids, topk_weights, out=None, stream=None):
         """tokens [T, hidden] bf16 (or int16 patterns), topk_ids [T, k] int32, topk_weights [T, k] float32 or None: device

@@ -135,3 +135,85 @@ def test_graphs_replayed_on_two_streams_do_not_meet(zb, weights):
         torch.cuda.synchronize()
         assert all(torch.equal(c[3], w) for c, w in zip(calls, want))
     assert int(ex.status.item()) == 0
+
+
+def held_for(fn):
+    """Device memory that is in use after fn() beyond what was in use before, and what it returned."""
+    import gc
+    import torch
+    gc.collect()
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    kept = fn()
+    gc.collect()
+    torch.cuda.synchronize()
+    return torch.cuda.memory_allocated() - before, kept
+
+
+def test_scratch_is_one_workspace_per_stream_whatever_the_batches_and_layers(zb, weights):
+    import torch
+    T_max = 256
+    tok, ids = torch.zeros(T_max, H, dtype=torch.int16, device="cuda"), torch.zeros(T_max, K, dtype=torch.int32, device="cuda")
+    out = torch.empty(T_max, H, dtype=torch.int16, device="cuda")
+    first = zb.ResidentExperts(weights, H, I)
+    largest = zb.zipmoe_expert_ffn_workspace_bytes(T_max, K, first.struct)
+
+    def rising(ex):
+        for T in list(range(1, 17)) + list(range(17, 129, 13)) + list(range(129, T_max + 1)):
+            ex.ffn(tok[:T], ids[:T], None, out[:T])
+
+    def other_layers():
+        layers = [zb.ResidentExperts(weights, H, I) for _ in range(5)]
+        for ex in layers:
+            rising(ex)
+        return layers
+
+    of_one, _ = held_for(lambda: rising(first))
+    assert largest <= of_one <= largest + (2 << 20)
+    of_more, layers = held_for(other_layers)
+    assert of_more <= 1 << 20                                    # their tables and status words
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+
+    def on_another_stream():
+        with torch.cuda.stream(side):
+            rising(first)
+            rising(layers[0])
+        side.synchronize()
+
+    of_stream, _ = held_for(on_another_stream)
+    assert largest <= of_stream <= largest + (2 << 20)
+    assert int(first.status.item()) == 0 and all(int(ex.status.item()) == 0 for ex in layers)
+
+
+def test_scratch_is_given_back_with_the_last_layer(zb, weights):
+    import torch
+
+    def life():
+        ex = zb.ResidentExperts(weights, H, I)
+        T = 200
+        ex.ffn(torch.zeros(T, H, dtype=torch.int16, device="cuda"), torch.zeros(T, K, dtype=torch.int32, device="cuda"), None)
+        torch.cuda.synchronize()
+        del ex
+
+    of_life, _ = held_for(life)
+    assert of_life <= 0
+
+
+def test_layers_of_different_sizes_share_a_workspace(zb):
+    """Calls of a large and a small layer in turn, few tokens and many: each leaves the workspace ready for the other."""
+    import torch
+    layers = []
+    for E2, H2, I2 in ((6, 512, 384), (3, 264, 1000)):
+        ws = [dev(inputs.gaussian((I2, H2) if j % 3 < 2 else (H2, I2), 0.05, 700 + j)) for j in range(3 * E2)]
+        calls = []
+        for T in (5, 130, 30, 2):
+            ids, wts = inputs.routing(T, n_experts=E2, k=2, seed=T)
+            calls.append((dev(inputs.tokens(T, H2, seed=T)), dev(ids), dev(wts)))
+        layers.append((zb.ResidentExperts(ws, H2, I2), calls))
+    want = [[ex.ffn(*c) for c in calls] for ex, calls in layers]
+    for _ in range(3):
+        for i in range(4):
+            for (ex, calls), w in zip(layers, want):
+                assert torch.equal(ex.ffn(*calls[i]), w[i])
+    assert all(int(ex.status.item()) == 0 for ex, _ in layers)
