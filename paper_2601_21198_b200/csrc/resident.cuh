@@ -3,6 +3,7 @@
 #include <cstdint>
 
 #include "zipmoe.h"
+#include "resident_choice.h"
 #include "tensor_core.cuh"
 
 namespace zipmoe_dev {
@@ -94,8 +95,6 @@ struct ResidentCall {
   uint32_t T, k, E, H, I, grid, extra_tx;
   int device;
 };
-// rows of W1 and of W2 that a block of that kernel owns, and takes at once (the box rows of the sliced maps)
-void resident_few_rows(uint32_t H, uint32_t I, uint32_t grid, uint32_t *R1, uint32_t *S1, uint32_t *R2, uint32_t *S2);
 zipmoe_status launch_resident_few(const ResidentCall &c, cudaStream_t stream);
 
 }  // namespace zipmoe_host

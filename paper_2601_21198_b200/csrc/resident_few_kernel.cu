@@ -414,14 +414,6 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
 
 namespace zipmoe_host {
 
-void resident_few_rows(uint32_t H, uint32_t I, uint32_t grid, uint32_t *R1, uint32_t *S1, uint32_t *R2, uint32_t *S2) {
-  auto up = [](uint32_t v, uint32_t d) { return (v + d - 1) / d; };
-  *R1 = up(I, grid);
-  *S1 = up(*R1, up(*R1, 16));
-  *R2 = up(H, grid);
-  *S2 = up(*R2, up(*R2, 32));
-}
-
 zipmoe_status launch_resident_few(const ResidentCall &c, cudaStream_t stream) {
   using namespace zipmoe_dev;
   FewArgs a;

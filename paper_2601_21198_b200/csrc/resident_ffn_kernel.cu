@@ -847,20 +847,6 @@ bool dims_ok(uint32_t E, uint32_t H, uint32_t I) {
          I <= kResidentMaxDim;
 }
 
-// Whether a block's whole rows are the faster way for few tokens.  They save 10 us of a call, but a chunk of 512 columns takes
-// a block 0.43 us however few rows it has; where that is longer than its bytes take, experts cost what is over.  8 tokens,
-// whole rows against shares: 8 experts of 2048 x 1408 34 against 41 us, 30 of them 96 against 90; 30 of 3008 x 1536 126 against
-// 137; 30 of 4096 x 256 118 against 50; 60 of 1024 x 512 111 against 47, but 8 of them (one token) 23 against 26.  (A second
-// column of eight tokens was built and taken out: 16 tokens, 16 experts of 1096 x 904: 60 us against 44.)
-bool whole_rows_pay(uint32_t choices, uint32_t E, uint32_t H, uint32_t I, uint32_t grid) {
-  uint32_t R1, S1, R2, S2;
-  zipmoe_host::resident_few_rows(H, I, grid, &R1, &S1, &R2, &S2);
-  const uint64_t chunks = (uint64_t)((R1 + S1 - 1) / S1) * std::max(1u, (H / 64 + 7) / 8) +
-                          (uint64_t)((R2 + S2 - 1) / S2) * std::max(1u, (I / 64 + 7) / 8);
-  const uint64_t chunk_ns = 430 * chunks, byte_ns = 6ull * H * I / 6464;   // of an expert
-  return chunk_ns <= byte_ns || std::min(choices, E) * (chunk_ns - byte_ns) <= 10000;
-}
-
 struct ResidentDevice {
   int sms = 0;
   bool ready = false;
@@ -1032,7 +1018,7 @@ extern "C" zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, c
   uint32_t tries = 0, extra_tx = 0;
   zipmoe_host::wait_fault_setting(&extra_tx, &tries);
   const uint64_t limit_ns = tries < zipmoe_host::kWaitTries ? 1000000ull : 1000000000ull;   // (1 ms in the tests of the limit)
-  if (T <= kResFewT && whole_rows_pay(T * k, ex->n_experts, ex->hidden, ex->inter, p.grid)) {
+  if (T <= kResFewT && zipmoe_host::whole_rows_pay(T * k, ex->n_experts, ex->hidden, ex->inter, p.grid)) {
     zipmoe_host::ResidentCall c;
     c.tokens = tokens;
     c.ids = topk_ids;
