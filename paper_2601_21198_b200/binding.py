@@ -789,7 +789,7 @@ def _scratch_of(device, index):
 
 class ResidentExperts:
     """Recovered experts of one layer: tensors[3*e + j] (j: 0 w1 [inter, hidden], 1 w3, 2 w2 [hidden, inter]) are dense
-    bf16 (or int16 pattern) device tensors, for example the slices of a DevicePlan.decode output."""
+    bf16 (or int16 pattern) device tensors of these shapes or flat, for example the slices of a DevicePlan.decode output."""
 
     def __init__(self, tensors, hidden, inter):
         import torch
@@ -799,9 +799,8 @@ class ResidentExperts:
         self.index = _device_of("tensor 0", tensors[0])
         addresses = []
         for i, t in enumerate(tensors):
-            if t.numel() != hidden * inter:
-                raise ValueError("tensor %d: %d elements, wanted %d x %d" % (i, t.numel(), hidden, inter))
-            addresses.append(_dense("a weight", t, t.shape, self.kinds.bf16, self.index))
+            shape = (hidden * inter,) if len(t.shape) == 1 else (hidden, inter) if i % 3 == 2 else (inter, hidden)
+            addresses.append(_dense("tensor %d" % i, t, shape, self.kinds.bf16, self.index))
         self.tensors = list(tensors)      # the experts' memory is theirs: keep it while the table points at it
         self.device = tensors[0].device
         self.hidden, self.inter = hidden, inter

@@ -130,3 +130,27 @@ def test_a_plan_for_a_device_of_another_size_is_refused(zb, grid):
         with pytest.raises(zb.ZipMoEError) as err:
             zb.zipmoe_expert_ffn(A, T, A, A, 2, ex, A, A, n)
         assert err.value.status == zb.ERR_INVALID_ARG
+
+
+def test_experts_of_another_orientation_are_refused(zb, monkeypatch):
+    """w1 and w3 are [inter, hidden] and w2 is [hidden, inter]: a matrix the other way round has as many elements and would
+    be read as something else.  Flat tensors (slices of a decode launch's output) have no orientation."""
+    import torch
+    devices = FakeDevices(zb, monkeypatch)
+    hidden, inter = 64, 128
+
+    def tensors(change=None):
+        shapes = [(inter, hidden), (inter, hidden), (hidden, inter)] * 2
+        if change is not None:
+            shapes[change] = shapes[change][::-1]
+        return [FakeTensor(s, torch.bfloat16, 0) for s in shapes]
+
+    zb.ResidentExperts(tensors(), hidden, inter)
+    zb.ResidentExperts([FakeTensor((hidden * inter,), torch.int16, 0) for _ in range(6)], hidden, inter)
+    del devices.seen[:]
+    for i in range(6):
+        with pytest.raises(ValueError):
+            zb.ResidentExperts(tensors(i), hidden, inter)
+    with pytest.raises(ValueError):
+        zb.ResidentExperts([FakeTensor((4, hidden * inter // 4), torch.bfloat16, 0)] + tensors()[1:], hidden, inter)
+    assert not devices.seen
