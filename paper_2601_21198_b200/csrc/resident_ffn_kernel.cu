@@ -274,7 +274,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
   const uint32_t w_ring = smem_addr(ring), x_ring = w_ring + n_w * kResStageA;
   const uint32_t acc_bufs = N <= 128 ? 2 : 1;                // two accumulators of N columns each, of 512 columns
   Phase ph[4];
-    const bool two_groups = (uint64_t)n_active * a.H * a.I * 6 >= (words[4] > kResEvenTokens ? kResTwoGroupsMany : kResTwoGroups);
+  const bool two_groups = (uint64_t)n_active * a.H * a.I * 6 >= (words[4] > kResEvenTokens ? kResTwoGroupsMany : kResTwoGroups);
   const uint32_t n_first = two_groups ? (n_active + 1) / 2 : n_active;
 #pragma unroll
   for (uint32_t p = 0; p < 4; ++p) {
@@ -299,19 +299,16 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
 
   if (warp == 0) {
     // ---- weights ----
-    // the tensor maps of the share's experts, four of each phase: one lane each makes its map visible to the copies
-    constexpr uint32_t kMaps = 4;
+    // the tensor maps of the share's experts, eight lanes for each phase: every map is made visible to the copies once
     if (!a.even) {
-      const uint32_t p = lane >> 3, r = lane & 7;
+      const uint32_t p = lane >> 3;
       const Phase f = p == 0 ? ph[0] : p == 1 ? ph[1] : p == 2 ? ph[2] : ph[3];
-      const uint32_t u = first(f), end = last(f);
-      if (u < end) {
-        const uint32_t per = f.KS * f.RB, ja = u / per + (r >> 1);
-        if (ja <= (end - 1) / per && (p < 2 || (r & 1) == 0)) {
-          const uint8_t *m = wide_map(a.table, act[f.a0 + ja].e, p < 2 ? (r & 1) : 2);
-          acquire_map(m);
-          prefetch_map(m);
-        }
+      const uint32_t u = first(f), end = last(f), per = f.KS * f.RB, kinds = p < 2 ? 2 : 1;
+      const uint32_t maps = u < end ? ((end - 1) / per - u / per + 1) * kinds : 0;
+      for (uint32_t r = lane & 7; r < maps; r += 8) {
+        const uint8_t *m = wide_map(a.table, act[f.a0 + u / per + r / kinds].e, p < 2 ? (r & 1) : 2);
+        acquire_map(m);
+        prefetch_map(m);
       }
     }
     __syncwarp();
@@ -325,7 +322,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
       for (uint32_t p = 0; p < 4 && ok; ++p) {
         const Phase f = p == 0 ? ph[0] : p == 1 ? ph[1] : p == 2 ? ph[2] : ph[3];
         uint32_t u = first(f);
-        const uint32_t end = last(f), a_first = f.a0 + (u < end ? u / (f.KS * f.RB) : 0);
+        const uint32_t end = last(f);
         Piece q;
         while (ok && next_piece(f, u, end, q)) {
           const uint32_t e = act[q.a].e;
@@ -336,10 +333,6 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
             m1 = &even.w[p < 2 ? 1 : 2];
           }
           const int32_t y0 = (int32_t)(q.rb * (p < 2 ? 128 : 256)), y1 = p < 2 ? y0 : y0 + 128;
-          if (!a.even && q.a >= a_first + kMaps) {
-            acquire_map(m0);
-            acquire_map(m1);
-          }
           for (uint32_t s = q.s0; s < q.s0 + q.n; ++s) {
             if (issued++ >= in_flight) {
               ok = wait_bar(w_full + 8 * behind.st, behind.round & 1, lim);
