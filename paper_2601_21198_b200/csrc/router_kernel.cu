@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(kRouterThreads) router_kernel(const __grid_con
   volatile uint32_t *dead = words + 1;
   const WaitLimit lim = {dead, a.status, a.limit_ns};
   const uint32_t t0 = (blockIdx.x / S) * kRouterRows, rows = min(kRouterRows, a.T - t0);
-  const uint32_t steps = (a.H + 63) / 64, s0 = rank * steps / S, s1 = (rank + 1) * steps / S;
+  const uint32_t steps = (a.H + 63) / 64, s0 = rank * steps / S, s1 = (rank + 1) * steps / S;   // at least one: S <= steps
 
   if (tid == 0) {
     for (uint32_t s = 0; s < a.stages; ++s) {
@@ -222,15 +222,12 @@ __global__ void __launch_bounds__(kRouterThreads) router_kernel(const __grid_con
   const uint32_t row = 32 * (warp & 3) + lane;
   if (ok && 32 * (warp & 3) < rows) {
     for (uint32_t c = 8 * (warp >> 2); c < a.N; c += 16) {
-      uint32_t v[8] = {};
-      if (s1 > s0) {
-        tmem_load8(tmem + ((32 * (warp & 3)) << 16) + c, v);
-        tmem_wait();
-      }
+      uint32_t v[8];
+      tmem_load8(tmem + ((32 * (warp & 3)) << 16) + c, v);
+      tmem_wait();
       float4 *to = reinterpret_cast<float4 *>(part + row * pitch + c);
-      const bool any = s1 > s0;
-      to[0] = any ? make_float4(__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]), __uint_as_float(v[3])) : make_float4(0.f, 0.f, 0.f, 0.f);
-      to[1] = any ? make_float4(__uint_as_float(v[4]), __uint_as_float(v[5]), __uint_as_float(v[6]), __uint_as_float(v[7])) : make_float4(0.f, 0.f, 0.f, 0.f);
+      to[0] = make_float4(__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]), __uint_as_float(v[3]));
+      to[1] = make_float4(__uint_as_float(v[4]), __uint_as_float(v[5]), __uint_as_float(v[6]), __uint_as_float(v[7]));
     }
   }
   __syncwarp();
