@@ -393,17 +393,6 @@ __global__ void __launch_bounds__(512, 2) add_rmsnorm_wide_kernel(const NormArgs
 
 namespace {
 
-int norm_sms() {
-  static int sms[64];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
-  if (sms[dev] == 0) {
-    int n = 0;
-    sms[dev] = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && n > 0 ? n : 148;
-  }
-  return sms[dev];
-}
-
 cudaError_t launch(void (*kernel)(zipmoe_dev::NormArgs), uint32_t blocks, uint32_t warps, const zipmoe_dev::NormArgs &a, cudaStream_t stream) {
   const cudaLaunchAttribute overlapped = zipmoe_host::overlapped();
   cudaLaunchConfig_t cfg = {};
@@ -420,7 +409,7 @@ cudaError_t launch(void (*kernel)(zipmoe_dev::NormArgs), uint32_t blocks, uint32
 template <typename Res, bool kAligned, int kScales>
 cudaError_t launch_sizes(const zipmoe_dev::NormArgs &a, cudaStream_t stream) {
   using namespace zipmoe_dev;
-  const uint32_t segments = (a.cols + 255) / 256, sms = norm_sms();
+  const uint32_t segments = (a.cols + 255) / 256, sms = zipmoe_host::current_sms();
   auto grid = [&](uint32_t warps) { return (uint32_t)std::min<uint64_t>(a.rows, (uint64_t)sms * std::min(32u, 32 / warps)); };
   if (segments > (kAligned ? 64 : 32)) {
     const uint32_t per_warp = (segments + 15) / 16, warps = (segments + per_warp - 1) / per_warp;

@@ -840,23 +840,9 @@ bool dims_ok(uint32_t E, uint32_t H, uint32_t I) {
          I <= kResidentMaxDim;
 }
 
-struct ResidentDevice {
-  int sms = 0;
-  bool ready = false;
-};
-ResidentDevice g_resident_dev[64];
+bool g_resident_ready[64];
 
-// SMs of the current device; 148 where there is none (a host-only size query)
-uint32_t resident_grid() {
-  int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < 64) {
-    if (g_resident_dev[dev].sms == 0 && cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess)
-      g_resident_dev[dev].sms = sms;
-    if (g_resident_dev[dev].sms > 0) return std::min<uint32_t>((uint32_t)g_resident_dev[dev].sms, zipmoe_dev::kResMaxGrid);
-  }
-  (void)cudaGetLastError();   // no device: not an error for a size query
-  return 148;
-}
+uint32_t resident_grid() { return std::min(zipmoe_host::current_sms(), zipmoe_dev::kResMaxGrid); }
 
 struct ResidentPlan {
   uint32_t grid, tmem_cols, ring, smem;
@@ -999,13 +985,13 @@ extern "C" zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, c
   if (ex->grid != p.grid || ex->reserved) return ZIPMOE_ERR_INVALID_ARG;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return ZIPMOE_ERR_CUDA;
-  if (!g_resident_dev[dev].ready) {
+  if (!g_resident_ready[dev]) {
     int major = 0;
     if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) return ZIPMOE_ERR_CUDA;
     if (major != 10) return ZIPMOE_ERR_UNSUPPORTED;
     if (cudaFuncSetAttribute(resident_ffn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024) != cudaSuccess)
       return ZIPMOE_ERR_CUDA;
-    g_resident_dev[dev].ready = true;
+    g_resident_ready[dev] = true;
   }
   uint8_t *ws = static_cast<uint8_t *>(workspace);
   uint32_t tries = 0, extra_tx = 0;

@@ -367,10 +367,10 @@ extern "C" zipmoe_status zipmoe_route(const zipmoe_route_args *r, zipmoe_stream 
   // two blocks per SM up to 128 experts, so that one streams while the other picks; then as many blocks per 128 tokens as
   // the device runs at once
   const uint32_t tiles = (T + kRouterRows - 1) / kRouterRows, steps = (hidden + 63) / 64, stage = (kRouterRows + a.N) * 128;
-  const uint32_t per_sm = a.N <= 128 ? 2 : 1;
+  const uint32_t per_sm = a.N <= 128 ? 2 : 1, at_once = zipmoe_host::current_sms() * per_sm;
   a.stages = std::min(kRouterMaxStages, (per_sm == 2 ? 108u : 216u) * 1024 / stage);
   uint32_t S = 8;
-  while (S > 1 && (S > steps || tiles * S > 148 * per_sm)) S >>= 1;
+  while (S > 1 && (S > steps || tiles * S > at_once)) S >>= 1;
   const uint32_t smem = 1024 + std::max(a.stages * stage, kRouterRows * (a.N + 4) * 4);
   CUtensorMap x_map, gate_map;
   if (!zipmoe_host::make_bf16_map(&x_map, r->tokens, T, hidden, r->token_pitch, kRouterRows, true) ||

@@ -174,6 +174,19 @@ __device__ __forceinline__ void arrive(uint32_t bar) {
 
 namespace zipmoe_host {
 
+// SMs of the current device; 148 where there is none (a host-only size query)
+inline uint32_t current_sms() {
+  static int known[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < 64) {
+    int sms = 0;
+    if (known[dev] == 0 && cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess) known[dev] = sms;
+    if (known[dev] > 0) return (uint32_t)known[dev];
+  }
+  (void)cudaGetLastError();
+  return 148;
+}
+
 inline cudaLaunchAttribute overlapped() {
   cudaLaunchAttribute a;
   a.id = cudaLaunchAttributeProgrammaticStreamSerialization;
