@@ -217,3 +217,36 @@ def test_layers_of_different_sizes_share_a_workspace(zb):
             for (ex, calls), w in zip(layers, want):
                 assert torch.equal(ex.ffn(*calls[i]), w[i])
     assert all(int(ex.status.item()) == 0 for ex, _ in layers)
+
+
+def test_a_decode_step_of_several_layers_in_one_graph(zb, weights):
+    """Norm, router and experts of three layers, captured without a call before it, replayed on new inputs: the launches that
+    are set up while their predecessors drain keep their order inside a graph too."""
+    import torch
+    T = 7
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    bf16 = dict(dtype=torch.bfloat16, device="cuda")
+    layers = [(zb.RmsNorm((1 + 0.1 * torch.randn(H, generator=g, device="cuda")).to(torch.bfloat16)),
+               zb.Router((0.05 * torch.randn(E, H, generator=g, device="cuda")).to(torch.bfloat16), K),
+               zb.ResidentExperts(weights, H, I)) for _ in range(3)]
+    x, residual = torch.zeros(T, H, **bf16), torch.zeros(T, H, **bf16)
+
+    def step(x, residual):
+        for norm, router, experts in layers:
+            h = norm.add_norm(x, residual, residual)
+            ids, wts = router.route(h)
+            x = experts.ffn(h, ids, wts)
+        return x
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = step(x, residual)
+    for _ in range(10):
+        new_x, new_residual = (torch.randn(T, H, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+        x.copy_(new_x)
+        residual.copy_(new_residual)
+        graph.replay()
+        want = step(new_x, new_residual)
+        assert torch.equal(y, want) and torch.equal(residual, new_residual)
+    assert all(int(router.status.item()) == 0 and int(experts.status.item()) == 0 for _, router, experts in layers)
