@@ -347,11 +347,12 @@ typedef struct {
  *     y = h / sqrt(mean(h^2) + eps) * weight (from the unrounded h, in fp32)
  *     out = bf16(y)
  *     scales = max |y| / 448 over the row, or over each `group` columns of it;  out_q = e4m3(y / scale)
- * A group of zeros has scale 0 and zeros (in a row that has a norm); q * scale gives the row back.  One launch on `stream`, asynchronous;
- * every input is read once.  A row whose sum of squares exceeds fp32 (elements of about 1e19) gives zeros, as the
- * formula in fp32 does (with a scale of a whole row NaN, where h * weight itself exceeds fp32); NaN and infinities
- * come out as NaN.  With eps = 0 a row whose sum of squares is zero, or below fp32's smallest normal number 1.2e-38, has
- * no norm: zeros come out as NaN, other elements as infinities, with scales that are not finite.
+ * A group of zeros has scale 0 and zeros (in a row that has a norm); q * scale gives the row back.  One launch on
+ * `stream`, asynchronous; every input is read once, rows of more than 16384 columns (8192 where rows or weight do not all
+ * start and end on 16-byte boundaries) twice.  A row whose sum of squares exceeds fp32 (elements of about 1e19) gives
+ * zeros, as the formula in fp32 does (with a scale of a whole row NaN, where h * weight itself exceeds fp32); NaN and
+ * infinities come out as NaN.  With eps = 0 a row whose sum of squares is zero, or below fp32's smallest normal number
+ * 1.2e-38, has no norm: zeros come out as NaN, other elements as infinities, with scales that are not finite.
  * group     : 32, 64, 128 or 256 columns; 0, or any value >= cols, is the whole row.
  * Pitches are at least cols.  Any element alignment; rows and weight that start on 16-byte boundaries are faster.
  * rows = 0 does nothing.  Limits: cols <= 32768 (ZIPMOE_ERR_UNSUPPORTED otherwise). */
