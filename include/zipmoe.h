@@ -430,8 +430,10 @@ zipmoe_status zipmoe_stream_capture_id(zipmoe_stream stream, uint64_t *capture_i
 /* Expert execution on recovered weights (Section 3.3: the GPU work p_n of the tokens routed to expert n, for experts
  * found in pool F): what zipmoe_decode_expert_ffn computes, from bf16 tensors.  For every token t and choice j with
  * e = topk_ids[t, j]:
- *     g = W1_e x_t,  u = W3_e x_t,  h = bf16(SiLU(g) * u),  y = W2_e h
+ *     g = W1_e x_t,  u = W3_e x_t,  h = SiLU(g) * u,  y = W2_e h
  *     out[t] = bf16( sum_j topk_weights[t, j] * y )
+ * with fp32 sums and 16 significant bits of h (which enters W2's product as the sum of two bf16 numbers; the call on
+ * compressed experts rounds it to one).
  * A negative id is no expert (zipmoe_route writes -1) and adds nothing; a token without experts gets zeros.  An id
  * of n_experts or more adds nothing either and sets status_word (code 1).  An expert listed twice by a token counts
  * with both weights.  Weights are read once for all tokens of the call, and only those of experts that have tokens.

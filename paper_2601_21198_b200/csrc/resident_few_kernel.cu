@@ -1,5 +1,5 @@
 // The resident experts for at most 8 tokens, where a call is short enough for every hand-over between blocks to show.
-//     g = W1 x,  u = W3 x,  h = bf16(SiLU(g) * u),  y = W2 h,  out[t] = bf16(sum_j w[t, j] * y)
+//     g = W1 x,  u = W3 x,  h = SiLU(g) * u,  y = W2 h,  out[t] = bf16(sum_j w[t, j] * y)
 // Bound: the active experts' weights, 6 * hidden * inter bytes each, read once; beyond that the latency of a call.
 //
 // Every block owns a slice of rows - inter / SMs rows of every W1 and W3, hidden / SMs rows of every W2 - and all of their
@@ -11,16 +11,17 @@
 //     its own, through an ordinary map.  (One bulk copy per row and 1 KB was tried: the copy engine takes 38 ns for each,
 //     4 TB/s.  Loads into registers were tried: 12 warps with 16 loads in flight each, 4.8 TB/s.)
 //     It runs ahead across experts, and asks the first chunks of W2 into the second-level cache before h is there.
-//   * Another warp adds the same columns of the expert's tokens (x, then h).
+//   * Another warp adds the same columns of the expert's tokens (x, then h, which is the sum of two bf16 numbers).
 //   * Eight warps take the chunk's 16-column steps in turn: ldmatrix, mma.sync m16n8k16 (weights the 16 rows, tokens the 8
-//     columns; fp32 sums in registers).  With so few tokens these need a tenth of the issue slots of the time that the
+//     columns; fp32 sums in registers).  The second numbers of h are columns 4 to 7 where an expert has up to 4 tokens (one
+//     product for both), and otherwise go through a second product.  With so few tokens these need a tenth of the issue slots of the time that the
 //     bytes take; a tcgen05 operand of 128 rows would be nine tenths empty with 10 to 28 rows per block.
 //   * At the end of a job (one expert's set of rows) they leave their partial sums in shared memory and go on; four more
 //     warps add them and finish the job.
-// One token, 2 experts of 4096 x 14336 (705 MB): 107 us, 6.6 TB/s, what a plain copy moves; 6 experts of 2048 x 1408
-// (104 MB): 27.5 us, 3.8 TB/s; 8 tokens, 30 of 3008 x 1536 (832 MB): 126 us, 6.6 TB/s; 4 experts of 1024 x 512 (13 MB): 16 us, the
+// One token, 2 experts of 4096 x 14336 (705 MB): 108 us, 6.5 TB/s, what a plain copy moves; 6 experts of 2048 x 1408
+// (104 MB): 28.0 us, 3.7 TB/s; 8 tokens, 30 of 3008 x 1536 (832 MB): 128 us, 6.5 TB/s; 4 experts of 1024 x 512 (13 MB): 16 us, the
 // latencies of a call: routing lists, the first weights, h seen by all, the last sums.
-// A chunk takes a block 0.43 us even if it has 4 rows (more stages change nothing), so many experts with narrow slices are
+// A chunk takes a block 0.42 us even if it has 4 rows (more stages change nothing), so many experts with narrow slices are
 // left to the other kernel.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -35,8 +36,10 @@ namespace zipmoe_dev {
 
 constexpr uint32_t kFewThreads = 64 + 256 + 128;       // weights, activations, eight warps of products, four of sums
 constexpr uint32_t kFewCols = 512, kFewRowBytes = kFewCols * 2;
-constexpr uint32_t kFewPitch = kFewRowBytes + 16;      // of a token's columns: eight tokens' words fall into different banks
-constexpr uint32_t kFewTokenBytes = 9 * 1024;          // eight of them
+// Bytes between tokens' columns, of x and of h (whose second numbers follow the first): eight tokens' words fall into different
+// banks.
+constexpr uint32_t kFewPitch = kFewRowBytes + 16, kFewPitchH = 2 * kFewRowBytes + 16;
+constexpr uint32_t kFewOneProduct = 4;                 // up to so many tokens both numbers of h are columns of one product
 constexpr uint32_t kFewAheadBytes = 192 * 1024;        // of W2 that a block asks into the cache before h is there
 constexpr uint32_t kFewSumPitch = 20;                  // floats between the columns of a warp's 16 rows of sums: no bank conflicts
 
@@ -47,12 +50,12 @@ struct FewArgs {
   const uint8_t *table;
   uint16_t *out;
   ResidentSync *sync;
-  uint16_t *h;              // [choices][I]
+  uint16_t *h;              // [choices][2 * I]: chunk by chunk the two numbers that h is the sum of (place_of_h)
   uint32_t *status;
   uint64_t limit_ns;
   uint32_t T, k, E, H, I, even;
   uint32_t R1, S1, R2, S2;  // rows of a block, rows of a set: of W1 and W3, of W2
-  uint32_t stages, w_bytes, extra_tx;
+  uint32_t ring_bytes, w_bytes, extra_tx;
 };
 
 // shared memory: [ring][sums, two sets][outputs][active experts][masks][ids, weights][barriers, words]
@@ -77,6 +80,12 @@ __device__ __forceinline__ uint32_t load_b(uint32_t addr) {
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
   return v;
 }
+// Column i's first number of h among a row's 2 * I: every chunk has its first numbers, then its second ones (`cols` further).
+__device__ __forceinline__ uint32_t place_of_h(uint32_t i, uint32_t I, uint32_t &cols) {
+  const uint32_t whole = I & ~63u, c0 = i < whole ? i & ~(kFewCols - 1) : whole;
+  cols = i < whole ? min(kFewCols, whole - c0) : I - whole;
+  return c0 + i;
+}
 __device__ __forceinline__ uint32_t nth_bit(uint32_t mask, uint32_t n) {   // place of the n-th set bit (counted from 0)
   for (; n > 0; --n) mask &= mask - 1;
   return __ffs(mask) - 1;
@@ -86,9 +95,8 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
                                                                       const FewArgs a) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x, G = gridDim.x, choices = a.T * a.k;
-  const uint32_t stage_bytes = a.w_bytes + kFewTokenBytes;
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  uint8_t *ctl = smem + a.stages * stage_bytes;
+  uint8_t *ctl = smem + a.ring_bytes;
   float *sums = reinterpret_cast<float *>(ctl);                       // [2][8 warps][2][8][kFewSumPitch]
   ctl += 2 * kFewSumBytes;
   float *outs = reinterpret_cast<float *>(ctl);                       // [T][32]
@@ -102,7 +110,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
   float *wts = reinterpret_cast<float *>(ctl);
   ctl += pad16(choices * 4);
   uint64_t *bars = reinterpret_cast<uint64_t *>(ctl);
-  uint32_t *words = reinterpret_cast<uint32_t *>(bars + 2 * kResMaxStages + 4);   // unused, dead, active
+  uint32_t *words = reinterpret_cast<uint32_t *>(bars + 2 * kResMaxStages + 4);   // unused, dead, active, most
   volatile uint32_t *dead = words + 1;
   const uint32_t ring = smem_addr(smem), full = smem_addr(bars), empty = full + 8 * kResMaxStages, sums_full = empty + 8 * kResMaxStages, sums_empty = sums_full + 16;
   const WaitLimit lim = {dead, a.status, a.limit_ns};
@@ -117,7 +125,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
   else if (tid >= 96 && tid < 99 && ((tid < 98 ? a.H : a.I) & 63) != 0) prefetch_map(&rests.w[tid - 96]);
   for (uint32_t i = tid; i < a.E; i += kFewThreads) mask[i] = 0;
   if (tid == 0) {
-    for (uint32_t s = 0; s < a.stages; ++s) {
+    for (uint32_t s = 0; s < kResMaxStages; ++s) {
       mbar_init(full + 8 * s, 2);
       mbar_init(empty + 8 * s, 8);
     }
@@ -138,19 +146,24 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
   __syncthreads();
   if (warp == 0) {   // experts per * lane .. per * lane + per - 1
     const uint32_t per = (a.E + 31) / 32;
-    uint32_t cnt[8], sum = 0;   // active experts << 16 | choices
+    uint32_t cnt[8], sum = 0, most = 0;   // sum: active experts << 16 | choices
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
       cnt[i] = i < per && per * lane + i < a.E ? __popc(mask[per * lane + i]) : 0;
       sum += (cnt[i] ? 1u << 16 : 0) + cnt[i];
+      most = max(most, cnt[i]);
     }
+    most = __reduce_max_sync(0xFFFFFFFFu, most);
     uint32_t at = sum;
 #pragma unroll
     for (uint32_t d = 1; d < 32; d <<= 1) {
       const uint32_t p = __shfl_up_sync(0xFFFFFFFFu, at, d);
       if (lane >= d) at += p;
     }
-    if (lane == 31) words[2] = at >> 16;
+    if (lane == 31) {
+      words[2] = at >> 16;
+      words[3] = most;
+    }
     at -= sum;
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i)
@@ -162,6 +175,10 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
   __syncthreads();
   const bool prepared = magic == kResMagic;
   const uint32_t n_active = prepared ? words[2] : 0;
+  // a stage has room for as many tokens as an expert of this call has, and no less than for 8 tokens' x: with less, more stages
+  // are in flight, which only delays everybody else (one token, 2 experts of 4096 x 14336: 111 us instead of 108)
+  const uint32_t stage_bytes = a.w_bytes + (max(words[3] * kFewPitchH, 8 * kFewPitch) + 1023) / 1024 * 1024;
+  const uint32_t stages = min(kResMaxStages, a.ring_bytes / stage_bytes);
   // this block's rows, in sets; a phase's chunks run over experts, sets and columns (gate/up) or sets, experts and columns
   const uint32_t row0[2] = {min(a.I, cta * a.R1), min(a.H, cta * a.R2)}, row1[2] = {min(a.I, (cta + 1) * a.R1), min(a.H, (cta + 1) * a.R2)};
   const uint32_t sets[2] = {(row1[0] - row0[0] + a.S1 - 1) / a.S1, (row1[1] - row0[1] + a.S2 - 1) / a.S2};
@@ -210,7 +227,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
             mbar_expect_tx(bar, (p == 0 ? 2 : 1) * per_set * kFewRowBytes + a.extra_tx);
             tma_load_4d(dst, m0, 0, r0, (int32_t)(c / 64), z, bar, policy);
             if (p == 0) tma_load_4d(dst + per_set * kFewRowBytes, m1, 0, r0, (int32_t)(c / 64), z, bar, policy);
-            at.next(a.stages);
+            at.next(stages);
           }
           if (whole < K && ok) {
             if (at.round > 0 && !wait_bar(empty + 8 * at.st, (at.round - 1) & 1, lim)) {
@@ -221,7 +238,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
             mbar_expect_tx(bar, (p == 0 ? 2 : 1) * per_set * 128 + a.extra_tx);
             tma_load_3d(dst, rest_of(e, p == 0 ? 0 : 2), (int32_t)whole, r0, z, bar, policy);
             if (p == 0) tma_load_3d(dst + per_set * kFewRowBytes, rest_of(e, 1), (int32_t)whole, r0, z, bar, policy);
-            at.next(a.stages);
+            at.next(stages);
           }
         }
         if (p == 0 && ok) {   // the beginning of W2, in the order in which it will be wanted
@@ -235,7 +252,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
       }
     }
   } else if (warp == 1) {
-    // ---- activations: lane r copies the columns of the expert's r-th token ----
+    // ---- activations: lane r copies the columns of the expert's r-th token (of h, both numbers at once) ----
     const uint64_t policy = policy_evict_last();
     RingAt at;
     bool ok = true;
@@ -249,17 +266,17 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
         const uint32_t ai = p == 0 ? j / sets[0] : j % n_active;
         const Active ex = act[ai];
         const uint16_t *src = a.tokens;
-        if (lane < ex.n)
-          src = p == 0 ? a.tokens + (size_t)nth_bit(mask[ex.e], lane) * K : a.h + (size_t)(ex.slot + lane) * K;
+        if (lane < ex.n) src = p == 0 ? a.tokens + (size_t)nth_bit(mask[ex.e], lane) * K : a.h + (size_t)(ex.slot + lane) * 2 * K;
         for (uint32_t c = 0, cols; c < K; c += cols) {
           cols = c < whole ? min(kFewCols, whole - c) : K - c;
           ok = __all_sync(0xFFFFFFFFu, at.round == 0 || wait_bar(empty + 8 * at.st, (at.round - 1) & 1, lim));
           if (!ok) break;
-          const uint32_t bytes = cols * 2, bar = full + 8 * at.st;
+          const uint32_t numbers = p + 1, bytes = numbers * cols * 2, bar = full + 8 * at.st;
           if (lane == 0) mbar_expect_tx(bar, ex.n * bytes);
           __syncwarp();
-          if (lane < ex.n) bulk_load(ring + at.st * stage_bytes + a.w_bytes + lane * kFewPitch, src + c, bytes, bar, policy);
-          at.next(a.stages);
+          if (lane < ex.n)
+            bulk_load(ring + at.st * stage_bytes + a.w_bytes + lane * (p == 0 ? kFewPitch : kFewPitchH), src + numbers * c, bytes, bar, policy);
+          at.next(stages);
         }
       }
     }
@@ -267,7 +284,6 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
     // ---- products ----
     const uint32_t cw = warp - 2;
     const uint32_t a_row = lane & 15, a_half = lane >> 4;   // ldmatrix: this lane's row and half of 16 columns
-    const uint32_t b_at = a.w_bytes + (lane >> 2) * kFewPitch + (lane & 3) * 4;
     RingAt at;
     uint32_t job = 0;
     bool ok = true;
@@ -276,10 +292,16 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
       const bool two = p == 0 || per_set > 16;
       for (uint32_t j = 0; j < jobs && ok; ++j, ++job) {
         float d[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        // where this lane's token begins; in down the second numbers are a product of their own, or those of tokens 4 to 7
+        // (columns without a token repeat the last one's, and give sums that nobody reads)
+        const uint32_t n = act[p == 0 ? j / sets[0] : j % n_active].n;
+        const bool again = p == 1 && n > kFewOneProduct, halves = p == 1 && !again;
+        const uint32_t token = min(halves ? (lane >> 2) & 3 : lane >> 2, n - 1), second = halves ? lane >> 4 : 0;
+        const uint32_t b_at = a.w_bytes + token * (p == 0 ? kFewPitch : kFewPitchH) + (lane & 3) * 4;
         for (uint32_t c = 0; c < whole; c += kFewCols) {
           ok = __all_sync(0xFFFFFFFFu, wait_bar(full + 8 * at.st, at.round & 1, lim));
           if (!ok) break;
-          const uint32_t left = min(kFewCols, whole - c), base = ring + at.st * stage_bytes;
+          const uint32_t left = min(kFewCols, whole - c), base = ring + at.st * stage_bytes, b_base = base + b_at + second * left * 2;
 #pragma unroll 4
           for (uint32_t q = cw * 16; q < left; q += 128) {
             // 64 columns are per_set lines of 128 bytes; the second 16 rows are W3's box, or the lines after the first
@@ -288,31 +310,42 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
             load_a(base + line * 128 + ((chunk ^ (line & 7)) << 4), w0);
             if (p == 0) load_a(base + per_set * kFewRowBytes + line * 128 + ((chunk ^ (line & 7)) << 4), w1);
             else if (two) load_a(base + (line + 16) * 128 + ((chunk ^ (line & 7)) << 4), w1);
-            const uint32_t b0 = load_b(base + b_at + q * 2), b1 = load_b(base + b_at + q * 2 + 16);
+            const uint32_t b0 = load_b(b_base + q * 2), b1 = load_b(b_base + q * 2 + 16);
             mma_16816(d[0], w0, b0, b1);
             if (two) mma_16816(d[1], w1, b0, b1);
+            if (again) {
+              const uint32_t c0 = load_b(b_base + (left + q) * 2), c1 = load_b(b_base + (left + q) * 2 + 16);
+              mma_16816(d[0], w0, c0, c1);
+              if (two) mma_16816(d[1], w1, c0, c1);
+            }
           }
           __syncwarp();
           if (lane == 0) arrive(empty + 8 * at.st);
-          at.next(a.stages);
+          at.next(stages);
         }
         if (whole < K && ok) {   // up to 64 columns more: a step for each of the first warps
           ok = __all_sync(0xFFFFFFFFu, wait_bar(full + 8 * at.st, at.round & 1, lim));
           if (!ok) break;
-          const uint32_t left = K - whole, base = ring + at.st * stage_bytes, q = cw * 16;
+          const uint32_t left = K - whole, base = ring + at.st * stage_bytes, q = cw * 16, b_base = base + b_at + second * left * 2;
           if (q < left) {
             const uint32_t place = a_row * 128 + (((q >> 3) + a_half) ^ (a_row & 7)) * 16;
             uint32_t w0[4], w1[4];
             load_a(base + place, w0);
             if (two) load_a(base + place + (p == 0 ? per_set * kFewRowBytes : 16 * 128), w1);
             // (the last 8 of 16 columns may lie behind the row: weights are zero there, tokens have to be)
-            const uint32_t b0 = load_b(base + b_at + q * 2), behind = load_b(base + b_at + q * 2 + 16), b1 = q + 8 < left ? behind : 0u;
+            const uint32_t b0 = load_b(b_base + q * 2), behind = load_b(b_base + q * 2 + 16), b1 = q + 8 < left ? behind : 0u;
             mma_16816(d[0], w0, b0, b1);
             if (two) mma_16816(d[1], w1, b0, b1);
+            if (again) {
+              const uint32_t c0 = load_b(b_base + (left + q) * 2), after = load_b(b_base + (left + q) * 2 + 16);
+              const uint32_t c1 = q + 8 < left ? after : 0u;
+              mma_16816(d[0], w0, c0, c1);
+              if (two) mma_16816(d[1], w1, c0, c1);
+            }
           }
           __syncwarp();
           if (lane == 0) arrive(empty + 8 * at.st);
-          at.next(a.stages);
+          at.next(stages);
         }
         const uint32_t buf = job & 1;
         ok = ok && __all_sync(0xFFFFFFFFu, job < 2 || wait_bar(sums_empty + 8 * buf, ((job >> 1) - 1) & 1, lim));
@@ -356,17 +389,21 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
               v[0] += from[r];
               v[1] += from[8 * kFewSumPitch + r];
             } else {
-              v[0] += from[(r >> 4) * 8 * kFewSumPitch + (r & 15)];
+              const float *column = from + (r >> 4) * 8 * kFewSumPitch + (r & 15);
+              v[0] += column[0];
+              if (ex.n <= kFewOneProduct) v[1] += column[4 * kFewSumPitch];   // of h's second number
             }
           }
           if (p == 0) {
-            a.h[(size_t)(ex.slot + n) * a.I + r0 + r] = __bfloat16_as_ushort(__float2bfloat16_rn(silu_times(v[0], v[1])));
+            uint32_t cols;
+            uint16_t *h = a.h + (size_t)(ex.slot + n) * 2 * a.I + place_of_h(r0 + r, a.I, cols);
+            split_h(silu_times(v[0], v[1]), h[0], h[cols]);
           } else {
             const uint32_t t = nth_bit(mask[ex.e], n);
             float wt = 0.f;
             for (uint32_t c = 0; c < a.k; ++c)
               if (ids[t * a.k + c] == (int32_t)ex.e) wt += wts[t * a.k + c];
-            outs[t * 32 + r] += wt * v[0];
+            outs[t * 32 + r] += wt * (v[0] + v[1]);
           }
         }
         __syncwarp();
@@ -440,8 +477,8 @@ zipmoe_status launch_resident_few(const ResidentCall &c, cudaStream_t stream) {
   a.I = c.I;
   resident_few_rows(c.H, c.I, c.grid, &a.R1, &a.S1, &a.R2, &a.S2);
   a.w_bytes = (2 * a.S1 > a.S2 ? 2 * a.S1 : a.S2) * kFewRowBytes;
-  const uint32_t control = few_control_bytes(c.E, c.T, c.k) + 1024, room = 227 * 1024 - control, stage = a.w_bytes + kFewTokenBytes;
-  a.stages = room / stage < kResMaxStages ? room / stage : kResMaxStages;
+  const uint32_t control = few_control_bytes(c.E, c.T, c.k) + 1024;
+  a.ring_bytes = (227 * 1024 - control) & ~15u;
   static bool ready[64];
   if (!ready[c.device]) {
     if (cudaFuncSetAttribute(resident_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024) != cudaSuccess)
@@ -457,7 +494,7 @@ zipmoe_status launch_resident_few(const ResidentCall &c, cudaStream_t stream) {
   cfg.numAttrs = 1;
   cfg.gridDim = dim3(c.grid);
   cfg.blockDim = dim3(kFewThreads);
-  cfg.dynamicSmemBytes = control + a.stages * stage;
+  cfg.dynamicSmemBytes = control + a.ring_bytes;
   return cudaLaunchKernelEx(&cfg, resident_few_kernel, even, rests, a) == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
 }
 

@@ -1,6 +1,6 @@
 // The routed SwiGLU experts of a few tokens on recovered bf16 weights (pool F of the planner): the counterpart of
 // the fused decode + FFN for experts that need no decoding.
-//     g = W1 x,  u = W3 x,  h = bf16(SiLU(g) * u),  y = W2 h,  out[t] = bf16(sum_j w[t, j] * y)
+//     g = W1 x,  u = W3 x,  h = SiLU(g) * u,  y = W2 h,  out[t] = bf16(sum_j w[t, j] * y)
 //
 // Bound: the active experts' weights, 6 * hidden * inter bytes each, read once.  At up to 256 tokens the products
 // are a fraction of what the tensor cores do in that time, so everything here serves one aim: that the weight stream
@@ -16,18 +16,20 @@
 //     ring allows, across jobs and phases.
 //   * Another warp adds the activations of every step, 64 columns of the expert's own tokens: for gate/up gathered from
 //     the token matrix four rows at a time (few tokens), or, once all blocks have packed the tokens in the order the
-//     tensor core wants them, one bulk copy; for down the tokens' h rows, which gate/up stores in that order.
+//     tensor core wants them, one bulk copy; for down the tokens' h rows, which gate/up stores in that order, as the sum of two
+//     bf16 numbers: up to 128 tokens both are rows of one operand, whose sums are added when they are read back; more are two
+//     stages of activations and two rounds of MMAs for a stage of weights.
 //   * One thread issues the MMAs: weights are the M = 128 operand, the expert's tokens the N operand, two accumulators
-//     (g and u of the same rows, or two row blocks of y) in tensor memory, double-buffered where no expert has more
-//     than 128 tokens.
+//     (g and u of the same rows, or two row blocks of y) in tensor memory, double-buffered where no operand of the phase is
+//     wider than 128.
 //   * Every block works out the same routing lists for itself, and sizes its rings by the most tokens that an expert
 //     of this call has: few tokens, more stages.
 //   * Eight warps read the accumulators back.  A job inside one share goes straight on.  Of a job that is cut, each
 //     block stores its partial sums; for gate/up the block that is done last adds them in share order and goes on, for
 //     down the combination of the experts adds them.  No atomics on values: the same bits whatever the timing.
 // Blocks wait for one another (tokens packed, h stored, y stored), hence the cooperative launch.
-// 64 tokens, 8 experts of 4096 x 14336 (2.8 GB): 431 us, 6.5 TB/s (as fast as a plain copy); 256 tokens: 485 us (90 %); 37
-// tokens, 55 experts of 2048 x 1416 (957 MB): 165 us, 5.8 TB/s; 12 tokens, 8 of 2048 x 1408 (138 MB): 43 us, 3.2 TB/s.
+// 64 tokens, 8 experts of 4096 x 14336 (2.8 GB): 435 us, 6.5 TB/s (as fast as a plain copy); 256 tokens: 535 us (82 %); 37
+// tokens, 55 experts of 2048 x 1416 (957 MB): 166 us, 5.8 TB/s; 12 tokens, 8 of 2048 x 1408 (138 MB): 44 us, 3.1 TB/s.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -44,17 +46,17 @@ namespace zipmoe_dev {
 constexpr uint32_t kResReaders = 8;                         // warps that read accumulators back: two per 32 lanes of tensor memory
 constexpr uint32_t kResThreads = 128 + 32 * kResReaders;
 constexpr uint32_t kResStageA = 32768;                      // weights of a step
-constexpr uint32_t kResInFlight = 4;                        // steps asked for and not there yet (2: 473 us, 3: 447, 4: 442 for 64
+constexpr uint32_t kResInFlight = 4;                        // steps asked for and not there yet (2: 456 us, 3: 429, 4: 430 for 64
                                                             // tokens through 8 large experts); more only delays everybody else
 constexpr uint32_t kResFewT = 8;   // up to this many tokens the kernel that gives every block whole rows may run instead
 constexpr uint32_t kResGatherRows = 16;   // a gather of four rows takes the copy engine about 130 ns: up to this many tokens
                                           // per expert they are gathered in every step, beyond it packed once
 
 // Bytes of weights from which on the experts are taken in two groups.  One group waits between gate/up and down, two cut
-// more jobs.  One against two: 16 experts of 1024 x 512, 32 tokens (50 MB) 32 against 41 us; 8 of 2048 x 1408, 12 tokens
-// (138 MB) 42 against 47; 24 of them, 12 tokens (415 MB) 80 against 81; 40 of 2048 x 1000, 16 tokens (490 MB) 94 against 90; 60
-// of 2048 x 1408, 32 tokens (1.04 GB) 176 against 170.  Where experts have many tokens a cut costs more: 8 of 4096 x 3584, 256
-// tokens (705 MB) 167 against 173; 60 of 2048 x 1408, 256 tokens 226 against 216.
+// more jobs.  One against two: 16 experts of 1024 x 512, 32 tokens (50 MB) 37 against 49 us; 8 of 2048 x 1408, 12 tokens
+// (138 MB) 45 against 51; 24 of them, 12 tokens (415 MB) 79 against 80; 40 of 2048 x 1000, 16 tokens (490 MB) 93 against 92; 60
+// of 2048 x 1408, 32 tokens (1.04 GB) 171 against 168.  Where experts have many tokens a cut costs more: 8 of 4096 x 3584, 256
+// tokens (705 MB) 177 against 191; 60 of 2048 x 1408, 256 tokens 231 against 219.
 constexpr uint64_t kResTwoGroups = 450000000, kResTwoGroupsMany = 1000000000;
 
 struct ResidentArgs {
@@ -65,7 +67,8 @@ struct ResidentArgs {
   uint16_t *out;
   ResidentSync *sync;
   uint8_t *x;               // the experts' tokens in the same order as h, [hidden / 64] columns (where tokens are packed)
-  uint8_t *h;               // per active expert: [inter / 64][rows padded to 8][64] bf16, swizzled as the operand wants it
+  uint8_t *h;               // per active expert: [inter / 64][2][rows padded to 8][64] bf16, swizzled as the operand wants it:
+                            // the two numbers that h is the sum of
   float *part;              // [group][block][2][2][T][128]: partial sums of a share's two cut jobs (0: begun by others, 1: begun here);
                             // gate/up's have been read when down begins, and down's are stored over them
   float *y;                 // [choices][H]: jobs that lie inside one share
@@ -77,11 +80,11 @@ struct ResidentArgs {
 // Phases 0, 1: gate/up of the two groups of experts; 2, 3: down.  Jobs of KS steps, RB row blocks per active expert.
 // The steps (units) are shared out among P blocks by weight: a unit at position p of W belongs to block floor(p * P / W), so
 // block c begins with the first unit at or behind c * W / P.  A step costs what its bytes take: 32 KB from memory at the
-// SM's share of its bandwidth, or, with many tokens, 32 KB + 128 bytes per token into shared memory at 56 GB/s - the same
-// up to 72 tokens.  Weights are in KB of the latter, and all 1 where no expert has more tokens.
+// SM's share of its bandwidth, or, with many tokens, 32 KB + 128 bytes per token (twice that in down) into shared memory at 56
+// GB/s - the same up to 72 tokens (36).  Weights are in KB of the latter, and all 1 where no expert has more tokens.
 struct Phase {
   uint32_t KS, RB, U, P, a0;   // a0: the group's first active expert
-  uint32_t W, each, left;      // each, left: W / P, W % P   (W < 2^31: at most 2^25 units of weight 64)
+  uint32_t W, each, left;      // each, left: W / P, W % P   (W < 2^31: at most 2^17 units per expert, weights of 11008 in all)
   const uint16_t *weight;      // sums of the active experts' weights before each of them; null: all 1
   __device__ __forceinline__ void share(uint32_t total) {
     W = total;
@@ -116,8 +119,15 @@ struct Phase {
     return lo * per + (x - per * (weight[a0 + lo] - weight[a0]) + w - 1) / w;
   }
 };
-__device__ __forceinline__ uint32_t step_weight(uint32_t tokens) { return max(41u, 32 + (tokens + 7) / 8); }
-constexpr uint32_t kResEvenTokens = 72;   // up to here all steps weigh the same
+__device__ __forceinline__ uint32_t gate_up_weight(uint32_t tokens) { return max(41u, 32 + (tokens + 7) / 8); }
+__device__ __forceinline__ uint32_t down_weight(uint32_t tokens) { return max(41u, 32 + (tokens + 3) / 4); }
+// Up to this many tokens the two numbers of their h are rows of one operand (256 at most).
+constexpr uint32_t kResOneOperand = 128;
+__host__ __device__ inline uint32_t down_columns(uint32_t tokens) {
+  const uint32_t rows = (tokens + 7) & ~7u;
+  return rows <= kResOneOperand ? 2 * rows : (tokens + 15) & ~15u;
+}
+constexpr uint32_t kResEvenTokens = 72, kResEvenTokensDown = 36;   // up to here all steps weigh the same
 struct Piece {
   uint32_t job, a, rb, s0, n;   // steps s0 .. s0 + n of one job: active expert a, row block rb
 };
@@ -133,12 +143,12 @@ __device__ __forceinline__ bool next_piece(const Phase &p, uint32_t &u, uint32_t
   return true;
 }
 
-// shared memory after the ring: [token masks of the experts][active experts][expert -> active][sums of weights][place of every choice
-// among its expert's tokens][tokens of the active experts, padded to 8 each][barriers and words]
+// shared memory after the ring: [token masks of the experts][active experts][expert -> active][sums of weights: gate/up, down][place of
+// every choice among its expert's tokens][tokens of the active experts, padded to 8 each][barriers and words]
 __host__ __device__ inline uint32_t resident_rows(uint32_t E, uint32_t choices) { return choices + 7 * (E < choices ? E : choices); }
 __host__ __device__ inline uint32_t resident_control_bytes(uint32_t E, uint32_t T, uint32_t k) {
-  return pad16(E * ((T + 31) / 32) * 4) + E * (uint32_t)sizeof(Active) + pad16(E * 2) + pad16((E + 1) * 2) + pad16(T * k * 2) +
-         pad16(resident_rows(E, T * k) * 2) + (4 * kResMaxStages + 4) * 8 + 32;
+  return pad16(E * ((T + 31) / 32) * 4) + E * (uint32_t)sizeof(Active) + pad16(E * 2) + 2 * pad16((E + 1) * 2) +
+         pad16(T * k * 2) + pad16(resident_rows(E, T * k) * 2) + (4 * kResMaxStages + 4) * 8 + 32;
 }
 
 // the choice's place among its expert's tokens (in token order; a token that lists the expert twice has one place)
@@ -150,6 +160,23 @@ __device__ __forceinline__ void place_choice(uint32_t at, int32_t e, const Resid
   place[at] = (uint16_t)before;
   token[act[active_of[e]].h_row + before] = (uint16_t)t;
 }
+
+// The accumulators in turn, as the thread that fills them and the warps that read them both count them: two of D columns a
+// buffer, one or two buffers.
+struct AccRing {
+  uint32_t D, bufs, b = 0, uses0 = 0, uses1 = 0;
+  __device__ __forceinline__ void start(uint32_t columns) {
+    D = columns;
+    bufs = D <= 128 ? 2 : 1;
+    b = 0;
+  }
+  __device__ __forceinline__ uint32_t uses() const { return b ? uses1 : uses0; }   // of the present buffer so far
+  __device__ __forceinline__ void next() {
+    if (b) ++uses1;
+    else ++uses0;
+    if (bufs == 2) b ^= 1;
+  }
+};
 
 __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ EvenMaps even,
                                                                       const ResidentArgs a) {
@@ -174,14 +201,17 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
   ctl += a.E * sizeof(Active);
   uint16_t *active_of = reinterpret_cast<uint16_t *>(ctl);
   ctl += pad16(a.E * 2);
-  uint16_t *weight = reinterpret_cast<uint16_t *>(ctl);
+  uint16_t *weight_gu = reinterpret_cast<uint16_t *>(ctl);
+  ctl += pad16((a.E + 1) * 2);
+  uint16_t *weight_dn = reinterpret_cast<uint16_t *>(ctl);
   ctl += pad16((a.E + 1) * 2);
   uint16_t *place = reinterpret_cast<uint16_t *>(ctl);
   ctl += pad16(choices * 2);
   uint16_t *token = reinterpret_cast<uint16_t *>(ctl);
   ctl += pad16(n_rows_max * 2);
+  constexpr uint32_t kBars = 4 * kResMaxStages + 4;
   uint64_t *bars = reinterpret_cast<uint64_t *>(ctl);
-  uint32_t *words = reinterpret_cast<uint32_t *>(bars + 4 * kResMaxStages + 4);   // tmem, dead, active, last, most
+  uint32_t *words = reinterpret_cast<uint32_t *>(bars + kBars);   // tmem, dead, active, last, most, two for the readers, widest
   volatile uint32_t *dead = words + 1;
   // barriers: weights there / used, activations there / used, accumulators there / read
   const uint32_t w_full = smem_addr(bars), w_empty = w_full + 8 * kResMaxStages, x_full = w_empty + 8 * kResMaxStages,
@@ -191,7 +221,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
   for (uint32_t i = tid; i < a.E * W; i += kResThreads) mask[i] = 0;
   for (uint32_t i = tid; i < n_rows_max; i += kResThreads) token[i] = 0;   // (the rows that fill up to 8 are token 0's)
   if (warp == 3) {
-    for (uint32_t b = lane; b < 4 * kResMaxStages + 4; b += 32) mbar_init(w_full + 8 * b, b >= 4 * kResMaxStages + 2 ? kResReaders : 1);
+    for (uint32_t b = lane; b < kBars; b += 32) mbar_init(w_full + 8 * b, b >= kBars - 2 ? kResReaders : 1);
     if (lane == 0) {
       *dead = 0;
       prefetch_map(&x_map);
@@ -215,7 +245,8 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
   __syncthreads();
   if (warp == 0) {   // experts per * lane .. per * lane + per - 1
     const uint32_t per = (a.E + 31) / 32;
-    uint32_t cnt[8], n_act = 0, sums = 0, most = 0, heavy = 0;   // sums: padded rows << 16 | choices; heavy: weights
+    uint32_t cnt[8], n_act = 0, sums = 0, most = 0, widest = 16, heavy = 0;   // sums: padded rows << 16 | choices; heavy: weights
+    auto weights_of = [](uint32_t tokens) { return tokens ? gate_up_weight(tokens) | down_weight(tokens) << 16 : 0u; };
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
       const uint32_t e = per * lane + i;
@@ -223,11 +254,13 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
       if (i < per && e < a.E)
         for (uint32_t w = 0; w < W; ++w) cnt[i] += __popc(mask[e * W + w]);
       n_act += cnt[i] ? 1 : 0;
-      heavy += cnt[i] ? step_weight(cnt[i]) : 0;
+      heavy += weights_of(cnt[i]);
       sums += ((cnt[i] + 7) & ~7u) << 16 | cnt[i];
       most = max(most, cnt[i]);
+      widest = max(widest, down_columns(cnt[i]));
     }
     most = __reduce_max_sync(0xFFFFFFFFu, most);
+    widest = __reduce_max_sync(0xFFFFFFFFu, widest);
     uint32_t at = n_act, sum = sums, before = heavy;   // inclusive sums over the lanes
 #pragma unroll
     for (uint32_t d = 1; d < 32; d <<= 1) {
@@ -241,7 +274,9 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
     if (lane == 31) {
       words[2] = at;
       words[4] = most;
-      weight[at] = (uint16_t)before;
+      words[7] = widest;
+      weight_gu[at] = (uint16_t)before;
+      weight_dn[at] = (uint16_t)(before >> 16);
     }
     at -= n_act;
     sum -= sums;
@@ -252,9 +287,10 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
         const uint32_t e = per * lane + i;
         act[at] = Active{e, cnt[i], sum >> 16, sum & 0xFFFFu};
         active_of[e] = (uint16_t)at;
-        weight[at] = (uint16_t)before;
+        weight_gu[at] = (uint16_t)before;
+        weight_dn[at] = (uint16_t)(before >> 16);
         ++at;
-        before += step_weight(cnt[i]);
+        before += weights_of(cnt[i]);
         sum += ((cnt[i] + 7) & ~7u) << 16 | cnt[i];
       }
     }
@@ -263,16 +299,13 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
   const bool prepared = magic == kResMagic;
   const uint32_t n_active = prepared ? words[2] : 0;
   const bool packed = words[4] > kResGatherRows && n_active > 0;
-  const uint32_t N = max(16u, (words[4] + 15) & ~15u);       // the widest operand of this call
-  // as many stages of both kinds as fit; one more for weights if three are left for activations
-  const uint32_t x_stage = N * 128;
-  uint32_t n_w = min(kResMaxStages, a.ring_bytes / (kResStageA + x_stage)), n_x = n_w;
-  if (n_w < kResMaxStages && a.ring_bytes >= (n_w + 1) * kResStageA + 3 * x_stage) {
-    ++n_w;
-    n_x = min(kResMaxStages, (a.ring_bytes - n_w * kResStageA) / x_stage);
-  }
+  const uint32_t N_gu = max(16u, (words[4] + 15) & ~15u), N_dn = words[7];   // the widest operands of this call (N_gu <= N_dn)
+  const uint32_t x_stage = N_dn * 128;
+  // as many stages of weights as leave two for activations (as many of either kind as fit instead: 256 tokens, 60 experts of
+  // 2048 x 1408 238 us, so 234; 128 tokens, 8 of 4096 x 14336 468, so 462; the widest operands of 8 of 4096 x 14336 532, so 534)
+  const uint32_t n_w = min(kResMaxStages, (a.ring_bytes - 2 * x_stage) / kResStageA);
+  const uint32_t n_x = min(kResMaxStages, (a.ring_bytes - n_w * kResStageA) / x_stage);
   const uint32_t w_ring = smem_addr(ring), x_ring = w_ring + n_w * kResStageA;
-  const uint32_t acc_bufs = N <= 128 ? 2 : 1;                // two accumulators of N columns each, of 512 columns
   Phase ph[4];
   const bool two_groups = (uint64_t)n_active * a.H * a.I * 6 >= (words[4] > kResEvenTokens ? kResTwoGroupsMany : kResTwoGroups);
   const uint32_t n_first = two_groups ? (n_active + 1) / 2 : n_active;
@@ -285,9 +318,10 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
     ph[p].P = min(G, ph[p].U);
     ph[p].weight = nullptr;
     ph[p].share(ph[p].U);
-    if (words[4] > kResEvenTokens && ph[p].U > 0) {
+    const uint16_t *weight = p < 2 ? weight_gu : weight_dn;
+    if (words[4] > (p < 2 ? kResEvenTokens : kResEvenTokensDown) && ph[p].U > 0) {
       const uint32_t total = ph[p].KS * ph[p].RB * (weight[p & 1 ? n_active : n_first] - weight[ph[p].a0]);
-      if (total >= step_weight(words[4]) * ph[p].P) {   // (every block gets a unit)
+      if (total >= (p < 2 ? gate_up_weight(words[4]) : down_weight(words[4])) * ph[p].P) {   // (every block gets a unit)
         ph[p].weight = weight;
         ph[p].share(total);
       }
@@ -387,21 +421,23 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
       Piece q;
       while (ok && next_piece(f, u, end, q)) {
         const uint32_t rows = (act[q.a].n + 7) & ~7u, first_row = act[q.a].h_row;
-        const uint8_t *src = (p < 2 ? a.x : a.h) + ((size_t)first_row * f.KS) * 128;
+        const uint8_t *src = p < 2 ? a.x + (size_t)first_row * f.KS * 128 : a.h + (size_t)first_row * f.KS * 256;
         int32_t tok[4];
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i) tok[i] = 4 * lane < rows ? token[first_row + 4 * lane + i] : 0;
-        for (uint32_t s = q.s0; s < q.s0 + q.n; ++s) {
+        // a stage per step, or two, one for each number of h
+        const uint32_t per_step = p >= 2 && rows > kResOneOperand ? 2 : 1, bytes = p >= 2 && per_step == 1 ? rows * 256 : rows * 128;
+        for (uint32_t s = q.s0 * per_step; s < (q.s0 + q.n) * per_step; ++s) {
           ok = __all_sync(kLanes, at.round == 0 || wait_bar(x_empty + 8 * at.st, (at.round - 1) & 1, lim));
           if (!ok) break;
           const uint32_t dst = x_ring + at.st * x_stage, bar = x_full + 8 * at.st;
-          if (lane == 0) mbar_expect_tx(bar, rows * 128);
+          if (lane == 0) mbar_expect_tx(bar, bytes);
           __syncwarp(kLanes);
           if (p < 2 && !packed) {
             if (4 * lane < rows)
               tma_gather4(dst + lane * 512, &x_map, (int32_t)(s * 64), tok[0], tok[1], tok[2], tok[3], bar, policy);
           } else if (lane == 0) {
-            bulk_load(dst, src + (size_t)s * rows * 128, rows * 128, bar, policy);
+            bulk_load(dst, src + (size_t)s * bytes, bytes, bar, policy);
           }
           at.next(n_x);
         }
@@ -410,49 +446,60 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
   } else if (warp == 2 && lane == 0) {
     // ---- MMAs ----
     RingAt wa, xa;
-    uint32_t piece = 0;
+    AccRing acc;
     bool ok = true;
 #pragma unroll 1
     for (uint32_t p = 0; p < 4 && ok; ++p) {
       const Phase f = p == 0 ? ph[0] : p == 1 ? ph[1] : p == 2 ? ph[2] : ph[3];
+      if (p == 0) acc.start(N_gu);
+      if (p == 2) {   // other columns from here on: whatever was accumulated has to have been read
+        ok = (acc.uses0 == 0 || wait_bar(acc_empty, (acc.uses0 - 1) & 1, lim)) &&
+             (acc.uses1 == 0 || wait_bar(acc_empty + 8, (acc.uses1 - 1) & 1, lim));
+        acc.start(N_dn);
+      }
       uint32_t u = first(f);
       const uint32_t end = last(f);
       Piece q;
       while (ok && next_piece(f, u, end, q)) {
-        const uint32_t b = piece % acc_bufs, use = piece / acc_bufs;
+        const uint32_t b = acc.b, use = acc.uses();
         if (use > 0 && !wait_bar(acc_empty + 8 * b, (use - 1) & 1, lim)) {
           ok = false;
           break;
         }
         tc_after_sync();
         // columns: the expert's tokens (the rows after them hold what was there before, and give columns that nobody reads)
-        const uint32_t idesc = bf16_idesc((act[q.a].n + 15) & ~15u);
-        const uint32_t d0 = tmem + b * 2 * N, d1 = d0 + N;
+        const uint32_t n = act[q.a].n, parts = p >= 2 && n > kResOneOperand ? 2 : 1;
+        const uint32_t idesc = bf16_idesc(p < 2 ? (n + 15) & ~15u : down_columns(n));
+        const uint32_t d0 = tmem + b * 2 * acc.D, d1 = d0 + acc.D;
         for (uint32_t s = 0; s < q.n; ++s) {
-          if (!wait_bar(w_full + 8 * wa.st, wa.round & 1, lim) || !wait_bar(x_full + 8 * xa.st, xa.round & 1, lim)) {
-            ok = false;
-            break;
-          }
-          tc_after_sync();
+          ok = wait_bar(w_full + 8 * wa.st, wa.round & 1, lim);
           const uint32_t at = w_ring + wa.st * kResStageA;
-          const uint64_t a0 = swizzled_desc(at), a1 = swizzled_desc(at + 16384), bd = swizzled_desc(x_ring + xa.st * x_stage);
+          const uint64_t a0 = swizzled_desc(at), a1 = swizzled_desc(at + 16384);
+          for (uint32_t part = 0; ok && part < parts; ++part) {
+            ok = wait_bar(x_full + 8 * xa.st, xa.round & 1, lim);
+            if (!ok) break;
+            tc_after_sync();
+            const uint64_t bd = swizzled_desc(x_ring + xa.st * x_stage);
 #pragma unroll
-          for (uint32_t j = 0; j < 4; ++j) {
-            tc_mma(d0, a0 + 2 * j, bd + 2 * j, idesc, s > 0 || j > 0);
-            tc_mma(d1, a1 + 2 * j, bd + 2 * j, idesc, s > 0 || j > 0);
+            for (uint32_t j = 0; j < 4; ++j) {
+              tc_mma(d0, a0 + 2 * j, bd + 2 * j, idesc, s > 0 || part > 0 || j > 0);
+              tc_mma(d1, a1 + 2 * j, bd + 2 * j, idesc, s > 0 || part > 0 || j > 0);
+            }
+            tc_commit(x_empty + 8 * xa.st);
+            xa.next(n_x);
           }
+          if (!ok) break;
           tc_commit(w_empty + 8 * wa.st);
-          tc_commit(x_empty + 8 * xa.st);
           wa.next(n_w);
-          xa.next(n_x);
         }
         if (ok) tc_commit(acc_full + 8 * b);
-        ++piece;
+        acc.next();
       }
     }
   } else if (warp >= 4) {
     // ---- accumulators back; a thread has one row of the job's 128 (twice), and every second group of 8 tokens ----
     const uint32_t w = warp & 3, half = (warp - 4) >> 2, row = 32 * w + lane, rtid = tid - 128;
+    AccRing acc;
     uint32_t piece = 0;
     bool ok = true;
     if (packed) {
@@ -489,23 +536,29 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
       const Phase f = p == 0 ? ph[0] : p == 1 ? ph[1] : p == 2 ? ph[2] : ph[3];
       uint32_t u = first(f);
       const uint32_t end = last(f);
+      if (p == 0 || p == 2) acc.start(p == 0 ? N_gu : N_dn);
       float *part = a.part + (p & 1) * a.part_phase;
       Piece q;
       while (ok && next_piece(f, u, end, q)) {
-        const uint32_t b = piece % acc_bufs, use = piece / acc_bufs;
+        const uint32_t b = acc.b, use = acc.uses();
+        acc.next();
         ++piece;
         const Active ex = act[q.a];
         const bool whole = q.n == f.KS;
         float *mine = part + ((size_t)cta * 2 + (q.s0 > 0 ? 0 : 1)) * (2 * a.T * 128) + row;
         // a finished pair of sums of the expert's i-th token
         const uint32_t rows = (ex.n + 7) & ~7u, ir = q.rb * 128 + row;
-        uint8_t *h = a.h + ((size_t)ex.h_row * ph[2].KS + (size_t)(ir >> 6) * rows) * 128 + (ir & 7) * 2;
+        uint8_t *h = a.h + ((size_t)ex.h_row * ph[2].KS + (size_t)(ir >> 6) * rows) * 256 + (ir & 7) * 2;
         const uint32_t chunk = (ir & 63) >> 3;
         auto finish = [&](uint32_t i, float v0, float v1) {
           if (p < 2) {
-            if (ir < ph[2].KS * 64)     // (rows between inter and the next multiple of 64 are zeros: W2 has no columns there)
-              *reinterpret_cast<uint16_t *>(h + i * 128 + ((chunk ^ (i & 7)) << 4)) =
-                  ir < a.I ? __bfloat16_as_ushort(__float2bfloat16_rn(silu_times(v0, v1))) : (uint16_t)0;
+            if (ir < ph[2].KS * 64) {   // (rows between inter and the next multiple of 64 are zeros: W2 has no columns there)
+              uint16_t first, second;
+              split_h(ir < a.I ? silu_times(v0, v1) : 0.f, first, second);
+              uint8_t *to = h + i * 128 + ((chunk ^ (i & 7)) << 4);
+              *reinterpret_cast<uint16_t *>(to) = first;
+              *reinterpret_cast<uint16_t *>(to + rows * 128) = second;
+            }
           } else {
             float *y = a.y + (size_t)(ex.slot + i) * a.H;
             const uint32_t c = q.rb * 256 + row;
@@ -532,7 +585,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
         ok = all_agree<32 * kResReaders>(ok);
         if (!ok) break;
         tc_after_sync();
-        const uint32_t d0 = tmem + ((32 * w) << 16) + b * 2 * N, d1 = d0 + N;
+        const uint32_t d0 = tmem + ((32 * w) << 16) + b * 2 * acc.D, d1 = d0 + acc.D;
         if (*others_there) {
           const size_t next_block = 2 * (2 * a.T * 128);
           const float *from = part + (c0 + 1) * next_block + row;
@@ -578,7 +631,19 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
           uint32_t v0[8], v1[8];
           tmem_load8(d0 + c, v0);
           tmem_load8(d1 + c, v1);
-          tmem_wait();
+          if (p >= 2 && rows <= kResOneOperand) {   // the sums over h's second number are `rows` columns further
+            uint32_t w0[8], w1[8];
+            tmem_load8(d0 + rows + c, w0);
+            tmem_load8(d1 + rows + c, w1);
+            tmem_wait();
+#pragma unroll
+            for (uint32_t n = 0; n < 8; ++n) {
+              v0[n] = __float_as_uint(__uint_as_float(v0[n]) + __uint_as_float(w0[n]));
+              v1[n] = __float_as_uint(__uint_as_float(v1[n]) + __uint_as_float(w1[n]));
+            }
+          } else {
+            tmem_wait();
+          }
 #pragma unroll
           for (uint32_t n = 0; n < 8; ++n)
             if (c + n < ex.n) emit(c + n, __uint_as_float(v0[n]), __uint_as_float(v1[n]));
@@ -616,7 +681,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
           // many tokens: a warp per token, four rows per lane; four tokens' parts are asked for at a time (10 us less for 231
           // tokens of one expert, 3 us more for one)
           const uint32_t row4 = 4 * lane, ir4 = q.rb * 128 + row4, h_rows = ph[2].KS * 64;
-          uint8_t *to = a.h + ((size_t)ex.h_row * ph[2].KS + (size_t)(ir4 >> 6) * rows) * 128 + (ir4 & 7) * 2;
+          uint8_t *to = a.h + ((size_t)ex.h_row * ph[2].KS + (size_t)(ir4 >> 6) * rows) * 256 + (ir4 & 7) * 2;
           const uint32_t chunk4 = (ir4 & 63) >> 3;
           for (uint32_t n0 = warp - 4; n0 < ex.n; n0 += 4 * kResReaders) {
             float4 g[4], v[4];
@@ -642,10 +707,16 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
               const uint32_t i = n0 + n * kResReaders;
               if (i >= ex.n || ir4 >= h_rows) continue;
               // (inter is a multiple of 8: four rows are all inside it or all behind it)
-              const __nv_bfloat162 lo = __floats2bfloat162_rn(silu_times(g[n].x, v[n].x), silu_times(g[n].y, v[n].y));
-              const __nv_bfloat162 hi = __floats2bfloat162_rn(silu_times(g[n].z, v[n].z), silu_times(g[n].w, v[n].w));
-              const uint2 packed4 = make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
-              *reinterpret_cast<uint2 *>(to + i * 128 + ((chunk4 ^ (i & 7)) << 4)) = ir4 < a.I ? packed4 : make_uint2(0, 0);
+              ushort4 first = make_ushort4(0, 0, 0, 0), second = first;
+              if (ir4 < a.I) {
+                split_h(silu_times(g[n].x, v[n].x), first.x, second.x);
+                split_h(silu_times(g[n].y, v[n].y), first.y, second.y);
+                split_h(silu_times(g[n].z, v[n].z), first.z, second.z);
+                split_h(silu_times(g[n].w, v[n].w), first.w, second.w);
+              }
+              uint8_t *at = to + i * 128 + ((chunk4 ^ (i & 7)) << 4);
+              *reinterpret_cast<ushort4 *>(at) = first;
+              *reinterpret_cast<ushort4 *>(at + rows * 128) = second;
             }
           }
         }
@@ -854,10 +925,11 @@ zipmoe_status resident_plan(uint32_t T, uint32_t k, const zipmoe_resident_expert
     return ZIPMOE_ERR_UNSUPPORTED;
   const uint64_t H = ex->hidden, I = ex->inter;
   p->grid = resident_grid();
-  // two accumulators for as many tokens as an expert can have, twice if they fit (the kernel goes by the call's own most)
+  // two accumulators for both numbers of as many tokens as an expert can have, twice if they fit (the kernel goes by the
+  // call's own most)
   const uint32_t N = std::max(16u, (T + 15) / 16 * 16);
   p->tmem_cols = 32;
-  while (p->tmem_cols < std::min(512u, 4 * N)) p->tmem_cols <<= 1;
+  while (p->tmem_cols < std::min(512u, 8 * N)) p->tmem_cols <<= 1;
   const uint32_t control = zipmoe_dev::resident_control_bytes(ex->n_experts, T, k) + 1024;
   p->ring = (227u * 1024u - control) & ~15u;
   p->smem = control + p->ring;
@@ -865,7 +937,7 @@ zipmoe_status resident_plan(uint32_t T, uint32_t k, const zipmoe_resident_expert
   const uint64_t choices = (uint64_t)T * k, rows = zipmoe_dev::resident_rows(ex->n_experts, T * k);
   uint64_t at = up(sizeof(zipmoe_dev::ResidentSync));
   p->off_x = at; at = up(at + rows * ((H + 63) / 64) * 128);
-  p->off_h = at; at = up(at + rows * ((I + 63) / 64) * 128);
+  p->off_h = at; at = up(at + rows * ((I + 63) / 64) * 256);
   p->part_phase = (uint64_t)T * p->grid * 2 * 2 * 128;
   p->off_part = at; at = up(at + 2 * p->part_phase * 4);
   p->off_y = at; at = up(at + choices * H * 4);

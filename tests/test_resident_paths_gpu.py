@@ -1,9 +1,9 @@
 """Paths of zipmoe_expert_ffn that small layers do not reach: experts taken in two groups (from 450 MB of active weights, or 1 GB
 where an expert has more than 72 tokens), the combination of five to eight choices of many tokens, and, for up to 8 tokens,
 the whole-rows kernel's handling of choices that are no expert, repeated experts, NaN and infinities.  Against the formula
-in fp64 (computed on the device for the large layers), with every output held to a bound from its own terms: h is rounded
-to bf16 (by half a step, 2^(e - 8) in [2^e, 2^(e+1)), which reaches the output through |w| |W2|), the output once more, and
-the fp32 sums contribute 2e-6 of the sum of the magnitudes they add."""
+in fp64 (computed on the device for the large layers), with every output held to a bound from its own terms: one rounding of h
+to bf16 (half a step, 2^(e - 8) in [2^e, 2^(e+1)), which reaches the output through |w| |W2|; the kernels keep more of it), one
+of the output, and the fp32 sums contribute 2e-6 of the sum of the magnitudes they add."""
 import numpy as np
 import pytest
 
