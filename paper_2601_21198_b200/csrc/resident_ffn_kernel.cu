@@ -566,6 +566,30 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
             if (c + 128 < a.H) y[c + 128] = v1;
           }
         };
+        // finished sums of gate/up, 8 tokens of which the first is a multiple of 8: neighbouring lanes, which have neighbouring rows,
+        // swap every second token, so that each stores two rows of a token at once
+        uint8_t *h2 = h - (ir & 1) * 2;
+        auto store_h = [&](uint32_t t0, const float (&g)[8], const float (&u)[8]) {
+#pragma unroll
+          for (uint32_t m = 0; m < 8; m += 2) {
+            if (t0 + m >= ex.n) break;
+            uint32_t own[2];
+#pragma unroll
+            for (uint32_t e = 0; e < 2; ++e) {
+              uint16_t first, second;
+              split_h(ir < a.I ? silu_times(g[m + e], u[m + e]) : 0.f, first, second);
+              own[e] = first | (uint32_t)second << 16;
+            }
+            const bool odd = lane & 1;
+            const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, odd ? own[0] : own[1], 1), t = t0 + m + odd;
+            const uint32_t even_row = odd ? got : own[0], odd_row = odd ? own[1] : got;
+            if (t < ex.n && ir < ph[2].KS * 64) {
+              uint8_t *to = h2 + t * 128 + ((chunk ^ (t & 7)) << 4);
+              *reinterpret_cast<uint32_t *>(to) = __byte_perm(even_row, odd_row, 0x5410);
+              *reinterpret_cast<uint32_t *>(to + rows * 128) = __byte_perm(even_row, odd_row, 0x7632);
+            }
+          }
+        };
         auto emit = [&](uint32_t i, float v0, float v1) {
           if (whole) {
             finish(i, v0, v1);
@@ -617,9 +641,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
                   g[m][n] += __ldcg(from + o * next_block + (size_t)t * 128);
                   v[m][n] += __ldcg(from + o * next_block + (size_t)(a.T + t) * 128);
                 }
-#pragma unroll
-              for (uint32_t n = 0; n < 8; ++n)
-                if (t0 + n < ex.n) finish(t0 + n, g[m][n], v[m][n]);
+              store_h(t0, g[m], v[m]);
             }
           }
           tc_before_sync();
@@ -643,6 +665,16 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
             }
           } else {
             tmem_wait();
+          }
+          if (whole && p < 2) {
+            float g[8], u[8];
+#pragma unroll
+            for (uint32_t n = 0; n < 8; ++n) {
+              g[n] = __uint_as_float(v0[n]);
+              u[n] = __uint_as_float(v1[n]);
+            }
+            store_h(c, g, u);
+            continue;
           }
 #pragma unroll
           for (uint32_t n = 0; n < 8; ++n)
