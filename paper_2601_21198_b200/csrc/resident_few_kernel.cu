@@ -14,8 +14,8 @@
 //   * Another warp adds the same columns of the expert's tokens (x, then h, which is the sum of two bf16 numbers).
 //   * Eight warps take the chunk's 16-column steps in turn: ldmatrix, mma.sync m16n8k16 (weights the 16 rows, tokens the 8
 //     columns; fp32 sums in registers).  The second numbers of h are columns 4 to 7 where an expert has up to 4 tokens (one
-//     product for both), and otherwise go through a second product.  With so few tokens these need a tenth of the issue slots of the time that the
-//     bytes take; a tcgen05 operand of 128 rows would be nine tenths empty with 10 to 28 rows per block.
+//     product for both), and otherwise go through a second product.  With so few tokens these need a tenth of the issue slots
+//     of the time that the bytes take; a tcgen05 operand of 128 rows would be nine tenths empty with 10 to 28 rows per block.
 //   * At the end of a job (one expert's set of rows) they leave their partial sums in shared memory and go on; four more
 //     warps add them and finish the job.
 // One token, 2 experts of 4096 x 14336 (705 MB): 108 us, 6.5 TB/s, what a plain copy moves; 6 experts of 2048 x 1408
@@ -26,6 +26,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <cstring>
 
@@ -40,6 +41,7 @@ constexpr uint32_t kFewCols = 512, kFewRowBytes = kFewCols * 2;
 // banks.
 constexpr uint32_t kFewPitch = kFewRowBytes + 16, kFewPitchH = 2 * kFewRowBytes + 16;
 constexpr uint32_t kFewOneProduct = 4;                 // up to so many tokens both numbers of h are columns of one product
+constexpr uint32_t kFewTokenBytes = 9 * 1024;          // eight tokens' x, four tokens' h
 constexpr uint32_t kFewAheadBytes = 192 * 1024;        // of W2 that a block asks into the cache before h is there
 constexpr uint32_t kFewSumPitch = 20;                  // floats between the columns of a warp's 16 rows of sums: no bank conflicts
 
@@ -55,7 +57,7 @@ struct FewArgs {
   uint64_t limit_ns;
   uint32_t T, k, E, H, I, even;
   uint32_t R1, S1, R2, S2;  // rows of a block, rows of a set: of W1 and W3, of W2
-  uint32_t ring_bytes, w_bytes, extra_tx;
+  uint32_t ring_bytes, w_bytes, stages, extra_tx;   // stages: of kFewTokenBytes
 };
 
 // shared memory: [ring][sums, two sets][outputs][active experts][masks][ids, weights][barriers, words]
@@ -175,10 +177,11 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
   __syncthreads();
   const bool prepared = magic == kResMagic;
   const uint32_t n_active = prepared ? words[2] : 0;
-  // a stage has room for as many tokens as an expert of this call has, and no less than for 8 tokens' x: with less, more stages
-  // are in flight, which only delays everybody else (one token, 2 experts of 4096 x 14336: 111 us instead of 108)
-  const uint32_t stage_bytes = a.w_bytes + (max(words[3] * kFewPitchH, 8 * kFewPitch) + 1023) / 1024 * 1024;
-  const uint32_t stages = min(kResMaxStages, a.ring_bytes / stage_bytes);
+  // a stage has room for 8 tokens' x, which is 4 tokens' h, or for the h of as many tokens as an expert of this call has (with
+  // room for one token more stages are in flight, which only delays everybody else: 2 experts of 4096 x 14336 111 us instead of 108)
+  const bool wide = words[3] > kFewOneProduct;
+  const uint32_t stage_bytes = a.w_bytes + (wide ? (words[3] * kFewPitchH + 1023) / 1024 * 1024 : kFewTokenBytes);
+  const uint32_t stages = wide ? min(kResMaxStages, a.ring_bytes / stage_bytes) : a.stages;
   // this block's rows, in sets; a phase's chunks run over experts, sets and columns (gate/up) or sets, experts and columns
   const uint32_t row0[2] = {min(a.I, cta * a.R1), min(a.H, cta * a.R2)}, row1[2] = {min(a.I, (cta + 1) * a.R1), min(a.H, (cta + 1) * a.R2)};
   const uint32_t sets[2] = {(row1[0] - row0[0] + a.S1 - 1) / a.S1, (row1[1] - row0[1] + a.S2 - 1) / a.S2};
@@ -293,10 +296,10 @@ __global__ void __launch_bounds__(kFewThreads, 1) resident_few_kernel(const __gr
       for (uint32_t j = 0; j < jobs && ok; ++j, ++job) {
         float d[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
         // where this lane's token begins; in down the second numbers are a product of their own, or those of tokens 4 to 7
-        // (columns without a token repeat the last one's, and give sums that nobody reads)
-        const uint32_t n = act[p == 0 ? j / sets[0] : j % n_active].n;
-        const bool again = p == 1 && n > kFewOneProduct, halves = p == 1 && !again;
-        const uint32_t token = min(halves ? (lane >> 2) & 3 : lane >> 2, n - 1), second = halves ? lane >> 4 : 0;
+        // (columns without a token are whatever lies there, and give sums that nobody reads)
+        const uint32_t n = p == 1 && a.T > kFewOneProduct ? act[j % n_active].n : 0;
+        const bool again = n > kFewOneProduct, halves = p == 1 && !again;
+        const uint32_t token = halves ? (lane >> 2) & 3 : again ? min(lane >> 2, n - 1) : lane >> 2, second = halves ? lane >> 4 : 0;
         const uint32_t b_at = a.w_bytes + token * (p == 0 ? kFewPitch : kFewPitchH) + (lane & 3) * 4;
         for (uint32_t c = 0; c < whole; c += kFewCols) {
           ok = __all_sync(0xFFFFFFFFu, wait_bar(full + 8 * at.st, at.round & 1, lim));
@@ -479,6 +482,7 @@ zipmoe_status launch_resident_few(const ResidentCall &c, cudaStream_t stream) {
   a.w_bytes = (2 * a.S1 > a.S2 ? 2 * a.S1 : a.S2) * kFewRowBytes;
   const uint32_t control = few_control_bytes(c.E, c.T, c.k) + 1024;
   a.ring_bytes = (227 * 1024 - control) & ~15u;
+  a.stages = std::min(kResMaxStages, a.ring_bytes / (a.w_bytes + kFewTokenBytes));
   static bool ready[64];
   if (!ready[c.device]) {
     if (cudaFuncSetAttribute(resident_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024) != cudaSuccess)
