@@ -28,8 +28,8 @@
 //     block stores its partial sums; for gate/up the block that is done last adds them in share order and goes on, for
 //     down the combination of the experts adds them.  No atomics on values: the same bits whatever the timing.
 // Blocks wait for one another (tokens packed, h stored, y stored), hence the cooperative launch.
-// 64 tokens, 8 experts of 4096 x 14336 (2.8 GB): 435 us, 6.5 TB/s (as fast as a plain copy); 256 tokens: 535 us (82 %); 37
-// tokens, 55 experts of 2048 x 1416 (957 MB): 166 us, 5.8 TB/s; 12 tokens, 8 of 2048 x 1408 (138 MB): 44 us, 3.1 TB/s.
+// 64 tokens, 8 experts of 4096 x 14336 (2.8 GB): 427 us, 6.6 TB/s (as fast as a plain copy); 256 tokens: 515 us (85 %); 37
+// tokens, 55 experts of 2048 x 1416 (957 MB): 165 us, 5.8 TB/s; 12 tokens, 8 of 2048 x 1408 (138 MB): 44 us, 3.1 TB/s.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 

@@ -89,3 +89,29 @@ def test_experts_with_many_tokens_beside_others_with_few(zb):
         out, off = expected(ws, x, ids, wts)
         assert ((got - out).abs() <= half_step(out.abs() + off) + off).all(), most
         assert int(ex.status.item()) == 0
+
+
+@pytest.mark.parametrize("T", [1, 6, 40, 200])
+def test_infinite_weights_and_activations_give_infinities(zb, T):
+    """W2 with an infinite weight, and g so large that h leaves fp32: the formula's infinities, with their signs."""
+    import torch
+    E, H, I = 1, 128, 192
+    g = torch.Generator(device="cuda")
+    g.manual_seed(T)
+    ws = layer(E, H, I, 17)
+    x = torch.randn(T, H, generator=g, device="cuda").to(torch.bfloat16)
+    ids, wts = torch.zeros(T, 1, dtype=torch.int32, device="cuda"), torch.ones(T, 1, device="cuda")
+    sound, _ = expected(ws, x, ids, wts)
+    h = (lambda a, b: a / (1 + torch.exp(-a)) * b)(x.double() @ ws[0].double().t(), x.double() @ ws[1].double().t())
+    ws[2][7, 100] = float("inf")
+    got = zb.ResidentExperts(ws, H, I).ffn(x, ids, wts).double()
+    assert torch.equal(got[:, 7], torch.sign(h[:, 100]) * float("inf"))
+    rest = torch.arange(H, device="cuda") != 7
+    assert torch.isfinite(got[:, rest]).all() and (got - sound)[:, rest].norm() <= 0.01 * sound.norm()
+    # h beyond fp32 in one place: every output is that place's weight times infinity
+    ws[2][7, 100] = 1.0
+    ws[0][50], ws[1][50] = 0, 0
+    ws[0][50, 0], ws[1][50, 0] = 1e30, 1e30
+    x[:, 0] = 1.0
+    got = zb.ResidentExperts(ws, H, I).ffn(x, ids, wts).double()
+    assert torch.equal(got, torch.sign(ws[2][:, 50].double()).expand_as(got) * float("inf"))
