@@ -448,6 +448,116 @@ zipmoe_status zipmoe_expert_ffn(const uint16_t *tokens, uint32_t T, const int32_
                                 uint32_t k, const zipmoe_resident_experts *experts, uint16_t *out, void *workspace,
                                 uint64_t workspace_bytes, uint32_t *status_word, zipmoe_stream stream);
 
+/* ---- the experts' products for prompts, and products in 8-bit integers (device) ----
+ * zipmoe_expert_ffn takes up to 256 tokens.  A longer prompt goes the same way in four calls: its choices are grouped by
+ * expert, every expert's tokens are multiplied by W1 and W3 (a pair, with the gated activation behind it), the result by W2,
+ * and every token's rows are added with their weights.  The same product takes 8-bit integers with a scale per row and per
+ * column, grouped or, with one group, for a dense projection.  Kernels are launched with programmatic stream serialization
+ * (see above). */
+
+/* One call of zipmoe_group_tokens.  A HOST struct holding DEVICE pointers. */
+typedef struct {
+  const int32_t *topk_ids;     /* in: [T, k]; a negative id is no expert                                            */
+  int32_t *offsets;            /* out: [n_experts + 1]: expert e's rows are offsets[e] .. offsets[e + 1] - 1        */
+  int32_t *order;              /* out: [T * k]: the choice t * k + j that each row is; entries behind
+                                  offsets[n_experts] are left as they were                                          */
+  int32_t *place;              /* out: [T, k]: the row of each choice, -1 for no expert; may be NULL                */
+  uint32_t *status_word;       /* as for zipmoe_decode: code 1 for an id of n_experts or more, which counts as no
+                                  expert; may be NULL                                                               */
+  uint32_t T, k, n_experts;
+  uint32_t reserved;           /* zero                                                                              */
+} zipmoe_group_args;
+
+/* The choices of T tokens grouped by expert: rows in ascending order of (expert, choice).  One launch on `stream`,
+ * asynchronous, no workspace.  A token may choose an expert twice: it then has two rows there.
+ * Limits: n_experts <= 256, k <= 8, T * k <= 2^30 (ZIPMOE_ERR_UNSUPPORTED otherwise).  T = 0 writes the offsets (zeros). */
+zipmoe_status zipmoe_group_tokens(const zipmoe_group_args *args, zipmoe_stream stream);
+
+#define ZIPMOE_GROUPED_PAIR 1u /* weights: two matrices per group, and SiLU(first) * second of their products */
+#define ZIPMOE_GROUPED_INT8 2u /* weights: 8-bit integers with scales (else bf16)                             */
+#define ZIPMOE_GROUPED_F32 4u  /* rows of fp32 (else bf16 patterns)                                           */
+
+/* The weights of a grouped product.  A HOST struct that zipmoe_grouped_weights_plan fills; the caller then sets `table` to
+ * where it has copied the table on the device (not needed where `even` is 1). */
+typedef struct {
+  uint32_t n_groups, rows, cols, flags;
+  uint32_t even;               /* 1: each kind of matrix lies at equal distances from group to group                */
+  uint32_t reserved;           /* zero                                                                              */
+  const void *table;           /* device [n_groups * ZIPMOE_GROUPED_ENTRY_BYTES], 64-byte aligned                   */
+  uint8_t maps[2 * 128];       /* opaque                                                                            */
+} zipmoe_grouped_weights;
+#define ZIPMOE_GROUPED_ENTRY_BYTES 256u
+
+/* Describes weights to zipmoe_grouped_matmul, once, and again when a tensor moves.  Weights at equal distances, in ascending
+ * order, are found faster.
+ * host in : tensors[n_groups] (with ZIPMOE_GROUPED_PAIR tensors[2 * n_groups], tensors[2e] = W1, 2e+1 = W3 of group e) DEVICE
+ *           addresses of dense row-major [rows, cols] matrices, 16-byte aligned; flags: ZIPMOE_GROUPED_PAIR, _INT8.  The memory
+ *           itself is not touched.
+ * host out: table[n_groups * ZIPMOE_GROUPED_ENTRY_BYTES]; *weights, but for its `table`
+ * Limits: n_groups <= 256, rows <= 2^20, cols a multiple of 8 (16 for 8-bit integers) and <= 65536 (ZIPMOE_ERR_UNSUPPORTED
+ * otherwise). */
+zipmoe_status zipmoe_grouped_weights_plan(const void *const *tensors, uint32_t n_groups, uint32_t rows, uint32_t cols, uint32_t flags,
+                                          void *table, zipmoe_grouped_weights *weights);
+
+/* One call of zipmoe_grouped_matmul.  A HOST struct holding DEVICE pointers; pitches in elements between rows. */
+typedef struct {
+  const void *x;               /* in: [x_rows] of cols bf16 patterns or 8-bit integers, x_pitch apart; 16-byte aligned,
+                                  and so is the pitch                                                               */
+  uint64_t x_pitch;
+  const int32_t *offsets;      /* in: [n_groups + 1], ascending, from 0 to at most `rows`: group e's rows are offsets[e] ..
+                                  offsets[e + 1] - 1; may be NULL where there is one group: it then has all rows     */
+  const int32_t *order;        /* in: row r of the product is row order[r] / k of x; NULL: row r of x                */
+  const float *row_scales;     /* in: [x_rows] scales of the rows of x; NULL exactly where weights are bf16          */
+  const float *col_scales;     /* in: [n_groups, rows of the weights] scales of the weights' rows (with
+                                  ZIPMOE_GROUPED_PAIR those of all groups' W1, then of all W3); NULL likewise        */
+  void *out;                   /* out: [rows] of one element per row of the weights, out_pitch apart, bf16 patterns or
+                                  (ZIPMOE_GROUPED_F32) fp32; may overlap nothing that is read                        */
+  uint64_t out_pitch;
+  uint32_t *status_word;       /* as for zipmoe_decode: code 1 where offsets or order point outside, 3 when a wait ran
+                                  out; may be NULL                                                                  */
+  uint32_t x_rows, rows, k, flags;
+  uint32_t reserved[2];        /* zero                                                                              */
+} zipmoe_grouped_args;
+
+/* Matrix products grouped by expert, group sizes known on the device alone: for every group e and its rows r
+ *     acc[r, n] = sum_c x[src(r), c] * W_e[n, c]             (fp32 sums; 8-bit integers: exact)
+ *     out[r, n] = acc[r, n]                                  bf16
+ *               = acc[r, n] * row_scales[src(r)] * col_scales[e, n]              8-bit integers
+ *     out[r, n] = SiLU(first) * second                       of these, with ZIPMOE_GROUPED_PAIR
+ * rounded once.  Rows of `out` that belong to no group are left as they were; a group may be empty.  A row whose `order` points
+ * outside x is taken as zeros; where the offsets are not in order, are negative or reach past `rows`, nothing is computed.  Both
+ * set status_word (code 1).  One launch on `stream`, asynchronous, no workspace; results do not depend on timing.
+ * Limits: rows and x_rows <= 2^30, k <= 8 (ZIPMOE_ERR_UNSUPPORTED otherwise).  rows = 0 does nothing. */
+zipmoe_status zipmoe_grouped_matmul(const zipmoe_grouped_weights *weights, const zipmoe_grouped_args *args, zipmoe_stream stream);
+
+/* One call of zipmoe_combine_rows.  A HOST struct holding DEVICE pointers; pitches in elements between rows. */
+typedef struct {
+  const void *y;               /* in: [rows] of cols bf16 patterns or (ZIPMOE_GROUPED_F32) fp32, y_pitch apart       */
+  uint64_t y_pitch;
+  const int32_t *place;        /* in: [T, k]: the row of each choice; a negative one is none                        */
+  const float *weights;        /* in: [T, k]; may be NULL (= 1.0)                                                   */
+  uint16_t *out;               /* out: [T] of cols bf16 patterns, out_pitch apart                                   */
+  uint64_t out_pitch;
+  uint32_t *status_word;       /* as for zipmoe_decode: code 1 where `place` points outside; may be NULL            */
+  uint32_t T, k, cols, rows, flags;
+  uint32_t reserved;           /* zero                                                                              */
+} zipmoe_combine_args;
+
+/* The choices' rows back to their tokens: out[t] = bf16( sum_j weights[t, j] * y[place[t, j]] ), added in fp32 in the order of j.
+ * A choice that is none adds nothing; a token without any gets zeros.  One launch on `stream`, asynchronous.
+ * Limits: k <= 8, cols <= 2^20, T * k <= 2^30 (ZIPMOE_ERR_UNSUPPORTED otherwise).  T = 0 does nothing. */
+zipmoe_status zipmoe_combine_rows(const zipmoe_combine_args *args, zipmoe_stream stream);
+
+/* Rows of bf16 to 8-bit integers: a = max |x| of the row, q = rint(127 x / a) (half to even), scale = a / 127, so that
+ * q * scale ~ x and |q| <= 127.  A row of zeros has scale 0 and zeros; one with a NaN or an infinity has scale NaN and zeros.
+ * For activations (a scale per token) and, once, for weights (a scale per output channel).  One launch on `stream`,
+ * asynchronous; rows of whole 16-byte vectors are faster.
+ * device in : x [rows] of cols bf16 patterns, x_pitch elements apart
+ * device out: q [rows] of cols integers, q_pitch apart; scales [rows]
+ * Limits: cols <= 65536, rows <= 2^30 (ZIPMOE_ERR_UNSUPPORTED otherwise).  rows = 0 does nothing. */
+zipmoe_status zipmoe_quantize_rows(const uint16_t *x, uint64_t x_pitch, uint32_t rows, uint32_t cols, int8_t *q, uint64_t q_pitch,
+                                   float *scales, zipmoe_stream stream);
+
 /* ---- cache-pool planning (host only, no CUDA) ------------------------------
  * The paper's planner sizes four cache pools for experts in different compression states -- F full
  * tensors, C compressed (E-chunks and SM-chunks), S SM-chunks only, E E-chunks only -- from a

@@ -429,6 +429,73 @@ def zipmoe_expert_ffn(tokens, T, topk_ids, topk_weights, k, experts, out, worksp
                                   _ptr(workspace), workspace_bytes, _ptr(status_word), _ptr(stream)))
 
 
+# ---- the experts' products for prompts, and products in 8-bit integers -----------------------------------
+GROUPED_PAIR, GROUPED_INT8, GROUPED_F32 = 1, 2, 4
+GROUPED_ENTRY_BYTES = 256
+
+
+class GroupedWeightsStruct(ctypes.Structure):
+    """zipmoe_grouped_weights."""
+    _fields_ = [("n_groups", _u32), ("rows", _u32), ("cols", _u32), ("flags", _u32), ("even", _u32), ("reserved", _u32),
+                ("table", _vp), ("maps", ctypes.c_uint8 * 256)]
+
+
+# zipmoe_group_args, zipmoe_grouped_args and zipmoe_combine_args
+_GROUP_ARGS = struct.Struct("<5Q4I")
+_GROUPED_ARGS = struct.Struct("<9Q6I")
+_COMBINE_ARGS = struct.Struct("<7Q6I")
+assert _GROUP_ARGS.size == 56 and _GROUPED_ARGS.size == 96 and _COMBINE_ARGS.size == 80
+_lib.zipmoe_group_tokens.argtypes = [ctypes.c_char_p, _vp]
+_lib.zipmoe_grouped_weights_plan.argtypes = [ctypes.POINTER(_vp), _u32, _u32, _u32, _u32, _vp, ctypes.POINTER(GroupedWeightsStruct)]
+_lib.zipmoe_grouped_matmul.argtypes = [ctypes.POINTER(GroupedWeightsStruct), ctypes.c_char_p, _vp]
+_lib.zipmoe_combine_rows.argtypes = [ctypes.c_char_p, _vp]
+_lib.zipmoe_quantize_rows.argtypes = [_vp, _u64, _u32, _u32, _vp, _u64, _vp, _vp]
+for _f in ("zipmoe_group_tokens", "zipmoe_grouped_weights_plan", "zipmoe_grouped_matmul", "zipmoe_combine_rows", "zipmoe_quantize_rows"):
+    getattr(_lib, _f).restype = _int
+
+
+def zipmoe_group_tokens(topk_ids, T, k, n_experts, offsets, order, place=None, status_word=None, stream=None):
+    """Pointer arguments are device tensors (or raw device addresses, or None)."""
+    args = _GROUP_ARGS.pack(_ptr(topk_ids) or 0, _ptr(offsets) or 0, _ptr(order) or 0, _ptr(place) or 0, _ptr(status_word) or 0, T, k,
+                            n_experts, 0)
+    _check("zipmoe_group_tokens", _lib.zipmoe_group_tokens(args, _ptr(stream)))
+
+
+def zipmoe_grouped_weights_plan(tensors, n_groups, rows, cols, flags=0):
+    """tensors: n_groups device tensors (or addresses), 2 * n_groups with GROUPED_PAIR.  Returns (table: numpy uint8, to be
+    copied to the device unless the struct's `even` is 1; GroupedWeightsStruct, whose `table` is then to be set to that copy's
+    address)."""
+    if len(tensors) != (2 if flags & GROUPED_PAIR else 1) * n_groups:
+        raise ValueError("a tensor per group, or two of a pair, are wanted")
+    ptrs = (_vp * max(len(tensors), 1))(*[_ptr(t) for t in tensors])
+    table = np.zeros(n_groups * GROUPED_ENTRY_BYTES, np.uint8)
+    weights = GroupedWeightsStruct()
+    _check("zipmoe_grouped_weights_plan",
+           _lib.zipmoe_grouped_weights_plan(ptrs, n_groups, rows, cols, flags, _ptr(table), ctypes.byref(weights)))
+    return table, weights
+
+
+def zipmoe_grouped_matmul(weights, x, x_pitch, x_rows, out, out_pitch, rows, offsets=None, order=None, k=0, row_scales=None,
+                          col_scales=None, flags=0, status_word=None, stream=None):
+    """Pointer arguments are device tensors (or raw device addresses, or None); `weights` is a GroupedWeightsStruct."""
+    args = _GROUPED_ARGS.pack(_ptr(x) or 0, x_pitch, _ptr(offsets) or 0, _ptr(order) or 0, _ptr(row_scales) or 0, _ptr(col_scales) or 0,
+                              _ptr(out) or 0, out_pitch, _ptr(status_word) or 0, x_rows, rows, k, flags, 0, 0)
+    _check("zipmoe_grouped_matmul", _lib.zipmoe_grouped_matmul(ctypes.byref(weights), args, _ptr(stream)))
+
+
+def zipmoe_combine_rows(y, y_pitch, rows, place, weights, T, k, cols, out, out_pitch, flags=0, status_word=None, stream=None):
+    """Pointer arguments are device tensors (or raw device addresses, or None)."""
+    args = _COMBINE_ARGS.pack(_ptr(y) or 0, y_pitch, _ptr(place) or 0, _ptr(weights) or 0, _ptr(out) or 0, out_pitch,
+                              _ptr(status_word) or 0, T, k, cols, rows, flags, 0)
+    _check("zipmoe_combine_rows", _lib.zipmoe_combine_rows(args, _ptr(stream)))
+
+
+def zipmoe_quantize_rows(x, x_pitch, rows, cols, q, q_pitch, scales, stream=None):
+    """Pointer arguments are device tensors (or raw device addresses); pitches in elements."""
+    _check("zipmoe_quantize_rows",
+           _lib.zipmoe_quantize_rows(_ptr(x), x_pitch, rows, cols, _ptr(q), q_pitch, _ptr(scales), _ptr(stream)))
+
+
 class LaunchInfo(ctypes.Structure):
     _fields_ = [("payload_bytes", _u64), ("sm_bytes", _u64), ("out_elems", _u64), ("n_chunks", _u32), ("n_tiles", _u32),
                 ("n_tables", _u32), ("max_record_bytes", _u32), ("max_code_len", _u32), ("flags", _u32)]
@@ -572,6 +639,7 @@ class _Kinds:
         self.e4m3 = (torch.float8_e4m3fn, torch.uint8)
         self.fp32 = (torch.float32,)
         self.int32 = (torch.int32,)
+        self.int8 = (torch.int8,)
         self.current_stream = torch._C._cuda_getCurrentRawStream   # handle of a device's current stream
         self.capturing = torch._C._cuda_isCurrentStreamCapturing
         self.current_device = torch._C._cuda_getDevice
@@ -812,6 +880,7 @@ class ResidentExperts:
         self.status_at = self.status.data_ptr()
         self._struct_at = ctypes.byref(self.struct)
         self._scratch, self._need = _scratch_of(self.device, self.index), {}
+        self._prompt = None
 
     @classmethod
     def from_decode(cls, plan, out, hidden, inter):
@@ -851,3 +920,218 @@ class ResidentExperts:
         if status:
             raise ZipMoEError("zipmoe_expert_ffn", status)
         return out
+
+    def ffn_prompt(self, tokens, topk_ids, topk_weights, out=None, stream=None):
+        """What ffn computes, for any number of tokens: the choices are grouped by expert, every expert's tokens go through W1
+        and W3 and then W2 as grouped products, and each token's rows are added.  The gated activations between the products are
+        rounded to bf16.  tokens' rows may lie apart.  The lists, activations and rows between the calls are new memory of
+        the stream's pool: calls on different streams and captures are independent of one another.  An id of n_experts or more
+        sets `status` to 1."""
+        kinds, index = self.kinds, self.index
+        if kinds.current_device() != index:
+            with _on_device(index):
+                return self.ffn_prompt(tokens, topk_ids, topk_weights, out, stream)
+        gate_up, down = self._products()
+        _rows("tokens", tokens, (topk_ids.shape[0], self.hidden), kinds.bf16, index)
+        if topk_weights is not None:
+            _dense("topk_weights", topk_weights, topk_ids.shape, kinds.fp32, index)
+        groups = group_tokens(topk_ids, len(self.tensors) // 3, status=self.status, stream=stream)
+        h = gate_up.product(tokens, groups, gather=True, stream=stream)
+        y = down.product(h, groups, out=_empty((h.shape[0], self.hidden), kinds.fp32[0], self.device, stream), stream=stream)
+        if out is None:
+            out = _empty((topk_ids.shape[0], self.hidden), tokens.dtype, self.device, stream)
+        return combine_rows(y, groups, topk_weights, out=out, stream=stream)
+
+    def _products(self):
+        """The two grouped products of ffn_prompt, described at its first call."""
+        found = self._prompt
+        if found is None:
+            shaped = [t.view(self.hidden, self.inter) if i % 3 == 2 else t.view(self.inter, self.hidden) for i, t in enumerate(self.tensors)]
+            found = self._prompt = (GroupedMatrix(shaped[0::3], up=shaped[1::3], status=self.status),
+                                    GroupedMatrix(shaped[2::3], status=self.status))
+        return found
+
+
+class TokenGroups:
+    """The choices of `topk_ids` [T, k] grouped by expert, as zipmoe_group_tokens lists them: offsets [n_experts + 1], order
+    [T * k] (the choice that each row is), place [T, k] (the row of each choice, -1 for none), int32 device tensors."""
+
+    def __init__(self, offsets, order, place, n_experts):
+        self.offsets, self.order, self.place, self.n_experts = offsets, order, place, n_experts
+        self.tokens, self.k = place.shape
+        self.rows = order.shape[0]
+        self.index = place.get_device()
+
+
+def group_tokens(topk_ids, n_experts, offsets=None, order=None, place=None, status=None, stream=None):
+    """topk_ids [T, k] int32 -> TokenGroups.  offsets, order and place, if given, are the tensors to be filled (entries of order
+    behind the last group are left as they were); status [1] int32, if given, gets code 1 for an id of n_experts or more."""
+    kinds, index = _get_kinds(), _device_of("topk_ids", topk_ids)
+    if kinds.current_device() != index:
+        with _on_device(index):
+            return group_tokens(topk_ids, n_experts, offsets, order, place, status, stream)
+    T, k = shape = topk_ids.shape
+    int32 = kinds.int32
+    ids_at = _dense("topk_ids", topk_ids, shape, int32, index)
+    if offsets is None:
+        offsets = _empty((n_experts + 1,), int32[0], topk_ids.device, stream)
+    if order is None:
+        order = _empty((T * k,), int32[0], topk_ids.device, stream)
+    if place is None:
+        place = _empty(shape, int32[0], topk_ids.device, stream)
+    args = _GROUP_ARGS.pack(ids_at, _dense("offsets", offsets, (n_experts + 1,), int32, index), _dense("order", order, (T * k,), int32, index),
+                            _dense("place", place, shape, int32, index), 0 if status is None else _dense("status", status, (1,), int32, index),
+                            T, k, n_experts, 0)
+    status_code = _lib.zipmoe_group_tokens(args, _handle(kinds, index, stream))
+    if status_code:
+        raise ZipMoEError("zipmoe_group_tokens", status_code)
+    return TokenGroups(offsets, order, place, n_experts)
+
+
+class GroupedMatrix:
+    """The weights of one grouped product: matrices[e] [rows, cols] of group e, all bf16 (or int16 patterns) or all int8, dense;
+    `up`, if given, holds the second matrices of pairs: the product is then SiLU(first) * second.  int8 matrices have scales
+    [rows] or [n_groups, rows] fp32 (up_scales for the second ones)."""
+
+    def __init__(self, matrices, up=None, scales=None, up_scales=None, status=None):
+        import torch
+        kinds = self.kinds = _get_kinds()
+        if not matrices or (up is not None and len(up) != len(matrices)):
+            raise ValueError("a matrix per group, and as many second ones, are wanted")
+        index = self.index = _device_of("matrix 0", matrices[0])
+        self.device = matrices[0].device
+        self.n_groups, (self.rows, self.cols) = len(matrices), matrices[0].shape
+        self.int8, self.pair = matrices[0].dtype in kinds.int8, up is not None
+        self.kind = kinds.int8 if self.int8 else kinds.bf16
+        self.tensors = list(matrices) if up is None else [m for both in zip(matrices, up) for m in both]
+        addresses = [_dense("matrix %d" % i, t, (self.rows, self.cols), self.kind, index) for i, t in enumerate(self.tensors)]
+        self.scales, self.scales_at = None, 0
+        if self.int8:
+            if scales is None or self.pair != (up_scales is not None):
+                raise ValueError("int8 matrices have scales, and second ones theirs")
+            shape = (self.n_groups, self.rows)
+            both = [s.view(shape) if s.dim() == 1 and self.n_groups == 1 else s for s in ((scales, up_scales) if self.pair else (scales,))]
+            for name, s in zip(("scales", "up_scales"), both):
+                _dense(name, s, shape, kinds.fp32, index)
+            self.scales = torch.cat(both) if self.pair else both[0]
+            self.scales_at = self.scales.data_ptr()
+        elif scales is not None or up_scales is not None:
+            raise ValueError("scales go with int8 matrices")
+        flags = (GROUPED_PAIR if self.pair else 0) | (GROUPED_INT8 if self.int8 else 0)
+        with _on_device(index):
+            table, self.struct = zipmoe_grouped_weights_plan(addresses, self.n_groups, self.rows, self.cols, flags)
+        self.table = None
+        if not self.struct.even:      # evenly spaced weights need no table
+            if kinds.capturing():
+                raise ValueError("weights that lie unevenly are described before a capture, not within it")
+            self.table = torch.from_numpy(table).to(self.device)
+            self.struct.table = self.table.data_ptr()
+        self._struct_at = ctypes.byref(self.struct)
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.device) if status is None else status
+        self.status_at = _dense("status", self.status, (1,), kinds.int32, index)
+
+    def product(self, x, groups=None, gather=False, row_scales=None, out=None, stream=None):
+        """x [x_rows, cols] of the weights' kind -> out [rows, rows of the matrices], bf16 (x's dtype; torch.bfloat16 for int8)
+        unless `out` is given, which may be fp32.  groups None: one group, all rows of x.  gather: row r of the product is the
+        token that choice groups.order[r] belongs to (x is [groups.tokens, cols]); else row r of x (x is [groups.rows, cols]).
+        row_scales [x_rows] fp32 goes with int8.  Rows of no group are left as they were."""
+        kinds, index = self.kinds, self.index
+        if kinds.current_device() != index:
+            with _on_device(index):
+                return self.product(x, groups, gather, row_scales, out, stream)
+        offsets_at = order_at = k = 0
+        if groups is None:
+            if self.n_groups != 1 or gather:
+                raise ValueError("the groups' lists are wanted")
+            x_rows = rows = x.shape[0]
+        else:
+            if groups.n_experts != self.n_groups or groups.index != index:
+                raise ValueError("lists of %d groups on CUDA device %d are wanted, not of %d on device %d" %
+                                 (self.n_groups, index, groups.n_experts, groups.index))
+            rows, x_rows, offsets_at = groups.rows, groups.rows, groups.offsets.data_ptr()
+            if gather:
+                x_rows, order_at, k = groups.tokens, groups.order.data_ptr(), groups.k
+        x_at, x_pitch = _rows("x", x, (x_rows, self.cols), self.kind, index)
+        scales_at = 0
+        if self.int8:
+            if row_scales is None:
+                raise ValueError("int8 rows have scales")
+            scales_at = _dense("row_scales", row_scales, (x_rows,), kinds.fp32, index)
+        elif row_scales is not None:
+            raise ValueError("scales go with int8 rows")
+        if out is None:
+            out = _empty((rows, self.rows), kinds.bf16[0] if self.int8 else x.dtype, self.device, stream)
+        f32 = out.dtype in kinds.fp32
+        out_at, out_pitch = _rows("out", out, (rows, self.rows), kinds.fp32 if f32 else kinds.bf16, index)
+        args = _GROUPED_ARGS.pack(x_at, x_pitch, offsets_at, order_at, scales_at, self.scales_at, out_at, out_pitch, self.status_at,
+                                  x_rows, rows, k, GROUPED_F32 if f32 else 0, 0, 0)
+        status = _lib.zipmoe_grouped_matmul(self._struct_at, args, _handle(kinds, index, stream))
+        if status:
+            raise ZipMoEError("zipmoe_grouped_matmul", status)
+        return out
+
+
+def combine_rows(y, groups, weights, out=None, stream=None):
+    """y [groups.rows, cols] bf16 (or int16 patterns) or fp32, weights [T, k] fp32 or None -> out [T, cols] bf16: every token's rows,
+    added with their weights."""
+    kinds, index = _get_kinds(), _device_of("y", y)
+    if kinds.current_device() != index:
+        with _on_device(index):
+            return combine_rows(y, groups, weights, out, stream)
+    if groups.index != index:
+        raise ValueError("lists on CUDA device %d are wanted, not on device %d" % (index, groups.index))
+    T, k, cols = groups.tokens, groups.k, y.shape[1]
+    f32 = y.dtype in kinds.fp32
+    y_at, y_pitch = _rows("y", y, (groups.rows, cols), kinds.fp32 if f32 else kinds.bf16, index)
+    weights_at = 0 if weights is None else _dense("weights", weights, (T, k), kinds.fp32, index)
+    if out is None:
+        out = _empty((T, cols), kinds.bf16[0] if f32 else y.dtype, y.device, stream)
+    out_at, out_pitch = _rows("out", out, (T, cols), kinds.bf16, index)
+    args = _COMBINE_ARGS.pack(y_at, y_pitch, groups.place.data_ptr(), weights_at, out_at, out_pitch, 0, T, k, cols, groups.rows,
+                              GROUPED_F32 if f32 else 0, 0)
+    status = _lib.zipmoe_combine_rows(args, _handle(kinds, index, stream))
+    if status:
+        raise ZipMoEError("zipmoe_combine_rows", status)
+    return out
+
+
+def quantize_rows(x, q=None, scales=None, stream=None):
+    """x [rows, cols] bf16 (or int16 patterns) whose rows may lie apart -> q [rows, cols] int8, scales [rows] fp32."""
+    kinds, index = _get_kinds(), _device_of("x", x)
+    if kinds.current_device() != index:
+        with _on_device(index):
+            return quantize_rows(x, q, scales, stream)
+    rows, cols = shape = x.shape
+    x_at, x_pitch = _rows("x", x, shape, kinds.bf16, index)
+    if q is None:
+        q = _empty(shape, kinds.int8[0], x.device, stream)
+    if scales is None:
+        scales = _empty((rows,), kinds.fp32[0], x.device, stream)
+    q_at, q_pitch = _rows("q", q, shape, kinds.int8, index)
+    status = _lib.zipmoe_quantize_rows(x_at, x_pitch, rows, cols, q_at, q_pitch, _dense("scales", scales, (rows,), kinds.fp32, index),
+                                       _handle(kinds, index, stream))
+    if status:
+        raise ZipMoEError("zipmoe_quantize_rows", status)
+    return q, scales
+
+
+class Int8Linear:
+    """A dense projection in 8-bit integers: weight [rows, cols] int8 and scales [rows] fp32, or from_bf16's of a bf16 weight."""
+
+    def __init__(self, weight, scales):
+        self.matrix = GroupedMatrix([weight], scales=scales)
+        self.rows, self.cols, self.status = self.matrix.rows, self.matrix.cols, self.matrix.status
+
+    @classmethod
+    def from_bf16(cls, weight):
+        """weight [rows, cols] bf16 (or int16 patterns), for example a tensor that was decoded: each output channel with a scale
+        of its own."""
+        return cls(*quantize_rows(weight))
+
+    def product(self, x, out=None, stream=None):
+        """x [tokens, cols] bf16 (or int16 patterns) -> out [tokens, rows], bf16 (x's dtype) unless `out` is given, which may be
+        fp32: every token is rounded to 8 bits with a scale of its own, the sums are exact."""
+        q, scales = quantize_rows(x, stream=stream)
+        if out is None:
+            out = _empty((x.shape[0], self.rows), x.dtype, x.device, stream)
+        return self.matrix.product(q, row_scales=scales, out=out, stream=stream)

@@ -1,0 +1,267 @@
+// The lists that group the router's choices by expert, and the weighted sum that takes grouped rows back to their tokens.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "zipmoe.h"
+#include "tensor_core.cuh"
+
+namespace zipmoe_dev {
+
+// ---- grouping: a stable counting sort of the choices by expert -----------------
+// Bound: latency (12 bytes per choice are nothing).  One cluster of 1 to 8 blocks; every warp owns a run of consecutive choices
+// and counts its experts in a row of its own in shared memory, 32 choices at a time: lanes with the same expert find one
+// another with one match instruction, so that nothing is added atomically and the order is the choices' own.  The blocks' sums
+// meet through distributed shared memory; then every warp knows where its first choice of each expert goes, and walks its run
+// a second time.
+constexpr uint32_t kGroupMaxExperts = 256;
+
+struct GroupArgs {
+  const int32_t *ids;
+  int32_t *offsets, *order, *place;
+  uint32_t *status;
+  uint32_t n, E;
+};
+
+constexpr uint32_t kGroupHeld = 8;   // ids per lane that stay in registers between the two walks
+
+__global__ void __launch_bounds__(1024) group_kernel(const GroupArgs a) {
+  extern __shared__ uint32_t count[];                    // [warps][E]: choices of the warp's run; then where its next one goes
+  __shared__ uint32_t total[kGroupMaxExperts], sums[8];  // the block's choices of every expert
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, warps = blockDim.x >> 5, rank = cluster_rank(), S = cluster_size();
+  uint32_t *mine = count + warp * a.E;
+  for (uint32_t i = lane; i < a.E; i += 32) mine[i] = 0;
+  after_predecessor();
+  // the warp's run of whole 32s
+  const uint32_t pieces = (a.n + 31) / 32, w = rank * warps + warp, W = S * warps;
+  const uint32_t p0 = (uint32_t)((uint64_t)pieces * w / W), p1 = (uint32_t)((uint64_t)pieces * (w + 1) / W);
+  int32_t held[kGroupHeld];
+  auto load = [&](uint32_t p) {
+    const uint32_t at = p * 32 + lane;
+    return at < a.n ? __ldcg(a.ids + at) : -1;
+  };
+#pragma unroll
+  for (uint32_t i = 0; i < kGroupHeld; ++i) held[i] = p0 + i < p1 ? load(p0 + i) : -1;
+  __syncwarp();
+  auto count_piece = [&](int32_t id) {
+    const bool there = id >= 0 && id < (int32_t)a.E;
+    const uint32_t same = __match_any_sync(0xFFFFFFFFu, there ? id : -1);
+    if (there && lane == (uint32_t)__ffs(same) - 1) mine[id] += __popc(same);
+    if (id >= (int32_t)a.E) report(a.status, kStatusBadDescriptor);
+    __syncwarp();
+  };
+#pragma unroll
+  for (uint32_t i = 0; i < kGroupHeld; ++i)
+    if (p0 + i < p1) count_piece(held[i]);
+  for (uint32_t p = p0 + kGroupHeld; p < p1; ++p) count_piece(load(p));
+  __syncthreads();
+  // exclusive sums over the block's warps, expert by expert
+  for (uint32_t e = tid; e < a.E; e += blockDim.x) {
+    uint32_t sum = 0;
+    for (uint32_t i = 0; i < warps; ++i) {
+      const uint32_t c = count[i * a.E + e];
+      count[i * a.E + e] = sum;
+      sum += c;
+    }
+    total[e] = sum;
+  }
+  cluster_sync();
+  // over the blocks, then over the experts
+  uint32_t all = 0, before = 0;
+  if (tid < a.E) {
+    const uint32_t at = smem_addr(total + tid);
+    for (uint32_t r = 0; r < S; ++r) {
+      uint32_t c;
+      asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c) : "r"(in_block(at, r)));
+      if (r < rank) before += c;
+      all += c;
+    }
+  }
+  uint32_t upto = all;   // inclusive over the warp's experts
+#pragma unroll
+  for (uint32_t d = 1; d < 32; d <<= 1) {
+    const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+    if (lane >= d) upto += v;
+  }
+  if (warp < 8 && lane == 31) sums[warp] = upto;
+  cluster_sync();        // (also: nobody overwrites its totals, or leaves, while a neighbour reads them)
+  if (tid < a.E) {
+    uint32_t begin = upto - all;
+    for (uint32_t i = 0; i < warp; ++i) begin += sums[i];
+    if (rank == 0) {
+      a.offsets[tid] = (int32_t)begin;
+      if (tid == a.E - 1) a.offsets[a.E] = (int32_t)(begin + all);
+    }
+    total[tid] = begin + before;
+  }
+  __syncthreads();
+  for (uint32_t i = lane; i < a.E; i += 32) mine[i] += total[i];
+  __syncwarp();
+  auto place_piece = [&](uint32_t p, int32_t id) {
+    const uint32_t at = p * 32 + lane;
+    const bool there = id >= 0 && id < (int32_t)a.E;
+    const uint32_t same = __match_any_sync(0xFFFFFFFFu, there ? id : -1);
+    uint32_t to = 0;
+    if (there) to = mine[id] + __popc(same & ((1u << lane) - 1));
+    __syncwarp();
+    if (there && lane == (uint32_t)__ffs(same) - 1) mine[id] += __popc(same);
+    __syncwarp();
+    if (there) a.order[to] = (int32_t)at;
+    if (a.place && at < a.n) a.place[at] = there ? (int32_t)to : -1;
+  };
+#pragma unroll
+  for (uint32_t i = 0; i < kGroupHeld; ++i)
+    if (p0 + i < p1) place_piece(p0 + i, held[i]);
+  for (uint32_t p = p0 + kGroupHeld; p < p1; ++p) place_piece(p, load(p));
+}
+
+// ---- combination: out[t] = sum over j of weights[t, j] * y[place[t, j]] --------
+// Bound: the bytes of y.  A thread has four neighbouring columns of a token and asks for all its choices' at once; they are
+// added in the order of the choices, in fp32.
+struct CombineArgs {
+  const void *y;
+  const int32_t *place;
+  const float *weights;
+  __nv_bfloat16 *out;
+  uint64_t y_pitch, out_pitch;
+  uint32_t *status;
+  uint32_t T, k, cols, rows;
+};
+
+template <bool kF32, bool kWide>
+__global__ void __launch_bounds__(256) combine_rows_kernel(const CombineArgs a) {
+  constexpr uint32_t kV = kWide ? 4 : 1;
+  after_predecessor();
+  const uint32_t units = a.cols / kV;
+  for (uint32_t t = blockIdx.y * blockDim.y + threadIdx.y; t < a.T; t += gridDim.y * blockDim.y)
+    for (uint32_t c = blockIdx.x * blockDim.x + threadIdx.x; c < units; c += gridDim.x * blockDim.x) {
+      float v[8][kV], w[8];
+#pragma unroll
+      for (uint32_t j = 0; j < 8; ++j) {
+        w[j] = 0.f;
+        if (j >= a.k) continue;
+        const int32_t at = __ldcg(a.place + (uint64_t)t * a.k + j);
+        const bool there = at >= 0 && (uint32_t)at < a.rows;
+        if (!there && at >= 0) report(a.status, kStatusBadDescriptor);
+        w[j] = a.weights ? __ldcg(a.weights + (uint64_t)t * a.k + j) : 1.f;
+        const uint64_t from = (there ? (uint64_t)at : 0) * a.y_pitch + (uint64_t)c * kV;
+        if constexpr (kWide && kF32) {
+          const float4 x = there ? __ldcs(reinterpret_cast<const float4 *>(static_cast<const float *>(a.y) + from)) : make_float4(0.f, 0.f, 0.f, 0.f);
+          v[j][0] = x.x;
+          v[j][1] = x.y;
+          v[j][2] = x.z;
+          v[j][3] = x.w;
+        } else if constexpr (kWide) {
+          const uint2 x = there ? __ldcs(reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(a.y) + from)) : make_uint2(0, 0);
+          v[j][0] = __uint_as_float(x.x << 16);
+          v[j][1] = __uint_as_float(x.x & 0xFFFF0000u);
+          v[j][2] = __uint_as_float(x.y << 16);
+          v[j][3] = __uint_as_float(x.y & 0xFFFF0000u);
+        } else if constexpr (kF32) {
+          v[j][0] = there ? __ldcs(static_cast<const float *>(a.y) + from) : 0.f;
+        } else {
+          v[j][0] = there ? __uint_as_float((uint32_t)__ldcs(static_cast<const uint16_t *>(a.y) + from) << 16) : 0.f;
+        }
+        if (!there) w[j] = 0.f;   // (a choice that is none adds nothing, whatever its weight)
+      }
+      float sum[kV];
+#pragma unroll
+      for (uint32_t i = 0; i < kV; ++i) {
+        sum[i] = 0.f;
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j)
+          if (j < a.k) sum[i] = fmaf(w[j], v[j][i], sum[i]);
+      }
+      __nv_bfloat16 *to = a.out + (uint64_t)t * a.out_pitch + (uint64_t)c * kV;
+      if constexpr (kWide) {
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(sum[0], sum[1]), hi = __floats2bfloat162_rn(sum[2], sum[3]);
+        *reinterpret_cast<uint2 *>(to) = make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
+      } else {
+        *to = __float2bfloat16_rn(sum[0]);
+      }
+    }
+}
+
+}  // namespace zipmoe_dev
+
+namespace {
+
+uintptr_t bits(const void *p) { return reinterpret_cast<uintptr_t>(p); }
+
+zipmoe_status current_device(int *dev) {
+  static bool ready[64];
+  if (cudaGetDevice(dev) != cudaSuccess || *dev < 0 || *dev >= 64) return ZIPMOE_ERR_CUDA;
+  if (!ready[*dev]) {
+    int major = 0;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, *dev) != cudaSuccess) return ZIPMOE_ERR_CUDA;
+    if (major != 10) return ZIPMOE_ERR_UNSUPPORTED;
+    ready[*dev] = true;
+  }
+  return ZIPMOE_OK;
+}
+
+}  // namespace
+
+extern "C" zipmoe_status zipmoe_group_tokens(const zipmoe_group_args *g, zipmoe_stream stream) {
+  using namespace zipmoe_dev;
+  zipmoe_host::TraceRange trace("zipmoe_group_tokens");
+  if (!g) return ZIPMOE_ERR_INVALID_ARG;
+  if (g->n_experts == 0 || g->n_experts > kGroupMaxExperts || g->k == 0 || g->k > 8 || (uint64_t)g->T * g->k > 1u << 30) return ZIPMOE_ERR_UNSUPPORTED;
+  if (g->reserved || !g->offsets || (g->T && (!g->topk_ids || !g->order))) return ZIPMOE_ERR_INVALID_ARG;
+  if ((bits(g->topk_ids) | bits(g->offsets) | bits(g->order) | bits(g->place) | bits(g->status_word)) & 3) return ZIPMOE_ERR_INVALID_ARG;
+  int dev = 0;
+  const zipmoe_status rc = current_device(&dev);
+  if (rc != ZIPMOE_OK) return rc;
+  const GroupArgs a = {g->topk_ids, g->offsets, g->order, g->place, g->status_word, g->T * g->k, g->n_experts};
+  // a warp takes up to 256 choices before another block is worth its exchange
+  const uint32_t pieces = (a.n + 31) / 32, threads = std::max(256u, std::min(1024u, (pieces + 3) / 4 * 32));
+  uint32_t S = 1;
+  while (S < 8 && pieces > S * 32 * 4) S <<= 1;
+  cudaLaunchAttribute attrs[2];
+  attrs[0].id = cudaLaunchAttributeClusterDimension;
+  attrs[0].val.clusterDim.x = S;
+  attrs[0].val.clusterDim.y = attrs[0].val.clusterDim.z = 1;
+  attrs[1] = zipmoe_host::overlapped();
+  cudaLaunchConfig_t cfg = {};
+  cfg.stream = reinterpret_cast<cudaStream_t>(stream);
+  cfg.attrs = attrs;
+  cfg.numAttrs = 2;
+  cfg.gridDim = dim3(S);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = threads / 32 * a.E * 4;   // at most 32 KB
+  return cudaLaunchKernelEx(&cfg, group_kernel, a) == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
+}
+
+extern "C" zipmoe_status zipmoe_combine_rows(const zipmoe_combine_args *c, zipmoe_stream stream) {
+  using namespace zipmoe_dev;
+  zipmoe_host::TraceRange trace("zipmoe_combine_rows");
+  if (!c) return ZIPMOE_ERR_INVALID_ARG;
+  if (c->k == 0 || c->k > 8 || c->cols == 0 || c->cols > 1u << 20 || (uint64_t)c->T * c->k > 1u << 30) return ZIPMOE_ERR_UNSUPPORTED;
+  if ((c->flags & ~ZIPMOE_GROUPED_F32) || c->reserved) return ZIPMOE_ERR_INVALID_ARG;
+  if (c->T == 0) return ZIPMOE_OK;
+  if (!c->y || !c->place || !c->out || c->y_pitch < c->cols || c->out_pitch < c->cols) return ZIPMOE_ERR_INVALID_ARG;
+  const bool f32 = c->flags & ZIPMOE_GROUPED_F32;
+  if ((bits(c->y) & (f32 ? 3 : 1)) || (bits(c->out) & 1) || ((bits(c->place) | bits(c->weights) | bits(c->status_word)) & 3))
+    return ZIPMOE_ERR_INVALID_ARG;
+  int dev = 0;
+  const zipmoe_status rc = current_device(&dev);
+  if (rc != ZIPMOE_OK) return rc;
+  const CombineArgs a = {c->y, c->place, c->weights, reinterpret_cast<__nv_bfloat16 *>(c->out), c->y_pitch, c->out_pitch, c->status_word,
+                         c->T, c->k, c->cols, c->rows};
+  const bool wide = c->cols % 4 == 0 && c->y_pitch % 4 == 0 && c->out_pitch % 4 == 0 && (bits(c->y) & (f32 ? 15 : 7)) == 0 && (bits(c->out) & 7) == 0;
+  const uint32_t units = wide ? c->cols / 4 : c->cols;
+  uint32_t x = 32;
+  while (x < 256 && x < units) x <<= 1;
+  cudaLaunchAttribute attr = zipmoe_host::overlapped();
+  cudaLaunchConfig_t cfg = {};
+  cfg.stream = reinterpret_cast<cudaStream_t>(stream);
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  cfg.blockDim = dim3(x, 256 / x);
+  cfg.gridDim = dim3((units + x - 1) / x, std::min(65535u, (c->T + 256 / x - 1) / (256 / x)));
+  const cudaError_t err = f32 ? (wide ? cudaLaunchKernelEx(&cfg, combine_rows_kernel<true, true>, a) : cudaLaunchKernelEx(&cfg, combine_rows_kernel<true, false>, a))
+                              : (wide ? cudaLaunchKernelEx(&cfg, combine_rows_kernel<false, true>, a) : cudaLaunchKernelEx(&cfg, combine_rows_kernel<false, false>, a));
+  return err == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
+}

@@ -114,31 +114,6 @@ __device__ __forceinline__ void pick_experts(const float (&l)[kPer], uint32_t k,
   }
 }
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ uint32_t cluster_size() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %cluster_nctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank) {   // the same place in another block's shared memory
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-  return r;
-}
-// four neighbouring floats of another block's shared memory.  Volatile: it stays behind the cluster's barrier.
-__device__ __forceinline__ float4 load_cluster(uint32_t addr) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
-  return v;
-}
-
 // kPer: experts per lane, E <= 8 * kPer
 template <int kPer>
 __global__ void __launch_bounds__(kRouterThreads) router_kernel(const __grid_constant__ CUtensorMap x_map,
