@@ -484,9 +484,9 @@ typedef struct {
   uint32_t even;               /* 1: each kind of matrix lies at equal distances from group to group                */
   uint32_t reserved;           /* zero                                                                              */
   const void *table;           /* device [n_groups * ZIPMOE_GROUPED_ENTRY_BYTES], 64-byte aligned                   */
-  uint8_t maps[2 * 128];       /* opaque                                                                            */
+  uint8_t maps[4 * 128];       /* opaque                                                                            */
 } zipmoe_grouped_weights;
-#define ZIPMOE_GROUPED_ENTRY_BYTES 256u
+#define ZIPMOE_GROUPED_ENTRY_BYTES 512u
 
 /* Describes weights to zipmoe_grouped_matmul, once, and again when a tensor moves.  Weights at equal distances, in ascending
  * order, are found faster.
@@ -515,9 +515,17 @@ typedef struct {
   uint64_t out_pitch;
   uint32_t *status_word;       /* as for zipmoe_decode: code 1 where offsets or order point outside, 3 when a wait ran
                                   out; may be NULL                                                                  */
+  void *workspace;             /* scratch of at least zipmoe_grouped_workspace_bytes, 16-byte aligned, not shared by calls that
+                                  may overlap; may be NULL where that is 0                                          */
+  uint64_t workspace_bytes;
   uint32_t x_rows, rows, k, flags;
   uint32_t reserved[2];        /* zero                                                                              */
 } zipmoe_grouped_args;
+
+/* Scratch zipmoe_grouped_matmul needs for `rows` rows, gathered (non-zero: `order` is given) or not: room for the gathered rows
+ * of a call with many, else 0.  Host only. */
+zipmoe_status zipmoe_grouped_workspace_bytes(const zipmoe_grouped_weights *weights, uint32_t rows, uint32_t gathered,
+                                             uint64_t *workspace_bytes);
 
 /* Matrix products grouped by expert, group sizes known on the device alone: for every group e and its rows r
  *     acc[r, n] = sum_c x[src(r), c] * W_e[n, c]             (fp32 sums; 8-bit integers: exact)
@@ -526,7 +534,8 @@ typedef struct {
  *     out[r, n] = SiLU(first) * second                       of these, with ZIPMOE_GROUPED_PAIR
  * rounded once.  Rows of `out` that belong to no group are left as they were; a group may be empty.  A row whose `order` points
  * outside x is taken as zeros; where the offsets are not in order, are negative or reach past `rows`, nothing is computed.  Both
- * set status_word (code 1).  One launch on `stream`, asynchronous, no workspace; results do not depend on timing.
+ * set status_word (code 1).  One launch on `stream`, or two where rows are gathered, asynchronous; results do not depend on
+ * timing.
  * Limits: rows and x_rows <= 2^30, k <= 8 (ZIPMOE_ERR_UNSUPPORTED otherwise).  rows = 0 does nothing. */
 zipmoe_status zipmoe_grouped_matmul(const zipmoe_grouped_weights *weights, const zipmoe_grouped_args *args, zipmoe_stream stream);
 

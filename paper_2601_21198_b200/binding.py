@@ -431,23 +431,25 @@ def zipmoe_expert_ffn(tokens, T, topk_ids, topk_weights, k, experts, out, worksp
 
 # ---- the experts' products for prompts, and products in 8-bit integers -----------------------------------
 GROUPED_PAIR, GROUPED_INT8, GROUPED_F32 = 1, 2, 4
-GROUPED_ENTRY_BYTES = 256
+GROUPED_ENTRY_BYTES = 512
 
 
 class GroupedWeightsStruct(ctypes.Structure):
     """zipmoe_grouped_weights."""
     _fields_ = [("n_groups", _u32), ("rows", _u32), ("cols", _u32), ("flags", _u32), ("even", _u32), ("reserved", _u32),
-                ("table", _vp), ("maps", ctypes.c_uint8 * 256)]
+                ("table", _vp), ("maps", ctypes.c_uint8 * 512)]
 
 
 # zipmoe_group_args, zipmoe_grouped_args and zipmoe_combine_args
 _GROUP_ARGS = struct.Struct("<5Q4I")
-_GROUPED_ARGS = struct.Struct("<9Q6I")
+_GROUPED_ARGS = struct.Struct("<11Q6I")
 _COMBINE_ARGS = struct.Struct("<7Q6I")
-assert _GROUP_ARGS.size == 56 and _GROUPED_ARGS.size == 96 and _COMBINE_ARGS.size == 80
+assert _GROUP_ARGS.size == 56 and _GROUPED_ARGS.size == 112 and _COMBINE_ARGS.size == 80
 _lib.zipmoe_group_tokens.argtypes = [ctypes.c_char_p, _vp]
 _lib.zipmoe_grouped_weights_plan.argtypes = [ctypes.POINTER(_vp), _u32, _u32, _u32, _u32, _vp, ctypes.POINTER(GroupedWeightsStruct)]
 _lib.zipmoe_grouped_matmul.argtypes = [ctypes.POINTER(GroupedWeightsStruct), ctypes.c_char_p, _vp]
+_lib.zipmoe_grouped_workspace_bytes.argtypes = [ctypes.POINTER(GroupedWeightsStruct), _u32, _u32, ctypes.POINTER(_u64)]
+_lib.zipmoe_grouped_workspace_bytes.restype = _int
 _lib.zipmoe_combine_rows.argtypes = [ctypes.c_char_p, _vp]
 _lib.zipmoe_quantize_rows.argtypes = [_vp, _u64, _u32, _u32, _vp, _u64, _vp, _vp]
 for _f in ("zipmoe_group_tokens", "zipmoe_grouped_weights_plan", "zipmoe_grouped_matmul", "zipmoe_combine_rows", "zipmoe_quantize_rows"):
@@ -475,11 +477,19 @@ def zipmoe_grouped_weights_plan(tensors, n_groups, rows, cols, flags=0):
     return table, weights
 
 
+def zipmoe_grouped_workspace_bytes(weights, rows, gathered):
+    out = _u64(0)
+    _check("zipmoe_grouped_workspace_bytes",
+           _lib.zipmoe_grouped_workspace_bytes(ctypes.byref(weights), rows, int(gathered), ctypes.byref(out)))
+    return out.value
+
+
 def zipmoe_grouped_matmul(weights, x, x_pitch, x_rows, out, out_pitch, rows, offsets=None, order=None, k=0, row_scales=None,
-                          col_scales=None, flags=0, status_word=None, stream=None):
+                          col_scales=None, flags=0, workspace=None, workspace_bytes=0, status_word=None, stream=None):
     """Pointer arguments are device tensors (or raw device addresses, or None); `weights` is a GroupedWeightsStruct."""
     args = _GROUPED_ARGS.pack(_ptr(x) or 0, x_pitch, _ptr(offsets) or 0, _ptr(order) or 0, _ptr(row_scales) or 0, _ptr(col_scales) or 0,
-                              _ptr(out) or 0, out_pitch, _ptr(status_word) or 0, x_rows, rows, k, flags, 0, 0)
+                              _ptr(out) or 0, out_pitch, _ptr(status_word) or 0, _ptr(workspace) or 0, workspace_bytes, x_rows, rows, k,
+                              flags, 0, 0)
     _check("zipmoe_grouped_matmul", _lib.zipmoe_grouped_matmul(ctypes.byref(weights), args, _ptr(stream)))
 
 
@@ -1026,7 +1036,7 @@ class GroupedMatrix:
                 raise ValueError("weights that lie unevenly are described before a capture, not within it")
             self.table = torch.from_numpy(table).to(self.device)
             self.struct.table = self.table.data_ptr()
-        self._struct_at = ctypes.byref(self.struct)
+        self._struct_at, self._need = ctypes.byref(self.struct), {}
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device) if status is None else status
         self.status_at = _dense("status", self.status, (1,), kinds.int32, index)
 
@@ -1063,8 +1073,16 @@ class GroupedMatrix:
             out = _empty((rows, self.rows), kinds.bf16[0] if self.int8 else x.dtype, self.device, stream)
         f32 = out.dtype in kinds.fp32
         out_at, out_pitch = _rows("out", out, (rows, self.rows), kinds.fp32 if f32 else kinds.bf16, index)
+        need, scratch_at = 0, 0
+        if gather:
+            need = self._need.get(rows)
+            if need is None:
+                need = self._need[rows] = zipmoe_grouped_workspace_bytes(self.struct, rows, True)
+            if need:      # (given back to the stream's pool on return: what is queued there comes before its next use)
+                scratch = _empty((need,), kinds.e4m3[1], self.device, stream)
+                scratch_at = scratch.data_ptr()
         args = _GROUPED_ARGS.pack(x_at, x_pitch, offsets_at, order_at, scales_at, self.scales_at, out_at, out_pitch, self.status_at,
-                                  x_rows, rows, k, GROUPED_F32 if f32 else 0, 0, 0)
+                                  scratch_at, need, x_rows, rows, k, GROUPED_F32 if f32 else 0, 0, 0)
         status = _lib.zipmoe_grouped_matmul(self._struct_at, args, _handle(kinds, index, stream))
         if status:
             raise ZipMoEError("zipmoe_grouped_matmul", status)

@@ -9,7 +9,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libzipmoe.so")
 SOURCES = ["zipmoe_host.cpp", "planner.cpp", "scheduler.cpp", "decode_kernel.cu", "ffn_kernels.cu", "recover_kernel.cu",
            "norm_kernel.cu", "router_kernel.cu", "resident_ffn_kernel.cu", "resident_few_kernel.cu", "group_kernel.cu",
-           "quantize_kernel.cu", "grouped_matmul.cu", "grouped_few_kernel.cu"]
+           "quantize_kernel.cu", "grouped_matmul.cu", "grouped_few_kernel.cu",
+           "grouped_wide_kernel.cu"]
 HEADERS = ["zipmoe_format.h", "decode_device.cuh", "tile_geometry.h", "tensor_core.cuh", "resident.cuh", "resident_choice.h",
            "grouped.cuh", "grouped_launch.h", os.path.join(ROOT, "include", "zipmoe.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "--use_fast_math",

@@ -254,13 +254,13 @@ extern "C" zipmoe_status zipmoe_combine_rows(const zipmoe_combine_args *c, zipmo
   const uint32_t units = wide ? c->cols / 4 : c->cols;
   uint32_t x = 32;
   while (x < 256 && x < units) x <<= 1;
-  cudaLaunchAttribute attr = zipmoe_host::overlapped();
   cudaLaunchConfig_t cfg = {};
   cfg.stream = reinterpret_cast<cudaStream_t>(stream);
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
   cfg.blockDim = dim3(x, 256 / x);
   cfg.gridDim = dim3((units + x - 1) / x, std::min(65535u, (c->T + 256 / x - 1) / (256 / x)));
+  cudaLaunchAttribute attr = zipmoe_host::overlapped_if_whole((uint64_t)cfg.gridDim.x * cfg.gridDim.y, zipmoe_host::current_sms());
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
   const cudaError_t err = f32 ? (wide ? cudaLaunchKernelEx(&cfg, combine_rows_kernel<true, true>, a) : cudaLaunchKernelEx(&cfg, combine_rows_kernel<true, false>, a))
                               : (wide ? cudaLaunchKernelEx(&cfg, combine_rows_kernel<false, true>, a) : cudaLaunchKernelEx(&cfg, combine_rows_kernel<false, false>, a));
   return err == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;

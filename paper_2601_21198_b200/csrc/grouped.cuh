@@ -10,13 +10,14 @@
 namespace zipmoe_dev {
 
 constexpr uint32_t kMaxGroups = 256;
-constexpr uint32_t kPairRows = 16;   // rows of a box of W1 or W3: they alternate in the operand, 16 rows of the one and 16 of the other,
-                                     // so that one warp reads back both values of an output
+constexpr uint32_t kPairRows = 64;   // rows of W1, then as many of W3, make the 128 of an operand
 
-// The maps of all groups' weights at once, where they lie at equal distances (second one: of a pair's W3).
+// The maps of all groups' weights at once, where they lie at equal distances, in the order of a table's entry: boxes of 128 rows of
+// W1 (or the one matrix) and W3, and for pairs boxes of 64.
 struct GroupedMaps {
-  CUtensorMap w[2];
+  CUtensorMap w[4];
 };
+constexpr uint32_t kPairMap = 2 * sizeof(CUtensorMap);   // where an entry's boxes of 64 rows begin
 
 struct GroupedArgs {
   const uint8_t *x;         // rows of Kb bytes, x_pitch bytes apart
@@ -28,7 +29,7 @@ struct GroupedArgs {
   uint8_t *out;             // rows of N elements, out_pitch elements apart
   uint32_t *status;
   uint64_t x_pitch, out_pitch, limit_ns;
-  uint32_t x_rows, k, R, E, N, Kb, even, out_f32, wide, extra_tx;   // wide: rows of out may be stored 16 bytes at a time
+  uint32_t x_rows, k, R, E, N, Kb, even, out_f32, wide, whole, extra_tx;   // wide: rows of out may be stored four elements, whole: 16 bytes at a time
 };
 
 // One product of a step: 32 bytes of K.  kInt8: s8 x s8 -> s32, else bf16 x bf16 -> fp32; a is the weights' operand.
@@ -56,7 +57,7 @@ __device__ __forceinline__ bool group_rows(const GroupedArgs &a, uint32_t e, uin
     count = e == 0 ? a.R : 0;
     return true;
   }
-  const int32_t b = __ldg(a.offsets + e), n = __ldg(a.offsets + e + 1);
+  const int32_t b = __ldcg(a.offsets + e), n = __ldcg(a.offsets + e + 1);
   const bool fine = b >= 0 && n >= b && n <= (int32_t)a.R;
   begin = fine ? b : 0;
   count = fine ? n - b : 0;
@@ -66,7 +67,7 @@ __device__ __forceinline__ bool group_rows(const GroupedArgs &a, uint32_t e, uin
 // The row of x that row r of the product reads; -1 where `order` points outside.
 __device__ __forceinline__ int32_t source_row(const GroupedArgs &a, uint32_t r) {
   if (!a.order) return r < a.x_rows ? (int32_t)r : -1;
-  const int32_t c = __ldg(a.order + r);
+  const int32_t c = __ldcg(a.order + r);
   const uint32_t t = (uint32_t)c / a.k;
   return c >= 0 && t < a.x_rows ? (int32_t)t : -1;
 }
@@ -98,6 +99,4 @@ inline bool make_byte_map(CUtensorMap *map, const void *base, uint64_t rows, uin
   return encode && encode(map, int8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims,
                           strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-}  // namespace zipmoe_host
+}}  // namespace zipmoe_host

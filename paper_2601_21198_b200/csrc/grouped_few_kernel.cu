@@ -55,8 +55,8 @@ __global__ void __launch_bounds__(kFewThreads, 2) grouped_few_kernel(const __gri
     *dead = 0;
     words[2] = 0;
     if (a.even) {
-      prefetch_map(&maps.w[0]);
-      if constexpr (kPair) prefetch_map(&maps.w[1]);
+      prefetch_map(&maps.w[kPair ? 2 : 0]);
+      if constexpr (kPair) prefetch_map(&maps.w[3]);
     }
     fence_barrier_init();
   }
@@ -110,10 +110,10 @@ __global__ void __launch_bounds__(kFewThreads, 2) grouped_few_kernel(const __gri
   if (work && warp == 0 && lane == 0) {
     // ---- weights ----
     const uint64_t policy = policy_evict_first();
-    const void *m0 = &maps.w[0], *m1 = &maps.w[1];
+    const void *m0 = &maps.w[kPair ? 2 : 0], *m1 = &maps.w[3];
     if (!a.even) {
-      m0 = a.table + (size_t)u.e * ZIPMOE_GROUPED_ENTRY_BYTES;
-      m1 = a.table + (size_t)u.e * ZIPMOE_GROUPED_ENTRY_BYTES + 128;
+      m0 = a.table + (size_t)u.e * ZIPMOE_GROUPED_ENTRY_BYTES + (kPair ? kPairMap : 0);
+      m1 = a.table + (size_t)u.e * ZIPMOE_GROUPED_ENTRY_BYTES + kPairMap + 128;
       acquire_map(m0);
       if constexpr (kPair) acquire_map(m1);
     }
@@ -125,11 +125,8 @@ __global__ void __launch_bounds__(kFewThreads, 2) grouped_few_kernel(const __gri
       const int32_t x = (int32_t)(s * (kInt8 ? 128 : 64));
       mbar_expect_tx(bar, kFewWeights + a.extra_tx);
       if constexpr (kPair) {
-#pragma unroll
-        for (uint32_t c = 0; c < 4; ++c) {
-          tma_load_3d(dst + c * 4096, m0, x, (int32_t)(u.rows0 + c * kPairRows), z, bar, policy);
-          tma_load_3d(dst + c * 4096 + 2048, m1, x, (int32_t)(u.rows0 + c * kPairRows), z, bar, policy);
-        }
+        tma_load_3d(dst, m0, x, (int32_t)u.rows0, z, bar, policy);
+        tma_load_3d(dst + kFewWeights / 2, m1, x, (int32_t)u.rows0, z, bar, policy);
       } else {
         tma_load_3d(dst, m0, x, (int32_t)u.rows0, z, bar, policy);
       }
@@ -231,14 +228,13 @@ __global__ void __launch_bounds__(kFewThreads, 2) grouped_few_kernel(const __gri
     uint32_t base[8];
 #pragma unroll
     for (uint32_t r = 0; r < 8; ++r) base[r] = in_block(ring0, r < S ? r : 0);
-    const uint32_t col = kPair ? u.rows0 + (lane >> 3) * kPairRows + (lane & 3) * 4 : u.rows0 + lane * 4;
-    const bool mine = kPair ? (lane & 4) == 0 && col < a.N : col < a.N;
+    const uint32_t col = u.rows0 + (kPair ? lane & 15 : lane) * 4;   // (lanes 16-31 have W3's sums of a pair)
+    const bool mine = (!kPair || lane < 16) && col < a.N;
     float scale[4] = {1.f, 1.f, 1.f, 1.f};
     if constexpr (kInt8) {
-      const float *from = a.col_scales + (size_t)u.e * a.N + (kPair && (lane & 4) ? (size_t)a.E * a.N : 0);
-      const uint32_t c0 = kPair ? u.rows0 + (lane >> 3) * kPairRows + (lane & 3) * 4 : col;
+      const float *from = a.col_scales + (size_t)u.e * a.N + (kPair && lane >= 16 ? (size_t)a.E * a.N : 0);
 #pragma unroll
-      for (uint32_t i = 0; i < 4; ++i) scale[i] = c0 + i < a.N ? __ldcg(from + c0 + i) : 0.f;
+      for (uint32_t i = 0; i < 4; ++i) scale[i] = col + i < a.N ? __ldcg(from + col + i) : 0.f;
     }
     for (uint32_t t = rank + S * warp; t < u.n; t += S * (kFewThreads / 32)) {
       float4 v[8];
@@ -273,7 +269,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) grouped_few_kernel(const __gri
       if constexpr (kPair) {
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i) {
-          const float up = __shfl_down_sync(0xFFFFFFFFu, sum[i], 4);
+          const float up = __shfl_down_sync(0xFFFFFFFFu, sum[i], 16);
           sum[i] = silu_product(sum[i], up);
         }
       }
@@ -331,7 +327,7 @@ zipmoe_status launch(int dev, const zipmoe_dev::GroupedMaps &maps, const zipmoe_
   attrs[0].id = cudaLaunchAttributeClusterDimension;
   attrs[0].val.clusterDim.x = S;
   attrs[0].val.clusterDim.y = attrs[0].val.clusterDim.z = 1;
-  attrs[1] = zipmoe_host::overlapped();
+  attrs[1] = zipmoe_host::overlapped_if_whole(units * S, at_once);
   cudaLaunchConfig_t cfg = {};
   cfg.stream = stream;
   cfg.attrs = attrs;

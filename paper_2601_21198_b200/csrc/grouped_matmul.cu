@@ -1,6 +1,7 @@
 // The entry points of the grouped products: how a layer's weights are described once, and the checks of a call.
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <cstring>
 
@@ -17,39 +18,59 @@ bool sizes_ok(uint32_t n_groups, uint32_t rows, uint32_t cols, uint32_t flags) {
          cols % (flags & ZIPMOE_GROUPED_INT8 ? 16 : 8) == 0;
 }
 
+// Which kernel takes a call.
+bool wide_pays(const zipmoe_grouped_weights *w, uint32_t rows) {
+  return rows > 64 * std::min(w->n_groups, rows);   // TODO
+}
+
+uint64_t workspace_need(const zipmoe_grouped_weights *w, uint32_t rows, bool gathered) {
+  return gathered && wide_pays(w, rows) ? (uint64_t)rows * w->cols * (w->flags & ZIPMOE_GROUPED_INT8 ? 1 : 2) : 0;
+}
+
 }  // namespace
+
+extern "C" zipmoe_status zipmoe_grouped_workspace_bytes(const zipmoe_grouped_weights *w, uint32_t rows, uint32_t gathered,
+                                                        uint64_t *workspace_bytes) {
+  if (!w || !workspace_bytes || (w->flags & ~kFlags)) return ZIPMOE_ERR_INVALID_ARG;
+  if (!sizes_ok(w->n_groups, w->rows, w->cols, w->flags) || rows > 1u << 30) return ZIPMOE_ERR_UNSUPPORTED;
+  *workspace_bytes = workspace_need(w, rows, gathered != 0);
+  return ZIPMOE_OK;
+}
 
 extern "C" zipmoe_status zipmoe_grouped_weights_plan(const void *const *tensors, uint32_t n_groups, uint32_t rows, uint32_t cols, uint32_t flags,
                                                      void *table, zipmoe_grouped_weights *weights) {
   if (flags & ~kFlags) return ZIPMOE_ERR_INVALID_ARG;
   if (!sizes_ok(n_groups, rows, cols, flags)) return ZIPMOE_ERR_UNSUPPORTED;
   if (!tensors || !table || !weights) return ZIPMOE_ERR_INVALID_ARG;
-  static_assert(2 * sizeof(CUtensorMap) == ZIPMOE_GROUPED_ENTRY_BYTES, "an entry is two tensor maps");
+  static_assert(4 * sizeof(CUtensorMap) == ZIPMOE_GROUPED_ENTRY_BYTES, "an entry is four tensor maps");
   const uint32_t each = flags & ZIPMOE_GROUPED_PAIR ? 2 : 1;
   const bool int8 = flags & ZIPMOE_GROUPED_INT8;
   for (uint32_t i = 0; i < each * n_groups; ++i)
     if (!tensors[i] || (bits(tensors[i]) & 15)) return ZIPMOE_ERR_INVALID_ARG;
   const uint64_t row_bytes = (uint64_t)cols * (int8 ? 1 : 2), bytes = rows * row_bytes;
-  const uint32_t box_rows = each == 2 ? zipmoe_dev::kPairRows : 128;
   std::memset(weights, 0, sizeof(*weights));
   std::memset(table, 0, (size_t)n_groups * ZIPMOE_GROUPED_ENTRY_BYTES);
-  auto describe = [&](uint8_t *to, const void *base, uint64_t n, uint64_t distance) {
+  // the maps of matrix j of an entry (0 the one matrix or W1, 1 W3), of n groups
+  auto describe = [&](uint8_t *entry, uint32_t j, const void *base, uint64_t n, uint64_t distance) {
     CUtensorMap map;
-    if (!zipmoe_host::make_byte_map(&map, base, rows, row_bytes, row_bytes, box_rows, n, distance, int8)) return false;
-    std::memcpy(to, &map, sizeof(map));
+    if (!zipmoe_host::make_byte_map(&map, base, rows, row_bytes, row_bytes, 128, n, distance, int8)) return false;
+    std::memcpy(entry + 128 * j, &map, sizeof(map));
+    if (each == 1) return true;
+    if (!zipmoe_host::make_byte_map(&map, base, rows, row_bytes, row_bytes, zipmoe_dev::kPairRows, n, distance, int8)) return false;
+    std::memcpy(entry + zipmoe_dev::kPairMap + 128 * j, &map, sizeof(map));
     return true;
   };
   for (uint32_t i = 0; i < each * n_groups; ++i)
-    if (!describe(static_cast<uint8_t *>(table) + (size_t)(i / each) * ZIPMOE_GROUPED_ENTRY_BYTES + 128 * (i % each), tensors[i], 1, (bytes + 15) & ~15ull))
+    if (!describe(static_cast<uint8_t *>(table) + (size_t)(i / each) * ZIPMOE_GROUPED_ENTRY_BYTES, i % each, tensors[i], 1, bytes))
       return ZIPMOE_ERR_CUDA;
   // evenly spaced groups: one map serves them all
   bool even = true;
   for (uint32_t j = 0; j < each && even; ++j) {
-    const uintptr_t first = bits(tensors[j]), second = n_groups > 1 ? bits(tensors[each + j]) : first + ((bytes + 15) & ~15ull);
+    const uintptr_t first = bits(tensors[j]), second = n_groups > 1 ? bits(tensors[each + j]) : first + bytes;
     const uint64_t distance = second - first;
     even = second > first && distance >= bytes && distance < 1ull << 40;
     for (uint32_t e = 2; e < n_groups && even; ++e) even = bits(tensors[each * e + j]) == first + e * distance;
-    if (even && !describe(weights->maps + 128 * j, tensors[j], n_groups, distance)) return ZIPMOE_ERR_CUDA;
+    if (even && !describe(weights->maps, j, tensors[j], n_groups, distance)) return ZIPMOE_ERR_CUDA;
   }
   weights->n_groups = n_groups;
   weights->rows = rows;
@@ -75,6 +96,9 @@ extern "C" zipmoe_status zipmoe_grouped_matmul(const zipmoe_grouped_weights *w, 
   if ((bits(g->x) & 15) || (bits(w->table) & 63) || (bits(g->out) & (f32 ? 3 : 1)) ||
       ((bits(g->offsets) | bits(g->order) | bits(g->row_scales) | bits(g->col_scales) | bits(g->status_word)) & 3))
     return ZIPMOE_ERR_INVALID_ARG;
+  const uint64_t need = workspace_need(w, g->rows, g->order != nullptr);
+  if (need && (!g->workspace || (bits(g->workspace) & 15))) return ZIPMOE_ERR_INVALID_ARG;
+  if (g->workspace_bytes < need) return ZIPMOE_ERR_BUFFER_TOO_SMALL;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return ZIPMOE_ERR_CUDA;
   static bool ready[64];
@@ -107,7 +131,9 @@ extern "C" zipmoe_status zipmoe_grouped_matmul(const zipmoe_grouped_weights *w, 
   a.even = w->even;
   a.out_f32 = f32;
   a.wide = g->out_pitch % 4 == 0 && (bits(g->out) & (f32 ? 15 : 7)) == 0;
+  a.whole = g->out_pitch % (f32 ? 4 : 8) == 0 && (bits(g->out) & 15) == 0;
   GroupedMaps maps;
   std::memcpy(&maps, w->maps, sizeof(maps));
+  if (wide_pays(w, g->rows)) return zipmoe_host::launch_grouped_wide(dev, int8, pair, maps, a, g->workspace, reinterpret_cast<cudaStream_t>(stream));
   return zipmoe_host::launch_grouped_few(dev, int8, pair, maps, a, reinterpret_cast<cudaStream_t>(stream));
 }

@@ -114,7 +114,7 @@ namespace {
 template <uint32_t kThreads>
 cudaError_t launch(const zipmoe_dev::QuantizeArgs &a, bool wide, cudaStream_t stream) {
   constexpr uint32_t kRows = kThreads < 128 ? 128 / kThreads : 1;
-  cudaLaunchAttribute attr = zipmoe_host::overlapped();
+  cudaLaunchAttribute attr = zipmoe_host::overlapped_if_whole((a.rows + kRows - 1) / kRows, zipmoe_host::current_sms());
   cudaLaunchConfig_t cfg = {};
   cfg.stream = stream;
   cfg.attrs = &attr;

@@ -38,21 +38,6 @@ struct Active {
 
 __host__ __device__ inline uint32_t pad16(uint32_t bytes) { return (bytes + 15) & ~15u; }
 
-// The warps that share named barrier 1 give up together or not at all: the barrier counts all of them.
-template <int kThreads>
-__device__ __forceinline__ bool all_agree(bool ok) {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\t"
-      "barrier.cta.red.and.pred p, 1, %2, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(r)
-      : "r"((uint32_t)ok), "n"(kThreads)
-      : "memory");
-  return r != 0;
-}
-template <int kThreads>
-__device__ __forceinline__ void sync_group() { asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory"); }
-
 __device__ __forceinline__ float silu_times(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
 
 // h enters W2's product as the sum of two bf16 numbers, 16 significant bits together: rounded to one, outputs were 1.35 to 1.6

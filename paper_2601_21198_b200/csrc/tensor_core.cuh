@@ -170,6 +170,21 @@ __device__ __forceinline__ void arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+// The warps that share named barrier 1 give up together or not at all: the barrier counts all of them.
+template <int kThreads>
+__device__ __forceinline__ bool all_agree(bool ok) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\t"
+      "barrier.cta.red.and.pred p, 1, %2, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r)
+      : "r"((uint32_t)ok), "n"(kThreads)
+      : "memory");
+  return r != 0;
+}
+template <int kThreads>
+__device__ __forceinline__ void sync_group() { asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory"); }
+
 // ---- blocks of a cluster ----
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -217,6 +232,14 @@ inline cudaLaunchAttribute overlapped() {
   cudaLaunchAttribute a;
   a.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   a.val.programmaticStreamSerializationAllowed = 1;
+  return a;
+}
+
+// The same for a grid of `blocks`, of which `at_once` fit the device: one that does not fit as a whole is not set up ahead, since
+// its waiting blocks would take registers and slots that its predecessor's last blocks may need.
+inline cudaLaunchAttribute overlapped_if_whole(uint64_t blocks, uint64_t at_once) {
+  cudaLaunchAttribute a = overlapped();
+  a.val.programmaticStreamSerializationAllowed = blocks <= at_once;
   return a;
 }
 

@@ -39,8 +39,8 @@ def test_grouped_matmul_refusals(zb):
     def weights(E=4, rows=64, cols=64, flags=0, even=1, table=None):
         return zb.GroupedWeightsStruct(E, rows, cols, flags, even, 0, table)
 
-    def call(w=None, x=A, xp=64, xr=8, out=A, op=64, rows=8, offsets=A, order=None, k=0, rs=None, cs=None, flags=0, status=None):
-        zb.zipmoe_grouped_matmul(w or weights(), x, xp, xr, out, op, rows, offsets, order, k, rs, cs, flags, status)
+    def call(w=None, x=A, xp=64, xr=8, out=A, op=64, rows=8, offsets=A, order=None, k=0, rs=None, cs=None, flags=0, ws=None, n=0, status=None):
+        zb.zipmoe_grouped_matmul(w or weights(), x, xp, xr, out, op, rows, offsets, order, k, rs, cs, flags, ws, n, status)
 
     for kw in (dict(x=None), dict(out=None), dict(xr=0), dict(xr=7), dict(xp=56), dict(op=63), dict(offsets=None), dict(order=A),
                dict(w=weights(even=0)), dict(w=weights(even=2)), dict(w=weights(flags=4)), dict(flags=1), dict(rs=A), dict(cs=A),
@@ -52,6 +52,14 @@ def test_grouped_matmul_refusals(zb):
                dict(w=weights(rows=(1 << 20) + 1), op=1 << 21), dict(rows=(1 << 30) + 1), dict(xr=(1 << 30) + 1)):
         refused(zb, zb.ERR_UNSUPPORTED, call, **kw)
     call(rows=0)
+    # gathered rows need room where there are many
+    need = zb.zipmoe_grouped_workspace_bytes(weights(), 10000, True)
+    assert need == 10000 * 64 * 2 and zb.zipmoe_grouped_workspace_bytes(weights(), 10000, False) == 0
+    assert zb.zipmoe_grouped_workspace_bytes(weights(), 1, True) == 0
+    many = dict(rows=10000, xr=10000, order=A, k=1)
+    refused(zb, zb.ERR_INVALID_ARG, call, ws=None, n=need, **many)
+    refused(zb, zb.ERR_INVALID_ARG, call, ws=A + 8, n=need, **many)
+    refused(zb, zb.ERR_BUFFER_TOO_SMALL, call, ws=A, n=need - 1, **many)
 
 
 def test_plan_refusals(zb):
