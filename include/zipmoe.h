@@ -567,6 +567,28 @@ zipmoe_status zipmoe_combine_rows(const zipmoe_combine_args *args, zipmoe_stream
 zipmoe_status zipmoe_quantize_rows(const uint16_t *x, uint64_t x_pitch, uint32_t rows, uint32_t cols, int8_t *q, uint64_t q_pitch,
                                    float *scales, zipmoe_stream stream);
 
+/* One call of zipmoe_linear_int8.  A HOST struct holding DEVICE pointers; pitches in elements between rows. */
+typedef struct {
+  const uint16_t *x;           /* in: [rows] of cols bf16 patterns, x_pitch apart                                   */
+  uint64_t x_pitch;
+  const float *col_scales;     /* in: scales of the weights' rows                                                   */
+  void *out;                   /* out: as for zipmoe_grouped_matmul                                                 */
+  uint64_t out_pitch;
+  void *workspace;             /* scratch of at least zipmoe_linear_int8_workspace_bytes, 16-byte aligned, not shared by calls
+                                  that may overlap                                                                  */
+  uint64_t workspace_bytes;
+  uint32_t *status_word;       /* as for zipmoe_grouped_matmul; may be NULL                                         */
+  uint32_t rows, flags;        /* flags: 0 or ZIPMOE_GROUPED_F32                                                    */
+  uint64_t reserved;           /* zero                                                                              */
+} zipmoe_linear_args;
+
+/* Scratch zipmoe_linear_int8 needs for `rows` rows.  Host only. */
+zipmoe_status zipmoe_linear_int8_workspace_bytes(const zipmoe_grouped_weights *weights, uint32_t rows, uint64_t *workspace_bytes);
+
+/* A dense projection of bf16 rows in 8-bit integers: zipmoe_quantize_rows of x, then zipmoe_grouped_matmul of one group.
+ * weights: one group of 8-bit integers, no pair.  Two launches on `stream`, asynchronous.  rows = 0 does nothing. */
+zipmoe_status zipmoe_linear_int8(const zipmoe_grouped_weights *weights, const zipmoe_linear_args *args, zipmoe_stream stream);
+
 /* ---- cache-pool planning (host only, no CUDA) ------------------------------
  * The paper's planner sizes four cache pools for experts in different compression states -- F full
  * tensors, C compressed (E-chunks and SM-chunks), S SM-chunks only, E E-chunks only -- from a

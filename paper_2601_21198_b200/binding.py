@@ -440,17 +440,21 @@ class GroupedWeightsStruct(ctypes.Structure):
                 ("table", _vp), ("maps", ctypes.c_uint8 * 512)]
 
 
-# zipmoe_group_args, zipmoe_grouped_args and zipmoe_combine_args
+# zipmoe_group_args, zipmoe_grouped_args, zipmoe_combine_args and zipmoe_linear_args
 _GROUP_ARGS = struct.Struct("<5Q4I")
 _GROUPED_ARGS = struct.Struct("<11Q6I")
 _COMBINE_ARGS = struct.Struct("<7Q6I")
-assert _GROUP_ARGS.size == 56 and _GROUPED_ARGS.size == 112 and _COMBINE_ARGS.size == 80
+_LINEAR_ARGS = struct.Struct("<8Q2IQ")
+assert _GROUP_ARGS.size == 56 and _GROUPED_ARGS.size == 112 and _COMBINE_ARGS.size == 80 and _LINEAR_ARGS.size == 80
 _lib.zipmoe_group_tokens.argtypes = [ctypes.c_char_p, _vp]
 _lib.zipmoe_grouped_weights_plan.argtypes = [ctypes.POINTER(_vp), _u32, _u32, _u32, _u32, _vp, ctypes.POINTER(GroupedWeightsStruct)]
 _lib.zipmoe_grouped_matmul.argtypes = [ctypes.POINTER(GroupedWeightsStruct), ctypes.c_char_p, _vp]
 _lib.zipmoe_grouped_workspace_bytes.argtypes = [ctypes.POINTER(GroupedWeightsStruct), _u32, _u32, ctypes.POINTER(_u64)]
 _lib.zipmoe_grouped_workspace_bytes.restype = _int
 _lib.zipmoe_combine_rows.argtypes = [ctypes.c_char_p, _vp]
+_lib.zipmoe_linear_int8_workspace_bytes.argtypes = [ctypes.POINTER(GroupedWeightsStruct), _u32, ctypes.POINTER(_u64)]
+_lib.zipmoe_linear_int8.argtypes = [ctypes.POINTER(GroupedWeightsStruct), ctypes.c_char_p, _vp]
+_lib.zipmoe_linear_int8_workspace_bytes.restype = _lib.zipmoe_linear_int8.restype = _int
 _lib.zipmoe_quantize_rows.argtypes = [_vp, _u64, _u32, _u32, _vp, _u64, _vp, _vp]
 for _f in ("zipmoe_group_tokens", "zipmoe_grouped_weights_plan", "zipmoe_grouped_matmul", "zipmoe_combine_rows", "zipmoe_quantize_rows"):
     getattr(_lib, _f).restype = _int
@@ -504,6 +508,20 @@ def zipmoe_quantize_rows(x, x_pitch, rows, cols, q, q_pitch, scales, stream=None
     """Pointer arguments are device tensors (or raw device addresses); pitches in elements."""
     _check("zipmoe_quantize_rows",
            _lib.zipmoe_quantize_rows(_ptr(x), x_pitch, rows, cols, _ptr(q), q_pitch, _ptr(scales), _ptr(stream)))
+
+
+def zipmoe_linear_int8_workspace_bytes(weights, rows):
+    out = _u64(0)
+    _check("zipmoe_linear_int8_workspace_bytes", _lib.zipmoe_linear_int8_workspace_bytes(ctypes.byref(weights), rows, ctypes.byref(out)))
+    return out.value
+
+
+def zipmoe_linear_int8(weights, x, x_pitch, rows, col_scales, out, out_pitch, workspace, workspace_bytes, flags=0, status_word=None,
+                       stream=None):
+    """Pointer arguments are device tensors (or raw device addresses, or None); `weights` is a GroupedWeightsStruct."""
+    args = _LINEAR_ARGS.pack(_ptr(x) or 0, x_pitch, _ptr(col_scales) or 0, _ptr(out) or 0, out_pitch, _ptr(workspace) or 0,
+                             workspace_bytes, _ptr(status_word) or 0, rows, flags, 0)
+    _check("zipmoe_linear_int8", _lib.zipmoe_linear_int8(ctypes.byref(weights), args, _ptr(stream)))
 
 
 class LaunchInfo(ctypes.Structure):
@@ -1149,7 +1167,23 @@ class Int8Linear:
     def product(self, x, out=None, stream=None):
         """x [tokens, cols] bf16 (or int16 patterns) -> out [tokens, rows], bf16 (x's dtype) unless `out` is given, which may be
         fp32: every token is rounded to 8 bits with a scale of its own, the sums are exact."""
-        q, scales = quantize_rows(x, stream=stream)
+        m = self.matrix
+        kinds, index = m.kinds, m.index
+        if kinds.current_device() != index:
+            with _on_device(index):
+                return self.product(x, out, stream)
+        rows = x.shape[0]
+        x_at, x_pitch = _rows("x", x, (rows, self.cols), kinds.bf16, index)
         if out is None:
-            out = _empty((x.shape[0], self.rows), x.dtype, x.device, stream)
-        return self.matrix.product(q, row_scales=scales, out=out, stream=stream)
+            out = _empty((rows, self.rows), x.dtype, x.device, stream)
+        f32 = out.dtype in kinds.fp32
+        out_at, out_pitch = _rows("out", out, (rows, self.rows), kinds.fp32 if f32 else kinds.bf16, index)
+        # the integers and their scales; given back to the stream's pool on return: what is queued there comes before its next use
+        need = rows * (self.cols + 4)
+        scratch = _empty((need,), kinds.e4m3[1], x.device, stream)
+        args = _LINEAR_ARGS.pack(x_at, x_pitch, m.scales_at, out_at, out_pitch, scratch.data_ptr(), need, m.status_at, rows,
+                                 GROUPED_F32 if f32 else 0, 0)
+        status = _lib.zipmoe_linear_int8(m._struct_at, args, _handle(kinds, index, stream))
+        if status:
+            raise ZipMoEError("zipmoe_linear_int8", status)
+        return out

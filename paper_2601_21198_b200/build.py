@@ -12,7 +12,7 @@ SOURCES = ["zipmoe_host.cpp", "planner.cpp", "scheduler.cpp", "decode_kernel.cu"
            "quantize_kernel.cu", "grouped_matmul.cu", "grouped_few_kernel.cu",
            "grouped_wide_kernel.cu"]
 HEADERS = ["zipmoe_format.h", "decode_device.cuh", "tile_geometry.h", "tensor_core.cuh", "resident.cuh", "resident_choice.h",
-           "grouped.cuh", "grouped_launch.h", os.path.join(ROOT, "include", "zipmoe.h")]
+           "grouped.cuh", "grouped_launch.h", "grouped_choice.h", os.path.join(ROOT, "include", "zipmoe.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "--use_fast_math",
               "-Xcompiler", "-fPIC,-O3,-Wall", "-shared", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 

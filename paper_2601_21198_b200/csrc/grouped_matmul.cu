@@ -1,11 +1,11 @@
 // The entry points of the grouped products: how a layer's weights are described once, and the checks of a call.
 #include <cuda_runtime.h>
 
-#include <algorithm>
 #include <cstdint>
 #include <cstring>
 
 #include "zipmoe.h"
+#include "grouped_choice.h"
 #include "grouped_launch.h"
 
 namespace {
@@ -18,13 +18,14 @@ bool sizes_ok(uint32_t n_groups, uint32_t rows, uint32_t cols, uint32_t flags) {
          cols % (flags & ZIPMOE_GROUPED_INT8 ? 16 : 8) == 0;
 }
 
-// Which kernel takes a call.
-bool wide_pays(const zipmoe_grouped_weights *w, uint32_t rows) {
-  return rows > 64 * std::min(w->n_groups, rows);   // TODO
+bool wide_pays(const zipmoe_grouped_weights *w, uint32_t rows, bool gathered) {
+  return zipmoe_host::grouped_wide_pays({w->n_groups, rows, w->rows, w->cols * (w->flags & ZIPMOE_GROUPED_INT8 ? 1 : 2),
+                                         (w->flags & ZIPMOE_GROUPED_INT8) != 0, (w->flags & ZIPMOE_GROUPED_PAIR) != 0, gathered},
+                                        zipmoe_host::current_sms());
 }
 
 uint64_t workspace_need(const zipmoe_grouped_weights *w, uint32_t rows, bool gathered) {
-  return gathered && wide_pays(w, rows) ? (uint64_t)rows * w->cols * (w->flags & ZIPMOE_GROUPED_INT8 ? 1 : 2) : 0;
+  return gathered && wide_pays(w, rows, true) ? (uint64_t)rows * w->cols * (w->flags & ZIPMOE_GROUPED_INT8 ? 1 : 2) : 0;
 }
 
 }  // namespace
@@ -134,6 +135,41 @@ extern "C" zipmoe_status zipmoe_grouped_matmul(const zipmoe_grouped_weights *w, 
   a.whole = g->out_pitch % (f32 ? 4 : 8) == 0 && (bits(g->out) & 15) == 0;
   GroupedMaps maps;
   std::memcpy(&maps, w->maps, sizeof(maps));
-  if (wide_pays(w, g->rows)) return zipmoe_host::launch_grouped_wide(dev, int8, pair, maps, a, g->workspace, reinterpret_cast<cudaStream_t>(stream));
+  if (wide_pays(w, g->rows, g->order != nullptr)) return zipmoe_host::launch_grouped_wide(dev, int8, pair, maps, a, g->workspace, reinterpret_cast<cudaStream_t>(stream));
   return zipmoe_host::launch_grouped_few(dev, int8, pair, maps, a, reinterpret_cast<cudaStream_t>(stream));
+}
+
+extern "C" zipmoe_status zipmoe_linear_int8_workspace_bytes(const zipmoe_grouped_weights *w, uint32_t rows, uint64_t *workspace_bytes) {
+  if (!w || !workspace_bytes || w->flags != ZIPMOE_GROUPED_INT8 || w->n_groups != 1) return ZIPMOE_ERR_INVALID_ARG;
+  if (!sizes_ok(1, w->rows, w->cols, w->flags) || rows > 1u << 30) return ZIPMOE_ERR_UNSUPPORTED;
+  *workspace_bytes = (uint64_t)rows * w->cols + 4ull * rows;
+  return ZIPMOE_OK;
+}
+
+extern "C" zipmoe_status zipmoe_linear_int8(const zipmoe_grouped_weights *w, const zipmoe_linear_args *l, zipmoe_stream stream) {
+  zipmoe_host::TraceRange trace("zipmoe_linear_int8");
+  if (!l || l->reserved) return ZIPMOE_ERR_INVALID_ARG;
+  uint64_t need = 0;
+  zipmoe_status rc = zipmoe_linear_int8_workspace_bytes(w, l->rows, &need);
+  if (rc != ZIPMOE_OK || l->rows == 0) return rc;
+  if (!l->workspace || (bits(l->workspace) & 15)) return ZIPMOE_ERR_INVALID_ARG;
+  if (l->workspace_bytes < need) return ZIPMOE_ERR_BUFFER_TOO_SMALL;
+  int8_t *q = static_cast<int8_t *>(l->workspace);
+  float *scales = reinterpret_cast<float *>(q + (uint64_t)l->rows * w->cols);   // (cols are whole 16s)
+  zipmoe_grouped_args g = {};
+  g.x = q;
+  g.x_pitch = w->cols;
+  g.row_scales = scales;
+  g.col_scales = l->col_scales;
+  g.out = l->out;
+  g.out_pitch = l->out_pitch;
+  g.status_word = l->status_word;
+  g.x_rows = g.rows = l->rows;
+  g.flags = l->flags;
+  // (what the product would refuse is refused before anything is launched)
+  if ((l->flags & ~ZIPMOE_GROUPED_F32) || !l->out || !l->col_scales || l->out_pitch < w->rows || w->even != 1 || w->reserved ||
+      (bits(l->out) & (l->flags & ZIPMOE_GROUPED_F32 ? 3 : 1)) || ((bits(l->col_scales) | bits(l->status_word)) & 3))
+    return ZIPMOE_ERR_INVALID_ARG;
+  rc = zipmoe_quantize_rows(l->x, l->x_pitch, l->rows, w->cols, q, w->cols, scales, stream);
+  return rc == ZIPMOE_OK ? zipmoe_grouped_matmul(w, &g, stream) : rc;
 }

@@ -1,8 +1,9 @@
 // Rows of bf16 to 8-bit integers with a scale per row:  a = max |x|,  q = rint(127 x / a),  scale = a / 127.
 // Bound: 3 bytes per element.  A row stays in registers between its maximum and its stores.
-// 127 x is exact in fp32 (8 + 7 significant bits), and where the quotient 127 x / a is not itself half way between two integers
-// it is at least 1 / (2 * 255 * 127) of its value away from there: the correctly rounded division gives the integer that the
-// real numbers give.
+// With x = X 2^i and a = A 2^j, X and A whole numbers below 256, the quotient t = 127 X 2^(i-j) / A is either half way between two
+// integers, or |254 X - (2m + 1) A 2^(j-i)| / (2A 2^(j-i)) >= t / (254 X) > t 2^-16 away from there.  x * (127 / a) with two roundings
+// is off by t 2^-23 at most: rounded to 19 significant bits (t 2^-20 at most from there) it is the half where t is one, and on
+// the right side of it where t is not.  So the integers are those that the real numbers give, without a division per element.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -22,17 +23,22 @@ struct QuantizeArgs {
   uint32_t rows, cols;
 };
 
-// The correctly rounded quotient, subnormal numbers included (which this library's compilation would flush otherwise).
+// The product and the quotient, correctly rounded, subnormal numbers included (which this library's compilation flushes otherwise).
+__device__ __forceinline__ float times(float x, float y) {
+  float r;
+  asm("mul.rn.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+  return r;
+}
 __device__ __forceinline__ float divided(float x, float y) {
   float r;
   asm("div.rn.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
   return r;
 }
-// Where a row has a NaN or an infinity its scale is NaN and its integers are 0, so that whatever is computed from it is NaN.
-__device__ __forceinline__ uint32_t quantized(float x, float a, float by) {   // by: 127, as often halved as a is
-  float p;
-  asm("mul.rn.f32 %0, %1, %2;" : "=f"(p) : "f"(x), "f"(by));
-  return (uint32_t)__float2int_rn(divided(p, a)) & 0xFFu;
+// x * by, rounded to 19 bits, rounded to an integer.  Where a row has a NaN or an infinity its scale is NaN and its integers are 0,
+// so that whatever is computed from it is NaN.
+__device__ __forceinline__ uint32_t quantized(float x, float by) {
+  const float t = __fmul_rn(x, by), c = __fmul_rn(t, 33.f);
+  return (uint32_t)__float2int_rn(__fsub_rn(c, __fsub_rn(c, t))) & 0xFFu;
 }
 
 // kThreads threads per row, 8 vectors of 8 columns each (kWide) or 64 single columns; blocks of 128 threads at least.
@@ -81,7 +87,8 @@ __global__ void __launch_bounds__(kThreads < 128 ? 128 : kThreads) quantize_kern
   const float m = __uint_as_float(top);
   if (t == 0) a.scales[row] = finite ? divided(m, 127.f) : __uint_as_float(0x7FC00000u);
   const bool zeros = top == 0 || !finite;
-  const float halved = m >= 0x1p100f ? 0x1p-64f : 1.f, a_max = m >= 0x1p100f ? m * halved : m, by = 127.f * halved;   // 127 x may not overflow
+  // 127 / a is a number, and x * (127 / a) loses nothing, while a is neither very small nor very large; others are moved by 2^96
+  const float move = m >= 0x1p100f ? 0x1p-96f : m < 0x1p-90f ? 0x1p96f : 1.f, by = zeros ? 0.f : divided(127.f, times(m, move));
   int8_t *q = a.q + (uint64_t)row * a.q_pitch;
   if constexpr (kWide) {
 #pragma unroll
@@ -93,7 +100,12 @@ __global__ void __launch_bounds__(kThreads < 128 ? 128 : kThreads) quantize_kern
       if (!zeros)
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) {
-          const uint32_t lo = quantized(__uint_as_float(w[j] << 16), a_max, by), hi = quantized(__uint_as_float(w[j] & 0xFFFF0000u), a_max, by);
+          float x0 = __uint_as_float(w[j] << 16), x1 = __uint_as_float(w[j] & 0xFFFF0000u);
+          if (move != 1.f) {
+            x0 = times(x0, move);
+            x1 = times(x1, move);
+          }
+          const uint32_t lo = quantized(x0, by), hi = quantized(x1, by);
           o[j >> 1] |= (lo | hi << 8) << (16 * (j & 1));
         }
       *reinterpret_cast<uint2 *>(q + c) = make_uint2(o[0], o[1]);
@@ -102,7 +114,7 @@ __global__ void __launch_bounds__(kThreads < 128 ? 128 : kThreads) quantize_kern
 #pragma unroll
     for (uint32_t i = 0; i < kV; ++i) {
       const uint32_t c = i * kThreads + t;
-      if (c < a.cols) q[c] = zeros ? 0 : (int8_t)quantized(__uint_as_float((uint32_t)s[i] << 16), a_max, by);
+      if (c < a.cols) q[c] = zeros ? 0 : (int8_t)quantized(times(__uint_as_float((uint32_t)s[i] << 16), move), by);
     }
   }
 }

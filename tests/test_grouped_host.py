@@ -53,10 +53,11 @@ def test_grouped_matmul_refusals(zb):
         refused(zb, zb.ERR_UNSUPPORTED, call, **kw)
     call(rows=0)
     # gathered rows need room where there are many
-    need = zb.zipmoe_grouped_workspace_bytes(weights(), 10000, True)
-    assert need == 10000 * 64 * 2 and zb.zipmoe_grouped_workspace_bytes(weights(), 10000, False) == 0
-    assert zb.zipmoe_grouped_workspace_bytes(weights(), 1, True) == 0
-    many = dict(rows=10000, xr=10000, order=A, k=1)
+    big = weights(rows=4096, cols=4096)
+    need = zb.zipmoe_grouped_workspace_bytes(big, 10000, True)
+    assert need == 10000 * 4096 * 2 and zb.zipmoe_grouped_workspace_bytes(big, 10000, False) == 0
+    assert zb.zipmoe_grouped_workspace_bytes(big, 1, True) == 0
+    many = dict(w=big, xp=4096, op=4096, rows=10000, xr=10000, order=A, k=1)
     refused(zb, zb.ERR_INVALID_ARG, call, ws=None, n=need, **many)
     refused(zb, zb.ERR_INVALID_ARG, call, ws=A + 8, n=need, **many)
     refused(zb, zb.ERR_BUFFER_TOO_SMALL, call, ws=A, n=need - 1, **many)
@@ -100,6 +101,26 @@ def test_combine_and_quantize_refusals(zb):
     for kw in (dict(cols=0), dict(cols=65537, xp=70000, qp=70000), dict(rows=(1 << 30) + 1)):
         refused(zb, zb.ERR_UNSUPPORTED, quantize, **kw)
     quantize(rows=0)
+
+
+def test_linear_refusals(zb):
+    def weights(E=1, rows=64, cols=64, flags=2, even=1):
+        return zb.GroupedWeightsStruct(E, rows, cols, flags, even, 0, None)
+
+    need = zb.zipmoe_linear_int8_workspace_bytes(weights(), 8)
+    assert need == 8 * 64 + 8 * 4
+
+    def call(w=None, x=A, xp=64, rows=8, cs=A, out=A, op=64, ws=A, n=need, flags=0, status=None):
+        zb.zipmoe_linear_int8(w or weights(), x, xp, rows, cs, out, op, ws, n, flags, status)
+
+    for kw in (dict(x=None), dict(cs=None), dict(out=None), dict(ws=None), dict(xp=63), dict(op=63), dict(x=A + 1), dict(cs=A + 2),
+               dict(out=A + 1), dict(out=A + 2, flags=4), dict(ws=A + 8), dict(flags=1), dict(status=A + 1), dict(w=weights(E=2)),
+               dict(w=weights(flags=0)), dict(w=weights(flags=3)), dict(w=weights(even=0))):
+        refused(zb, zb.ERR_INVALID_ARG, call, **kw)
+    for kw in (dict(w=weights(rows=0)), dict(w=weights(cols=72), xp=72), dict(rows=(1 << 30) + 1)):
+        refused(zb, zb.ERR_UNSUPPORTED, call, **kw)
+    refused(zb, zb.ERR_BUFFER_TOO_SMALL, call, n=need - 1)
+    call(rows=0)
 
 
 def test_oracle_lists():
