@@ -139,8 +139,9 @@ __global__ void __launch_bounds__(1024) group_kernel(const GroupArgs a) {
 
 // ---- combination: out[t] = sum over j of weights[t, j] * y[place[t, j]] --------
 // Bound: the bytes of y.  A thread has four neighbouring columns and walks over tokens: all its choices' columns are asked for at
-// once, and the next token's places and weights with them.  They are added in the order of the choices, in fp32.  (A block per
-// token: 138 us for 8192 tokens of six choices of 2048 columns; the places came before anything else could be asked for.)
+// once, and the next token's places and weights with them.  They are added in the order of the choices, in fp32.  8192 tokens of six
+// choices of 2048 columns of fp32: 67 us, 6.5 TB/s, as fast as a copy.  (A block per token: 138 us; the places came before anything
+// else could be asked for.)
 struct CombineArgs {
   const void *y;
   const int32_t *place;
@@ -151,8 +152,12 @@ struct CombineArgs {
   uint32_t T, k, cols, rows;
 };
 
+// Blocks of an SM at once.  8192 tokens of six choices of 2048 columns: 70.6 us with three, 66.7 with four, 78.4 with five (which spill);
+// 4096 tokens of two of 4096: 35.9 with four, 28.5 with six.
+__host__ __device__ constexpr uint32_t combine_blocks(uint32_t k) { return k <= 2 ? 6 : k <= 4 ? 5 : 4; }
+
 template <bool kF32, bool kWide, uint32_t kK>
-__global__ void __launch_bounds__(256) combine_rows_kernel(const CombineArgs a) {
+__global__ void __launch_bounds__(256, combine_blocks(kK)) combine_rows_kernel(const CombineArgs a) {
   constexpr uint32_t kV = kWide ? 4 : 1;
   after_predecessor();
   const uint32_t units = a.cols / kV, stride = gridDim.y * blockDim.y;
@@ -296,17 +301,24 @@ extern "C" zipmoe_status zipmoe_combine_rows(const zipmoe_combine_args *c, zipmo
   cfg.stream = reinterpret_cast<cudaStream_t>(stream);
   cfg.blockDim = dim3(x, 256 / x);
   // blocks that stay: as many as the device runs at once
-  const uint32_t across = (units + x - 1) / x, at_once = zipmoe_host::current_sms() * 4;
+  const uint32_t most = c->k <= 2 ? 2 : c->k <= 4 ? 4 : c->k <= 6 ? 6 : 8;
+  const uint32_t across = (units + x - 1) / x, at_once = zipmoe_host::current_sms() * combine_blocks(most);
   cfg.gridDim = dim3(std::min(across, at_once), std::min(std::max(1u, at_once / across), (c->T + 256 / x - 1) / (256 / x)));
   cudaLaunchAttribute attr = zipmoe_host::overlapped();
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  const auto call = [&](auto of_f32, auto of_wide) {
-    constexpr bool kF32 = decltype(of_f32)::value, kWide = decltype(of_wide)::value;
-    return c->k <= 4 ? cudaLaunchKernelEx(&cfg, combine_rows_kernel<kF32, kWide, 4>, a) : cudaLaunchKernelEx(&cfg, combine_rows_kernel<kF32, kWide, 8>, a);
+  const auto call = [&](auto of_f32, auto of_wide, auto of_k) {
+    return cudaLaunchKernelEx(&cfg, combine_rows_kernel<decltype(of_f32)::value, decltype(of_wide)::value, decltype(of_k)::value>, a);
   };
-  const std::true_type yes;
-  const std::false_type no;
-  const cudaError_t err = f32 ? (wide ? call(yes, yes) : call(yes, no)) : (wide ? call(no, yes) : call(no, no));
+  const auto by_type = [&](auto of_k) {
+    const std::true_type yes;
+    const std::false_type no;
+    return f32 ? (wide ? call(yes, yes, of_k) : call(yes, no, of_k)) : (wide ? call(no, yes, of_k) : call(no, no, of_k));
+  };
+  using std::integral_constant;
+  const cudaError_t err = most == 2   ? by_type(integral_constant<uint32_t, 2>())
+                          : most == 4 ? by_type(integral_constant<uint32_t, 4>())
+                          : most == 6 ? by_type(integral_constant<uint32_t, 6>())
+                                      : by_type(integral_constant<uint32_t, 8>());
   return err == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
 }

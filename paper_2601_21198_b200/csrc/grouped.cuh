@@ -50,18 +50,13 @@ __device__ __forceinline__ uint32_t grouped_idesc(uint32_t n) {
   return kInt8 ? (2u << 4) | (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (8u << 24) : bf16_idesc(n);
 }
 
-// The rows of group e; false, and none, where they do not lie inside the product's R rows.
-__device__ __forceinline__ bool group_rows(const GroupedArgs &a, uint32_t e, uint32_t &begin, uint32_t &count) {
-  if (!a.offsets) {
-    begin = 0;
-    count = e == 0 ? a.R : 0;
-    return true;
-  }
-  const int32_t b = __ldcg(a.offsets + e), n = __ldcg(a.offsets + e + 1);
-  const bool fine = b >= 0 && n >= b && n <= (int32_t)a.R;
-  begin = fine ? b : 0;
-  count = fine ? n - b : 0;
-  return fine;
+// The rows of a group between two offsets (without offsets there is one group, of all rows); false where they do not lie in order
+// inside the product's R rows.
+__device__ __forceinline__ uint32_t rows_between(const GroupedArgs &a, int32_t begin, int32_t end, bool &fine) {
+  if (!a.offsets) return a.R;
+  const bool here = begin >= 0 && end >= begin && end <= (int32_t)a.R;
+  fine &= here;
+  return here ? (uint32_t)(end - begin) : 0;
 }
 
 // The row of x that row r of the product reads; -1 where `order` points outside.

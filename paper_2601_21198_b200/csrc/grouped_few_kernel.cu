@@ -63,20 +63,21 @@ __global__ void __launch_bounds__(kFewThreads, 2) grouped_few_kernel(const __gri
   if (warp == 1) tmem_alloc(smem_addr(words), tmem_cols);
   after_predecessor();
   if (warp == 0) {
-    // units before each group: lane l has groups 8 l .. 8 l + 7
-    uint32_t first[8], n[8], units = 0;
+    // units before each group: lane l has the groups from per * l on; all loads are asked for before any is looked at
+    const uint32_t per = (a.E + 31) / 32, e0 = lane * per;
+    int32_t at[9];
+    uint32_t n[8], units = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < 9; ++i) at[i] = a.offsets && i <= per ? __ldcg(a.offsets + min(e0 + i, a.E)) : 0;
     bool fine = true;
 #pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) {
-      n[i] = 0;
-      if (lane * 8 + i < a.E) fine &= group_rows(a, lane * 8 + i, first[i], n[i]);
-      units += (n[i] + NT - 1) / NT * NB;
-    }
-    if (!__all_sync(0xFFFFFFFFu, fine)) {   // rows could belong to two groups: nothing is computed
-      if (lane == 0 && blockIdx.x == 0) report(a.status, kStatusBadDescriptor);
-      units = 0;
+    for (uint32_t i = 0; i < 8; ++i) n[i] = i < per && e0 + i < a.E ? rows_between(a, at[i], at[i + 1], fine) : 0;
+    fine = __all_sync(0xFFFFFFFFu, fine);
+    if (!fine && lane == 0 && blockIdx.x == 0) report(a.status, kStatusBadDescriptor);
 #pragma unroll
-      for (uint32_t i = 0; i < 8; ++i) n[i] = 0;
+    for (uint32_t i = 0; i < 8; ++i) {
+      if (!fine) n[i] = 0;   // rows could belong to two groups: nothing is computed
+      units += (n[i] + kFewTokens - 1) / kFewTokens * NB;
     }
     uint32_t before = units;
 #pragma unroll
@@ -91,10 +92,10 @@ __global__ void __launch_bounds__(kFewThreads, 2) grouped_few_kernel(const __gri
     } else if (unit >= before && unit < before + units) {
 #pragma unroll
       for (uint32_t i = 0; i < 8; ++i) {
-        const uint32_t tiles = (n[i] + NT - 1) / NT, mine = tiles * NB;
+        const uint32_t tiles = (n[i] + kFewTokens - 1) / kFewTokens, mine = tiles * NB;
         if (unit >= before && unit < before + mine) {   // token tiles of the same weights stand next to one another
-          const uint32_t at = unit - before, block = at / tiles, tile = at - block * tiles;
-          unit_at = FewUnit{lane * 8 + i, first[i] + tile * NT, min(NT, n[i] - tile * NT), block * kCols};
+          const uint32_t in = unit - before, block = tiles == 1 ? in : in / tiles, tile = in - block * tiles;
+          unit_at = FewUnit{e0 + i, (uint32_t)at[i] + tile * kFewTokens, min(kFewTokens, n[i] - tile * kFewTokens), block * kCols};
         }
         before += mine;
       }

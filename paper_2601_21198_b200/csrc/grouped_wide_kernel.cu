@@ -185,16 +185,16 @@ struct WideTile {
   uint32_t shared;                     // whether other tiles of the group read the same weights
 };
 constexpr uint32_t kWideTiles = 4;     // tiles that are worked out ahead
-// A group's tokens in tiles of at most `most` columns, evenly by whole 32s: the first tiles may have 32 more than the others.
-__device__ __forceinline__ uint32_t token_tiles(uint32_t n, uint32_t most) { return (n + most - 1) / most; }
-__device__ __forceinline__ WideTile tile_at(const WideLists &l, uint32_t t, uint32_t E, uint32_t blocks, uint32_t most) {
+// A group's tokens in tiles of at most 256 columns, evenly by whole 32s: the first tiles may have 32 more than the others.
+__device__ __forceinline__ uint32_t token_tiles(uint32_t n) { return (n + kWideCols - 1) / kWideCols; }
+__device__ __forceinline__ WideTile tile_at(const WideLists &l, uint32_t t, uint32_t E, uint32_t blocks) {
   uint32_t lo = 0, hi = E;   // the last group whose tiles begin at or before t
   while (hi - lo > 1) {
     const uint32_t mid = (lo + hi) / 2;
     if (l.before[mid] <= t) lo = mid;
     else hi = mid;
   }
-  const uint32_t n = l.n[lo], tiles = token_tiles(n, most), at = t - l.before[lo];
+  const uint32_t n = l.n[lo], tiles = token_tiles(n), at = t - l.before[lo];
   const uint32_t band = at / (kWideBand * blocks), in_band = at - band * kWideBand * blocks, width = min(kWideBand, tiles - band * kWideBand);
   WideTile r;
   r.e = lo;
@@ -232,8 +232,7 @@ __global__ void __launch_bounds__(32 * kPackRows) pack_rows_kernel(const Grouped
 }
 
 template <bool kInt8, bool kPair, bool kF32>
-__global__ void __launch_bounds__(kWideThreads, 1) grouped_wide_kernel(const __grid_constant__ WideMaps maps, const GroupedArgs a,
-                                                                      const uint32_t most) {
+__global__ void __launch_bounds__(kWideThreads, 1) grouped_wide_kernel(const __grid_constant__ WideMaps maps, const GroupedArgs a) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t bars[2 * kWideStages + 4 + 2 * kWideTiles];
   __shared__ WideTile todo[kWideTiles];
@@ -287,19 +286,21 @@ __global__ void __launch_bounds__(kWideThreads, 1) grouped_wide_kernel(const __g
   tc_after_sync();
   after_predecessor();   // (only now: nobody who comes after takes the tensor memory first)
   if (warp == 0) {
-    uint32_t first[8], n[8], tiles = 0;
+    // lane l has the groups from per * l on; all loads are asked for before any is looked at
+    const uint32_t per = (a.E + 31) / 32, e0 = lane * per;
+    int32_t at[9];
+    uint32_t n[8], tiles = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < 9; ++i) at[i] = a.offsets && i <= per ? __ldcg(a.offsets + min(e0 + i, a.E)) : 0;
     bool fine = true;
 #pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) {
-      first[i] = n[i] = 0;
-      if (lane * 8 + i < a.E) fine &= group_rows(a, lane * 8 + i, first[i], n[i]);
-    }
+    for (uint32_t i = 0; i < 8; ++i) n[i] = i < per && e0 + i < a.E ? rows_between(a, at[i], at[i + 1], fine) : 0;
     fine = __all_sync(0xFFFFFFFFu, fine);
     if (!fine && lane == 0 && blockIdx.x == 0) report(a.status, kStatusBadDescriptor);
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
       if (!fine) n[i] = 0;   // rows could belong to two groups: nothing is computed
-      tiles += token_tiles(n[i], most) * blocks;
+      tiles += token_tiles(n[i]) * blocks;
     }
     uint32_t before = tiles;
 #pragma unroll
@@ -311,11 +312,11 @@ __global__ void __launch_bounds__(kWideThreads, 1) grouped_wide_kernel(const __g
     before -= tiles;
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i)
-      if (lane * 8 + i < a.E) {
-        lists.before[lane * 8 + i] = before;
-        lists.first[lane * 8 + i] = first[i];
-        lists.n[lane * 8 + i] = n[i];
-        before += token_tiles(n[i], most) * blocks;
+      if (i < per && e0 + i < a.E) {
+        lists.before[e0 + i] = before;
+        lists.first[e0 + i] = (uint32_t)at[i];
+        lists.n[e0 + i] = n[i];
+        before += token_tiles(n[i]) * blocks;
       }
   }
   __syncthreads();
@@ -561,9 +562,9 @@ __global__ void __launch_bounds__(kWideThreads, 1) grouped_wide_kernel(const __g
       for (uint32_t v = pair; ok; v += pairs) {
         WideTile u = {};
         if (v < whole) {
-          u = tile_at(lists, v, a.E, blocks, most);
+          u = tile_at(lists, v, a.E, blocks);
         } else if (v < all) {
-          u = tile_at(lists, whole + (v - whole) / cuts, a.E, blocks, most);
+          u = tile_at(lists, whole + (v - whole) / cuts, a.E, blocks);
           const uint32_t part = (v - whole) % cuts, units = u.cols / 32, each = units / cuts, more = units - each * cuts;
           const uint32_t skip = (part * each + min(part, more)) * 32;
           u.cols = (each + (part < more ? 1 : 0)) * 32;
@@ -597,7 +598,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) grouped_wide_kernel(const __g
 namespace {
 
 template <bool kInt8, bool kPair, bool kF32>
-zipmoe_status launch(int dev, const zipmoe_dev::WideMaps &maps, const zipmoe_dev::GroupedArgs &a, uint32_t most, cudaStream_t stream) {
+zipmoe_status launch(int dev, const zipmoe_dev::WideMaps &maps, const zipmoe_dev::GroupedArgs &a, cudaStream_t stream) {
   using namespace zipmoe_dev;
   constexpr uint32_t kSmem = 1024 + kWideStages * kWideStage;
   static bool ready[64];
@@ -621,7 +622,7 @@ zipmoe_status launch(int dev, const zipmoe_dev::WideMaps &maps, const zipmoe_dev
   cfg.gridDim = dim3(zipmoe_host::current_sms() / 2 * 2);
   cfg.blockDim = dim3(kWideThreads);
   cfg.dynamicSmemBytes = kSmem;
-  return cudaLaunchKernelEx(&cfg, grouped_wide_kernel<kInt8, kPair, kF32>, maps, a, most) == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, grouped_wide_kernel<kInt8, kPair, kF32>, maps, a) == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
 }
 
 }  // namespace
@@ -644,10 +645,9 @@ zipmoe_status zipmoe_host::launch_grouped_wide(int dev, bool int8, bool pair, co
   if (!make_byte_map(&maps.x128, x, rows, a.Kb, pitch, 128, 1, pitch * rows, int8) ||
       !make_byte_map(&maps.x16, x, rows, a.Kb, pitch, 16, 1, pitch * rows, int8))
     return ZIPMOE_ERR_CUDA;
-  const uint32_t most = 256;
   const auto call = [&](auto of_int8, auto of_pair) {
     constexpr bool kInt8 = decltype(of_int8)::value, kPair = decltype(of_pair)::value;
-    return a.out_f32 ? launch<kInt8, kPair, true>(dev, maps, a, most, stream) : launch<kInt8, kPair, false>(dev, maps, a, most, stream);
+    return a.out_f32 ? launch<kInt8, kPair, true>(dev, maps, a, stream) : launch<kInt8, kPair, false>(dev, maps, a, stream);
   };
   const std::true_type yes;
   const std::false_type no;

@@ -41,18 +41,18 @@ __device__ __forceinline__ uint32_t quantized(float x, float by) {
   return (uint32_t)__float2int_rn(__fsub_rn(c, __fsub_rn(c, t))) & 0xFFu;
 }
 
-// kThreads threads per row, 8 vectors of 8 columns each (kWide) or 64 single columns; blocks of 128 threads at least.
-template <uint32_t kThreads, bool kWide>
+// kThreads threads per row, kVectors vectors of 8 columns each (kWide) or as many single columns; blocks of 128 threads at least.
+template <uint32_t kThreads, uint32_t kVectors, bool kWide>
 __global__ void __launch_bounds__(kThreads < 128 ? 128 : kThreads) quantize_kernel(const QuantizeArgs a) {
-  constexpr uint32_t kRows = kThreads < 128 ? 128 / kThreads : 1, kV = kWide ? 8 : 64;
+  constexpr uint32_t kRows = kThreads < 128 ? 128 / kThreads : 1, kV = kWide ? kVectors : 8 * kVectors;
   __shared__ uint32_t tops[32];
   after_predecessor();
   const uint32_t t = threadIdx.x % kThreads, row = blockIdx.x * kRows + threadIdx.x / kThreads;
   const bool there = row < a.rows;
   const uint16_t *x = a.x + (there ? (uint64_t)row * a.x_pitch : 0);
   uint32_t top = 0;    // magnitudes order as their bits do, infinity and NaN above all numbers
-  uint4 v[kWide ? 8 : 1];
-  uint16_t s[kWide ? 1 : 64];
+  uint4 v[kWide ? kV : 1];
+  uint16_t s[kWide ? 1 : kV];
   if constexpr (kWide) {
 #pragma unroll
     for (uint32_t i = 0; i < kV; ++i) {
@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(kThreads < 128 ? 128 : kThreads) quantize_kern
 
 namespace {
 
-template <uint32_t kThreads>
+template <uint32_t kThreads, uint32_t kVectors>
 cudaError_t launch(const zipmoe_dev::QuantizeArgs &a, bool wide, cudaStream_t stream) {
   constexpr uint32_t kRows = kThreads < 128 ? 128 / kThreads : 1;
   cudaLaunchAttribute attr = zipmoe_host::overlapped_if_whole((a.rows + kRows - 1) / kRows, zipmoe_host::current_sms());
@@ -133,8 +133,8 @@ cudaError_t launch(const zipmoe_dev::QuantizeArgs &a, bool wide, cudaStream_t st
   cfg.numAttrs = 1;
   cfg.gridDim = dim3((a.rows + kRows - 1) / kRows);
   cfg.blockDim = dim3(kThreads < 128 ? 128 : kThreads);
-  return wide ? cudaLaunchKernelEx(&cfg, zipmoe_dev::quantize_kernel<kThreads, true>, a)
-              : cudaLaunchKernelEx(&cfg, zipmoe_dev::quantize_kernel<kThreads, false>, a);
+  return wide ? cudaLaunchKernelEx(&cfg, zipmoe_dev::quantize_kernel<kThreads, kVectors, true>, a)
+              : cudaLaunchKernelEx(&cfg, zipmoe_dev::quantize_kernel<kThreads, kVectors, false>, a);
 }
 
 }  // namespace
@@ -159,10 +159,13 @@ extern "C" zipmoe_status zipmoe_quantize_rows(const uint16_t *x, uint64_t x_pitc
   const bool wide = cols % 8 == 0 && x_pitch % 8 == 0 && q_pitch % 8 == 0 && (bits(x) & 15) == 0 && (bits(q) & 7) == 0;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t err;
-  if (cols <= 2048) err = launch<32>(a, wide, s);
-  else if (cols <= 8192) err = launch<128>(a, wide, s);
-  else if (cols <= 16384) err = launch<256>(a, wide, s);
-  else if (cols <= 32768) err = launch<512>(a, wide, s);
-  else err = launch<1024>(a, wide, s);
+  // few registers, so that many rows are under way on an SM
+  if (cols <= 1024) err = launch<32, 4>(a, wide, s);
+  else if (cols <= 2048) err = launch<64, 4>(a, wide, s);
+  else if (cols <= 4096) err = launch<128, 4>(a, wide, s);
+  else if (cols <= 8192) err = launch<256, 4>(a, wide, s);
+  else if (cols <= 16384) err = launch<512, 4>(a, wide, s);
+  else if (cols <= 32768) err = launch<1024, 4>(a, wide, s);
+  else err = launch<1024, 8>(a, wide, s);
   return err == cudaSuccess ? ZIPMOE_OK : ZIPMOE_ERR_CUDA;
 }
