@@ -693,7 +693,7 @@ zipmoe_status zipmoe_plan_schedule(const zipmoe_sched_task *tasks, uint32_t n_ta
  * still terminates.  That path cannot be reached with sound inputs, so this switch provokes it without a fault:
  * from now on zipmoe_decode and zipmoe_decode_expert_ffn arm the barrier of every tile-record copy for
  * extra_tx_bytes more than the copy delivers (so that the barrier never completes although the copy does) and give
- * up after `tries` tries; zipmoe_route and zipmoe_expert_ffn do the same with the barriers of their weights, and give
+ * up after `tries` tries; zipmoe_route, zipmoe_expert_ffn and zipmoe_grouped_matmul do the same with the barriers of their weights, and give
  * up after a millisecond.  (0, 0) restores normal operation.  Process-wide; not for concurrent use. */
 void zipmoe_test_wait_fault(uint32_t extra_tx_bytes, uint32_t tries);
 
@@ -704,6 +704,11 @@ void zipmoe_test_wait_fault(uint32_t extra_tx_bytes, uint32_t tries);
  * fills the counter of such a launch with a tag that no launch carries instead of zeroing it.  0 restores normal
  * operation.  Process-wide; not for concurrent use. */
 void zipmoe_test_foreign_counter(uint32_t on);
+
+/* For the library's own tests (the paper has no counterpart).  zipmoe_grouped_matmul has two kernels and takes the one that it
+ * reckons to be faster; either computes any sizes.  1: from now on the one made for few tokens, 2: the one made for many,
+ * 0 restores normal operation.  Process-wide; not for concurrent use. */
+void zipmoe_test_grouped_kernel(uint32_t which);
 
 /* Name of a status code (static string). */
 const char *zipmoe_status_string(zipmoe_status s);

@@ -460,6 +460,15 @@ for _f in ("zipmoe_group_tokens", "zipmoe_grouped_weights_plan", "zipmoe_grouped
     getattr(_lib, _f).restype = _int
 
 
+_lib.zipmoe_test_grouped_kernel.argtypes = [_u32]
+_lib.zipmoe_test_grouped_kernel.restype = None
+
+
+def zipmoe_test_grouped_kernel(which):
+    """Test switch: 1 zipmoe_grouped_matmul's kernel for few tokens, 2 the one for many, 0 normal."""
+    _lib.zipmoe_test_grouped_kernel(int(which))
+
+
 def zipmoe_group_tokens(topk_ids, T, k, n_experts, offsets, order, place=None, status_word=None, stream=None):
     """Pointer arguments are device tensors (or raw device addresses, or None)."""
     args = _GROUP_ARGS.pack(_ptr(topk_ids) or 0, _ptr(offsets) or 0, _ptr(order) or 0, _ptr(place) or 0, _ptr(status_word) or 0, T, k,
@@ -1054,7 +1063,7 @@ class GroupedMatrix:
                 raise ValueError("weights that lie unevenly are described before a capture, not within it")
             self.table = torch.from_numpy(table).to(self.device)
             self.struct.table = self.table.data_ptr()
-        self._struct_at, self._need = ctypes.byref(self.struct), {}
+        self._struct_at = ctypes.byref(self.struct)
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device) if status is None else status
         self.status_at = _dense("status", self.status, (1,), kinds.int32, index)
 
@@ -1093,9 +1102,7 @@ class GroupedMatrix:
         out_at, out_pitch = _rows("out", out, (rows, self.rows), kinds.fp32 if f32 else kinds.bf16, index)
         need, scratch_at = 0, 0
         if gather:
-            need = self._need.get(rows)
-            if need is None:
-                need = self._need[rows] = zipmoe_grouped_workspace_bytes(self.struct, rows, True)
+            need = zipmoe_grouped_workspace_bytes(self.struct, rows, True)
             if need:      # (given back to the stream's pool on return: what is queued there comes before its next use)
                 scratch = _empty((need,), kinds.e4m3[1], self.device, stream)
                 scratch_at = scratch.data_ptr()

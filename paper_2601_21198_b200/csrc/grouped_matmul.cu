@@ -1,6 +1,7 @@
 // The entry points of the grouped products: how a layer's weights are described once, and the checks of a call.
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 #include <cstring>
 
@@ -18,7 +19,10 @@ bool sizes_ok(uint32_t n_groups, uint32_t rows, uint32_t cols, uint32_t flags) {
          cols % (flags & ZIPMOE_GROUPED_INT8 ? 16 : 8) == 0;
 }
 
+std::atomic<uint32_t> g_test_kernel{0};   // 1: the kernel for few tokens, 2: the other
+
 bool wide_pays(const zipmoe_grouped_weights *w, uint32_t rows, bool gathered) {
+  if (const uint32_t forced = g_test_kernel.load()) return forced == 2;
   return zipmoe_host::grouped_wide_pays({w->n_groups, rows, w->rows, w->cols * (w->flags & ZIPMOE_GROUPED_INT8 ? 1 : 2),
                                          (w->flags & ZIPMOE_GROUPED_INT8) != 0, (w->flags & ZIPMOE_GROUPED_PAIR) != 0, gathered},
                                         zipmoe_host::current_sms());
@@ -173,3 +177,5 @@ extern "C" zipmoe_status zipmoe_linear_int8(const zipmoe_grouped_weights *w, con
   rc = zipmoe_quantize_rows(l->x, l->x_pitch, l->rows, w->cols, q, w->cols, scales, stream);
   return rc == ZIPMOE_OK ? zipmoe_grouped_matmul(w, &g, stream) : rc;
 }
+
+extern "C" void zipmoe_test_grouped_kernel(uint32_t which) { g_test_kernel.store(which); }

@@ -21,6 +21,14 @@ def zb():
     return binding
 
 
+@pytest.fixture(params=[1, 2], ids=["few", "many"])
+def kernel(zb, request):
+    """Either kernel on every size: which one a call takes is a matter of speed."""
+    zb.zipmoe_test_grouped_kernel(request.param)
+    yield request.param
+    zb.zipmoe_test_grouped_kernel(0)
+
+
 def half_step(v):
     return np.exp2(np.floor(np.log2(np.maximum(np.abs(v), 2.0 ** -126))) - 8)
 
@@ -84,12 +92,13 @@ def test_lists_of_no_tokens_repeated_and_wrong_ids(zb):
 
 # ---- products ---------------------------------------------------------------------------------------------------
 SHAPES = [(1, 1, 1, 8, 8), (1, 2, 2, 64, 64), (5, 3, 2, 72, 40), (40, 1, 1, 136, 200), (64, 4, 2, 2048, 128), (65, 4, 1, 256, 129), (100, 7, 3, 520, 257),
-          (300, 2, 1, 192, 384), (777, 60, 4, 264, 136), (30, 256, 8, 64, 72), (1100, 3, 2, 1032, 520), (2500, 8, 2, 128, 264)]
+          (300, 2, 1, 192, 384), (777, 60, 4, 264, 136), (30, 256, 8, 64, 72), (1100, 3, 2, 1032, 520), (2500, 8, 2, 128, 264),
+          (33, 1, 1, 320, 256), (257, 1, 1, 384, 513), (512, 1, 1, 448, 512), (513, 1, 1, 512, 768), (600, 2, 1, 64, 700), (256, 1, 1, 3000, 8)]
 
 
 @pytest.mark.parametrize("T,E,k,K,N", SHAPES)
 @pytest.mark.parametrize("gather", [False, True])
-def test_product_is_the_rounded_sum(zb, T, E, k, K, N, gather):
+def test_product_is_the_rounded_sum(zb, kernel, T, E, k, K, N, gather):
     import torch
     ids = routing(T, k, E, T, dropped=0.1 if T > 4 else 0.0)
     g = zb.group_tokens(gpu(ids), E)
@@ -113,7 +122,7 @@ def check_gated(h, first, second):
 
 @pytest.mark.parametrize("T,E,k,K,N", SHAPES)
 @pytest.mark.parametrize("gather", [False, True])
-def test_pairs(zb, T, E, k, K, N, gather):
+def test_pairs(zb, kernel, T, E, k, K, N, gather):
     import torch
     ids = routing(T, k, E, T + 1, dropped=0.1 if T > 4 else 0.0)
     g = zb.group_tokens(gpu(ids), E)
@@ -127,10 +136,11 @@ def test_pairs(zb, T, E, k, K, N, gather):
     assert (out[len(order):] == 7.0).all() and int(m.status.item()) == 0
 
 
-@pytest.mark.parametrize("T,E,k,K,N", [(3, 2, 1, 32, 8), (70, 3, 2, 144, 136), (600, 5, 2, 1040, 264), (2500, 3, 1, 128, 130)])
+@pytest.mark.parametrize("T,E,k,K,N", [(3, 2, 1, 32, 8), (70, 3, 2, 144, 136), (600, 5, 2, 1040, 264), (2500, 3, 1, 128, 130),
+                                       (300, 1, 1, 896, 520)])
 @pytest.mark.parametrize("pair", [False, True])
 @pytest.mark.parametrize("gather", [False, True])
-def test_int8_groups(zb, T, E, k, K, N, pair, gather):
+def test_int8_groups(zb, kernel, T, E, k, K, N, pair, gather):
     import torch
     rng = np.random.default_rng(K)
     ids = routing(T, k, E, T + 2, dropped=0.1 if T > 4 else 0.0)
@@ -158,7 +168,7 @@ def test_int8_groups(zb, T, E, k, K, N, pair, gather):
     assert (out[len(order):] == 7.0).all() and int(m.status.item()) == 0
 
 
-def test_one_group_without_lists(zb):
+def test_one_group_without_lists(zb, kernel):
     import torch
     x, w = coarse((333, 200), 6, 1 / 16), coarse((72, 200), 7, 1 / 64)
     m = zb.GroupedMatrix([bf16(w)])
@@ -170,7 +180,7 @@ def test_one_group_without_lists(zb):
 
 @pytest.mark.parametrize("T", [6, 500])
 @pytest.mark.parametrize("pair", [False, True])
-def test_strides_and_scattered_weights(zb, T, pair):
+def test_strides_and_scattered_weights(zb, kernel, T, pair):
     """Rows of x and out that lie apart (out even off any vector's boundary), weights in no order, int16 patterns."""
     import torch
     E, k, K, N = 5, 2, 136, 90
@@ -196,7 +206,7 @@ def test_strides_and_scattered_weights(zb, T, pair):
 
 
 @pytest.mark.parametrize("T", [20, 700])
-def test_empty_and_lopsided_groups(zb, T):
+def test_empty_and_lopsided_groups(zb, kernel, T):
     """All tokens on one expert, the others without any; rows of other groups and behind the last hold NaN and infinities."""
     import torch
     E, K, N = 9, 128, 140
@@ -227,7 +237,7 @@ def test_empty_and_lopsided_groups(zb, T):
 
 
 @pytest.mark.parametrize("rows", [10, 600])
-def test_wrong_lists_are_reported(zb, rows):
+def test_wrong_lists_are_reported(zb, kernel, rows):
     """Offsets out of order or past the end leave everything as it was, a row that is nowhere counts as zeros."""
     import torch
     E, K, N = 3, 64, 64
@@ -309,7 +319,7 @@ def expected(ws, tok, ids, wts):
 
 
 @pytest.mark.parametrize("T,E,k,H,I", [(1, 4, 2, 512, 768), (300, 9, 3, 264, 200), (1500, 4, 2, 256, 136), (700, 16, 8, 128, 64)])
-def test_prompt_of_a_layer(zb, T, E, k, H, I):
+def test_prompt_of_a_layer(zb, kernel, T, E, k, H, I):
     import torch
     ws = layer(E, H, I, 500 + E)
     ex = zb.ResidentExperts([gpu(w.view(np.int16)) for w in ws], H, I)
@@ -368,7 +378,7 @@ def test_prompt_on_streams_and_in_a_graph(zb):
 
 
 @pytest.mark.parametrize("T", [5, 700])
-def test_a_wait_that_runs_out_is_reported(zb, T):
+def test_a_wait_that_runs_out_is_reported(zb, kernel, T):
     """The weights' barriers armed for more than their copies bring: the call ends and says so, and the next one is sound."""
     import torch
     E, K, N = 4, 512, 300

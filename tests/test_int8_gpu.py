@@ -20,6 +20,14 @@ def zb():
     return binding
 
 
+@pytest.fixture(params=[1, 2], ids=["few", "many"])
+def kernel(zb, request):
+    """Either kernel on every size: which one a call takes is a matter of speed."""
+    zb.zipmoe_test_grouped_kernel(request.param)
+    yield request.param
+    zb.zipmoe_test_grouped_kernel(0)
+
+
 def gpu(a):
     import torch
     return torch.from_numpy(np.ascontiguousarray(a)).cuda()
@@ -80,7 +88,7 @@ def test_rows_that_are_not_finite(zb):
 
 @pytest.mark.parametrize("T,K,N", [(1, 16, 1), (1, 4096, 300), (3, 48, 7), (16, 1424, 129), (17, 2048, 64), (64, 256, 2051), (65, 272, 130), (300, 1040, 257),
                                    (513, 128, 520), (1531, 1424, 130), (5, 16384, 40), (1, 65536, 24), (300, 65536, 24)])
-def test_linear(zb, T, K, N):
+def test_linear(zb, kernel, T, K, N):
     import torch
     rng = np.random.default_rng(K)
     x = inputs.tokens(T, K, seed=T)
@@ -101,7 +109,7 @@ def test_linear(zb, T, K, N):
     assert int(lin.status.item()) == 0
 
 
-def test_largest_sums(zb):
+def test_largest_sums(zb, kernel):
     """The longest rows of the largest integers: 65536 * 128 * 128 = 2^30."""
     import torch
     K, N = 65536, 16
