@@ -2,8 +2,10 @@
 
     residual += x;  h = norm(residual)         zipmoe_add_rmsnorm   (bf16 rows, and 8-bit rows with scales beside them)
     ids, weights = top-k of h @ gate^T         zipmoe_route
-    y = sum of the chosen experts' FFNs        zipmoe_expert_ffn on the experts that are recovered (the planner's pool F),
-                                               zipmoe_decode_expert_ffn on those that stay compressed
+    y = sum of the chosen experts' FFNs        zipmoe_expert_ffn on the experts that are recovered (the planner's pool F), or, for a
+                                               prompt of more than 256 tokens, the grouped products (zipmoe_group_tokens,
+                                               zipmoe_grouped_matmul, zipmoe_combine_rows); zipmoe_decode_expert_ffn on those that
+                                               stay compressed
 
 A layer may keep some of its experts recovered and the others compressed.  The call on recovered experts takes -1 for a choice
 that is not its own.  The call on compressed experts wants every id in range, so each choice is a row of its own there, those
@@ -48,7 +50,8 @@ class ExpertSublayer:
         ids, weights = self.router.route(h)
         y = torch.zeros(x.shape, device=x.device)
         if self.recovered is not None:
-            y += self.recovered.ffn(h, torch.where(ids < self.n_resident, ids, -1), weights)
+            ffn = self.recovered.ffn if len(h) <= 256 else self.recovered.ffn_prompt
+            y += ffn(h, torch.where(ids < self.n_resident, ids, -1), weights)
         if self.compressed is not None:
             T, k = ids.shape
             away = (ids - self.n_resident).reshape(T * k, 1)

@@ -1058,14 +1058,17 @@ class GroupedMatrix:
         with _on_device(index):
             table, self.struct = zipmoe_grouped_weights_plan(addresses, self.n_groups, self.rows, self.cols, flags)
         self.table = None
-        if not self.struct.even:      # evenly spaced weights need no table
-            if kinds.capturing():
-                raise ValueError("weights that lie unevenly are described before a capture, not within it")
+        prepared = status is None or not self.struct.even or (self.int8 and self.pair)      # something is put on the device here
+        if prepared and kinds.capturing():
+            raise ValueError("weights are described before a capture, not within it")
+        if not self.struct.even:      # (evenly spaced weights need no table)
             self.table = torch.from_numpy(table).to(self.device)
             self.struct.table = self.table.data_ptr()
         self._struct_at = ctypes.byref(self.struct)
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device) if status is None else status
         self.status_at = _dense("status", self.status, (1,), kinds.int32, index)
+        if prepared:      # calls may come on any stream
+            torch.cuda.current_stream(self.device).synchronize()
 
     def product(self, x, groups=None, gather=False, row_scales=None, out=None, stream=None):
         """x [x_rows, cols] of the weights' kind -> out [rows, rows of the matrices], bf16 (x's dtype; torch.bfloat16 for int8)

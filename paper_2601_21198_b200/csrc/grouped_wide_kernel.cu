@@ -121,8 +121,6 @@ template <bool kF32>
 __device__ __forceinline__ uint32_t chunk_col(uint32_t i, uint32_t lane) {
   return kF32 ? i : ((i >> 2) & 1) * 8 + (lane & 3) * 2 + (i & 1);
 }
-// A warp's 16 tokens x 32 columns of the output, by way of its own 2 KB: whole 16-byte pieces of rows leave, where stores of single
-// elements took 53 cycles each.
 // What a thread keeps of a chunk: fp32, or pairs of neighbouring tokens in bf16.
 template <bool kF32>
 struct Chunk {
@@ -137,6 +135,8 @@ struct Chunk {
     }
   }
 };
+// Stores a warp's 16 tokens x 32 columns of the output, by way of its own 2 KB: whole 16-byte pieces of rows leave, where stores of single
+// elements took 53 cycles each.
 template <bool kF32>
 __device__ __forceinline__ void store_chunk(const Chunk<kF32> &f, uint8_t *buf, uint32_t lane, const GroupedArgs &a, uint64_t row, uint32_t rows,
                                             uint32_t col) {
@@ -642,8 +642,7 @@ zipmoe_status zipmoe_host::launch_grouped_wide(int dev, bool int8, bool pair, co
     pack_rows_kernel<<<(a.R + kPackRows - 1) / kPackRows, 32 * kPackRows, 0, stream>>>(a, static_cast<uint8_t *>(packed));
     if (cudaGetLastError() != cudaSuccess) return ZIPMOE_ERR_CUDA;
   }
-  if (!make_byte_map(&maps.x128, x, rows, a.Kb, pitch, 128, 1, pitch * rows, int8) ||
-      !make_byte_map(&maps.x16, x, rows, a.Kb, pitch, 16, 1, pitch * rows, int8))
+  if (!make_byte_map(&maps.x128, x, rows, a.Kb, pitch, 128, 1, pitch, int8) || !make_byte_map(&maps.x16, x, rows, a.Kb, pitch, 16, 1, pitch, int8))
     return ZIPMOE_ERR_CUDA;
   const auto call = [&](auto of_int8, auto of_pair) {
     constexpr bool kInt8 = decltype(of_int8)::value, kPair = decltype(of_pair)::value;

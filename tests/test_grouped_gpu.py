@@ -328,6 +328,7 @@ def test_prompt_of_a_layer(zb, kernel, T, E, k, H, I):
     if T > 1:
         ids[3] = -1
         ids[4, 0] = -1
+        ids[5] = ids[5, 0]            # an expert listed k times counts with all its weights
     for w in (wts, None):
         out = ex.ffn_prompt(gpu(tok.view(np.int16)), gpu(ids), None if w is None else gpu(w))
         want, bound = expected(ws, tok, ids, w)
@@ -345,7 +346,7 @@ def test_prompt_of_a_layer(zb, kernel, T, E, k, H, I):
     torch.cuda.synchronize()
 
 
-def test_prompt_on_streams_and_in_a_graph(zb):
+def test_prompt_on_streams_and_in_a_graph(zb, kernel):
     """Two streams at once, and a captured prompt replayed on other inputs while eager calls run between the replays."""
     import torch
     T, E, k, H, I = 400, 6, 2, 256, 136
@@ -375,6 +376,55 @@ def test_prompt_on_streams_and_in_a_graph(zb):
         torch.cuda.synchronize()
         assert torch.equal(out, w) and torch.equal(other, want[1])
     assert int(ex.status.item()) == 0
+
+
+def test_first_prompt_within_a_capture(zb):
+    """Evenly spaced experts need nothing on the device; others are described before."""
+    import torch
+    T, E, k, H, I = 300, 4, 2, 128, 72
+    ws = layer(E, H, I, 90)
+    tok, (ids, wts) = inputs.tokens(T, H, seed=1), inputs.routing(T, n_experts=E, k=k, seed=1)
+    args = gpu(tok.view(np.int16)), gpu(ids), gpu(wts)
+    flat = gpu(np.concatenate([w.ravel() for w in ws]).view(np.int16))
+    even = zb.ResidentExperts(list(flat.view(3 * E, H * I)), H, I)
+    apart = zb.ResidentExperts([gpu(w.view(np.int16)) for w in reversed(ws)][::-1], H, I)
+    want = apart.ffn_prompt(*args)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = even.ffn_prompt(*args)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    fresh = zb.ResidentExperts([gpu(w.view(np.int16)) for w in reversed(ws)][::-1], H, I)
+    if not fresh.struct.even:
+        refused = []
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            args[0].add_(0)
+            try:
+                fresh.ffn_prompt(*args)
+            except ValueError as err:
+                refused.append(err)
+        assert refused
+
+
+def test_offsets_beyond_32_bits(zb, kernel):
+    """Outputs, rows of x and sums that begin more than 2^32 bytes and elements into their buffers."""
+    import torch
+    R, N, K, pitch = 300000, 16384, 64, 16384
+    x, w = coarse((R, K), 30, 1 / 16), coarse((2, N, K), 31, 1 / 64)
+    wide = torch.empty(R, pitch, dtype=torch.bfloat16, device="cuda")
+    wide[:, 512:512 + K] = bf16(x)
+    ids = np.zeros((R, 1), np.int32)
+    ids[R - 70:] = 1
+    g = zb.group_tokens(gpu(ids), 2)
+    m = zb.GroupedMatrix(list(bf16(w)))
+    out = m.product(wide[:, 512:512 + K], g)
+    rows = np.r_[0:3, R // 2:R // 2 + 3, R - 72:R]
+    want = np.stack([x[r] @ w[ids[r, 0]].T for r in rows])
+    assert torch.equal(out[gpu(rows)], torch.from_numpy(want).cuda().to(torch.bfloat16)) and int(m.status.item()) == 0
+    del wide
+    back = zb.combine_rows(out, g, None)
+    assert torch.equal(back, out)
 
 
 @pytest.mark.parametrize("T", [5, 700])
