@@ -493,7 +493,7 @@ typedef struct {
  * host in : tensors[n_groups] (with ZIPMOE_GROUPED_PAIR tensors[2 * n_groups], tensors[2e] = W1, 2e+1 = W3 of group e) DEVICE
  *           addresses of dense row-major [rows, cols] matrices, 16-byte aligned; flags: ZIPMOE_GROUPED_PAIR, _INT8.  The memory
  *           itself is not touched.
- * host out: table[n_groups * ZIPMOE_GROUPED_ENTRY_BYTES]; *weights, but for its `table`
+ * host out: table[n_groups * ZIPMOE_GROUPED_ENTRY_BYTES] (zeros where *weights has even = 1); *weights, but for its `table`
  * Limits: n_groups <= 256, rows <= 2^20, cols a multiple of 8 (16 for 8-bit integers) and <= 65536 (ZIPMOE_ERR_UNSUPPORTED
  * otherwise). */
 zipmoe_status zipmoe_grouped_weights_plan(const void *const *tensors, uint32_t n_groups, uint32_t rows, uint32_t cols, uint32_t flags,

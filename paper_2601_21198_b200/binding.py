@@ -1067,7 +1067,7 @@ class GroupedMatrix:
         self._struct_at = ctypes.byref(self.struct)
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device) if status is None else status
         self.status_at = _dense("status", self.status, (1,), kinds.int32, index)
-        if prepared:      # calls may come on any stream
+        if self.table is not None or (self.int8 and self.pair):      # calls may come on any stream
             torch.cuda.current_stream(self.device).synchronize()
 
     def product(self, x, groups=None, gather=False, row_scales=None, out=None, stream=None):

@@ -65,9 +65,6 @@ extern "C" zipmoe_status zipmoe_grouped_weights_plan(const void *const *tensors,
     std::memcpy(entry + zipmoe_dev::kPairMap + 128 * j, &map, sizeof(map));
     return true;
   };
-  for (uint32_t i = 0; i < each * n_groups; ++i)
-    if (!describe(static_cast<uint8_t *>(table) + (size_t)(i / each) * ZIPMOE_GROUPED_ENTRY_BYTES, i % each, tensors[i], 1, bytes))
-      return ZIPMOE_ERR_CUDA;
   // evenly spaced groups: one map serves them all
   bool even = true;
   for (uint32_t j = 0; j < each && even; ++j) {
@@ -77,6 +74,9 @@ extern "C" zipmoe_status zipmoe_grouped_weights_plan(const void *const *tensors,
     for (uint32_t e = 2; e < n_groups && even; ++e) even = bits(tensors[each * e + j]) == first + e * distance;
     if (even && !describe(weights->maps, j, tensors[j], n_groups, distance)) return ZIPMOE_ERR_CUDA;
   }
+  for (uint32_t i = 0; i < each * n_groups && !even; ++i)
+    if (!describe(static_cast<uint8_t *>(table) + (size_t)(i / each) * ZIPMOE_GROUPED_ENTRY_BYTES, i % each, tensors[i], 1, bytes))
+      return ZIPMOE_ERR_CUDA;
   weights->n_groups = n_groups;
   weights->rows = rows;
   weights->cols = cols;
