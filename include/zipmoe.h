@@ -504,8 +504,9 @@ typedef struct {
   const void *x;               /* in: [x_rows] of cols bf16 patterns or 8-bit integers, x_pitch apart; 16-byte aligned,
                                   and so is the pitch                                                               */
   uint64_t x_pitch;
-  const int32_t *offsets;      /* in: [n_groups + 1], ascending, from 0 to at most `rows`: group e's rows are offsets[e] ..
-                                  offsets[e + 1] - 1; may be NULL where there is one group: it then has all rows     */
+  const int32_t *offsets;      /* in: [n_groups + 1], ascending, between 0 and `rows`: group e's rows are offsets[e] ..
+                                  offsets[e + 1] - 1 (part of longer offsets are those of some of the experts); may be
+                                  NULL where there is one group: it then has all rows                               */
   const int32_t *order;        /* in: row r of the product is row order[r] / k of x; NULL: row r of x                */
   const float *row_scales;     /* in: [x_rows] scales of the rows of x; NULL exactly where weights are bf16          */
   const float *col_scales;     /* in: [n_groups, rows of the weights] scales of the weights' rows (with
@@ -545,7 +546,7 @@ typedef struct {
   uint64_t y_pitch;
   const int32_t *place;        /* in: [T, k]: the row of each choice; a negative one is none                        */
   const float *weights;        /* in: [T, k]; may be NULL (= 1.0)                                                   */
-  uint16_t *out;               /* out: [T] of cols bf16 patterns, out_pitch apart                                   */
+  uint16_t *out;               /* out: [T] of cols bf16 patterns, out_pitch apart; may overlap nothing that is read   */
   uint64_t out_pitch;
   uint32_t *status_word;       /* as for zipmoe_decode: code 1 where `place` points outside; may be NULL            */
   uint32_t T, k, cols, rows, flags;
@@ -562,7 +563,7 @@ zipmoe_status zipmoe_combine_rows(const zipmoe_combine_args *args, zipmoe_stream
  * For activations (a scale per token) and, once, for weights (a scale per output channel).  One launch on `stream`,
  * asynchronous; rows of whole 16-byte vectors are faster.
  * device in : x [rows] of cols bf16 patterns, x_pitch elements apart
- * device out: q [rows] of cols integers, q_pitch apart; scales [rows]
+ * device out: q [rows] of cols integers, q_pitch apart; scales [rows]; neither may overlap x
  * Limits: cols <= 65536, rows <= 2^30 (ZIPMOE_ERR_UNSUPPORTED otherwise).  rows = 0 does nothing. */
 zipmoe_status zipmoe_quantize_rows(const uint16_t *x, uint64_t x_pitch, uint32_t rows, uint32_t cols, int8_t *q, uint64_t q_pitch,
                                    float *scales, zipmoe_stream stream);

@@ -2,7 +2,9 @@
 // W3 of a pair) by up to 256 tokens of a group.
 //
 // Bound: what shared memory takes in and gives out beside the tensor cores.  A tcgen05 MMA reads its operands there at 64 of the 128
-// bytes a cycle, so every byte that the copies bring costs.
+// bytes a cycle, so every byte that the copies bring costs.  (8192 x 8192 x 8192 in bf16: 661 to 710 us, 1.55 to 1.66 PFLOP/s; 8192
+// tokens of 8-bit integers, 4096 x 14336: 305 us, 3.2 POP/s; 8192 tokens' six of 64 experts, pairs of 2048 x 1408: 458 to 470 us, 1.22
+// PFLOP/s.  A tile of 512 x 256 x 2048 takes 34.9 K cycles, 32.8 K of them products.  Runs of some 0.1 s are at the power limit.)
 //   * Two blocks of a cluster share one MMA (cta_group::2): each brings 128 rows of either half of the weights and half of the
 //     tokens, and keeps the sums of its own weights in its tensor memory, two halves of [128 x tokens] of 32 bits.  Per step of 128
 //     bytes of K that is 48 KB for two MMAs' worth of 256 x 256 sums, where tiles of 256 x 256 would take in 64 KB.
@@ -211,11 +213,12 @@ __device__ __forceinline__ WideTile tile_at(const WideLists &l, uint32_t t, uint
 // The rows of x that `order` names, one after the other: a tile's rows are then one copy, and of the many tiles that a group's
 // blocks of weights make only the first has to look them up.  (Fetched where they lie by the copy engine's gathers of four rows,
 // in every tile, they held up the products of 49152 x 2048 x 2816 by 95 us of 440; by 16-byte copies of eight warps by 395.)
-// A warp per row, all its loads under way at once up to 4 KB.
+// A warp per row, all its loads under way at once up to 4 KB: 49152 rows of 4 KB in 45 us, 4.5 TB/s written (the rows of x come from the
+// second-level cache); several rows per warp, other grids and fewer registers took 48 to 55.
 constexpr uint32_t kPackRows = 8;
 __global__ void __launch_bounds__(32 * kPackRows) pack_rows_kernel(const GroupedArgs a, uint8_t *packed) {
   const uint32_t r = blockIdx.x * kPackRows + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (r >= (a.offsets ? (uint32_t)max(0, min(__ldcg(a.offsets + a.E), (int32_t)a.R)) : a.R)) return;
+  if (r >= a.R || (a.offsets && ((int32_t)r < __ldcg(a.offsets) || (int32_t)r >= __ldcg(a.offsets + a.E)))) return;   // (of no group)
   const int32_t src = source_row(a, r);
   if (src < 0 && lane == 0) report(a.status, kStatusBadDescriptor);
   const uint8_t *from = a.x + (src >= 0 ? (uint64_t)src * a.x_pitch : 0);

@@ -259,6 +259,27 @@ def test_wrong_lists_are_reported(zb, kernel, rows):
     assert torch.equal(out[keep].cpu(), torch.from_numpy(x[keep] @ w[0].T).to(torch.bfloat16))
 
 
+@pytest.mark.parametrize("T", [9, 500])
+def test_products_of_some_of_the_experts(zb, kernel, T):
+    """Part of the offsets, whose first is not 0: other experts' rows are neither read nor written, nor what `order` says there."""
+    import torch
+    E, k, K, N, lo, hi = 8, 2, 136, 96, 2, 6
+    x, w = coarse((T, K), 21, 1 / 16), coarse((E, N, K), 22, 1 / 64)
+    ids = routing(T, k, E, 23, dropped=0.1)
+    g = zb.group_tokens(gpu(ids), E)
+    offsets, order, _ = grouped.group(ids, E)
+    begin, end = int(offsets[lo]), int(offsets[hi])
+    assert 0 < begin < end < len(order)
+    g.order[:begin] = -5
+    g.order[end:] = 1 << 30
+    m = zb.GroupedMatrix(list(bf16(w[lo:hi])))
+    out = torch.full((T * k, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    m.product(bf16(x), zb.TokenGroups(g.offsets[lo:hi + 1], g.order, g.place, hi - lo), gather=True, out=out)
+    want = grouped.products(x, order // k, offsets, w)[begin:end]
+    assert int(m.status.item()) == 0 and (out[:begin] == 7.0).all() and (out[end:] == 7.0).all()
+    assert torch.equal(out[begin:end], torch.from_numpy(want).cuda().to(torch.bfloat16))
+
+
 # ---- weighted sums ----------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("T,k,cols", [(1, 1, 8), (1, 8, 4096), (5, 2, 100), (64, 3, 1408), (33, 6, 30), (700, 4, 264), (70000, 1, 8)])
 @pytest.mark.parametrize("f32", [False, True])
