@@ -3,6 +3,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstdint>
 #include <type_traits>
 
@@ -12,12 +13,11 @@
 namespace zipmoe_dev {
 
 // ---- grouping: a stable counting sort of the choices by expert -----------------
-// Bound: latency (12 bytes per choice are nothing).  One cluster of 1 to 8 blocks; every warp owns a run of consecutive choices
+// Bound: latency (12 bytes per choice are nothing).  One cluster of 1 to 16 blocks; every warp owns a run of consecutive choices
 // and counts its experts in a row of its own in shared memory, 32 choices at a time.  Lanes with the same expert find one another
 // with a ballot per bit of its number (the match instruction takes longer, the more experts differ: 8.8 us for 777 x 4 choices of
-// 60, so 6.4), so that nothing is added atomically and the order is the choices' own.  64 x 2 choices of 8: 3.0 us; 8192 x 6 of 64: 9.8.
-// The blocks' sums meet through distributed
-// shared memory; then every warp knows where its first choice of each expert goes.
+// 60, so 6.4, both in one block), so that nothing is added atomically and the order is the choices' own.  The blocks' sums meet
+// through distributed shared memory; then every warp knows where its first choice of each expert goes.
 constexpr uint32_t kGroupMaxExperts = 256;
 
 struct GroupArgs {
@@ -246,6 +246,28 @@ zipmoe_status current_device(int *dev) {
   return ZIPMOE_OK;
 }
 
+// Blocks that a cluster of group_kernel may have on the device: 8 everywhere, 16 where it says that such clusters fit.
+uint32_t largest_cluster(int dev) {
+  static std::atomic<uint32_t> known[64];
+  if (const uint32_t n = known[dev].load(std::memory_order_relaxed)) return n;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = 16;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  cfg.gridDim = dim3(16);
+  cfg.blockDim = dim3(1024);
+  cfg.dynamicSmemBytes = 32 * zipmoe_dev::kGroupMaxExperts * 4;
+  int clusters = 0;
+  const bool fits = cudaFuncSetAttribute(zipmoe_dev::group_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                    cudaOccupancyMaxActiveClusters(&clusters, zipmoe_dev::group_kernel, &cfg) == cudaSuccess && clusters > 0;
+  if (!fits) cudaGetLastError();   // (nobody else is to find it)
+  known[dev].store(fits ? 16 : 8, std::memory_order_relaxed);
+  return fits ? 16 : 8;
+}
+
 }  // namespace
 
 extern "C" zipmoe_status zipmoe_group_tokens(const zipmoe_group_args *g, zipmoe_stream stream) {
@@ -259,10 +281,11 @@ extern "C" zipmoe_status zipmoe_group_tokens(const zipmoe_group_args *g, zipmoe_
   const zipmoe_status rc = current_device(&dev);
   if (rc != ZIPMOE_OK) return rc;
   const GroupArgs a = {g->topk_ids, g->offsets, g->order, g->place, g->status_word, g->T * g->k, g->n_experts};
-  // a warp takes up to 256 choices before another block is worth its exchange
-  const uint32_t pieces = (a.n + 31) / 32, threads = std::max(256u, std::min(1024u, (pieces + 3) / 4 * 32));
+  // As many blocks as leave a warp 32 choices: 2000 x 4 choices of 64 take 7.4 us in two blocks and 4.7 in eight, 8192 x 6 take 9.8 in
+  // eight and 7.3 in sixteen.
+  const uint32_t pieces = (a.n + 31) / 32, threads = std::max(256u, std::min(1024u, pieces * 32)), most = largest_cluster(dev);
   uint32_t S = 1;
-  while (S < 8 && pieces > S * 32 * 4) S <<= 1;
+  while (S < most && pieces > S * 32) S <<= 1;
   cudaLaunchAttribute attrs[2];
   attrs[0].id = cudaLaunchAttributeClusterDimension;
   attrs[0].val.clusterDim.x = S;

@@ -79,6 +79,16 @@ def test_lists(zb, T, k, E, dropped):
     assert np.array_equal(g.place.cpu().numpy(), place) and int(status.item()) == 0
 
 
+@pytest.mark.parametrize("T,k,E", [(40000, 8, 64), (70001, 5, 256), (131073, 1, 3)])
+def test_lists_of_many_choices(zb, T, k, E):
+    """More than the warps of the largest cluster hold in registers."""
+    ids = np.random.default_rng(T).integers(-1, E, (T, k)).astype(np.int32)
+    g = zb.group_tokens(gpu(ids), E)
+    offsets, want, place = grouped.group(ids, E)
+    assert np.array_equal(g.offsets.cpu().numpy(), offsets)
+    assert np.array_equal(g.order.cpu().numpy()[:want.size], want) and np.array_equal(g.place.cpu().numpy(), place)
+
+
 def test_lists_of_no_tokens_repeated_and_wrong_ids(zb):
     import torch
     g = zb.group_tokens(torch.empty(0, 3, dtype=torch.int32, device="cuda"), 7)
