@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) grouped_wide_kernel(const __g
   tc_before_sync();
   __syncthreads();
   tc_after_sync();
-  after_predecessor();   // (only now: nobody who comes after takes the tensor memory first)
+  if (a.offsets) after_predecessor();   // (only now: nobody who comes after takes the tensor memory first)
   if (warp == 0) {
     // lane l has the groups from per * l on; all loads are asked for before any is looked at
     const uint32_t per = (a.E + 31) / 32, e0 = lane * per;
@@ -324,6 +324,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) grouped_wide_kernel(const __g
   }
   __syncthreads();
   cluster_sync();   // both blocks' barriers are set up
+  if (!a.offsets) after_predecessor();   // (what is to be done was known without it)
   const uint32_t tmem = words[0], tiles = words[2];
   // the pair's i-th tile; false behind the last, or where a wait has run out
   auto next_tile = [&](uint32_t i, WideTile &u) {
