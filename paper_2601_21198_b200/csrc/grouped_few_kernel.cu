@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) grouped_few_kernel(const __gri
     fence_barrier_init();
   }
   if (warp == 1) tmem_alloc(smem_addr(words), tmem_cols);
-  if (a.offsets) after_predecessor();
+  if (a.offsets) wait_predecessor();
   if (warp == 0) {
     // units before each group: lane l has the groups from per * l on; all loads are asked for before any is looked at
     const uint32_t per = (a.E + 31) / 32, e0 = lane * per;
@@ -108,7 +108,8 @@ __global__ void __launch_bounds__(kFewThreads, 2) grouped_few_kernel(const __gri
   const uint32_t tmem = words[0];
   const FewUnit u = unit_at;
   const bool work = u.n > 0;
-  if (!a.offsets) after_predecessor();   // (what is to be done was known without it)
+  if (!a.offsets) wait_predecessor();   // (what is to be done was known without it)
+  let_successor();
 
   if (work && warp == 0 && lane == 0) {
     // ---- weights ----

@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
   extern __shared__ uint8_t smem_raw[];
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x, G = gridDim.x;
   const uint32_t W = (a.T + 31) / 32, choices = a.T * a.k, n_rows_max = resident_rows(a.E, choices);
-  after_predecessor();
+  wait_predecessor();
   // every thread's ids (up to 2048 choices), asked for before anything else
   constexpr uint32_t kIds = (256 * 8 + kResThreads - 1) / kResThreads;
   int32_t my_id[kIds];
@@ -232,6 +232,7 @@ __global__ void __launch_bounds__(kResThreads, 1) resident_ffn_kernel(const __gr
   tc_before_sync();
   __syncthreads();
   tc_after_sync();
+  let_successor();
   const uint32_t tmem = words[0];
 
   // ---- which tokens every expert has: the same in every block ----

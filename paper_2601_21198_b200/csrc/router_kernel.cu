@@ -143,10 +143,11 @@ __global__ void __launch_bounds__(kRouterThreads) router_kernel(const __grid_con
     fence_barrier_init();
   }
   if (warp == 1) tmem_alloc(smem_addr(words), a.tmem_cols);
-  after_predecessor();
+  wait_predecessor();
   tc_before_sync();
   __syncthreads();
   tc_after_sync();
+  let_successor();
   const uint32_t tmem = words[0];
 
   if (warp == 0 && lane == 0) {

@@ -64,9 +64,13 @@ __device__ __forceinline__ bool wait_count(const uint32_t *p, uint32_t want, con
 
 // A kernel launched with programmatic stream serialization is set up while its predecessor drains: it waits here before it
 // reads or writes anything, and lets its own successor do the same.  (Launched the ordinary way, the wait returns at once.)
+__device__ __forceinline__ void wait_predecessor() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// One thread's signal counts for its block.  A kernel that takes tensor memory gives it behind a barrier of the block behind the
+// allocation: a successor may take its own before it waits, and the two would then wait for each other.
+__device__ __forceinline__ void let_successor() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void after_predecessor() {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  wait_predecessor();
+  let_successor();
 }
 
 __device__ __forceinline__ uint64_t policy_evict_first() {
