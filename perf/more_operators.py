@@ -4,7 +4,8 @@ Beside a decode step (whose operators are measured elsewhere) a mixture-of-exper
 are grouped by expert (group_tokens), every expert's tokens go through W1 and W3 and the gated activation (GroupedMatrix of
 pairs), the result goes through W2 and each token's choices are added with their weights (GroupedMatrix, combine_rows).  The
 dense projections around the experts can run in 8-bit integers with a scale per token and per output channel (Int8Linear).
-Every case is one call of one of these four.
+Every case is a pass through one of these four; the products of either kind begin with the choices' lists in both forms, since
+a layer makes them anew for every prompt.
 
 `own` false: elementary torch operations in 32 bits.  `own` true: the calls that a program makes of the library."""
 import math
@@ -141,7 +142,6 @@ def prepare(case, seed):
             s["order"] = torch.full((T * k,), -1, dtype=torch.int32, device="cuda")   # (those behind the last group stay)
             s["place"] = torch.empty(T, k, dtype=torch.int32, device="cuda")
             return s
-        s["groups"] = zb.group_tokens(s["ids"], case["experts"])
         if case["op"] == "gate_up":
             s["gate_up"] = zb.GroupedMatrix(list(s["w1"]), up=list(s["w3"]))
             s["h"] = torch.zeros(T * k, case["inter"], dtype=torch.bfloat16, device="cuda")   # (rows behind the last group stay)
@@ -164,12 +164,15 @@ def run(s):
         return {"offsets": s["offsets"], "order": s["order"], "place": s["place"]}
     if op == "gate_up":
         if own:
-            return s["gate_up"].product(s["x"], s["groups"], gather=True, out=s["h"])
+            from paper_2601_21198_b200 import binding as zb
+            groups = zb.group_tokens(s["ids"], s["case"]["experts"])
+            return s["gate_up"].product(s["x"], groups, gather=True, out=s["h"])
         return _plain_gate_up(s["x"], s["ids"], s["w1"], s["w3"], s["most"])
     if own:
         from paper_2601_21198_b200 import binding as zb
-        s["down"].product(s["h"], s["groups"], out=s["y"])
-        return zb.combine_rows(s["y"], s["groups"], s["weights"], out=s["out"])
+        groups = zb.group_tokens(s["ids"], s["case"]["experts"])
+        s["down"].product(s["h"], groups, out=s["y"])
+        return zb.combine_rows(s["y"], groups, s["weights"], out=s["out"])
     return _plain_down(s["h"], s["ids"], s["w2"], s["weights"], s["most"])
 
 
