@@ -1028,7 +1028,9 @@ def group_tokens(topk_ids, n_experts, offsets=None, order=None, place=None, stat
 class GroupedMatrix:
     """The weights of one grouped product: matrices[e] [rows, cols] of group e, all bf16 (or int16 patterns) or all int8, dense;
     `up`, if given, holds the second matrices of pairs: the product is then SiLU(first) * second.  int8 matrices have scales
-    [rows] or [n_groups, rows] fp32 (up_scales for the second ones)."""
+    [rows] or [n_groups, rows] fp32 (up_scales for the second ones).  What this puts on the device is there on return, after
+    the current stream's work so far: products may be called on any stream.  With a `status` of the caller's, evenly spaced
+    bf16 or single int8 matrices need nothing there, and nothing is waited for."""
 
     def __init__(self, matrices, up=None, scales=None, up_scales=None, status=None):
         import torch
@@ -1057,9 +1059,10 @@ class GroupedMatrix:
         flags = (GROUPED_PAIR if self.pair else 0) | (GROUPED_INT8 if self.int8 else 0)
         with _on_device(index):
             table, self.struct = zipmoe_grouped_weights_plan(addresses, self.n_groups, self.rows, self.cols, flags)
+            capturing = kinds.capturing()
         self.table = None
         prepared = status is None or not self.struct.even or (self.int8 and self.pair)      # something is put on the device here
-        if prepared and kinds.capturing():
+        if prepared and capturing:
             raise ValueError("weights are described before a capture, not within it")
         if not self.struct.even:      # (evenly spaced weights need no table)
             self.table = torch.from_numpy(table).to(self.device)
@@ -1067,7 +1070,7 @@ class GroupedMatrix:
         self._struct_at = ctypes.byref(self.struct)
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device) if status is None else status
         self.status_at = _dense("status", self.status, (1,), kinds.int32, index)
-        if self.table is not None or (self.int8 and self.pair):      # calls may come on any stream
+        if prepared:      # calls may come on any stream
             torch.cuda.current_stream(self.device).synchronize()
 
     def product(self, x, groups=None, gather=False, row_scales=None, out=None, stream=None):
@@ -1171,7 +1174,7 @@ class Int8Linear:
     @classmethod
     def from_bf16(cls, weight):
         """weight [rows, cols] bf16 (or int16 patterns), for example a tensor that was decoded: each output channel with a scale
-        of its own."""
+        of its own.  It is rounded on the current stream, and the rounding has ended on return."""
         return cls(*quantize_rows(weight))
 
     def product(self, x, out=None, stream=None):
