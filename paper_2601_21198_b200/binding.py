@@ -917,7 +917,7 @@ class ResidentExperts:
         self.status_at = self.status.data_ptr()
         self._struct_at = ctypes.byref(self.struct)
         self._scratch, self._need = _scratch_of(self.device, self.index), {}
-        self._prompt = None
+        self._prompt, self._prompt_lock = None, threading.Lock()
 
     @classmethod
     def from_decode(cls, plan, out, hidden, inter):
@@ -981,12 +981,13 @@ class ResidentExperts:
 
     def _products(self):
         """The two grouped products of ffn_prompt, described at its first call."""
-        found = self._prompt
-        if found is None:
-            shaped = [t.view(self.hidden, self.inter) if i % 3 == 2 else t.view(self.inter, self.hidden) for i, t in enumerate(self.tensors)]
-            found = self._prompt = (GroupedMatrix(shaped[0::3], up=shaped[1::3], status=self.status),
+        if self._prompt is None:
+            with self._prompt_lock:      # one description for all threads: kernels read its tables as long as it is kept
+                if self._prompt is None:
+                    shaped = [t.view(self.hidden, self.inter) if i % 3 == 2 else t.view(self.inter, self.hidden) for i, t in enumerate(self.tensors)]
+                    self._prompt = (GroupedMatrix(shaped[0::3], up=shaped[1::3], status=self.status),
                                     GroupedMatrix(shaped[2::3], status=self.status))
-        return found
+        return self._prompt
 
 
 class TokenGroups:

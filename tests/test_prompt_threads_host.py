@@ -1,0 +1,55 @@
+"""Threads that make a layer's first prompt calls at once share one description of its weights.  A second one that replaced the
+first would give the first one's table back to the pool while kernels still read tensor maps in it.  The descriptions are
+stand-ins here, so no GPU is needed."""
+import threading
+import time
+
+import numpy as np
+import pytest
+
+from paper_2601_21198_b200 import build
+
+
+@pytest.fixture(scope="module")
+def zb():
+    build.build()
+    from paper_2601_21198_b200 import binding
+    return binding
+
+
+def layer_of(zb, monkeypatch):
+    """A layer of two experts whose constructor's GPU part is left out."""
+    import torch
+    hidden, inter = 8, 16
+    monkeypatch.setattr(zb, "_get_kinds", lambda: type("Kinds", (), {"bf16": (torch.bfloat16,)}))
+    monkeypatch.setattr(zb, "_device_of", lambda name, t: 0)
+    monkeypatch.setattr(zb, "_dense", lambda name, t, shape, kinds, index: t.data_ptr())
+    monkeypatch.setattr(zb, "_on_device", lambda index: torch.inference_mode())
+    monkeypatch.setattr(zb, "zipmoe_resident_experts_plan", lambda *sizes: (np.zeros(64, np.uint8), zb.ResidentExpertsStruct()))
+    monkeypatch.setattr(zb, "_scratch_of", lambda device, index: None)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: type("Stream", (), {"synchronize": lambda self: None})())
+    return zb.ResidentExperts([torch.zeros(hidden * inter, dtype=torch.bfloat16) for _ in range(6)], hidden, inter)
+
+
+def test_one_description_for_all_threads(zb, monkeypatch):
+    layer, made = layer_of(zb, monkeypatch), []
+
+    class Slow:
+        def __init__(self, matrices, up=None, status=None):
+            assert status is layer.status and len(matrices) == 2
+            time.sleep(0.05)
+            made.append(self)
+
+    monkeypatch.setattr(zb, "GroupedMatrix", Slow)
+    start, got = threading.Barrier(4), []
+
+    def first_call():
+        start.wait()
+        got.append(layer._products())
+
+    threads = [threading.Thread(target=first_call) for _ in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert len(made) == 2 and all(g is got[0] for g in got) and layer._products() is got[0]
