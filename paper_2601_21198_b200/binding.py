@@ -916,6 +916,7 @@ class ResidentExperts:
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self.status_at = self.status.data_ptr()
         self._struct_at = ctypes.byref(self.struct)
+        torch.cuda.current_stream(self.device).synchronize()      # calls may come on any stream
         self._scratch, self._need = _scratch_of(self.device, self.index), {}
         self._prompt, self._prompt_lock = None, threading.Lock()
 

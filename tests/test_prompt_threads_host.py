@@ -1,6 +1,7 @@
-"""Threads that make a layer's first prompt calls at once share one description of its weights.  A second one that replaced the
-first would give the first one's table back to the pool while kernels still read tensor maps in it.  The descriptions are
-stand-ins here, so no GPU is needed."""
+"""Calls on any thread and stream right behind a layer's construction.  Threads that make the first prompt calls at once share one
+description of its weights: a second one that replaced the first would give the first one's table back to the pool while kernels
+still read tensor maps in it.  And the constructor has waited for what it puts on the device.  Descriptions, devices and
+streams are stand-ins here, so no GPU is needed."""
 import threading
 import time
 
@@ -17,7 +18,7 @@ def zb():
     return binding
 
 
-def layer_of(zb, monkeypatch):
+def layer_of(zb, monkeypatch, wait=lambda: None):
     """A layer of two experts whose constructor's GPU part is left out."""
     import torch
     hidden, inter = 8, 16
@@ -27,7 +28,7 @@ def layer_of(zb, monkeypatch):
     monkeypatch.setattr(zb, "_on_device", lambda index: torch.inference_mode())
     monkeypatch.setattr(zb, "zipmoe_resident_experts_plan", lambda *sizes: (np.zeros(64, np.uint8), zb.ResidentExpertsStruct()))
     monkeypatch.setattr(zb, "_scratch_of", lambda device, index: None)
-    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: type("Stream", (), {"synchronize": lambda self: None})())
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: type("Stream", (), {"synchronize": lambda self: wait()})())
     return zb.ResidentExperts([torch.zeros(hidden * inter, dtype=torch.bfloat16) for _ in range(6)], hidden, inter)
 
 
@@ -53,3 +54,12 @@ def test_one_description_for_all_threads(zb, monkeypatch):
     for t in threads:
         t.join()
     assert len(made) == 2 and all(g is got[0] for g in got) and layer._products() is got[0]
+
+
+def test_the_status_is_zeroed_before_the_first_call(zb, monkeypatch):
+    """On another stream a call could otherwise report an error that the zeroing then clears."""
+    import torch
+    steps, zeros = [], torch.zeros
+    monkeypatch.setattr(torch, "zeros", lambda *size, **kw: steps.append("zeros") or zeros(*size, **kw))
+    layer_of(zb, monkeypatch, wait=lambda: steps.append("wait"))
+    assert "zeros" in steps and steps[-1] == "wait"
