@@ -993,13 +993,24 @@ class ResidentExperts:
 
 class TokenGroups:
     """The choices of `topk_ids` [T, k] grouped by expert, as zipmoe_group_tokens lists them: offsets [n_experts + 1], order
-    [T * k] (the choice that each row is), place [T, k] (the row of each choice, -1 for none), int32 device tensors."""
+    [T * k] (the choice that each row is), place [T, k] (the row of each choice, -1 for none), int32 device tensors.  Made by
+    hand, for example of part of another's offsets, they are checked like any tensor: for type, device, shape and density."""
 
     def __init__(self, offsets, order, place, n_experts):
-        self.offsets, self.order, self.place, self.n_experts = offsets, order, place, n_experts
+        int32, index = _get_kinds().int32, _device_of("place", place)
+        if len(place.shape) != 2:
+            raise ValueError("place: a row per token is wanted, not a tensor %s" % (tuple(place.shape),))
+        T, k = place.shape
+        _dense("place", place, (T, k), int32, index)
+        _dense("offsets", offsets, (n_experts + 1,), int32, index)
+        _dense("order", order, (T * k,), int32, index)
+        self._set(offsets, order, place, n_experts, index)
+
+    def _set(self, offsets, order, place, n_experts, index):
+        self.offsets, self.order, self.place, self.n_experts, self.index = offsets, order, place, n_experts, index
         self.tokens, self.k = place.shape
         self.rows = order.shape[0]
-        self.index = place.get_device()
+        return self
 
 
 def group_tokens(topk_ids, n_experts, offsets=None, order=None, place=None, status=None, stream=None):
@@ -1024,7 +1035,7 @@ def group_tokens(topk_ids, n_experts, offsets=None, order=None, place=None, stat
     status_code = _lib.zipmoe_group_tokens(args, _handle(kinds, index, stream))
     if status_code:
         raise ZipMoEError("zipmoe_group_tokens", status_code)
-    return TokenGroups(offsets, order, place, n_experts)
+    return TokenGroups.__new__(TokenGroups)._set(offsets, order, place, n_experts, index)      # (checked above)
 
 
 class GroupedMatrix:
