@@ -531,9 +531,10 @@ zipmoe_status zipmoe_grouped_workspace_bytes(const zipmoe_grouped_weights *weigh
 /* Matrix products grouped by expert, group sizes known on the device alone: for every group e and its rows r
  *     acc[r, n] = sum_c x[src(r), c] * W_e[n, c]             (fp32 sums; 8-bit integers: exact)
  *     out[r, n] = acc[r, n]                                  bf16
- *               = acc[r, n] * row_scales[src(r)] * col_scales[e, n]              8-bit integers
+ *               = acc[r, n] * row_scales[src(r)] * col_scales[e, n]              8-bit integers (fp32, from left to right)
  *     out[r, n] = SiLU(first) * second                       of these, with ZIPMOE_GROUPED_PAIR
- * rounded once.  Rows of `out` that belong to no group are left as they were; a group may be empty.  A row whose `order` points
+ * in fp32, and rounded once to the type of out.  Scales and scaled sums may be subnormal; fp32 sums of bf16 products and either
+ * factor of a pair may come as zeros where they are below 2^-126.  Rows of `out` that belong to no group are left as they were; a group may be empty.  A row whose `order` points
  * outside x is taken as zeros; where the offsets are not in order, are negative or reach past `rows`, nothing is computed.  Both
  * set status_word (code 1).  One launch on `stream`, or two where rows are gathered, asynchronous; results do not depend on
  * timing.

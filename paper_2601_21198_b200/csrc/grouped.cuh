@@ -67,6 +67,11 @@ __device__ __forceinline__ int32_t source_row(const GroupedArgs &a, uint32_t r) 
   return c >= 0 && t < a.x_rows ? (int32_t)t : -1;
 }
 
+// What an exact sum of 8-bit integers stands for.  Scales may be subnormal (a row of tiny numbers), their products need not be.
+__device__ __forceinline__ float scaled(int32_t sum, float row_scale, float col_scale) {
+  return times(times(__int2float_rn(sum), row_scale), col_scale);
+}
+
 __device__ __forceinline__ float silu_product(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
 
 // 16 bytes into shared memory, or 16 zero bytes

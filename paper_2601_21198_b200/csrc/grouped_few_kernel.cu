@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) grouped_few_kernel(const __gri
           }
         const float token = source[t] >= 0 ? __ldcg(a.row_scales + source[t]) : 0.f;
 #pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) sum[i] = __int2float_rn(acc[i]) * token * scale[i];
+        for (uint32_t i = 0; i < 4; ++i) sum[i] = scaled(acc[i], token, scale[i]);
       } else {
         sum[0] = sum[1] = sum[2] = sum[3] = 0.f;
 #pragma unroll

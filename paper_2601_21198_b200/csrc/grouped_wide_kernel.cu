@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) grouped_wide_kernel(const __g
       // the i-th value of a chunk that begins with the warp's tok0-th token
       auto value = [&](uint32_t v, const float *of, uint32_t tok0, uint32_t i) {
         if constexpr (kInt8)
-          return __int2float_rn((int32_t)v) * my_scale[tok0 + chunk_col<kF32>(i, lane)] * of[kF32 ? 0 : (i >> 3) * 2 + ((i >> 1) & 1)];
+          return scaled((int32_t)v, my_scale[tok0 + chunk_col<kF32>(i, lane)], of[kF32 ? 0 : (i >> 3) * 2 + ((i >> 1) & 1)]);
         else
           return __uint_as_float(v);
       };
@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) grouped_wide_kernel(const __g
       const uint32_t lanes = tmem + ((32 * w) << 16);
       // Sums leave tensor memory at once and wait in registers for their turn to be stored, which takes five times as long.
       auto first_of = [&](uint32_t c) { return (2 * (c >> 1) + side) * 32 + (c & 1) * 16; };   // first token of the warp's c-th chunk
-      auto fetch = [&](uint32_t h, const float *of, Chunk<kF32> *to, const float (*times)[16]) __attribute__((always_inline)) {
+      auto fetch = [&](uint32_t h, const float *of, Chunk<kF32> *to, const float (*gate)[16]) __attribute__((always_inline)) {
 #pragma unroll
         for (uint32_t c = 0; c < 8; ++c) {
           if (first_of(c) >= u.n) continue;
@@ -402,7 +402,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) grouped_wide_kernel(const __g
 #pragma unroll
           for (uint32_t i = 0; i < 16; i += 2) {
             const float x = value(v[i], of, c * 16, i), y = value(v[i + 1], of, c * 16, i + 1);
-            if constexpr (kPair) to[c].set(i, times[c][i] * x, times[c][i + 1] * y);
+            if constexpr (kPair) to[c].set(i, gate[c][i] * x, gate[c][i + 1] * y);
             else to[c].set(i, x, y);
           }
         }

@@ -23,12 +23,7 @@ struct QuantizeArgs {
   uint32_t rows, cols;
 };
 
-// The product and the quotient, correctly rounded, subnormal numbers included (which this library's compilation flushes otherwise).
-__device__ __forceinline__ float times(float x, float y) {
-  float r;
-  asm("mul.rn.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
-  return r;
-}
+// The quotient, correctly rounded, as times() rounds the product.
 __device__ __forceinline__ float divided(float x, float y) {
   float r;
   asm("div.rn.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));

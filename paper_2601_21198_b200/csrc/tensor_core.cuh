@@ -73,6 +73,13 @@ __device__ __forceinline__ void after_predecessor() {
   let_successor();
 }
 
+// The product, correctly rounded, subnormal numbers included (which this library's compilation flushes otherwise).
+__device__ __forceinline__ float times(float x, float y) {
+  float r;
+  asm("mul.rn.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+  return r;
+}
+
 __device__ __forceinline__ uint64_t policy_evict_first() {
   uint64_t p;
   asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
