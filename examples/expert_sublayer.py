@@ -4,8 +4,9 @@
     ids, weights = top-k of h @ gate^T         zipmoe_route
     y = sum of the chosen experts' FFNs        zipmoe_expert_ffn on the experts that are recovered (the planner's pool F), or, for a
                                                prompt of more than 256 tokens, the grouped products (zipmoe_group_tokens,
-                                               zipmoe_grouped_matmul, zipmoe_combine_rows); zipmoe_decode_expert_ffn on those that
-                                               stay compressed
+                                               zipmoe_grouped_matmul, zipmoe_combine_rows; they round the activations between the
+                                               products to 8 significant bits, zipmoe_expert_ffn to 16);
+                                               zipmoe_decode_expert_ffn on those that stay compressed
 
 A layer may keep some of its experts recovered and the others compressed.  The call on recovered experts takes -1 for a choice
 that is not its own.  The call on compressed experts wants every id in range, so each choice is a row of its own there, those

@@ -524,7 +524,8 @@ typedef struct {
 } zipmoe_grouped_args;
 
 /* Scratch zipmoe_grouped_matmul needs for `rows` rows, gathered (non-zero: `order` is given) or not: room for the gathered rows
- * of a call with many, else 0.  Host only. */
+ * of a call with many, else 0.  Asked with the call's device current: the number of its SMs decides which kernel is taken.  Host
+ * only. */
 zipmoe_status zipmoe_grouped_workspace_bytes(const zipmoe_grouped_weights *weights, uint32_t rows, uint32_t gathered,
                                              uint64_t *workspace_bytes);
 

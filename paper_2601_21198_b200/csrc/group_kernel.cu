@@ -154,7 +154,8 @@ struct CombineArgs {
 };
 
 // Blocks of an SM at once.  8192 tokens of six choices of 2048 columns: 70.6 us with three, 66.7 with four, 78.4 with five (which spill);
-// 4096 tokens of two of 4096: 35.9 with four, 28.5 with six.
+// 4096 tokens of two of 4096: 35.9 with four, 28.5 with six.  Seven and eight choices share an instance that spills with four (96 bytes
+// of fp32): 104 and 111 us for 8192 tokens, 4.8 and 5.2 TB/s, where two, four and six choices reach 5.0, 5.8 and 6.3.
 __host__ __device__ constexpr uint32_t combine_blocks(uint32_t k) { return k <= 2 ? 6 : k <= 4 ? 5 : 4; }
 
 template <bool kF32, bool kWide, uint32_t kK>

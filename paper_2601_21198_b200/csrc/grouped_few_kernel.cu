@@ -1,8 +1,9 @@
 // Grouped products of few tokens per group: out[r, n] = sum_k x[src(r), k] * W_e[n, k] for the rows r of group e, for bf16 and
 // 8-bit integers, with the gated activation of two products (pair) or scales per token and channel behind it.
 //
-// Bound: the weights' bytes, read once per 64 tokens of a group.  (One token through six pairs of 2048 x 1408, 69 MB: 15.7 us where
-// calls follow one another, of which 10 are the stream at 6.9 TB/s; 18.4 alone.  Two matrices of 4096 x 14336, 235 MB: 40 us, 5.8 TB/s.)
+// Bound: the weights' bytes, read once per 64 tokens of a group.  (One token through six pairs of 2048 x 1408, 69 MB: 16.2 to 16.5
+// us where calls follow one another, of which 10 are the stream at 6.9 TB/s; 18.6 alone.  Two matrices of 4096 x 14336, 235 MB: 40 us,
+// 5.9 TB/s.)
 //   * A unit is 128 rows of one group's weights (64 of W1 and 64 of W3 of a pair) and up to 64 of its tokens.  The weights are
 //     the M = 128 operand of a tcgen05 MMA and the tokens its N columns, so that a single token costs 16 columns, not 128 rows.
 //   * A cluster of 1 to 8 blocks takes a unit and splits K among its blocks; the partial sums meet through distributed shared

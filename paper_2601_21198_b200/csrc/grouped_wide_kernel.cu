@@ -3,8 +3,10 @@
 //
 // Bound: what shared memory takes in and gives out beside the tensor cores.  A tcgen05 MMA reads its operands there at 64 of the 128
 // bytes a cycle, so every byte that the copies bring costs.  (8192 x 8192 x 8192 in bf16: 661 to 710 us, 1.55 to 1.66 PFLOP/s; 8192
-// tokens of 8-bit integers, 4096 x 14336: 305 us, 3.2 POP/s; 8192 tokens' six of 64 experts, pairs of 2048 x 1408: 458 to 470 us, 1.22
-// PFLOP/s.  A tile of 512 x 256 x 2048 takes 34.9 K cycles, 32.8 K of them products.  Runs of some 0.1 s are at the power limit.)
+// tokens of 8-bit integers, 4096 x 14336: 297 to 305 us, 3.2 POP/s; 8192 tokens' six of 64 experts, pairs of 2048 x 1408, without the
+// packing: 458 to 470 us, 1.22 PFLOP/s.  These are ten calls behind one another after a pause.  In calls that go on for 0.15 s and
+// more the clock is at the power limit, and the last two take 360 and 544 us.  A tile of 512 x 256 x 2048 takes 34.9 K cycles, 32.8 K of
+// them products.)
 //   * Two blocks of a cluster share one MMA (cta_group::2): each brings 128 rows of either half of the weights and half of the
 //     tokens, and keeps the sums of its own weights in its tensor memory, two halves of [128 x tokens] of 32 bits.  Per step of 128
 //     bytes of K that is 48 KB for two MMAs' worth of 256 x 256 sums, where tiles of 256 x 256 would take in 64 KB.
@@ -13,8 +15,9 @@
 //     catches up the first is read back; while the next tile's first half gets ahead, the second is.
 //   * Of a pair the first half is W1's rows and the second W3's: both values of an output come back in the same lane, the first
 //     waits in registers for the second.
-//   * Tokens are the N operand: a tile has as many columns as it has tokens, rounded to 32, so the ragged end of a group costs what
-//     it is worth; a group's tokens are spread evenly over its tiles.
+//   * Tokens are the N operand: a tile has as many columns as it has tokens, rounded to 32; a group's tokens are spread evenly over
+//     its tiles.  Few columns do not make a tile short, since its weights have to come all the same: a step takes 0.50 us up to 96
+//     columns, 0.57 with 128, 0.72 with 192 and 0.90 with 256 (bf16, weights in the second-level cache).
 //   * One persistent pair of blocks per two SMs walks over the tiles of all groups; a group's tiles follow one another with the
 //     tokens inside, so that pairs at work at the same time read the same weights.  One thread of each block works the tiles out,
 //     ahead of the others.

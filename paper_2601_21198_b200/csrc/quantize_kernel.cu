@@ -2,7 +2,7 @@
 // Bound: 3 bytes per element.  A row stays in registers between its maximum and its stores.  8192 rows of 4096: 18.3 us, 5.5 TB/s.
 // With x = X 2^i and a = A 2^j, X and A whole numbers below 256, the quotient t = 127 X 2^(i-j) / A is either half way between two
 // integers, or |254 X - (2m + 1) A 2^(j-i)| / (2A 2^(j-i)) >= t / (254 X) > t 2^-16 away from there.  x * (127 / a) with two roundings
-// is off by t 2^-23 at most: rounded to 19 significant bits (t 2^-20 at most from there) it is the half where t is one, and on
+// is off by t 2^-23 at most: rounded to 19 significant bits (t 2^-19 at most from there) it is the half where t is one, and on
 // the right side of it where t is not.  So the integers are those that the real numbers give, without a division per element.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>

@@ -246,8 +246,9 @@ inline cudaLaunchAttribute overlapped() {
   return a;
 }
 
-// The same for a grid of `blocks`, of which `at_once` fit the device: one that does not fit as a whole is not set up ahead, since
-// its waiting blocks would take registers and slots that its predecessor's last blocks may need.
+// The same for a grid of `blocks`, of which `at_once` fit the device.  One that does not fit as a whole is not set up ahead: it
+// would gain next to nothing, since most of its blocks start late anyway, and its first ones would hold registers and slots of the
+// SMs while they wait.  (Its predecessor's blocks have all started by then, so it takes nothing from them.)
 inline cudaLaunchAttribute overlapped_if_whole(uint64_t blocks, uint64_t at_once) {
   cudaLaunchAttribute a = overlapped();
   a.val.programmaticStreamSerializationAllowed = blocks <= at_once;
