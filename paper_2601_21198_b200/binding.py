@@ -911,12 +911,12 @@ class ResidentExperts:
         self.hidden, self.inter = hidden, inter
         with _on_device(self.index):
             table, self.struct = zipmoe_resident_experts_plan(addresses, len(tensors) // 3, hidden, inter)
-        self.table = torch.from_numpy(table).to(self.device)
-        self.struct.table = self.table.data_ptr()
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self.status_at = self.status.data_ptr()
+        # calls may come on any stream: this copy from the host returns when it has arrived, and so have the zeros before it
+        self.table = torch.from_numpy(table).to(self.device)
+        self.struct.table = self.table.data_ptr()
         self._struct_at = ctypes.byref(self.struct)
-        torch.cuda.current_stream(self.device).synchronize()      # calls may come on any stream
         self._scratch, self._need = _scratch_of(self.device, self.index), {}
         self._prompt, self._prompt_lock = None, threading.Lock()
 

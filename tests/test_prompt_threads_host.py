@@ -1,7 +1,7 @@
 """Calls on any thread and stream right behind a layer's construction.  Threads that make the first prompt calls at once share one
 description of its weights: a second one that replaced the first would give the first one's table back to the pool while kernels
-still read tensor maps in it.  And the constructor has waited for what it puts on the device.  Descriptions, devices and
-streams are stand-ins here, so no GPU is needed."""
+still read tensor maps in it.  And the constructor returns when what it puts on the device is there.  Descriptions and
+devices are stand-ins here, so no GPU is needed."""
 import threading
 import time
 
@@ -18,7 +18,7 @@ def zb():
     return binding
 
 
-def layer_of(zb, monkeypatch, wait=lambda: None):
+def layer_of(zb, monkeypatch):
     """A layer of two experts whose constructor's GPU part is left out."""
     import torch
     hidden, inter = 8, 16
@@ -28,7 +28,6 @@ def layer_of(zb, monkeypatch, wait=lambda: None):
     monkeypatch.setattr(zb, "_on_device", lambda index: torch.inference_mode())
     monkeypatch.setattr(zb, "zipmoe_resident_experts_plan", lambda *sizes: (np.zeros(64, np.uint8), zb.ResidentExpertsStruct()))
     monkeypatch.setattr(zb, "_scratch_of", lambda device, index: None)
-    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: type("Stream", (), {"synchronize": lambda self: wait()})())
     return zb.ResidentExperts([torch.zeros(hidden * inter, dtype=torch.bfloat16) for _ in range(6)], hidden, inter)
 
 
@@ -57,9 +56,20 @@ def test_one_description_for_all_threads(zb, monkeypatch):
 
 
 def test_the_status_is_zeroed_before_the_first_call(zb, monkeypatch):
-    """On another stream a call could otherwise report an error that the zeroing then clears."""
+    """On another stream a call could otherwise report an error that the zeroing then clears.  The copy of the table from the host
+    returns when it and all before it on the stream is done, so it has to come last."""
     import torch
-    steps, zeros = [], torch.zeros
+    steps, zeros, from_numpy = [], torch.zeros, torch.from_numpy
+
+    class Table:
+        def __init__(self, array):
+            self.array = array
+
+        def to(self, device):
+            steps.append("copy")
+            return from_numpy(self.array)
+
+    monkeypatch.setattr(torch, "from_numpy", Table)
     monkeypatch.setattr(torch, "zeros", lambda *size, **kw: steps.append("zeros") or zeros(*size, **kw))
-    layer_of(zb, monkeypatch, wait=lambda: steps.append("wait"))
-    assert "zeros" in steps and steps[-1] == "wait"
+    layer_of(zb, monkeypatch)
+    assert "zeros" in steps and steps[-1] == "copy"
