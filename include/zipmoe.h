@@ -534,8 +534,8 @@ zipmoe_status zipmoe_grouped_workspace_bytes(const zipmoe_grouped_weights *weigh
  *     out[r, n] = acc[r, n]                                  bf16
  *               = acc[r, n] * row_scales[src(r)] * col_scales[e, n]              8-bit integers (fp32, from left to right)
  *     out[r, n] = SiLU(first) * second                       of these, with ZIPMOE_GROUPED_PAIR
- * in fp32, and rounded once to the type of out.  Scales and scaled sums may be subnormal; fp32 sums of bf16 products and either
- * factor of a pair may come as zeros where they are below 2^-126.  Rows of `out` that belong to no group are left as they were; a group may be empty.  A row whose `order` points
+ * in fp32, and rounded once to the type of out.  Scales and scaled sums may be subnormal; fp32 sums of bf16 products may come as
+ * zeros where they are below 2^-126, and the factors of a pair below 2^-119.  Rows of `out` that belong to no group are left as they were; a group may be empty.  A row whose `order` points
  * outside x is taken as zeros; where the offsets are not in order, are negative or reach past `rows`, nothing is computed.  Both
  * set status_word (code 1).  One launch on `stream`, or two where rows are gathered, asynchronous; results do not depend on
  * timing.
