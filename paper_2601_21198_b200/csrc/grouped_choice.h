@@ -15,7 +15,7 @@ struct GroupedSizes {
 // What either kernel takes, in ns on a device of `sms` SMs, if the rows are spread evenly over the groups.  (How they are spread is
 // known on the device alone: where most rows fall on one of many experts the kernel for few tokens reads that expert's weights once
 // per 64 of them.)  Both forms are sums of what the kernels do, with rates fitted to 264 measured pairs of times.  Of those they
-// are: few, 0.45 to 1.53 of the measured time; many, 0.56 to 1.48; one in five of either is off by more than a fifth.  They err
+// are: few, 0.45 to 1.53 of the measured time; many, 0.56 to 1.48; about one in five is off by more than a fifth.  They err
 // alike where it matters: the kernel that is taken costs at most 1.29 of the other's time.
 //   Few: weights from memory at 6.5 TB/s, whatever is taken in again for every further 64 tokens, and the tokens, at 10 TB/s (from the
 //   second-level cache), 2.5 us per block that an SM takes after another, 5.5 us besides.
